@@ -423,8 +423,9 @@ def run(state):
     elif op == "attend":
         b.tree_verify_attention_paged(tree, s["q"], s["k"][0], s["v"][0], s["table"], s["lens"], s["out"], s["ws"], shared_len=s["case"]["shared"], status=s["status"])
     elif op == "compact":
-        b.kv_compact_accepted_paged(tree, s["k_ptrs"], s["v_ptrs"], s["case"]["layers"], s["pool"], s["table"], s["lens"], s["new_lens"], s["accept_len"], s["acc_nodes"],
-                                    status=s["status"])
+        c = s["case"]
+        b.kv_compact_accepted_paged(tree, s["k_ptrs"], s["v_ptrs"], c["layers"], c["Hkv"], c["D"], s["pool"], s["table"], s["lens"], s["new_lens"],
+                                    s["accept_len"], s["acc_nodes"], status=s["status"])
     elif op == "logits":
         b.logits_constrain(tree, s["logits"], s["out"], s["rules"], s["tree_tok"])
     else:
