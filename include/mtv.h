@@ -16,6 +16,11 @@
  *                          position seq_len + depth
  *   lm_head_argmax         the base model's LM head with the per-node argmax fused in, and
  *   tree_accept_keys       the acceptance that reads its result instead of stored logits
+ * and the same step for a program that keeps K and V in pages and decodes under constraints:
+ *   tree_kv_append_rope_paged, kv_append_rope_paged, tree_verify_attention_paged (a prefix that the batch
+ *                          shares is attended to once for all), kv_compact_accepted_paged
+ *   logits_constrain, constrained_argmax_keys, token_counts_add
+ *                          penalties for repeated tokens, biases and grammar masks in front of the acceptance
  *
  * Conventions
  *   - Every function returns an int: MTV_OK (0) or a negative MTV_ERR_* code.
@@ -54,7 +59,8 @@ extern "C" {
 #define MTV_ERR_CAPACITY (-6) /* status[b]: seq_lens[b] + T exceeds the cache capacity */
 #define MTV_ERR_BOUNDS (-7)   /* device error word, -DMTV_DEBUG_BOUNDS builds only: an index read from device
                                  memory (a tree table, acc_nodes, accept_len, the sequence order) was out of
-                                 range; the access was skipped */
+                                 range; the access was skipped.  In every build: status[b] of the paged calls, and a
+                                 mask index of the constrained ones */
 
 #define MTV_MAX_K 8
 #define MTV_MAX_T 128
@@ -392,6 +398,119 @@ int attn_interleave_shards(int rows, int n_shards, int Hq_local, int D, const mt
                            void *stream);
 int keys_merge_shards(int n, int n_shards, int v_slab, const unsigned long long *key_shards,
                       unsigned long long *keys, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * K/V caches in pages (the paper's cache is contiguous; a serving program hands out pages as sequences grow, and lets
+ * sequences with the same prefix name the same pages).
+ *   pool           one buffer per layer for K and one for V; element (page, head, row, d) at
+ *                  page*stride_page + head*stride_h + row*stride_t + d: heads inside a page or rows, as the strides say
+ *   page_table     device [B][max_pages] int32: slot s of sequence b is row s % page_size of page page_table[b][s / page_size];
+ *                  entries behind a sequence's last slot are never followed
+ * page_size: a power of two from 16 to 65536; strides multiples of 8, stride_t >= D; pool base addresses 16-byte aligned;
+ * max_pages * page_size below 2^31 - 256.  Sequences may share pages that a call only reads; two sequences of a call that
+ * write rows of the same page race.
+ * status[b] of the calls below: MTV_OK; MTV_ERR_CAPACITY if seq_lens[b] is negative or the rows do not fit max_pages;
+ * MTV_ERR_BOUNDS if the table names no page of the pool where the call needs one (checked in every build).
+ */
+typedef struct {
+    int64_t stride_page, stride_h, stride_t;   /* elements */
+    int32_t page_size, n_pages;
+} mtv_pool_layout;
+
+/* tree_kv_append_rope_layers for such a cache: node i of sequence b at position seq_lens[b] + depth[i], its rotated K row
+ * and its V row to slot seq_lens[b] + i; k_pools / v_pools: device arrays of n_layers device pointers.  The rotated queries go to
+ * q_out_layers (which may be q_layers itself; otherwise the two must not overlap).  Same angles, arithmetic and rope_theta.
+ * MTV_ERR_CAPACITY: nothing of b is written.  MTV_ERR_BOUNDS: K/V rows whose page does not exist are left out, the rest of
+ * the sequence is written. */
+int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,
+                              mtv_bf16 *q_out_layers, const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers,
+                              mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool,
+                              const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta,
+                              int32_t *status, void *stream);
+
+/* The same for runs of consecutive tokens (prompts, chunks of them, single tokens): rows row_starts[b] .. row_starts[b+1] - 1 of
+ * q_layers, q_out_layers [n_layers][n_rows][Hq][D] and k_new_layers, v_new_layers [n_layers][n_rows][Hkv][D] belong to sequence b, the i-th
+ * of them at slot and position seq_lens[b] + i.  row_starts: device [B+1], ascending; a sequence may have no rows.  Rows outside
+ * [row_starts[0], row_starts[B]) are padding and left as they are.  n_rows may be 0.  seq_lens is not changed. */
+int kv_append_rope_paged(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
+                         const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, mtv_bf16 *const *k_pools,
+                         mtv_bf16 *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                         const int32_t *seq_lens, const int32_t *row_starts, float rope_theta, int32_t *status, void *stream);
+
+/* kv_compact_accepted for such a cache; the lengths behind the step, seq_lens[b] + accept_len[b] + 1, go to new_lens, which may be
+ * seq_lens itself.  accept_len[b] outside [0, K], a node outside [0, T) or a page that does not exist: MTV_ERR_BOUNDS, and b is
+ * skipped (no row moves, new_lens[b] is not written). */
+int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int n_layers, mtv_bf16 *const *k_pools,
+                              mtv_bf16 *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                              const int32_t *seq_lens, int32_t *new_lens, const int32_t *accept_len, const int32_t *acc_nodes,
+                              int32_t *status, void *stream);
+
+/* tree_verify_attention over such a cache, one layer.  The first shared_len slots of all sequences are the same keys — their
+ * page-table rows name the same pages there, or pages with the same content; row 0's are read — and are attended to once for the
+ * whole batch: the query rows of all sequences meet each of those keys together, the sequences' own keys follow, and the parts
+ * are joined.  shared_len: a multiple of page_size (0: nothing is shared), at most every seq_lens[b].
+ * A tree of its root alone is plain decoding of one token per sequence.
+ * Same formula, types and rounding as tree_verify_attention; scale == 0 means 1/sqrt(D), negative scales are refused.
+ * q, out [B][T][Hq][D] contiguous, 16-byte aligned.  B <= 1024.  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such
+ * a sequence is left as it was.  MTV_ERR_BOUNDS: keys on pages that do not exist count as zero rows, out[b] is of no use.
+ * NaN or infinities in the K/V rows of nodes that a node does not see, and in rows behind the last node, do not reach its output.
+ * ws: tree_attention_paged_workspace_bytes, device, 256-byte aligned; nothing in it outlives the call.  Calls that share a
+ * workspace must not overlap on the device; calls that share a tree may. */
+size_t tree_attention_paged_workspace_bytes(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int shared_len);
+int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, const mtv_bf16 *q, const mtv_bf16 *k_pool,
+                                const mtv_bf16 *v_pool, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                                int shared_len, const int32_t *seq_lens, float scale, mtv_bf16 *out, int32_t *status,
+                                void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Constrained decoding: what a serving program lays over the base model's logits before a token is chosen (the paper chooses by
+ * the plain argmax).  For sequence b, node i, token v, with c = occurrences of v in b's generated text plus those on the path
+ * from the root to i (root and i included), seen = c > 0 or v in b's prompt:
+ *   x = logits[b][i][v] as fp32
+ *   seen:   x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *           x = x - frequency[b] * c
+ *   c > 0:  x = x - presence[b]
+ *           x = x + bias                 (the sum of v's entries in b's list, in the list's order)
+ *   bit v of the row's mask is 0:  -inf  (whatever the logit holds)
+ * each operation rounded to fp32 by itself.
+ * All pointers device; NULL fields leave their part out.  words = ceil(V / 32); bit v % 32 of word v / 32 stands for token v.
+ *   counts [B][V], seen [B][words]: the text so far, without the tree's tokens (both or neither).  Bit 31 of a count:
+ *     v is in the prompt; lower bits: generated occurrences.  A token whose bit in `seen` is 0 counts as never seen.
+ *     token_counts_add keeps the two; a new sequence starts from zeros.
+ *   repetition, presence, frequency [B] fp32 (NULL: 1, 0, 0)
+ *   bias_ids [B][n_bias] int32, bias [B][n_bias] fp32: ids outside [0, V) are padding; n_bias <= 4096
+ *   mask [n_masks][words], mask_of [B][T] int32: the row's mask, negative for none.  An index >= n_masks counts as none and
+ *     sets the tree's device error word to MTV_ERR_BOUNDS.
+ */
+typedef struct {
+    const uint32_t *counts, *seen;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_ids;
+    const float *bias;
+    const uint32_t *mask;
+    const int32_t *mask_of;
+    int32_t n_bias, n_masks;
+} mtv_logit_rules;
+
+#define MTV_LOGITS_BF16 0
+#define MTV_LOGITS_F32 1
+
+/* The constrained logits, rounded once to the logits' type.  logits, out: row b*T + i at (b*T + i) * stride elements, stride >= V (what lies
+ * between rows is left alone); out may be logits itself (then with the same stride), otherwise the two must not overlap.
+ * tree_tok [B][T] or NULL: no path is counted.  A tree of its root alone: one row per sequence. */
+int logits_constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t stride_in, void *out,
+                     int64_t stride_out, const mtv_logit_rules *rules, const int32_t *tree_tok, void *stream);
+
+/* The argmax of the same values, never stored: keys [B*T] for tree_accept_keys, in the form of lm_head_argmax (compared in fp32;
+ * ties: lowest v; NaN is never chosen).  A row that has no token left (its mask allows none) gets the key 0: its argmax reads -1,
+ * which no drafted token equals, and next_root is -1 if the acceptance ends there. */
+int constrained_argmax_keys(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t stride_in,
+                            const mtv_logit_rules *rules, const int32_t *tree_tok, unsigned long long *keys, void *stream);
+
+/* Adds tokens [B][n] (the first lens[b] of row b; lens NULL: all) to counts and seen: prompt != 0 marks them as the prompt's, else each is
+ * one more generated occurrence.  Tokens outside [0, V) are skipped: acc_tok of an acceptance goes in as it is (n = K + 1). */
+int token_counts_add(int B, int V, int n, const int32_t *tokens, const int32_t *lens, int prompt, uint32_t *counts,
+                     uint32_t *seen, void *stream);
 
 /* ---------------------------------------------------------------------------
  * Measurement aid (the paper has no counterpart): per-kernel device timing.

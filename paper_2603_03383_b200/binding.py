@@ -32,7 +32,9 @@ EXPORTS = ["tree_build_static", "tree_gen_cartesian", "tree_gen_rank_prior", "tr
            "tree_accept_static_scratch", "tree_accept_static_scratch_capacity", "tree_kv_append_rope",
            "lm_head_argmax", "tree_accept_keys", "mtv_selftest_wait_timeout", "tree_kv_append_rope_layers",
            "mtv_verify_steps", "mtv_debug_bounds_enabled", "heads_merge_shards", "attn_interleave_shards",
-           "keys_merge_shards", "node_argmax_keys"]
+           "keys_merge_shards", "node_argmax_keys", "tree_kv_append_rope_paged", "kv_append_rope_paged",
+           "kv_compact_accepted_paged", "tree_attention_paged_workspace_bytes", "tree_verify_attention_paged",
+           "logits_constrain", "constrained_argmax_keys", "token_counts_add"]
 
 
 class MtvError(RuntimeError):
@@ -74,6 +76,16 @@ class StepArgs(C.Structure):
 
 class AppendArgs(C.Structure):
     _fields_ = [("k_new_layers", C.c_void_p), ("v_new_layers", C.c_void_p), ("rope_theta", C.c_float)]
+
+
+class PoolLayout(C.Structure):
+    _fields_ = [("stride_page", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class LogitRules(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("counts", "seen", "repetition", "presence", "frequency", "bias_ids", "bias",
+                                          "mask", "mask_of")] + [("n_bias", C.c_int32), ("n_masks", C.c_int32)]
 
 
 _lib = None
@@ -120,6 +132,18 @@ def lib():
         L.attn_interleave_shards.argtypes = [i32, i32, i32, i32, vp, vp, vp]
         L.keys_merge_shards.argtypes = [i32, i32, i32, vp, vp, vp]
         L.node_argmax_keys.argtypes = [vp, i32, i32, vp, vp, vp, sz, vp]
+        pool = C.POINTER(PoolLayout)
+        L.tree_kv_append_rope_paged.argtypes = [vp, i32, i32, i32, i32, i32] + [vp] * 6 + [pool, vp, i32, vp, C.c_float, vp, vp]
+        L.kv_append_rope_paged.argtypes = [i32] * 6 + [vp] * 6 + [pool, vp, i32, vp, vp, C.c_float, vp, vp]
+        L.kv_compact_accepted_paged.argtypes = [vp, i32, i32, i32, i32, vp, vp, pool, vp, i32] + [vp] * 6
+        L.tree_attention_paged_workspace_bytes.argtypes = [vp] + [i32] * 5
+        L.tree_attention_paged_workspace_bytes.restype = sz
+        L.tree_verify_attention_paged.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, pool, vp, i32, i32, vp, C.c_float, vp, vp,
+                                                  vp, sz, vp]
+        rules = C.POINTER(LogitRules)
+        L.logits_constrain.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, rules, vp, vp]
+        L.constrained_argmax_keys.argtypes = [vp, i32, i32, i32, vp, i64, rules, vp, vp, vp]
+        L.token_counts_add.argtypes = [i32, i32, i32, vp, vp, i32, vp, vp, vp]
         L.mtv_verify_steps.argtypes = [vp, C.POINTER(StepArgs), C.POINTER(AppendArgs), i32, vp]
         _lib = L
     return _lib
@@ -366,6 +390,112 @@ def mtv_verify_steps(tree, steps: Sequence[StepArgs], appends: Optional[Sequence
 def mtv_verify_step_host(tree, dev: StepArgs, host: StepArgs, stream=None):
     _check(lib().mtv_verify_step_host(tree.handle, C.byref(dev), C.byref(host), _stream(stream)),
            "mtv_verify_step_host")
+
+
+# ------------------------------------------------------------------------------------- caches in pages
+def pool_layout(pool: torch.Tensor) -> PoolLayout:
+    """Layout of a pool tensor [n_pages][Hkv][page_size][D] of any strides with the columns innermost (a pool whose pages hold
+    [page_size][Hkv][D] is passed as its transposed view)."""
+    assert pool.dim() == 4 and pool.stride(3) == 1
+    sp, sh, st = pool.stride()[:3]
+    return PoolLayout(sp, sh, st, pool.shape[2], pool.shape[0])
+
+
+def tree_kv_append_rope_paged(tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table,
+                              seq_lens, rope_theta=0.0, status=None, stream=None):
+    """q_layers, q_out_layers [n_layers][B][T][Hq][D], k_new_layers / v_new_layers [n_layers][B][T][Hkv][D]; k_ptrs / v_ptrs: device
+    arrays of the layers' pools (cache_pointer_array); page_table [B][max_pages]."""
+    n_layers, B, T, Hq, D = q_layers.shape
+    _check(lib().tree_kv_append_rope_paged(tree.handle, B, Hq, k_new_layers.shape[3], D, n_layers, _ptr(q_layers), _ptr(q_out_layers),
+                                           _ptr(k_new_layers), _ptr(v_new_layers), _ptr(k_ptrs), _ptr(v_ptrs), pool,
+                                           _ptr(page_table), page_table.shape[1], _ptr(seq_lens), rope_theta, _ptr(status),
+                                           _stream(stream)), "tree_kv_append_rope_paged")
+
+
+def kv_append_rope_paged(q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table, seq_lens,
+                         row_starts, rope_theta=0.0, status=None, stream=None):
+    """q_layers, q_out_layers [n_layers][n_rows][Hq][D], k_new_layers / v_new_layers [n_layers][n_rows][Hkv][D]; row_starts [B+1]."""
+    n_layers, n_rows, Hq, D = q_layers.shape
+    _check(lib().kv_append_rope_paged(page_table.shape[0], n_rows, Hq, k_new_layers.shape[2], D, n_layers, _ptr(q_layers), _ptr(q_out_layers),
+                                      _ptr(k_new_layers), _ptr(v_new_layers), _ptr(k_ptrs), _ptr(v_ptrs), pool,
+                                      _ptr(page_table), page_table.shape[1], _ptr(seq_lens), _ptr(row_starts), rope_theta,
+                                      _ptr(status), _stream(stream)), "kv_append_rope_paged")
+
+
+def kv_compact_accepted_paged(tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool: PoolLayout, page_table, seq_lens, new_lens, accept_len,
+                              acc_nodes, status=None, stream=None):
+    """new_lens may be seq_lens itself."""
+    B, max_pages = page_table.shape
+    _check(lib().kv_compact_accepted_paged(tree.handle, B, Hkv, D, n_layers, _ptr(k_ptrs), _ptr(v_ptrs), pool,
+                                           _ptr(page_table), max_pages, _ptr(seq_lens), _ptr(new_lens), _ptr(accept_len),
+                                           _ptr(acc_nodes), _ptr(status), _stream(stream)), "kv_compact_accepted_paged")
+
+
+def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
+    """Bytes of device scratch of tree_verify_attention_paged (0: sizes that it refuses)."""
+    return lib().tree_attention_paged_workspace_bytes(tree.handle, B, Hq, Hkv, D, shared_len)
+
+
+def tree_verify_attention_paged(tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len=0, scale=0.0, status=None,
+                                stream=None):
+    """q, out [B][T][Hq][D]; k_pool, v_pool [n_pages][Hkv][page_size][D] (see pool_layout), the same strides."""
+    B, T, Hq, D = q.shape
+    pool = pool_layout(k_pool)
+    assert v_pool.shape == k_pool.shape and v_pool.stride() == k_pool.stride()
+    _check(lib().tree_verify_attention_paged(tree.handle, B, Hq, k_pool.shape[1], D, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                             pool, page_table.data_ptr(), page_table.shape[1], shared_len,
+                                             seq_lens.data_ptr(), scale, out.data_ptr(), _ptr(status), ws.data_ptr(), ws.nbytes,
+                                             _stream(stream)), "tree_verify_attention_paged")
+
+
+# ------------------------------------------------------------------------------------- constrained decoding
+def logit_rules(counts=None, seen=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias=None, mask=None,
+                mask_of=None) -> LogitRules:
+    """counts [B][V], seen [B][words], repetition / presence / frequency [B] fp32, bias_ids / bias [B][n], mask [n_masks][words],
+    mask_of [B][T]; words of 32 tokens in int32 storage (see include/mtv.h).  The tensors have to outlive the rules' use."""
+    r = LogitRules(*[_ptr(t) for t in (counts, seen, repetition, presence, frequency, bias_ids, bias, mask, mask_of)])
+    r.n_bias = 0 if bias_ids is None else bias_ids.shape[-1]
+    r.n_masks = 0 if mask is None else mask.shape[0]
+    r.tensors = (counts, seen, repetition, presence, frequency, bias_ids, bias, mask, mask_of)
+    return r
+
+
+_LOGIT_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _logit_rows(x, where):
+    """(type, row stride) of logits [B][T][V] with rows at even distances; anything else is refused."""
+    B, T, V = x.shape
+    sb, st, sv = x.stride()
+    if (V > 1 and sv != 1) or (B > 1 and T > 1 and sb != T * st) or x.dtype not in _LOGIT_TYPES:
+        raise MtvError(-1, where)
+    return _LOGIT_TYPES[x.dtype], st if T > 1 else sb if B > 1 else V
+
+
+def logits_constrain(tree, logits, out, rules: LogitRules, tree_tok=None, stream=None):
+    """logits, out [B][T][V], bf16 or fp32, rows evenly spaced; out may be logits."""
+    B, T, V = logits.shape
+    dtype, stride = _logit_rows(logits, "logits_constrain")
+    dtype_out, stride_out = _logit_rows(out, "logits_constrain")
+    if out.shape != logits.shape or dtype_out != dtype:
+        raise MtvError(-1, "logits_constrain")
+    _check(lib().logits_constrain(tree.handle, B, V, dtype, _ptr(logits), stride, _ptr(out), stride_out, rules, _ptr(tree_tok),
+                                  _stream(stream)), "logits_constrain")
+
+
+def constrained_argmax_keys(tree, logits, keys, rules: LogitRules, tree_tok=None, stream=None):
+    """logits [B][T][V], bf16 or fp32, rows evenly spaced -> keys [B*T] (int64 storage of the uint64 keys)."""
+    B, T, V = logits.shape
+    dtype, stride = _logit_rows(logits, "constrained_argmax_keys")
+    _check(lib().constrained_argmax_keys(tree.handle, B, V, dtype, _ptr(logits), stride, rules, _ptr(tree_tok), _ptr(keys),
+                                         _stream(stream)), "constrained_argmax_keys")
+
+
+def token_counts_add(tokens, counts, seen, lens=None, prompt=False, stream=None):
+    """tokens [B][n] -> counts [B][V], seen [B][words]."""
+    B, n = tokens.shape
+    _check(lib().token_counts_add(B, counts.shape[1], n, _ptr(tokens), _ptr(lens), 1 if prompt else 0, _ptr(counts), _ptr(seen),
+                                  _stream(stream)), "token_counts_add")
 
 
 KERNELS = ["heads_resblock", "heads_vocab_topk", "heads_merge", "attn_partial", "attn_combine",

@@ -1,0 +1,369 @@
+// Penalties for repeated tokens, biases and grammar masks on the base model's logits at the tree's nodes, in front of the acceptance
+// (Section 3.2; the paper accepts on the plain argmax).  For row (b, i) and token v, with c = occurrences of v in sequence b's generated
+// text and on the path from the root to node i, seen = c > 0 or v in the prompt:
+//   x = logit;  seen: x = x > 0 ? x / repetition : x * repetition;  x = x - frequency * c;  c > 0: x = x - presence;
+//   x = x + bias;  not allowed by the row's mask: -inf
+// every operation rounded to fp32 by itself (no contraction), so that equal inputs give equal keys whatever the order they are met in.
+//
+// Bound by memory: the logits are read once (and written once in the form that writes).  What a token was counted, and whether it is
+// allowed, are bits (1/16 of the logits' bytes per sequence, 1/16 per mask); only the few tokens that are counted, biased or on
+// the path go through the formula.  A block takes a slab of the vocabulary for some of a sequence's nodes.  It first lists the slab's counted and
+// biased tokens once; a warp then takes a row's unit of 1024 tokens: a dense pass over those that are allowed and in no list (16-byte
+// loads, maximum or copy), and a sparse one over the lists.  Rows may begin at any element: vectors are cut at the addresses' 16-byte
+// boundaries, and the two that a unit shares with its neighbours are taken element by element.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace mtv {
+
+constexpr int CN_THREADS = 128, CN_WARPS = CN_THREADS / 32;
+constexpr int CN_UNIT = 1024, CN_WORDS = CN_UNIT / 32;
+constexpr int CN_SUBS = 2, CN_SLAB = CN_SUBS * CN_UNIT;
+constexpr int CN_PATH = MTV_MAX_K + 1;
+constexpr int CN_MAX_BIAS = 4096;
+constexpr uint32_t CN_PROMPT = 0x80000000u;
+
+struct ConstrainParams {
+    const void *logits;
+    void *out;                       // or null: keys
+    int64_t ld_in, ld_out;           // elements from row to row
+    unsigned long long *keys;        // [B*T], zero before the launch
+    const uint32_t *counts, *seen;   // [B][V], [B][words], or null
+    const float *repetition, *presence, *frequency;   // [B] or null
+    const int32_t *bias_ids;         // [B][n_bias]
+    const float *bias;
+    const uint32_t *mask;            // [n_masks][words]
+    const int32_t *mask_of;          // [B*T] or null
+    const int32_t *tree_tok;         // [B][T] or null
+    const uint64_t *anc;             // [T][2]
+    int32_t *dev_error;
+    int T, V, words, n_bias, n_masks, rows_per_block;
+};
+
+template <typename E> struct Elem;
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr int VEC = 8;
+    static __device__ __forceinline__ float get(const __nv_bfloat16 *p) { return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16); }
+    static __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+    static __device__ __forceinline__ float at(const uint4 &u, int e) {
+        const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    }
+    // what is not in `bits` becomes -inf
+    static __device__ __forceinline__ uint4 masked(uint4 u, uint32_t bits) {
+        uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!(bits >> (2 * k) & 1)) w[k] = (w[k] & 0xffff0000u) | 0xff80u;
+            if (!(bits >> (2 * k + 1) & 1)) w[k] = (w[k] & 0xffffu) | 0xff800000u;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Elem<float> {
+    static constexpr int VEC = 4;
+    static __device__ __forceinline__ float get(const float *p) { return *p; }
+    static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
+    static __device__ __forceinline__ float at(const uint4 &u, int e) { return __uint_as_float(e == 0 ? u.x : e == 1 ? u.y : e == 2 ? u.z : u.w); }
+    static __device__ __forceinline__ uint4 masked(uint4 u, uint32_t bits) {
+        return make_uint4(bits & 1 ? u.x : 0xff800000u, bits & 2 ? u.y : 0xff800000u, bits & 4 ? u.z : 0xff800000u, bits & 8 ? u.w : 0xff800000u);
+    }
+};
+
+// Order-preserving image of a value that is no NaN; both zeros are one.
+__device__ __forceinline__ uint32_t value_image(float v) {
+    const uint32_t u = __float_as_uint(v);
+    return v == 0.f ? 0x80000000u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct Penalties {
+    float r, p, f;
+    __device__ __forceinline__ float apply(float x, int c, bool seen, float bias) const {
+        if (seen) x = x > 0.f ? __fdiv_rn(x, r) : __fmul_rn(x, r);
+        x = __fsub_rn(x, __fmul_rn(f, (float)c));
+        if (c > 0) x = __fsub_rn(x, p);
+        return __fadd_rn(x, bias);
+    }
+};
+
+template <typename E, bool WRITE>
+__global__ void __launch_bounds__(CN_THREADS)
+constrain_kernel(const ConstrainParams p) {
+    using El = Elem<E>;
+    constexpr int VEC = El::VEC;
+    __shared__ uint32_t listed[CN_SUBS][CN_WORDS], biased[CN_SUBS][CN_WORDS], allowed_of[CN_WARPS][CN_WORDS + 1], dense_of[CN_WARPS][CN_WORDS + 1];
+    __shared__ uint32_t list_count[CN_SUBS][CN_UNIT];
+    __shared__ float list_bias[CN_SUBS][CN_UNIT];
+    __shared__ uint16_t list_at[CN_SUBS][CN_UNIT];
+    __shared__ int n_list[CN_SUBS];
+    __shared__ int32_t path[MTV_MAX_T][CN_PATH];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int b = blockIdx.z, slab = (int)blockIdx.x * CN_SLAB, row0 = (int)blockIdx.y * p.rows_per_block;
+    const int n_rows = min(p.rows_per_block, p.T - row0);
+    let_next_start();
+    previous_done();
+    // ---- the slab's counted and biased tokens, and the path of every row
+    if (tid < CN_SUBS * CN_WORDS) {
+        const int w = slab / 32 + tid;
+        listed[tid / CN_WORDS][tid % CN_WORDS] = p.seen && w < p.words ? p.seen[(size_t)b * p.words + w] : 0u;
+        biased[tid / CN_WORDS][tid % CN_WORDS] = 0u;
+    }
+    if (tid < CN_WARPS) allowed_of[tid][CN_WORDS] = dense_of[tid][CN_WORDS] = 0u;
+    for (int r = tid; r < n_rows; r += CN_THREADS) {
+        int n = 0;
+        if (p.tree_tok)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                for (uint64_t bits = p.anc[(row0 + r) * 2 + h]; bits && n < CN_PATH; bits &= bits - 1)
+                    path[r][n++] = p.tree_tok[(size_t)b * p.T + h * 64 + __ffsll((long long)bits) - 1];
+        while (n < CN_PATH) path[r][n++] = -1;
+    }
+    __syncthreads();
+    for (int k = tid; k < p.n_bias; k += CN_THREADS) {
+        const int v = p.bias_ids[(size_t)b * p.n_bias + k];
+        if (v >= slab && v - slab < CN_SLAB && v < p.V) {
+            const int at = v - slab;
+            atomicOr(&listed[at / CN_UNIT][at % CN_UNIT / 32], 1u << (at % 32));
+            atomicOr(&biased[at / CN_UNIT][at % CN_UNIT / 32], 1u << (at % 32));
+        }
+    }
+    __syncthreads();
+    if (warp < CN_SUBS) {
+        uint32_t w = listed[warp][lane];
+        const int mine = __popc(w);
+        int before = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += x;
+        }
+        if (lane == 31) n_list[warp] = before;
+        before -= mine;
+        for (; w; w &= w - 1) list_at[warp][before++] = (uint16_t)(lane * 32 + __ffs((int)w) - 1);
+    }
+    __syncthreads();
+    for (int s = 0; s < CN_SUBS; ++s)
+        for (int e = tid; e < n_list[s]; e += CN_THREADS) {
+            const int at = list_at[s][e], v = slab + s * CN_UNIT + at;
+            float sum = 0.f;
+            if (biased[s][at / 32] >> (at % 32) & 1)
+                for (int k = 0; k < p.n_bias; ++k)          // a token that is named more than once: in the list's order
+                    if (p.bias_ids[(size_t)b * p.n_bias + k] == v) sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + k]);
+            list_bias[s][e] = sum;
+            list_count[s][e] = p.counts && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
+        }
+    __syncthreads();
+    const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
+    // ---- rows: a warp per unit of 1024 tokens
+    for (int u = warp; u < n_rows * CN_SUBS; u += CN_WARPS) {
+        const int r = u / CN_SUBS, s = u % CN_SUBS, base = slab + s * CN_UNIT;
+        const int n_tok = min(CN_UNIT, p.V - base);
+        if (n_tok <= 0) continue;
+        const size_t row = (size_t)b * p.T + row0 + r;
+        const E *in = static_cast<const E *>(p.logits) + (int64_t)row * p.ld_in + base;
+        E *out = WRITE ? static_cast<E *>(p.out) + (int64_t)row * p.ld_out + base : nullptr;
+        int m = p.mask_of ? p.mask_of[row] : -1;
+        if (m >= p.n_masks) {
+            if (lane == 0) atomicExch(p.dev_error, MTV_ERR_BOUNDS);
+            m = -1;
+        }
+        uint32_t allowed = 0u;
+        if (lane * 32 < n_tok) {
+            allowed = m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + lane] : 0xffffffffu;
+            if (n_tok - lane * 32 < 32) allowed &= (1u << (n_tok - lane * 32)) - 1u;
+        }
+        int here = lane < CN_PATH ? path[r][lane] - base : -1;       // this lane's token of the path, where it lies in this unit
+        if (here < 0 || here >= n_tok) here = -1;
+        uint32_t dense = allowed & ~listed[s][lane];
+        for (uint32_t some = __ballot_sync(0xffffffffu, here >= 0); some; some &= some - 1) {
+            const int at = __shfl_sync(0xffffffffu, here, __ffs((int)some) - 1);
+            if (lane == at / 32) dense &= ~(1u << (at % 32));
+        }
+        allowed_of[warp][lane] = allowed;
+        dense_of[warp][lane] = dense;
+        __syncwarp();
+        const uint32_t *words = WRITE ? allowed_of[warp] : dense_of[warp];
+        // the vectors of the row's addresses: vector j holds tokens [j * VEC - off, (j + 1) * VEC - off) of the unit
+        const int off = (int)((uintptr_t)in / sizeof(E) % VEC);
+        const bool out_vec = WRITE && (int)((uintptr_t)out / sizeof(E) % VEC) == off;
+        const int n_vec = (off + n_tok + VEC - 1) / VEC;
+        float best = -INFINITY;
+        int at = -1;
+        bool low = false;        // an allowed -inf was met
+        auto one = [&](int t, float x) {
+            if (x > best || (x == best && t < at)) { best = x; at = t; }
+            low = low || x == -INFINITY;
+        };
+        auto vec_of = [&](int j, const uint4 &x) {
+            const int t0 = j * VEC - off;
+            const uint32_t bits = __funnelshift_r(words[t0 >> 5], words[(t0 >> 5) + 1], t0 & 31);
+            if (WRITE) {
+                const uint4 y = El::masked(x, bits);
+                if (out_vec) {
+                    *reinterpret_cast<uint4 *>(out + t0) = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) out[t0 + e] = reinterpret_cast<const E *>(&y)[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float v = El::at(x, e);
+                    if (bits >> e & 1) {
+                        if (v > best) { best = v; at = t0 + e; }
+                        low = low || v == -INFINITY;
+                    }
+                }
+            }
+        };
+        auto whole = [&](int j) { return j * VEC >= off && (j + 1) * VEC - off <= n_tok; };
+        for (int j0 = lane; j0 < n_vec; j0 += 32 * 4) {
+            uint4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (j0 + 32 * k < n_vec && whole(j0 + 32 * k)) x[k] = *reinterpret_cast<const uint4 *>(in + ((j0 + 32 * k) * VEC - off));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = j0 + 32 * k;
+                if (j >= n_vec) continue;
+                if (whole(j)) {
+                    vec_of(j, x[k]);
+                } else {
+                    for (int t = max(0, j * VEC - off); t < min(n_tok, (j + 1) * VEC - off); ++t) {
+                        const bool on = words[t >> 5] >> (t & 31) & 1;
+                        if (WRITE) {
+                            if (on) out[t] = in[t];
+                            else El::put(out + t, -INFINITY);
+                        } else if (on) {
+                            one(t, El::get(in + t));
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        // ---- listed tokens, then those of the path that are in no list
+        auto special = [&](int t, uint32_t counted, float bias) {
+            int c = (int)(counted & ~CN_PROMPT);
+            for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
+            const float x = pen.apply(El::get(in + t), c, c > 0 || counted & CN_PROMPT, bias);
+            if (WRITE) El::put(out + t, x);
+            else one(t, x);
+        };
+        for (int e = lane; e < n_list[s]; e += 32) {
+            const int t = list_at[s][e];
+            if (allowed_of[warp][t / 32] >> (t % 32) & 1) special(t, list_count[s][e], list_bias[s][e]);
+        }
+        if (here >= 0 && (allowed_of[warp][here / 32] >> (here % 32) & 1) && !(listed[s][here / 32] >> (here % 32) & 1)) {
+            bool first = true;          // the same token twice on a path: once
+            for (int k = 0; k < lane; ++k) first = first && path[r][k] != base + here;
+            if (first) special(here, 0u, 0.f);
+        }
+        if (!WRITE) {
+            // -inf alone: the first allowed one (its value is in no comparison above)
+            const bool any = __any_sync(0xffffffffu, at >= 0);
+            if (any || __any_sync(0xffffffffu, low)) {
+                if (!any) {
+                    for (int t = lane; t < n_tok && at < 0; t += 32)
+                        if (allowed_of[warp][t / 32] >> (t % 32) & 1) {
+                            int c = 0, bit = listed[s][t / 32] >> (t % 32) & 1;
+                            float x = El::get(in + t);
+                            for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
+                            if (bit || c) {
+                                float bias = 0.f;
+                                uint32_t counted = 0u;
+                                for (int e = 0; bit && e < n_list[s]; ++e)
+                                    if (list_at[s][e] == t) { bias = list_bias[s][e]; counted = list_count[s][e]; }
+                                c += (int)(counted & ~CN_PROMPT);
+                                x = pen.apply(x, c, c > 0 || counted & CN_PROMPT, bias);
+                            }
+                            if (x == -INFINITY) at = t;
+                        }
+                }
+                const uint32_t image = at >= 0 ? value_image(best) : 0u;
+                const uint32_t top = __reduce_max_sync(0xffffffffu, image);
+                const uint32_t first = __reduce_min_sync(0xffffffffu, at >= 0 && image == top ? (uint32_t)(base + at) : 0xffffffffu);
+                if (lane == 0) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - first));
+            }
+        }
+        __syncwarp();       // before the next unit's bits
+    }
+}
+
+// ---------------------------------------------------------------------------------------- counts
+// grid = (chunks of tokens, B).  Integer atomics: the order does not matter.
+__global__ void __launch_bounds__(256)
+token_counts_add_kernel(int V, int words, int n, int prompt, const int32_t *__restrict__ tokens, const int32_t *__restrict__ lens,
+                        uint32_t *counts, uint32_t *seen) {
+    let_next_start();
+    previous_done();
+    const int b = blockIdx.y, i = (int)blockIdx.x * 256 + threadIdx.x;
+    const int end = lens ? min(lens[b], n) : n;
+    if (i >= end) return;
+    const int v = tokens[(size_t)b * n + i];
+    if (v < 0 || v >= V) return;
+    if (prompt) atomicOr(counts + (size_t)b * V + v, CN_PROMPT);
+    else atomicAdd(counts + (size_t)b * V + v, 1u);
+    atomicOr(seen + (size_t)b * words + v / 32, 1u << (v % 32));
+}
+
+static int constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t ld_in, void *out, int64_t ld_out,
+                     unsigned long long *keys, const mtv_logit_rules *rules, const int32_t *tree_tok, cudaStream_t stream) {
+    if (!tree || !tree->on_device || !logits || !rules || (!out && !keys) || B < 1 || V < 1) return MTV_ERR_INVALID_ARG;
+    if (dtype != MTV_LOGITS_BF16 && dtype != MTV_LOGITS_F32) return MTV_ERR_INVALID_ARG;
+    const size_t size = dtype == MTV_LOGITS_BF16 ? 2 : 4;
+    if (ld_in < V || (out && ld_out < V) || (uintptr_t)logits % size || (uintptr_t)out % size) return MTV_ERR_INVALID_ARG;
+    if (out == logits && ld_out != ld_in) return MTV_ERR_INVALID_ARG;
+    if (!rules->counts != !rules->seen || rules->n_bias < 0 || rules->n_masks < 0) return MTV_ERR_INVALID_ARG;
+    if (rules->n_bias > 0 && (!rules->bias_ids || !rules->bias)) return MTV_ERR_INVALID_ARG;
+    if (rules->n_masks > 0 && (!rules->mask || !rules->mask_of)) return MTV_ERR_INVALID_ARG;
+    if (rules->n_bias > CN_MAX_BIAS || B > 65535 || V > 0x7fffffff - CN_SLAB) return MTV_ERR_UNSUPPORTED_SHAPE;
+    ConstrainParams p = {};
+    p.logits = logits; p.out = out; p.ld_in = ld_in; p.ld_out = ld_out; p.keys = keys;
+    p.counts = rules->counts; p.seen = rules->seen;
+    p.repetition = rules->repetition; p.presence = rules->presence; p.frequency = rules->frequency;
+    p.bias_ids = rules->bias_ids; p.bias = rules->bias; p.n_bias = rules->n_bias;
+    p.mask = rules->mask; p.mask_of = rules->n_masks > 0 ? rules->mask_of : nullptr; p.n_masks = rules->n_masks;
+    p.tree_tok = tree_tok; p.anc = tree->d_anc; p.dev_error = tree->d_error;
+    p.T = tree->T; p.V = V; p.words = (V + 31) / 32;
+    // every block lists its slab's tokens anew: as many rows to a block as leave about eight blocks per SM
+    const int slabs = (V + CN_SLAB - 1) / CN_SLAB;
+    long groups = (8L * sm_count() + (long)slabs * B - 1) / ((long)slabs * B);
+    groups = groups < 1 ? 1 : groups > p.T ? p.T : groups;
+    p.rows_per_block = (p.T + (int)groups - 1) / (int)groups;
+    const dim3 grid(slabs, (p.T + p.rows_per_block - 1) / p.rows_per_block, B);
+    if (keys) MTV_CUDA_CHECK(cudaMemsetAsync(keys, 0, (size_t)B * p.T * sizeof *keys, stream));
+    auto kernel = dtype == MTV_LOGITS_BF16 ? (keys ? constrain_kernel<__nv_bfloat16, false> : constrain_kernel<__nv_bfloat16, true>)
+                                           : (keys ? constrain_kernel<float, false> : constrain_kernel<float, true>);
+    MTV_CUDA_CHECK(launch_dependent(kernel, grid, CN_THREADS, 0, stream, p));
+    return MTV_OK;
+}
+
+}  // namespace mtv
+
+extern "C" int logits_constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t stride_in, void *out,
+                                int64_t stride_out, const mtv_logit_rules *rules, const int32_t *tree_tok, void *stream) {
+    MTV_RANGE("logits_constrain");
+    if (!out) return MTV_ERR_INVALID_ARG;
+    return mtv::constrain(tree, B, V, dtype, logits, stride_in, out, stride_out, nullptr, rules, tree_tok, (cudaStream_t)stream);
+}
+
+extern "C" int constrained_argmax_keys(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t stride_in,
+                                       const mtv_logit_rules *rules, const int32_t *tree_tok, unsigned long long *keys, void *stream) {
+    MTV_RANGE("constrained_argmax_keys");
+    if (!keys || (uintptr_t)keys % 8) return MTV_ERR_INVALID_ARG;
+    return mtv::constrain(tree, B, V, dtype, logits, stride_in, nullptr, 0, keys, rules, tree_tok, (cudaStream_t)stream);
+}
+
+extern "C" int token_counts_add(int B, int V, int n, const int32_t *tokens, const int32_t *lens, int prompt, uint32_t *counts, uint32_t *seen,
+                                void *stream) {
+    using namespace mtv;
+    MTV_RANGE("token_counts_add");
+    if (B < 1 || V < 1 || n < 0 || (n > 0 && !tokens) || !counts || !seen) return MTV_ERR_INVALID_ARG;
+    if (B > 65535) return MTV_ERR_UNSUPPORTED_SHAPE;
+    if (n == 0) return MTV_OK;
+    MTV_CUDA_CHECK(launch_dependent(token_counts_add_kernel, dim3((n + 255) / 256, B), 256, 0, (cudaStream_t)stream, V, (V + 31) / 32, n, prompt ? 1 : 0,
+                                    tokens, lens, counts, seen));
+    return MTV_OK;
+}
