@@ -406,7 +406,7 @@ int keys_merge_shards(int n, int n_shards, int v_slab, const unsigned long long 
  *                  page*stride_page + head*stride_h + row*stride_t + d: heads inside a page or rows, as the strides say
  *   page_table     device [B][max_pages] int32: slot s of sequence b is row s % page_size of page page_table[b][s / page_size];
  *                  entries behind a sequence's last slot are never followed
- * page_size: a power of two from 16 to 65536; strides multiples of 8, stride_t >= D; pool base addresses 16-byte aligned;
+ * page_size: a power of two from 16 to 65536; strides multiples of 8 and at least D; pool base addresses 16-byte aligned;
  * max_pages * page_size below 2^31 - 256.  Sequences may share pages that a call only reads; two sequences of a call that
  * write rows of the same page race.
  * status[b] of the calls below: MTV_OK; MTV_ERR_CAPACITY if seq_lens[b] is negative or the rows do not fit max_pages;
@@ -448,7 +448,8 @@ int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int
 /* tree_verify_attention over such a cache, one layer.  The first shared_len slots of all sequences are the same keys — their
  * page-table rows name the same pages there, or pages with the same content; row 0's are read — and are attended to once for the
  * whole batch: the query rows of all sequences meet each of those keys together, the sequences' own keys follow, and the parts
- * are joined.  shared_len: a multiple of page_size (0: nothing is shared), at most every seq_lens[b].
+ * are joined.  shared_len: a multiple of page_size (0: nothing is shared), at most every seq_lens[b]
+ * and max_pages * page_size.
  * A tree of its root alone is plain decoding of one token per sequence.
  * Same formula, types and rounding as tree_verify_attention; scale == 0 means 1/sqrt(D), negative scales are refused.
  * q, out [B][T][Hq][D] contiguous, 16-byte aligned.  B <= 1024.  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such

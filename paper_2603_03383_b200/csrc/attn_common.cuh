@@ -51,5 +51,7 @@ __device__ __forceinline__ int ld_acquire(const int32_t *p) {
 // of those already encoded.
 bool tensor_map_bf16(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes,
                      const cuuint32_t *box);
+// The same, encoded anew.
+bool encode_map_bf16(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes, const cuuint32_t *box);
 
 }  // namespace mtv

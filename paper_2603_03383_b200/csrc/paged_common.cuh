@@ -36,7 +36,7 @@ struct PagedRef {
 static inline int paged_ref(PagedRef &r, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages, int D) {
     if (!pool || !page_table || max_pages < 1 || pool->n_pages < 1) return MTV_ERR_INVALID_ARG;
     if (pool->page_size < 16 || pool->page_size > 65536 || (pool->page_size & (pool->page_size - 1))) return MTV_ERR_UNSUPPORTED_SHAPE;
-    if (pool->stride_page % 8 || pool->stride_h % 8 || pool->stride_t % 8 || pool->stride_t < D || pool->stride_h < 0 || pool->stride_page < 0)
+    if (pool->stride_page % 8 || pool->stride_h % 8 || pool->stride_t % 8 || pool->stride_t < D || pool->stride_h < D || pool->stride_page < D)
         return MTV_ERR_INVALID_ARG;
     r.table = page_table;
     r.stride_page = pool->stride_page; r.stride_h = pool->stride_h; r.stride_t = pool->stride_t;
