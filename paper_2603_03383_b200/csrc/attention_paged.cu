@@ -12,22 +12,28 @@
 // beside it is written out directly.
 //
 // One persistent CTA per SM.  Both phases keep two row tiles in flight, each with its own scores S / weights P and accumulator O in tensor
-// memory and its own four softmax warps (a thread per row): while the tensor core works for one, the other's exponentials are
-// taken.  In the phase of pairs the two tiles are those of an item and share K and V; in the other the CTA is two workers, whose K and V
-// take turns in one ring.  Warp 8 issues all products, in the order  O_0 += P_0 V, S_0 = Q_0 K, O_1 += P_1 V, S_1 = Q_1 K  with S one key
-// tile ahead of O: products of one thread are executed in order, so S may overwrite the P that the product in front of it reads, and
-// "S is complete" implies that O is complete up to the tile before.  Warp 9 requests Q, K and V (a box per page); warp 10 clears V rows behind
-// the last key (their weight is 0, but 0 * NaN is not) and takes non-finite values of the tree's V rows out (they are given to the rows that see
-// them at the end); warp 11 reports the sequences' status.
+// memory and its own eight softmax warps (two threads per row, 64 columns each): while the tensor core works for one, the other's
+// exponentials are taken.  In the phase of pairs the two tiles are those of an item and share K and V; in the other the CTA is two workers,
+// whose K and V take turns in one ring.
+//   warps 0-7 / 8-15  softmax of row tile 0 / 1
+//   warp 16           issues all products, in the order  O_0 += P_0 V, S_0 = Q_0 K, O_1 += P_1 V, S_1 = Q_1 K  with S one key tile ahead of O:
+//                     products of one thread are executed in order, so S may overwrite the P that the product in front of it reads,
+//                     and "S is complete" implies that O is complete up to the tile before
+//   warp 17           requests Q, K and V (a box per page)
+//   warp 18           clears V rows behind the last key (their weight is 0, but 0 * NaN is not) and takes non-finite values of the tree's
+//                     V rows out (they are given to the rows that see them at the end)
+//   warp 19           derives the pieces from the lengths and hands them to the other warps; reports the sequences' status
 //
-// The running maximum moves only when a tile's exceeds it by more than 8 (log2 units): O is rescaled rarely and P stays below 2^8.
+// The running maximum moves only when a tile's exceeds it by more than 8 (log2 units): O is rescaled rarely, P stays below 2^8, and the two
+// threads of a row exchange their maxima (through tensor memory) only then; otherwise a vote says that nobody needs it.
 #include "attn_common.cuh"
 #include "paged_common.cuh"
 
 namespace mtv {
 
-constexpr int PA_THREADS = 384;
-constexpr int PA_MMA_WARP = 8, PA_TMA_WARP = 9, PA_CLEAN_WARP = 10, PA_STATUS_WARP = 11;
+constexpr int PA_THREADS = 640;
+constexpr int PA_MMA_WARP = 16, PA_TMA_WARP = 17, PA_CLEAN_WARP = 18, PA_PLAN_WARP = 19;
+constexpr int PA_QUEUE = 4;               // pieces that are handed out ahead
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
 constexpr float PA_RESCALE = 8.f;
@@ -44,12 +50,15 @@ template <int D> struct PaSmem {
     static constexpr uint32_t IDESC_QK = IDESC | (128u >> 3) << 17;                               // N = 128 keys
     static constexpr uint32_t IDESC_PV = IDESC | (uint32_t)(D >> 3) << 17 | 1u << 16;             // N = D columns, B (= V) N-major
 };
-static_assert(sizeof(uint64_t) * (PA_MAX_B + 1) <= PaSmem<64>::OFF_RING, "the sequences' costs are summed in the query tiles' space");
 
 enum {
     PB_FULL = 0, PB_FREE = 10, PB_CLEAN = 20, PB_QFULL = 30, PB_QFREE = 32, PB_SREADY = 34, PB_PREADY = 36, PB_ODONE = 38, PB_FINAL = 40,
-    PB_COUNT = 41
+    PB_PIECE = 41,                         // [3 queues][PA_QUEUE]: pairs; single tiles of either half of the CTA
+    PB_TAKEN = PB_PIECE + 3 * PA_QUEUE,
+    PB_COUNT = PB_TAKEN + 3 * PA_QUEUE
 };
+constexpr uint32_t PA_OFF_MISC = PB_COUNT * 8, PA_OFF_QUEUE = (PA_OFF_MISC + 40 + 15) / 16 * 16;
+static_assert(PA_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1024, "barrier region");
 
 struct PaPhase {
     int prefix_items, seq_items;       // items of the prefix, and of each sequence
@@ -58,6 +67,7 @@ struct PaPhase {
     int workers, rows;                 // at most; rows of a slot
     float *o;                          // [slots][D / 8][rows][8]
     float2 *ml;                        // [slots][rows]
+    int2 *span;                        // [items]: first and last worker that has a piece of it
 };
 struct PaParams {
     PagedRef pages;
@@ -73,83 +83,30 @@ struct PaParams {
 
 // ---------------------------------------------------------------------------------------- the division of the work
 __device__ __forceinline__ int key_tiles(int keys) { return (keys + PA_KEYS - 1) / PA_KEYS; }
-__device__ __forceinline__ uint32_t item_cost(int tiles) { return tiles ? (uint32_t)tiles * TILE_COST + ITEM_COST : 0u; }
+__device__ __forceinline__ int item_cost(int tiles) { return tiles ? tiles * TILE_COST + ITEM_COST : 0; }
 // own key tiles of a sequence; 0: it is left out
 __device__ __forceinline__ int seq_tiles(const PaParams &p, int L) {
     return p.pages.fits(L, p.T) && L >= p.shared ? key_tiles(L - p.shared + p.T) : 0;
 }
 // tiles of an item in front of position y of its stretch of the line
-__device__ __forceinline__ int cut_at(int64_t y, int tiles) {
-    const int64_t t = (y - ITEM_COST + TILE_COST / 2) / TILE_COST;      // (truncation towards zero: below ITEM_COST the first tile is not reached)
-    return y <= ITEM_COST ? 0 : t > tiles ? tiles : (int)t;
-}
-__device__ __forceinline__ uint64_t line_length(const PaParams &p, const PaPhase &f, uint64_t seq_costs) {
-    return (uint64_t)f.prefix_items * item_cost(key_tiles(p.shared)) + seq_costs * f.seq_items;
-}
-// Workers that have a run: none shorter than a key tile, so that no worker in the middle of an item is left without a tile.
-__device__ __forceinline__ uint64_t line_workers(const PaPhase &f, uint64_t length) {
-    const uint64_t most = length / TILE_COST;
-    return most < (uint64_t)f.workers ? most : (uint64_t)f.workers;
-}
-// cum[b]: costs of an item of each sequence before b, for b <= B.  One warp.
-__device__ __forceinline__ void sum_costs(const PaParams &p, uint64_t *cum, int lane) {
-    uint64_t before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 32) {
-        uint64_t c = b0 + lane < p.B ? item_cost(seq_tiles(p, p.seq_lens[b0 + lane])) : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const uint64_t x = __shfl_up_sync(0xffffffffu, c, o);
-            if (lane >= o) c += x;
-        }
-        if (b0 + lane < p.B) cum[b0 + lane + 1] = before + c;
-        before += __shfl_sync(0xffffffffu, c, 31);
-    }
-    if (lane == 0) cum[0] = 0;
-}
-// A worker's run, and the item it begins in.
-struct PaStart {
-    uint64_t x0, x1, S;
-    int b, idx;
-};
-__device__ __forceinline__ PaStart find_start(const PaParams &p, const PaPhase &f, const uint64_t *cum, int worker) {
-    PaStart r = {};
-    const uint64_t W = line_length(p, f, cum[p.B]), n = line_workers(f, W);
-    if ((uint64_t)worker >= n) return r;                 // x0 = x1: nothing
-    r.x0 = W * worker / n;
-    r.x1 = W * (worker + 1) / n;
-    const uint64_t cost = item_cost(key_tiles(p.shared)), prefix = cost * f.prefix_items;
-    if (r.x0 < prefix) {
-        r.b = -1;
-        r.idx = (int)(r.x0 / cost);
-        r.S = r.idx * cost;
-        return r;
-    }
-    const uint64_t y = r.x0 - prefix;
-    int lo = 0, hi = p.B;                                // the last b with cum[b] * seq_items <= y < the next one's
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (cum[mid] * f.seq_items <= y) lo = mid; else hi = mid;
-    }
-    const uint64_t own = cum[lo + 1] - cum[lo];
-    r.b = lo;
-    r.idx = own ? (int)((y - cum[lo] * f.seq_items) / own) : 0;
-    r.S = prefix + cum[lo] * f.seq_items + r.idx * own;
-    return r;
-}
-struct PaPiece {
+__device__ __forceinline__ int cut_at(int y, int tiles) { return y <= ITEM_COST ? 0 : min((y - ITEM_COST + TILE_COST / 2) / TILE_COST, tiles); }
+
+struct __align__(16) PaPiece {
     int b;              // -1: the prefix
     int g, tile0;       // KV head, first row tile
-    int t0, t1, tiles;  // key tiles [t0, t1) of the item's
+    int t0, t1;         // key tiles; t1 = 0: no more pieces
     int L;              // keys in front of the tree, without the shared ones (prefix: the shared ones)
     int slot;
+    int whole;          // the item's only piece
 };
+static_assert(sizeof(PaPiece) == 32, "two 16-byte words");
+// The tile needs more than its copy: it holds rows of the tree, or rows behind them.
+__device__ __forceinline__ bool is_last(const PaPiece &s, int t) { return s.b >= 0 && (t + 1) * PA_KEYS > s.L; }
+
+// A worker's run of a phase's line (lines are shorter than 2^31: checked by the host).
 struct PaWalk {
-    uint64_t x0, x1, S;
+    int x0, x1, S;      // the run, and the position of the next item
     int b, idx, tiles, L, worker;
-    __device__ __forceinline__ void begin(const PaParams &p, const PaStart &s, int w) {
-        x0 = s.x0; x1 = s.x1; S = s.S; b = s.b; idx = s.idx; worker = w;
-        if (x0 < x1) load(p);
-    }
     __device__ __forceinline__ void load(const PaParams &p) {
         if (b < 0) {
             L = p.shared;
@@ -168,37 +125,92 @@ struct PaWalk {
                 load(p);
                 continue;
             }
-            s.t0 = cut_at((int64_t)x0 - (int64_t)S, tiles);
-            s.t1 = cut_at((int64_t)x1 - (int64_t)S, tiles);
+            s.t0 = cut_at(x0 - S, tiles);
+            s.t1 = cut_at(x1 - S, tiles);
             S += item_cost(tiles);
             const int i = idx++;
             if (s.t0 >= s.t1) continue;
-            const int per = b < 0 ? f.prefix_per_head : f.seq_per_head;
-            s.b = b; s.L = L; s.tiles = tiles;
+            const int per = b < 0 ? f.prefix_per_head : f.seq_per_head, item = b < 0 ? i : f.prefix_items + b * f.seq_items + i;
+            s.b = b; s.L = L;
             s.g = i / per;
             s.tile0 = (b < 0 ? f.prefix_tile0 : f.seq_tile0) + 2 * (i - s.g * per);
-            s.slot = (b < 0 ? i : f.prefix_items + b * f.seq_items + i) + worker;
+            s.slot = item + worker;
+            s.whole = s.t0 == 0 && s.t1 == tiles;
+            if (threadIdx.x % 32 == 0) {
+                if (s.t0 == 0) f.span[item].x = worker;
+                if (s.t1 == tiles) f.span[item].y = worker;
+            }
             return true;
         }
         return false;
     }
 };
-// The tile needs more than its copy: it holds rows of the tree, or rows behind them.
-__device__ __forceinline__ bool is_last(const PaPiece &s, int t) { return s.b >= 0 && (t + 1) * PA_KEYS > s.L; }
+// The runs of the workers of a CTA (pairs; single tiles of its halves) and the items they begin in.  One warp; two looks at the lengths.
+__device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], int cta, int n_cta, int lane) {
+    int total = 0;                       // cost of an item of every sequence
+    for (int b0 = 0; b0 < p.B; b0 += 32) total += __reduce_add_sync(0xffffffffu, b0 + lane < p.B ? item_cost(seq_tiles(p, p.seq_lens[b0 + lane])) : 0);
+    int y[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const PaPhase &f = p.phase[k > 0];
+        const int cost = item_cost(key_tiles(p.shared)), prefix = cost * f.prefix_items, length = prefix + total * f.seq_items;
+        w[k].worker = k == 2 ? cta + n_cta : cta;
+        // none shorter than a key tile, so that no worker in the middle of an item is left without a tile
+        const int run = max((length + f.workers - 1) / f.workers, TILE_COST);
+        w[k].x0 = (int)min((int64_t)length, (int64_t)run * w[k].worker);
+        w[k].x1 = (int)min((int64_t)length, (int64_t)w[k].x0 + run);
+        w[k].b = -1;
+        w[k].idx = 0;
+        w[k].S = 0;
+        y[k] = -1;
+        if (w[k].x0 < prefix) {
+            w[k].idx = w[k].x0 / cost;
+            w[k].S = w[k].idx * cost;
+        } else if (w[k].x0 < w[k].x1) {
+            y[k] = w[k].x0 - prefix;
+        }
+        if (w[k].x0 == w[k].x1) w[k].S = w[k].x1;
+    }
+    if (y[0] >= 0 || y[1] >= 0 || y[2] >= 0) {
+        int before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const int own = b0 + lane < p.B ? item_cost(seq_tiles(p, p.seq_lens[b0 + lane])) : 0;
+            int c = own;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int x = __shfl_up_sync(0xffffffffu, c, o);
+                if (lane >= o) c += x;
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const PaPhase &f = p.phase[k > 0];
+                const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * f.seq_items > y[k]);
+                if (y[k] < 0 || w[k].b >= 0 || !behind) continue;
+                const int at = __ffs((int)behind) - 1;
+                const int cost = __shfl_sync(0xffffffffu, own, at), first = (before + __shfl_sync(0xffffffffu, c, at) - cost) * f.seq_items;
+                w[k].b = b0 + at;
+                w[k].idx = (y[k] - first) / cost;
+                w[k].S = w[k].x0 - y[k] + first + w[k].idx * cost;
+            }
+            before += __shfl_sync(0xffffffffu, c, 31);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (w[k].x0 < w[k].x1) w[k].load(p);
+}
 
 // All of a phase's key tiles in the order in which the ring holds them: a round takes, list after list, V of the tile before and K of the
-// tile after.  f(list, piece and tile of V or none, piece and tile of K or none) -> whether to go on.
-template <int NL, typename F>
-__device__ __forceinline__ bool for_rounds(const PaParams &p, const PaPhase &ph, const PaStart *starts, int worker, int worker_step, F &&f) {
-    PaWalk w[NL];
+// tile after.  next(list, piece) -> whether there is one; f(list, piece and tile of V or none, piece and tile of K or none) -> whether to go on.
+template <int NL, typename N, typename F>
+__device__ __forceinline__ bool for_rounds(N &&next, F &&f) {
     PaPiece cur[NL], old[NL];
     int t[NL], old_t[NL];
     bool live[NL], pend[NL];
 #pragma unroll
     for (int l = 0; l < NL; ++l) {
-        w[l].begin(p, starts[l], worker + l * worker_step);
-        live[l] = w[l].next(p, ph, cur[l]);
-        t[l] = live[l] ? cur[l].t0 : 0;
+        live[l] = next(l, cur[l]);
+        t[l] = cur[l].t0;
         pend[l] = false;
         old[l] = cur[l];
         old_t[l] = 0;
@@ -215,8 +227,8 @@ __device__ __forceinline__ bool for_rounds(const PaParams &p, const PaPhase &ph,
                 old[l] = cur[l];
                 old_t[l] = t[l];
                 if (++t[l] == cur[l].t1) {
-                    live[l] = w[l].next(p, ph, cur[l]);
-                    t[l] = live[l] ? cur[l].t0 : 0;
+                    live[l] = next(l, cur[l]);
+                    t[l] = cur[l].t0;
                 }
             }
         }
@@ -237,6 +249,28 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 }
 __device__ __forceinline__ bool nonfinite16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
 
+// The two warps that hold the same rows: whether any of their threads says so.
+__device__ __forceinline__ bool any_of_rows(int barrier, bool mine) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "barrier.cta.red.or.pred q, %2, 64, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r) : "r"((uint32_t)mine), "r"(barrier) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void tmem_put(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float tmem_get(uint32_t taddr) {
+    float v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n"
+                 "tcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(taddr) : "memory");
+    return v;
+}
 __device__ __forceinline__ void pa_cta_sync() { asm volatile("bar.sync 1, %0;" ::"n"(PA_THREADS) : "memory"); }
 
 // ---------------------------------------------------------------------------------------- pieces
@@ -246,16 +280,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                   const __grid_constant__ PaParams p) {
     using SM = PaSmem<D>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ PaStart starts[3];        // pairs; single tiles of either half of the CTA
     let_next_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u, sbase = raw + pad;
     unsigned char *gbase = smem_raw + pad;
     const uint32_t bars = sbase + SM::OFF_BAR;
     auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + SM::OFF_BAR + PB_COUNT * 8);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + PB_COUNT * 8 + 4);
-    volatile int *bad = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + PB_COUNT * 8 + 8);   // [2][4]: 1 + the last piece with non-finite V
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + SM::OFF_BAR + PA_OFF_MISC);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + PA_OFF_MISC + 4);
+    volatile int *bad = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + PA_OFF_MISC + 8);   // [2][4]: 1 + the last piece with non-finite V
+    int4 *queue = reinterpret_cast<int4 *>(gbase + SM::OFF_BAR + PA_OFF_QUEUE);                    // [3][PA_QUEUE] pieces
 
     if (warp == PA_TMA_WARP && lane == 0) {
         ptx::prefetch_tensormap(&q_map);
@@ -270,10 +304,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             ptx::mbar_init(bar(PB_QFULL + s), 1);
             ptx::mbar_init(bar(PB_QFREE + s), 1);
             ptx::mbar_init(bar(PB_SREADY + s), 1);
-            ptx::mbar_init(bar(PB_PREADY + s), 4);
+            ptx::mbar_init(bar(PB_PREADY + s), 8);
             ptx::mbar_init(bar(PB_ODONE + s), 1);
         }
         ptx::mbar_init(bar(PB_FINAL), 1);
+        for (int q = 0; q < 3; ++q)
+            for (int i = 0; i < PA_QUEUE; ++i) {
+                ptx::mbar_init(bar(PB_PIECE + q * PA_QUEUE + i), 1);
+                ptx::mbar_init(bar(PB_TAKEN + q * PA_QUEUE + i), q ? 3 + 8 : 3 + 16);
+            }
         ptx::fence_mbar_init();
         *abort_flag = 0;
         for (int k = 0; k < 8; ++k) bad[k] = 0;
@@ -282,15 +321,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         ptx::tmem_relinquish();
     }
-    previous_done();
-    uint64_t *cum = reinterpret_cast<uint64_t *>(gbase);
-    if (warp == 0) sum_costs(p, cum, lane);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    previous_done();
     const int n_cta = gridDim.x, cta = blockIdx.x;
-    if (threadIdx.x < 3) starts[threadIdx.x] = find_start(p, p.phase[threadIdx.x > 0], cum, threadIdx.x == 2 ? cta + n_cta : cta);
-    __syncthreads();
     const uint32_t tmem = *tmem_slot;
     auto give_up = [&]() {
         *abort_flag = 1;
@@ -298,15 +333,24 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     };
     // a whole warp waits; the same answer for all lanes
     auto wait = [&](int b, uint32_t parity) {
-        const bool ok = !*abort_flag && ptx::mbar_wait(bar(b), parity);
+        const bool ok = ptx::mbar_wait(bar(b), parity);
         if (__all_sync(0xffffffffu, ok)) return true;
         if (lane == 0) give_up();
         return false;
     };
+    // the n-th piece of a queue; none (or nothing to be had): false
+    auto take = [&](int q, int n, PaPiece &s) {
+        const int at = q * PA_QUEUE + n % PA_QUEUE;
+        if (__any_sync(0xffffffffu, *abort_flag) || !wait(PB_PIECE + at, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
+        const int4 a = queue[at * 2], c = queue[at * 2 + 1];
+        s.b = a.x; s.g = a.y; s.tile0 = a.z; s.t0 = a.w; s.t1 = c.x; s.L = c.y; s.slot = c.z; s.whole = c.w;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(PB_TAKEN + at));
+        return s.t1 > 0;
+    };
 
     if (warp == PA_TMA_WARP) {
         // ------------------------------------------------------------ Q, K and V
-        ptx::fence_proxy_async();        // the sums above were written where queries are going to land
         int entry = 0, stage = 0, turns = 0;
         int n_q[2] = {0, 0};
         const int boxes = PA_KEYS / p.page_rows, box = lane % boxes, half = lane / boxes;
@@ -333,17 +377,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             if (++stage == SM::STAGES) { stage = 0; ++turns; }
             return true;
         };
-        auto phase = [&](auto lists, const PaPhase &ph, const PaStart *st) {
+        auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
-            int v_page[NL] = {}, v_row[NL] = {};
-            return for_rounds<NL>(p, ph, st, cta, n_cta, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            int v_page[NL] = {}, v_row[NL] = {}, k_page[NL] = {}, k_row[NL] = {}, n[NL] = {};
+            auto next = [&](int l, PaPiece &s) {
+                if (!take(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
+                k_page[l] = find(s, s.t0, &k_row[l]);
+                return true;
+            };
+            return for_rounds<NL>(next, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 if (v && !load(&v_map, v_page[l], v_row[l], vs.g)) return false;
                 if (!k) return true;
-                int row;
-                const int page = find(ks, kt, &row);
-                if (!load(&k_map, page, row, ks.g)) return false;
-                v_page[l] = page;
-                v_row[l] = row;
+                if (!load(&k_map, k_page[l], k_row[l], ks.g)) return false;
+                v_page[l] = k_page[l];
+                v_row[l] = k_row[l];
+                if (kt + 1 < ks.t1) k_page[l] = find(ks, kt + 1, &k_row[l]);     // on its way while others are requested
                 if (kt == ks.t0)
                     for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) {
                         if (n_q[s] && !wait(PB_QFREE + s, (n_q[s] - 1) & 1)) return false;
@@ -359,7 +407,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 return true;
             });
         };
-        if (!phase(std::integral_constant<int, 1>(), p.phase[0], starts) || !phase(std::integral_constant<int, 2>(), p.phase[1], starts + 1)) {
+        if (!phase(std::integral_constant<int, 1>()) || !phase(std::integral_constant<int, 2>()) || *abort_flag) {
             // copies in flight get a bounded chance to land before the CTA can exit
             for (int e = max(0, entry - SM::STAGES); e < entry; ++e) ptx::mbar_wait(bar(PB_FULL + e % SM::STAGES), (e / SM::STAGES) & 1);
             for (int s = 0; s < 2; ++s)
@@ -372,9 +420,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         int entry = 0;
         uint32_t cleaned = 0;            // parity of each stage's next cleaning
         int n_p[2] = {0, 0}, n_q[2] = {0, 0};
-        auto phase = [&](auto lists, const PaPhase &ph, const PaStart *st) {
+        auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
-            return for_rounds<NL>(p, ph, st, cta, n_cta, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            int n[NL] = {};
+            return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 const int ve = entry, ke = entry + (v ? 1 : 0);
                 entry = ke + (k ? 1 : 0);
                 const int v_stage = ve % SM::STAGES, k_stage = ke % SM::STAGES;
@@ -394,7 +443,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                         const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
 #pragma unroll
                         for (int kk = 0; kk < PA_KEYS / 16; ++kk)
-                            ptx::mma_ts_elect(tmem + 256 + s * D, tmem + s * 128 + kk * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
+                            ptx::mma_ts_elect(tmem + 256 + s * D, tmem + s * 128 + (kk / 4) * 64 + (kk % 4) * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
                         if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(PB_ODONE + s), leader);
                         if (s == s1 - 1) ptx::tc_commit_elect(bar(PB_FREE + v_stage), leader);
                     }
@@ -416,16 +465,17 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 return true;
             });
         };
-        phase(std::integral_constant<int, 1>(), p.phase[0], starts) && phase(std::integral_constant<int, 2>(), p.phase[1], starts + 1);
+        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
         // what was issued is complete, and has signalled, before the CTA can exit
         ptx::tc_commit_elect(bar(PB_FINAL), leader);
         ptx::mbar_wait(bar(PB_FINAL), 0);
     } else if (warp == PA_CLEAN_WARP) {
         // ------------------------------------------------------------ the last V tiles of a sequence
         int stage = 0, turns = 0, n_piece[2] = {0, 0};
-        auto phase = [&](auto lists, const PaPhase &ph, const PaStart *st) {
+        auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
-            return for_rounds<NL>(p, ph, st, cta, n_cta, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            int n[NL] = {};
+            return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 // Every entry is waited for, and handed back by this warp too: a parity wait cannot tell a phase from the one two
                 // before or behind, so nobody may be a turn of the ring ahead or late.
                 auto landed = [&]() { return wait(PB_FULL + stage, turns & 1); };
@@ -476,9 +526,55 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 return true;
             });
         };
-        phase(std::integral_constant<int, 1>(), p.phase[0], starts) && phase(std::integral_constant<int, 2>(), p.phase[1], starts + 1);
-    } else if (warp == PA_STATUS_WARP) {
-        // ------------------------------------------------------------ which sequences can be attended to
+        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+    } else if (warp == PA_PLAN_WARP) {
+        // ------------------------------------------------------------ pieces, and which sequences can be attended to
+        PaWalk w[3];
+        begin_walks(p, w, cta, n_cta, lane);
+        // Pairs first, then the two halves side by side: the warps that serve both wait for either one's next piece, so neither may be
+        // held up by the other's full queue.  A queue's end is a piece without tiles.
+        int n_put[3] = {0, 0, 0};
+        auto put = [&](int q, const PaPiece &s) {
+            const int at = q * PA_QUEUE + n_put[q]++ % PA_QUEUE;
+            if (lane == 0) {
+                queue[at * 2] = make_int4(s.b, s.g, s.tile0, s.t0);
+                queue[at * 2 + 1] = make_int4(s.t1, s.L, s.slot, s.whole);
+                ptx::mbar_arrive(bar(PB_PIECE + at));
+            }
+            __syncwarp();
+        };
+        auto room = [&](int q) {
+            const int n = n_put[q];
+            return n < PA_QUEUE || __all_sync(0xffffffffu, ptx::mbar_test(bar(PB_TAKEN + q * PA_QUEUE + n % PA_QUEUE), (n / PA_QUEUE - 1) & 1));
+        };
+        auto more = [&](int q) {                   // one piece more, or the end
+            PaPiece s = {};
+            const bool any = w[q].next(p, p.phase[q > 0], s);
+            if (!any) s.t0 = s.t1 = 0;
+            put(q, s);
+            return any;
+        };
+        long long since = clock64();
+        bool open[3] = {true, true, true};
+        while (open[0] || open[1] || open[2]) {
+            bool moved = false;
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+                if (open[q] && (q == 0 || !open[0]) && room(q)) {
+                    open[q] = more(q);
+                    moved = true;
+                }
+            if (moved) {
+                since = clock64();
+            } else {
+                __nanosleep(200);
+                const bool late = *abort_flag || clock64() - since > ptx::WAIT_CYCLE_LIMIT;
+                if (__any_sync(0xffffffffu, late)) {
+                    if (lane == 0) give_up();
+                    break;
+                }
+            }
+        }
         if (p.status && cta < p.B) {
             const int prefix = p.pages.check(0, 0, p.shared, lane);
             for (int b = cta; b < p.B; b += n_cta) {
@@ -489,44 +585,51 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             }
         }
     } else {
-        // ------------------------------------------------------------ softmax: a thread per row of row tile s
-        const int s = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lane_base + s * 128, t_o = tmem + lane_base + 256 + s * D;
-        const int node_in_tile = row / p.G, head = row % p.G;
+        // ------------------------------------------------------------ softmax: thread (row, hf) of row tile s: columns [64 hf, 64 hf + 64)
+        const int s = warp >> 3, hf = (warp >> 2) & 1, qd = warp & 3, row = qd * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
+        const uint32_t t_s = lane_base + s * 128 + hf * 64;      // this half's scores; P over their first 32 columns, what is exchanged behind
+        const uint32_t t_x = lane_base + s * 128 + (hf ^ 1) * 64;
+        const uint32_t t_o = lane_base + 256 + s * D + hf * (D / 2);
+        const int pair_bar = 2 + s * 4 + qd;
+        const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
         const bool in_tile = node_in_tile < p.npc;
         const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
+        // what the other half of the row has: both put theirs behind their P's place, where nothing is any more
+        auto exchange = [&](int col, float v) {
+            tmem_put(t_s + col, v);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            ptx::tc_fence_after();
+            return tmem_get(t_x + col);
+        };
         int n_s = 0, n_piece = 0;
         bool ok = true;
         for (int f = 0; f < 2 && ok; ++f) {
             const PaPhase &ph = p.phase[f];
-            PaWalk walk;
             PaPiece pc;
-            walk.begin(p, starts[f ? 1 + s : 0], f ? cta + s * n_cta : cta);
-            while (ok && walk.next(p, ph, pc)) {
+            for (int n = 0; ok && take(f ? 1 + s : 0, n, pc); ++n) {
                 const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
                 const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
                 const bool some = __any_sync(0xffffffffu, mine);
-                uint64_t alo = 0, ahi = 0;
-                if (mine && pc.b >= 0) { alo = p.anc[node * 2]; ahi = p.anc[node * 2 + 1]; }
                 // visibility of the tree rows as 32-bit words; the rows in front of them are visible to every node, those behind to none
-                auto anc_word = [&](int w) -> uint32_t {
-                    return w < 0 ? 0xffffffffu : w == 0 ? (uint32_t)alo : w == 1 ? (uint32_t)(alo >> 32) : w == 2 ? (uint32_t)ahi : w == 3 ? (uint32_t)(ahi >> 32) : 0u;
-                };
+                const uint32_t *anc = reinterpret_cast<const uint32_t *>(p.anc) + (mine && pc.b >= 0 ? node * 4 : 0);
+                auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w < 4 && mine && pc.b >= 0 ? anc[w] : 0u; };
                 float m_used = -INFINITY, l = 0.f;
                 for (int t = pc.t0; t < pc.t1; ++t) {
                     if (!wait(PB_SREADY + s, n_s++ & 1)) { ok = false; break; }
                     ptx::tc_fence_after();
                     if (some) {
-                        uint32_t sr[128];
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) ptx::tmem_ld32(t_s + h * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[h * 32]));
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[h * 32]));
+                        uint32_t sr[64];
+                        ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                        ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+                        ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                        ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
                         if ((t + 1) * PA_KEYS > pc.L) {
 #pragma unroll
-                            for (int h = 0; h < 4; ++h) {
-                                const int a0 = t * PA_KEYS + h * 32 - pc.L;      // tree row of the first column
+                            for (int h = 0; h < 2; ++h) {
+                                const int a0 = t * PA_KEYS + hf * 64 + h * 32 - pc.L;      // tree row of the first column
                                 const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
@@ -535,81 +638,88 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                         }
                         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int e = 0; e < 128; e += 8)
+                        for (int e = 0; e < 64; e += 8)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
                         float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * p.scale_log2;
-                        if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
-                        const float m_new = mxs <= m_used + PA_RESCALE ? m_used : mxs;   // (a NaN is taken over)
-                        const bool need = t > pc.t0 && m_new != m_used && m_used != -INFINITY && mine;
-                        if (__any_sync(0xffffffffu, need)) {
-                            const float alpha = need ? ex2(m_used - m_new) : 1.f;
+                        if (any_of_rows(pair_bar, mine && !(mxs <= m_used + PA_RESCALE))) {
+                            mxs = max_nan(mxs, exchange(40, mxs));
+                            if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+                            const float m_new = mxs <= m_used + PA_RESCALE ? m_used : mxs;   // (a NaN is taken over)
+                            const bool need = m_new != m_used && m_used != -INFINITY && mine;
+                            if (__any_sync(0xffffffffu, need)) {
+                                const float alpha = need ? ex2(m_used - m_new) : 1.f;
 #pragma unroll 1
-                            for (int h = 0; h < D / 16; ++h) {
-                                uint32_t o[16];
-                                ptx::tmem_ld16(t_o + h * 16, o);
-                                ptx::tmem_ld_wait_for16(o);
+                                for (int h = 0; h < D / 32; ++h) {
+                                    uint32_t o[16];
+                                    ptx::tmem_ld16(t_o + h * 16, o);
+                                    ptx::tmem_ld_wait_for16(o);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                                ptx::tmem_st16(t_o + h * 16, o);
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                                    ptx::tmem_st16(t_o + h * 16, o);
+                                }
+                                l *= alpha;
                             }
-                            l *= alpha;
+                            m_used = m_new;
                         }
-                        m_used = m_new;
                         const float m_eff = m_used == -INFINITY ? 0.f : m_used;
                         const float2 nm2 = make_float2(-m_eff, -m_eff);
                         float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+                        uint32_t pk[32];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t pk[32];
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                const uint32_t *x = sr + h * 64 + 2 * e;
-                                const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
-                                const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
-                                const float2 p01 = make_float2(ex2(x01.x), ex2(x01.y)), p23 = make_float2(ex2(x23.x), ex2(x23.y));
-                                la = __fadd2_rn(la, p01);
-                                lb = __fadd2_rn(lb, p23);
-                                pk[e] = pack2_bf16(p01.x, p01.y);
-                                pk[e + 1] = pack2_bf16(p23.x, p23.y);
+                        for (int e = 0; e < 32; e += 2) {
+                            const uint32_t *x = sr + 2 * e;
+                            const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
+                            const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
+                            float2 p01, p23;
+                            if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                p01 = exp2_poly2(x01);
+                                p23 = exp2_poly2(x23);
+                            } else {
+                                p01 = make_float2(ex2(x01.x), ex2(x01.y));
+                                p23 = make_float2(ex2(x23.x), ex2(x23.y));
                             }
-                            ptx::tmem_st32(t_s + h * 32, pk);
+                            la = __fadd2_rn(la, p01);
+                            lb = __fadd2_rn(lb, p23);
+                            pk[e] = pack2_bf16(p01.x, p01.y);
+                            pk[e + 1] = pack2_bf16(p23.x, p23.y);
                         }
+                        ptx::tmem_st32(t_s, pk);
                         l += (la.x + la.y) + (lb.x + lb.y);
+                        if (t == pc.t1 - 1) l += exchange(41, l);       // the row's sum; S is another tile's behind this one's P
                         ptx::tmem_st_wait();
                     }
                     ptx::tc_fence_before();
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(bar(PB_PREADY + s));
                 }
-                if (!ok) break;
-                if (!wait(PB_ODONE + s, n_piece & 1)) { ok = false; break; }
+                if (!ok || !wait(PB_ODONE + s, n_piece & 1)) { ok = false; break; }
                 ptx::tc_fence_after();
                 if (some) {
                     const bool odd = bad[s * 4 + (n_piece & 3)] == n_piece + 1;
-                    const bool direct = p.shared == 0 && pc.t0 == 0 && pc.t1 == pc.tiles;
+                    const bool direct = p.shared == 0 && pc.whole;
                     const float inv = direct ? 1.f / l : 1.f;
                     const int slot_row = f ? row : s * 128 + row;
-                    float *o_out = ph.o + (size_t)pc.slot * ph.rows * D + (size_t)slot_row * 8;
-                    __nv_bfloat16 *out = p.out + (((size_t)max(pc.b, 0) * p.T + node) * p.Hq + pc.g * p.G + head) * D;
+                    float *o_out = ph.o + ((size_t)pc.slot * ph.rows * (D / 8) + (size_t)(hf * (D / 16)) * ph.rows + slot_row) * 8;
+                    __nv_bfloat16 *out = p.out + (((size_t)max(pc.b, 0) * p.T + node) * p.Hq + pc.g * p.G + head) * D + hf * (D / 2);
 #pragma unroll 1
-                    for (int h = 0; h < D / 16; ++h) {
+                    for (int h = 0; h < D / 32; ++h) {
                         uint32_t o[16];
                         ptx::tmem_ld16(t_o + h * 16, o);
                         ptx::tmem_ld_wait_for16(o);
-                        if (odd && mine) {
+                        if (!mine) continue;
+                        if (odd) {
                             // V values that the tensor core did not see: an infinity or NaN with any weight is itself
                             for (int a = max(0, pc.t0 * PA_KEYS - pc.L); a < p.T && pc.L + a < pc.t1 * PA_KEYS; ++a) {
-                                if (!((a < 64 ? alo >> a : ahi >> (a - 64)) & 1)) continue;
+                                if (!(anc_word(a >> 5) >> (a & 31) & 1)) continue;
                                 const int64_t at = p.pages.row(pc.b, p.shared + pc.L + a);
                                 if (at < 0) continue;
-                                const uint16_t *v = reinterpret_cast<const uint16_t *>(p.v) + at + pc.g * p.pages.stride_h + h * 16;
+                                const uint16_t *v = reinterpret_cast<const uint16_t *>(p.v) + at + pc.g * p.pages.stride_h + hf * (D / 2) + h * 16;
 #pragma unroll
                                 for (int e = 0; e < 16; ++e)
                                     if (nonfinite16(v[e])) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float((uint32_t)v[e] << 16));
                             }
                         }
-                        if (!mine) continue;
                         if (direct) {
                             uint32_t w[8];
 #pragma unroll
@@ -621,7 +731,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                             ptx::st_global_32(o_out + (size_t)(2 * h + 1) * ph.rows * 8, *reinterpret_cast<const uint32_t(*)[8]>(&o[8]));
                         }
                     }
-                    if (mine && !direct) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(m_used, l);
+                    if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(m_used, l);
                 }
                 ++n_piece;
             }
@@ -637,82 +747,71 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 
 // ---------------------------------------------------------------------------------------- their combination
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the pieces s of a row's two items (the prefix' and the sequence's own), in the order
-// of the keys whoever worked them off.  A thread takes 8 columns of a row: neighbouring threads neighbouring rows, as the slots are laid out.
+// of the keys whoever worked them off.  16 neighbouring threads look at a row's maxima side by side; then a thread takes 8 columns of a
+// row, neighbouring threads neighbouring rows, as the slots are laid out.
 struct PaSource {
     const float *o;       // slot of the first piece, at the row
     const float2 *ml;
     int n, rows;
 };
-__device__ __forceinline__ PaSource find_source(const PaParams &p, const PaPhase &f, const uint64_t *cum, uint64_t S, int tiles, int item, int row, int D) {
-    const uint64_t W = line_length(p, f, cum[p.B]), n = line_workers(f, W);
-    // first: the last worker that begins at or before the item (the next one, if that one's run ends before the first tile); last: the
-    // last worker that begins before its end and has a tile of it
-    uint64_t w = S * n / W;
-    while (w > 0 && W * w / n > S) --w;
-    while (w + 1 < n && W * (w + 1) / n <= S) ++w;
-    while (w + 1 < n && cut_at((int64_t)(W * (w + 1) / n) - (int64_t)S, tiles) == 0) ++w;
-    const uint64_t end = S + item_cost(tiles);
-    uint64_t last = (end - 1) * n / W;
-    if (last >= n) last = n - 1;
-    while (last + 1 < n && W * (last + 1) / n < end) ++last;
-    while (last > w && cut_at((int64_t)(W * last / n) - (int64_t)S, tiles) >= tiles) --last;
-    PaSource r;
-    const size_t slot = (size_t)item + w;
-    r.o = f.o + slot * f.rows * D + (size_t)row * 8;
-    r.ml = f.ml + slot * f.rows + row;
-    r.n = (int)(last - w) + 1;
-    r.rows = f.rows;
-    return r;
-}
 
 template <int D>
 __global__ void __launch_bounds__(256)
 paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
     constexpr int CHUNKS = D / 8, ROWS = 256 / CHUNKS;
-    __shared__ uint64_t cum[PA_MAX_B + 1];
     __shared__ PaSource src[2][ROWS];
     __shared__ int64_t out_at[ROWS];
+    __shared__ float top[ROWS];
     let_next_start();
-    previous_done();
-    const int tid = threadIdx.x;
-    if (tid < 32) sum_costs(p, cum, tid);
-    __syncthreads();
-    const int per_seq = p.T * p.G;
+    const int tid = threadIdx.x, per_seq = p.T * p.G;
+    int b = p.B, g = 0, node = 0, head = 0;
     if (tid < ROWS) {
-        const int64_t r = (int64_t)blockIdx.x * ROWS + tid;
-        const int64_t bg = r / per_seq;
-        const int b = (int)(bg / p.Hkv), g = (int)(bg % p.Hkv), x = (int)(r % per_seq), node = x / p.G, head = x % p.G;
-        out_at[tid] = -1;
+        const int r = (int)blockIdx.x * ROWS + tid, bg = r / per_seq, x = r - bg * per_seq;
+        b = bg / p.Hkv; g = bg - b * p.Hkv; node = x / p.G; head = x - node * p.G;
+    }
+    previous_done();
+    if (tid < ROWS) {
+        int64_t at = -1;
         src[0][tid].n = src[1][tid].n = 0;
-        const int tiles = b < p.B ? seq_tiles(p, p.seq_lens[b]) : 0;
-        if (tiles) {
+        if (b < p.B && seq_tiles(p, p.seq_lens[b])) {
             // row tile and row in it -> phase, item and row of the slot
             auto find = [&](int n, bool prefix) {
                 const int tile = n / p.npc, per = prefix ? p.phase[0].prefix_per_head : p.phase[0].seq_per_head;
                 const int k = tile / 2 < per ? 0 : 1;
                 const PaPhase &f = p.phase[k];
                 const int row = (k ? 0 : (tile & 1) * 128) + (n - tile * p.npc) * p.G + head;
-                const int i = k ? g : g * per + tile / 2;
-                const uint64_t cost = item_cost(key_tiles(p.shared));
-                if (prefix) return find_source(p, f, cum, i * cost, key_tiles(p.shared), i, row, D);
-                return find_source(p, f, cum, f.prefix_items * cost + cum[b] * f.seq_items + (uint64_t)i * item_cost(tiles), tiles,
-                                   f.prefix_items + b * f.seq_items + i, row, D);
+                const int i = k ? g : g * per + tile / 2, item = prefix ? i : f.prefix_items + b * f.seq_items + i;
+                const int2 span = f.span[item];
+                const size_t slot = (size_t)item + span.x;
+                PaSource s;
+                s.o = f.o + (slot * CHUNKS * f.rows + row) * 8;
+                s.ml = f.ml + slot * f.rows + row;
+                s.n = span.y - span.x + 1;
+                s.rows = f.rows;
+                return s;
             };
             if (p.shared) src[0][tid] = find(b * p.T + node, true);
             src[1][tid] = find(node, false);
             // a single piece was written out by the kernel before
-            if (p.shared || src[1][tid].n > 1) out_at[tid] = (((int64_t)b * p.T + node) * p.Hq + g * p.G + head) * D;
+            if (p.shared || src[1][tid].n > 1) at = (((int64_t)b * p.T + node) * p.Hq + g * p.G + head) * D;
         }
+        out_at[tid] = at;
+    }
+    __syncthreads();
+    {
+        const int row = tid / CHUNKS;
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            for (int i = tid % CHUNKS; i < src[k][row].n; i += CHUNKS) m = max_nan(m, src[k][row].ml[(size_t)i * src[k][row].rows].x);
+#pragma unroll
+        for (int o = CHUNKS / 2; o; o /= 2) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (tid % CHUNKS == 0) top[row] = m;
     }
     __syncthreads();
     const int row = tid % ROWS, chunk = tid / ROWS;
     if (out_at[row] < 0) return;
-    float m = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const PaSource s = src[k][row];
-        for (int i = 0; i < s.n; ++i) m = max_nan(m, s.ml[(size_t)i * s.rows].x);
-    }
+    const float m = top[row];
     float acc[8] = {}, l = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -755,13 +854,24 @@ static size_t pa_plan(PaPhase (&ph)[2], int T, int B, int G, int Hkv, int D, int
         at += align_up(slots * x.rows * D * sizeof(float), 256);
         x.ml = reinterpret_cast<float2 *>(ws + at);
         at += align_up(slots * x.rows * sizeof(float2), 256);
+        x.span = reinterpret_cast<int2 *>(ws + at);
+        at += align_up(items * sizeof(int2), 256);
     }
     return at;
 }
 
 static bool pa_sizes_ok(const mtv_tree *tree, int B, int Hq, int Hkv, int D, int shared) {
     return tree && B >= 1 && B <= PA_MAX_B && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= 8 && (D == 64 || D == 128) && shared >= 0 &&
-           (int64_t)Hkv * B * tree->T <= 1 << 28;
+           (int64_t)Hq * B * tree->T <= 1 << 28;
+}
+// Lines of either phase stay below 2^31, whatever the lengths.
+static bool pa_lines_ok(const PaPhase (&ph)[2], int B, int shared, int64_t slots) {
+    for (const PaPhase &f : ph) {
+        const int64_t prefix = (shared / PA_KEYS + 1) * TILE_COST + ITEM_COST, own = (slots / PA_KEYS + 2) * TILE_COST + ITEM_COST;
+        if (own * B > 0x7fffffff || prefix > 0x7fffffff) return false;
+        if ((double)prefix * f.prefix_items + (double)own * B * f.seq_items > 2147000000.0) return false;
+    }
+    return true;
 }
 
 template <int D>
@@ -805,6 +915,7 @@ extern "C" int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq
     p.T = tree->T; p.B = B; p.G = Hq / Hkv; p.Hq = Hq; p.Hkv = Hkv;
     p.shared = shared_len;
     if (ws_bytes < pa_plan(p.phase, p.T, B, p.G, Hkv, D, shared_len, static_cast<char *>(ws))) return MTV_ERR_WORKSPACE;
+    if (!pa_lines_ok(p.phase, B, shared_len, (int64_t)max_pages * pool->page_size)) return MTV_ERR_UNSUPPORTED_SHAPE;
     p.npc = 128 / p.G;
     p.page_rows = pool->page_size < PA_KEYS ? pool->page_size : PA_KEYS;
     p.seq_lens = seq_lens; p.anc = tree->d_anc;

@@ -67,6 +67,8 @@ def check(tree, tb, Hq, Hkv, D, page, shared, lens, seed=1, tokens_outside=False
     (5, 128, 8, 1, 128, 256, 512, [600, 1000]),          # eight row tiles, pages longer than a tile, tree across three key tiles
     (5, 128, 16, 2, 64, 1024, 0, [5, 3000]),
     (5, 128, 5, 5, 128, 16, 160, [161, 161, 161]),       # groups of one
+    (1, 1, 4, 1, 64, 16, 0, [9000] + [1] * 300 + [5000] + [3] * 200),      # long pieces beside many short ones
+    (1, 1, 2, 2, 128, 32, 32, [40 + i % 50 for i in range(150)] + [6000]),
 ])
 def test_against_the_oracle(K, T, Hq, Hkv, D, page, shared, lens):
     tb, tree = make_tree("rank_prior", K, (), T) if T > 1 else make_tree("cartesian", 1, (1,))
