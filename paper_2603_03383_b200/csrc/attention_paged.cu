@@ -16,27 +16,30 @@
 // exponentials are taken.  In the phase of pairs the two tiles are those of an item and share K and V; in the other the CTA is two workers,
 // whose K and V take turns in one ring.
 //   warps 0-7 / 8-15  softmax of row tile 0 / 1
-//   warp 16           issues all products, in the order  O_0 += P_0 V, S_0 = Q_0 K, O_1 += P_1 V, S_1 = Q_1 K  with S one key tile ahead of O:
-//                     products of one thread are executed in order, so S may overwrite the P that the product in front of it reads,
-//                     and "S is complete" implies that O is complete up to the tile before
-//   warp 17           requests Q, K and V (a box per page)
-//   warp 18           clears V rows behind the last key (their weight is 0, but 0 * NaN is not) and takes non-finite values of the tree's
+//   warps 16, 17      issue the products of row tile 0 / 1, O += P V and then S = Q K of the next key tile: products of one thread are executed
+//                     in order, so S may overwrite the P that the product in front of it reads, and "S is complete" implies that O is
+//                     complete up to the tile before.  (A wait costs an issuing warp a hundred cycles even where there is nothing to wait for,
+//                     and the tensor core has only some two products queued: one warp for both row tiles left it idle a third of the time.)
+//   warp 18           derives the pieces from the lengths, hands them to the other warps, and requests their Q, K and V (a box per page);
+//                     reports the sequences' status at the end
+//   warp 19           clears V rows behind the last key (their weight is 0, but 0 * NaN is not) and takes non-finite values of the tree's
 //                     V rows out (they are given to the rows that see them at the end)
-//   warp 19           derives the pieces from the lengths and hands them to the other warps; reports the sequences' status
 //
-// The running maximum moves only when a tile's exceeds it by more than 8 (log2 units): O is rescaled rarely, P stays below 2^8, and the two
-// threads of a row exchange their maxima (through tensor memory) only then; otherwise a vote says that nobody needs it.
+// The reference of a row's exponentials is the maximum of the piece's first tile.  It moves only where a later tile's weights reach 2^64:
+// P, O and the sum are floating-point numbers, to which the reference's size is all the same as long as nothing overflows.  So an ordinary
+// tile forms no maximum; a vote of the two threads of a row says that neither needs the reference moved, and only otherwise they take
+// the scores again, exchange their maxima (through tensor memory) and rescale O.
 #include "attn_common.cuh"
 #include "paged_common.cuh"
 
 namespace mtv {
 
 constexpr int PA_THREADS = 640;
-constexpr int PA_MMA_WARP = 16, PA_TMA_WARP = 17, PA_CLEAN_WARP = 18, PA_PLAN_WARP = 19;
-constexpr int PA_QUEUE = 4;               // pieces that are handed out ahead
+constexpr int PA_MMA_WARP = 16, PA_TMA_WARP = 18, PA_CLEAN_WARP = 19;
+constexpr int PA_QUEUE = 4;               // pieces that are handed out and may not have been taken by all
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
-constexpr float PA_RESCALE = 8.f;
+constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
 constexpr int TILE_COST = 4, ITEM_COST = 4;   // what a piece's start and end take, in quarters of a key tile
 
 template <int D> struct PaSmem {
@@ -145,15 +148,19 @@ struct PaWalk {
         return false;
     }
 };
-// The runs of the workers of a CTA (pairs; single tiles of its halves) and the items they begin in.  One warp; two looks at the lengths.
+// The runs of the workers of a CTA (pairs; single tiles of its halves) and the items they begin in.  One warp.
 __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], int cta, int n_cta, int lane) {
-    int total = 0;                       // cost of an item of every sequence
-    for (int b0 = 0; b0 < p.B; b0 += 32) total += __reduce_add_sync(0xffffffffu, b0 + lane < p.B ? item_cost(seq_tiles(p, p.seq_lens[b0 + lane])) : 0);
+    auto cost_of = [&](int b) { return b < p.B ? item_cost(seq_tiles(p, p.seq_lens[b])) : 0; };
+    const int own0 = cost_of(lane);      // cost of an item of this lane's sequence
+    int total = own0;
+    for (int b0 = 32; b0 < p.B; b0 += 32) total += cost_of(b0 + lane);
+    total = __reduce_add_sync(0xffffffffu, total);
+    const int cost = item_cost(key_tiles(p.shared));
     int y[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         const PaPhase &f = p.phase[k > 0];
-        const int cost = item_cost(key_tiles(p.shared)), prefix = cost * f.prefix_items, length = prefix + total * f.seq_items;
+        const int prefix = cost * f.prefix_items, length = prefix + total * f.seq_items;
         w[k].worker = k == 2 ? cta + n_cta : cta;
         // none shorter than a key tile, so that no worker in the middle of an item is left without a tile
         const int run = max((length + f.workers - 1) / f.workers, TILE_COST);
@@ -161,7 +168,7 @@ __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], i
         w[k].x1 = (int)min((int64_t)length, (int64_t)w[k].x0 + run);
         w[k].b = -1;
         w[k].idx = 0;
-        w[k].S = 0;
+        w[k].S = w[k].x0 == w[k].x1 ? w[k].x1 : 0;
         y[k] = -1;
         if (w[k].x0 < prefix) {
             w[k].idx = w[k].x0 / cost;
@@ -169,31 +176,29 @@ __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], i
         } else if (w[k].x0 < w[k].x1) {
             y[k] = w[k].x0 - prefix;
         }
-        if (w[k].x0 == w[k].x1) w[k].S = w[k].x1;
     }
-    if (y[0] >= 0 || y[1] >= 0 || y[2] >= 0) {
-        int before = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const int own = b0 + lane < p.B ? item_cost(seq_tiles(p, p.seq_lens[b0 + lane])) : 0;
-            int c = own;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B && (y[0] >= 0 || y[1] >= 0 || y[2] >= 0); b0 += 32) {
+        const int own = b0 ? cost_of(b0 + lane) : own0;
+        int c = own;
 #pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int x = __shfl_up_sync(0xffffffffu, c, o);
-                if (lane >= o) c += x;
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                const PaPhase &f = p.phase[k > 0];
-                const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * f.seq_items > y[k]);
-                if (y[k] < 0 || w[k].b >= 0 || !behind) continue;
-                const int at = __ffs((int)behind) - 1;
-                const int cost = __shfl_sync(0xffffffffu, own, at), first = (before + __shfl_sync(0xffffffffu, c, at) - cost) * f.seq_items;
-                w[k].b = b0 + at;
-                w[k].idx = (y[k] - first) / cost;
-                w[k].S = w[k].x0 - y[k] + first + w[k].idx * cost;
-            }
-            before += __shfl_sync(0xffffffffu, c, 31);
+        for (int o = 1; o < 32; o *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, c, o);
+            if (lane >= o) c += x;
         }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const PaPhase &f = p.phase[k > 0];
+            const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * f.seq_items > y[k]);
+            if (y[k] < 0 || !behind) continue;
+            const int at = __ffs((int)behind) - 1;
+            const int each = __shfl_sync(0xffffffffu, own, at), first = (before + __shfl_sync(0xffffffffu, c, at) - each) * f.seq_items;
+            w[k].b = b0 + at;
+            w[k].idx = (y[k] - first) / each;
+            w[k].S = w[k].x0 - y[k] + first + w[k].idx * each;
+            y[k] = -1;
+        }
+        before += __shfl_sync(0xffffffffu, c, 31);
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k)
@@ -297,7 +302,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ptx::prefetch_tensormap(&v_map);
         for (int s = 0; s < SM::STAGES; ++s) {
             ptx::mbar_init(bar(PB_FULL + s), 1);
-            ptx::mbar_init(bar(PB_FREE + s), 2);      // the products, and the warp that looks at every entry
+            ptx::mbar_init(bar(PB_FREE + s), 3);      // the issuing warps, and the one that looks at every entry
             ptx::mbar_init(bar(PB_CLEAN + s), 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -307,7 +312,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             ptx::mbar_init(bar(PB_PREADY + s), 8);
             ptx::mbar_init(bar(PB_ODONE + s), 1);
         }
-        ptx::mbar_init(bar(PB_FINAL), 1);
+        ptx::mbar_init(bar(PB_FINAL), 2);
         for (int q = 0; q < 3; ++q)
             for (int i = 0; i < PA_QUEUE; ++i) {
                 ptx::mbar_init(bar(PB_PIECE + q * PA_QUEUE + i), 1);
@@ -350,7 +355,24 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     };
 
     if (warp == PA_TMA_WARP) {
-        // ------------------------------------------------------------ Q, K and V
+        // ------------------------------------------------------------ pieces; Q, K and V
+        PaWalk w[3];
+        begin_walks(p, w, cta, n_cta, lane);
+        // One piece more for a queue, or its end: a piece without tiles.  (There is room, or will be without this warp's doing: the queries
+        // of a piece are only requested when the scores of the one before are complete, so this warp is never three pieces ahead.)
+        auto hand_out = [&](int q, int n, PaPiece &s) {
+            const int at = q * PA_QUEUE + n % PA_QUEUE;
+            const bool any = w[q].next(p, p.phase[q > 0], s);
+            if (!any) s = PaPiece{};
+            if (n >= PA_QUEUE && !wait(PB_TAKEN + at, (n / PA_QUEUE - 1) & 1)) { s.t0 = s.t1 = 0; return false; }
+            if (lane == 0) {
+                queue[at * 2] = make_int4(s.b, s.g, s.tile0, s.t0);
+                queue[at * 2 + 1] = make_int4(s.t1, s.L, s.slot, s.whole);
+                ptx::mbar_arrive(bar(PB_PIECE + at));
+            }
+            __syncwarp();
+            return any;
+        };
         int entry = 0, stage = 0, turns = 0;
         int n_q[2] = {0, 0};
         const int boxes = PA_KEYS / p.page_rows, box = lane % boxes, half = lane / boxes;
@@ -381,7 +403,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             constexpr int NL = decltype(lists)::value;
             int v_page[NL] = {}, v_row[NL] = {}, k_page[NL] = {}, k_row[NL] = {}, n[NL] = {};
             auto next = [&](int l, PaPiece &s) {
-                if (!take(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
+                if (!hand_out(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
                 k_page[l] = find(s, s.t0, &k_row[l]);
                 return true;
             };
@@ -413,55 +435,75 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             for (int s = 0; s < 2; ++s)
                 if (n_q[s]) ptx::mbar_wait(bar(PB_QFULL + s), (n_q[s] - 1) & 1);
         }
-    } else if (warp == PA_MMA_WARP) {
-        // ------------------------------------------------------------ all products
+        // which sequences can be attended to
+        if (p.status && cta < p.B) {
+            const int prefix = p.pages.check(0, 0, p.shared, lane);
+            for (int b = cta; b < p.B; b += n_cta) {
+                const int L = p.seq_lens[b];
+                int code = seq_tiles(p, L) ? p.pages.check(b, p.shared, L - p.shared + p.T, lane) : MTV_ERR_CAPACITY;
+                if (code == MTV_OK) code = prefix;
+                if (lane == 0) p.status[b] = code;
+            }
+        }
+    } else if (warp == PA_MMA_WARP || warp == PA_MMA_WARP + 1) {
+        // ------------------------------------------------------------ products of row tile s
+        const int s = warp - PA_MMA_WARP;
         const bool leader = ptx::elect_one();
-        const uint32_t dq0 = ptx::desc_lo(sbase, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_RING, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_RING, SM::HALF);
-        int entry = 0;
+        const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_RING, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_RING, SM::HALF);
+        const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * D;
+        int entry = 0, n_p = 0, n_q = 0;
         uint32_t cleaned = 0;            // parity of each stage's next cleaning
-        int n_p[2] = {0, 0}, n_q[2] = {0, 0};
         auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
             int n[NL] = {};
-            return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            return for_rounds<NL>([&](int l, PaPiece &x) { return take(NL == 1 ? 0 : 1 + l, n[l]++, x); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 const int ve = entry, ke = entry + (v ? 1 : 0);
                 entry = ke + (k ? 1 : 0);
                 const int v_stage = ve % SM::STAGES, k_stage = ke % SM::STAGES;
-                const int s0 = l, s1 = NL == 1 ? 2 : l + 1;
-                for (int s = s0; s < s1; ++s) {
-                    if (v) {
-                        if (s == s0) {
-                            if (is_last(vs, vt)) {
-                                if (!wait(PB_CLEAN + v_stage, cleaned >> v_stage & 1)) return false;
-                                cleaned ^= 1u << v_stage;
-                            } else if (!wait(PB_FULL + v_stage, (ve / SM::STAGES) & 1)) {
-                                return false;
-                            }
-                        }
-                        if (!wait(PB_PREADY + s, n_p[s]++ & 1)) return false;
-                        ptx::tc_fence_after();
-                        const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
-#pragma unroll
-                        for (int kk = 0; kk < PA_KEYS / 16; ++kk)
-                            ptx::mma_ts_elect(tmem + 256 + s * D, tmem + s * 128 + (kk / 4) * 64 + (kk % 4) * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
-                        if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(PB_ODONE + s), leader);
-                        if (s == s1 - 1) ptx::tc_commit_elect(bar(PB_FREE + v_stage), leader);
-                    }
-                    if (k) {
-                        if (s == s0 && !wait(PB_FULL + k_stage, (ke / SM::STAGES) & 1)) return false;
-                        if (kt == ks.t0 && !wait(PB_QFULL + s, n_q[s]++ & 1)) return false;
-                        ptx::tc_fence_after();
-                        const uint32_t dq = dq0 + (uint32_t)s * (SM::TILE >> 4), dk = dk0 + (uint32_t)k_stage * (SM::TILE >> 4);
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t o = ((kk / 4) * SM::HALF + (kk % 4) * 32) >> 4;
-                            ptx::mma_ss_elect(tmem + s * 128, dq + o, dk + o, ptx::DESC_HI, SM::IDESC_QK, kk > 0, leader);
-                        }
-                        ptx::tc_commit_elect(bar(PB_SREADY + s), leader);
-                        if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(PB_QFREE + s), leader);
-                        if (s == s1 - 1) ptx::tc_commit_elect(bar(PB_FREE + k_stage), leader);
-                    }
+                const bool last_v = v && is_last(vs, vt);
+                const uint32_t clean_parity = cleaned >> v_stage & 1;
+                if (last_v) cleaned ^= 1u << v_stage;
+                if (NL == 2 && l != s) {
+                    // the other tile's: waited for and handed back all the same, so that this warp is never a turn of the ring ahead or
+                    // late (a parity wait cannot tell a phase from the one two before or behind)
+                    auto pass = [&](int e, int stage) {
+                        if (!wait(PB_FULL + stage, (e / SM::STAGES) & 1)) return false;
+                        if (lane == 0) ptx::mbar_arrive(bar(PB_FREE + stage));
+                        return true;
+                    };
+                    return (!v || pass(ve, v_stage)) && (!k || pass(ke, k_stage));
                 }
+                auto k_there = [&]() { return wait(PB_FULL + k_stage, (ke / SM::STAGES) & 1) && (kt != ks.t0 || wait(PB_QFULL + s, n_q++ & 1)); };
+                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be)
+                const bool ahead = v && k && kt != ks.t0;
+                if (ahead && !k_there()) return false;
+                if (v) {
+                    // (first that it has landed: only then is the stage's cleaning before this one known to be over)
+                    if (!wait(PB_FULL + v_stage, (ve / SM::STAGES) & 1) || (last_v && !wait(PB_CLEAN + v_stage, clean_parity))) return false;
+                    if (!wait(PB_PREADY + s, n_p++ & 1)) return false;
+                    ptx::tc_fence_after();
+                    const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < PA_KEYS / 16; ++kk)
+                        ptx::mma_ts_elect(t_o, t_s + (kk / 4) * 64 + (kk % 4) * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
+                    if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(PB_ODONE + s), leader);
+                }
+                if (k) {
+                    if (!ahead) {
+                        if (!k_there()) return false;
+                        ptx::tc_fence_after();
+                    }
+                    const uint32_t dk = dk0 + (uint32_t)k_stage * (SM::TILE >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t o = ((kk / 4) * SM::HALF + (kk % 4) * 32) >> 4;
+                        ptx::mma_ss_elect(t_s, dq + o, dk + o, ptx::DESC_HI, SM::IDESC_QK, kk > 0, leader);
+                    }
+                    ptx::tc_commit_elect(bar(PB_SREADY + s), leader);
+                    if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(PB_QFREE + s), leader);
+                }
+                if (v) ptx::tc_commit_elect(bar(PB_FREE + v_stage), leader);
+                if (k) ptx::tc_commit_elect(bar(PB_FREE + k_stage), leader);
                 return true;
             });
         };
@@ -476,8 +518,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             constexpr int NL = decltype(lists)::value;
             int n[NL] = {};
             return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
-                // Every entry is waited for, and handed back by this warp too: a parity wait cannot tell a phase from the one two
-                // before or behind, so nobody may be a turn of the ring ahead or late.
+                // Every entry is waited for, and handed back by this warp too (as above).
                 auto landed = [&]() { return wait(PB_FULL + stage, turns & 1); };
                 auto pass = [&]() {
                     __syncwarp();
@@ -527,63 +568,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             });
         };
         phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
-    } else if (warp == PA_PLAN_WARP) {
-        // ------------------------------------------------------------ pieces, and which sequences can be attended to
-        PaWalk w[3];
-        begin_walks(p, w, cta, n_cta, lane);
-        // Pairs first, then the two halves side by side: the warps that serve both wait for either one's next piece, so neither may be
-        // held up by the other's full queue.  A queue's end is a piece without tiles.
-        int n_put[3] = {0, 0, 0};
-        auto put = [&](int q, const PaPiece &s) {
-            const int at = q * PA_QUEUE + n_put[q]++ % PA_QUEUE;
-            if (lane == 0) {
-                queue[at * 2] = make_int4(s.b, s.g, s.tile0, s.t0);
-                queue[at * 2 + 1] = make_int4(s.t1, s.L, s.slot, s.whole);
-                ptx::mbar_arrive(bar(PB_PIECE + at));
-            }
-            __syncwarp();
-        };
-        auto room = [&](int q) {
-            const int n = n_put[q];
-            return n < PA_QUEUE || __all_sync(0xffffffffu, ptx::mbar_test(bar(PB_TAKEN + q * PA_QUEUE + n % PA_QUEUE), (n / PA_QUEUE - 1) & 1));
-        };
-        auto more = [&](int q) {                   // one piece more, or the end
-            PaPiece s = {};
-            const bool any = w[q].next(p, p.phase[q > 0], s);
-            if (!any) s.t0 = s.t1 = 0;
-            put(q, s);
-            return any;
-        };
-        long long since = clock64();
-        bool open[3] = {true, true, true};
-        while (open[0] || open[1] || open[2]) {
-            bool moved = false;
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-                if (open[q] && (q == 0 || !open[0]) && room(q)) {
-                    open[q] = more(q);
-                    moved = true;
-                }
-            if (moved) {
-                since = clock64();
-            } else {
-                __nanosleep(200);
-                const bool late = *abort_flag || clock64() - since > ptx::WAIT_CYCLE_LIMIT;
-                if (__any_sync(0xffffffffu, late)) {
-                    if (lane == 0) give_up();
-                    break;
-                }
-            }
-        }
-        if (p.status && cta < p.B) {
-            const int prefix = p.pages.check(0, 0, p.shared, lane);
-            for (int b = cta; b < p.B; b += n_cta) {
-                const int L = p.seq_lens[b];
-                int code = seq_tiles(p, L) ? p.pages.check(b, p.shared, L - p.shared + p.T, lane) : MTV_ERR_CAPACITY;
-                if (code == MTV_OK) code = prefix;
-                if (lane == 0) p.status[b] = code;
-            }
-        }
     } else {
         // ------------------------------------------------------------ softmax: thread (row, hf) of row tile s: columns [64 hf, 64 hf + 64)
         const int s = warp >> 3, hf = (warp >> 2) & 1, qd = warp & 3, row = qd * 32 + lane;
@@ -621,68 +605,78 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     if (!wait(PB_SREADY + s, n_s++ & 1)) { ok = false; break; }
                     ptx::tc_fence_after();
                     if (some) {
-                        uint32_t sr[64];
-                        ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-                        ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-                        ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-                        ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-                        if ((t + 1) * PA_KEYS > pc.L) {
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int a0 = t * PA_KEYS + hf * 64 + h * 32 - pc.L;      // tree row of the first column
-                                const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (!((vis >> e) & 1u)) sr[h * 32 + e] = 0xff800000u;   // -inf
-                            }
-                        }
-                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int e = 0; e < 64; e += 8)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
-                        float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * p.scale_log2;
-                        if (any_of_rows(pair_bar, mine && !(mxs <= m_used + PA_RESCALE))) {
-                            mxs = max_nan(mxs, exchange(40, mxs));
-                            if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
-                            const float m_new = mxs <= m_used + PA_RESCALE ? m_used : mxs;   // (a NaN is taken over)
-                            const bool need = m_new != m_used && m_used != -INFINITY && mine;
-                            if (__any_sync(0xffffffffu, need)) {
-                                const float alpha = need ? ex2(m_used - m_new) : 1.f;
-#pragma unroll 1
-                                for (int h = 0; h < D / 32; ++h) {
-                                    uint32_t o[16];
-                                    ptx::tmem_ld16(t_o + h * 16, o);
-                                    ptx::tmem_ld_wait_for16(o);
-#pragma unroll
-                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                                    ptx::tmem_st16(t_o + h * 16, o);
-                                }
-                                l *= alpha;
-                            }
-                            m_used = m_new;
-                        }
-                        const float m_eff = m_used == -INFINITY ? 0.f : m_used;
-                        const float2 nm2 = make_float2(-m_eff, -m_eff);
-                        float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
                         uint32_t pk[32];
+                        float2 la, lb;
+                        for (bool move = t == pc.t0;;) {
+                            uint32_t sr[64];
+                            ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                            ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+                            if ((t + 1) * PA_KEYS > pc.L) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const uint32_t *x = sr + 2 * e;
-                            const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
-                            const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
-                            float2 p01, p23;
-                            if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
-                                p01 = exp2_poly2(x01);
-                                p23 = exp2_poly2(x23);
-                            } else {
-                                p01 = make_float2(ex2(x01.x), ex2(x01.y));
-                                p23 = make_float2(ex2(x23.x), ex2(x23.y));
+                                for (int h = 0; h < 2; ++h) {
+                                    const int a0 = t * PA_KEYS + hf * 64 + h * 32 - pc.L;      // tree row of the first column
+                                    const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e)
+                                        if (!((vis >> e) & 1u)) sr[h * 32 + e] = 0xff800000u;   // -inf
+                                }
                             }
-                            la = __fadd2_rn(la, p01);
-                            lb = __fadd2_rn(lb, p23);
-                            pk[e] = pack2_bf16(p01.x, p01.y);
-                            pk[e + 1] = pack2_bf16(p23.x, p23.y);
+                            if (move) {
+                                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                                for (int e = 0; e < 64; e += 8)
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
+                                float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * p.scale_log2;
+                                mxs = max_nan(mxs, exchange(40, mxs));
+                                if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+                                const float m_new = mxs <= m_used ? m_used : mxs;            // (a NaN is taken over)
+                                const bool need = m_new != m_used && m_used != -INFINITY && mine;
+                                if (__any_sync(0xffffffffu, need)) {
+                                    const float alpha = need ? ex2(m_used - m_new) : 1.f;
+#pragma unroll 1
+                                    for (int h = 0; h < D / 32; ++h) {
+                                        uint32_t o[16];
+                                        ptx::tmem_ld16(t_o + h * 16, o);
+                                        ptx::tmem_ld_wait_for16(o);
+#pragma unroll
+                                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                                        ptx::tmem_st16(t_o + h * 16, o);
+                                    }
+                                    l *= alpha;
+                                }
+                                m_used = m_new;
+                            }
+                            const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+                            const float2 nm2 = make_float2(-m_eff, -m_eff);
+                            la = lb = make_float2(0.f, 0.f);
+                            float px = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const uint32_t *x = sr + 2 * e;
+                                const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
+                                const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
+                                float2 p01, p23;
+                                if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                    px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
+                                    p01 = exp2_poly2(x01);
+                                    p23 = exp2_poly2(x23);
+                                } else {
+                                    p01 = make_float2(ex2(x01.x), ex2(x01.y));
+                                    p23 = make_float2(ex2(x23.x), ex2(x23.y));
+                                }
+                                la = __fadd2_rn(la, p01);
+                                lb = __fadd2_rn(lb, p23);
+                                pk[e] = pack2_bf16(p01.x, p01.y);
+                                pk[e + 1] = pack2_bf16(p23.x, p23.y);
+                            }
+                            if (move) break;
+                            // a sum that is too large, infinite or NaN, and a row that has met no visible key yet
+                            const bool ask = !(max_nan(max_nan(la.x, la.y), max_nan(lb.x, lb.y)) < 1.8446744e19f) || !(px <= PA_LIMIT) || m_used == -INFINITY;
+                            if (!any_of_rows(pair_bar, mine && ask)) break;
+                            move = true;
                         }
                         ptx::tmem_st32(t_s, pk);
                         l += (la.x + la.y) + (lb.x + lb.y);
@@ -731,7 +725,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                             ptx::st_global_32(o_out + (size_t)(2 * h + 1) * ph.rows * 8, *reinterpret_cast<const uint32_t(*)[8]>(&o[8]));
                         }
                     }
-                    if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(m_used, l);
+                    if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(l == 0.f ? -INFINITY : m_used, l);
                 }
                 ++n_piece;
             }

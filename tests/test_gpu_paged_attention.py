@@ -76,3 +76,96 @@ def test_against_the_oracle(K, T, Hq, Hkv, D, page, shared, lens):
         tree = binding.tree_build_static(1, [])
         tb = dict(mask=[[1]])
     check(tree, tb, Hq, Hkv, D, page, shared, lens)
+
+
+def _tree(K, T):
+    if T == 1:
+        return dict(mask=[[1]]), binding.tree_build_static(1, [])
+    return make_tree("rank_prior", K, (), T)
+
+
+@pytest.mark.parametrize("D,T,G", [(128, 64, 4), (64, 1, 8), (128, 20, 3)])
+@pytest.mark.parametrize("size", [1.0, 30.0, 300.0])
+def test_scores_that_grow_along_the_keys(D, T, G, size):
+    """Keys that get longer: the running maximum of most rows rises from tile to tile, by up to hundreds, so that the reference has to
+    move; the softmax ends up on few keys."""
+    tb, tree = _tree(4, T)
+    g = torch.Generator().manual_seed(7)
+    shared, lens, page, Hkv = 320, [700, 1500], 32, 2
+    t, n_pages = table(g, 2, 1500 - shared + T, page, shared)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    grow = torch.ones(n_pages, page)
+    for b in range(2):
+        for i, pg in enumerate(t[b].tolist()):
+            grow[pg] = 0.05 + size * ((i * page + torch.arange(page)) / 1500.0)
+    kp = (kp.float() * grow[:, None, :, None]).to(torch.bfloat16)
+    q = torch.randn(2, T, Hkv * G, D, generator=g).to(torch.bfloat16)
+    out = run(tree, q, kp, vp, t, lens, shared)
+    want, absolute = want_of(q, kp, vp, t, lens, tb["mask"])
+    # scores up to S = 6 * size in natural units, their fp32 sums off by at most 128 products' rounding (2^-24 each, of S): relative error of a weight
+    # up to 128 * 2^-24 * S in front of the softmax; twice (numerator and sum)
+    slop = 2 * 128 * 2.0 ** -24 * 6 * size * absolute
+    assert ((out.double() - want).abs() / (bound(want, absolute) + slop)).max().item() <= 1.0
+
+
+@pytest.mark.parametrize("T", [1, 29, 64])
+@pytest.mark.parametrize("D", [64, 128])
+def test_non_finite_rows_reach_those_who_see_them(D, T):
+    """NaN and infinities in K and V rows of single nodes and behind the last node: nodes that do not see them have the results of a cache
+    without them, the others NaN or infinite where the oracle has it."""
+    tb, tree = _tree(4, T)
+    g = torch.Generator().manual_seed(11)
+    shared, lens, page, Hkv, G = 64, [130, 300, 64], 16, 2, 4
+    t, n_pages = table(g, 3, 300 - shared + T + 40, page, shared)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    q = torch.randn(3, T, Hkv * G, D, generator=g).to(torch.bfloat16)
+    clean, _ = want_of(q, kp, vp, t, lens, tb["mask"])
+    mask = torch.tensor(tb["mask"], dtype=torch.bool)
+    at = lambda b, s: (int(t[b, s // page]), s % page)  # noqa: E731
+    bad_v = {} if T == 1 else {0: (5, float("nan")), 1: (T - 1, float("inf")), 2: (T // 2, float("-inf"))}
+    for b, L in enumerate(lens):
+        for s in range(L + T, L + T + 30):       # behind the last node
+            pg, r = at(b, s)
+            kp[pg, :, r] = vp[pg, :, r] = float("nan")
+        if b in bad_v:
+            pg, r = at(b, L + bad_v[b][0])
+            vp[pg, 1, r, 3::7] = bad_v[b][1]
+    if T > 1:                                    # a K row of NaN: every row that sees it is NaN
+        pg, r = at(0, lens[0] + T - 2)
+        kp[pg, 0, r] = float("nan")
+    out = run(tree, q, kp, vp, t, lens, shared).double()
+    for b in range(3):
+        want = clean[b].clone()
+        if b in bad_v:
+            a, x = bad_v[b]
+            want[mask[:, a], G:, 3::7] = x
+        if b == 0 and T > 1:
+            want[mask[:, T - 2], :G] = float("nan")
+        fine = torch.isfinite(want)
+        assert torch.equal(torch.isnan(out[b]), torch.isnan(want)) and torch.equal(torch.isinf(out[b]), torch.isinf(want))
+        assert torch.equal(out[b][torch.isinf(want)], want[torch.isinf(want)])
+        assert (out[b][fine] - want[fine]).abs().max().item() <= 2e-2
+
+
+@pytest.mark.parametrize("where", ["q", "k", "k_inf"])
+def test_non_finite_scores(where):
+    """A NaN in a query row makes that row NaN; a NaN or an infinity in a prefix key every row of its head that has a finite query."""
+    tb, tree = _tree(4, 64)
+    g = torch.Generator().manual_seed(13)
+    shared, lens, page, Hkv, G, D = 128, [400, 200], 16, 2, 4, 128
+    for col in (0, 6, 12, 13, 14, 15, 70, 127):              # columns of either exponential
+        t, n_pages = table(g, 2, 400 - shared + 64, page, shared)
+        kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+        q = torch.randn(2, 64, Hkv * G, D, generator=g).to(torch.bfloat16)
+        want = torch.zeros(2, 64, Hkv * G, dtype=torch.bool)
+        if where == "q":
+            q[1, 9, 5, col] = float("nan")
+            want[1, 9, 5] = True
+        else:
+            s = 128 + 128 + col if where == "k" else 128 + col      # sequence 0 alone, second or first own tile
+            pg, r = int(t[0, s // page]), s % page
+            kp[pg, 1, r, 17] = float("nan") if where == "k" else float("inf")
+            q[..., 17] = 1.0                                  # +inf scores
+            want[0, :, G:] = True
+        out = run(tree, q, kp, vp, t, lens, shared)
+        assert torch.equal(torch.isnan(out).all(-1), want) and torch.equal(torch.isnan(out).any(-1), want), col
