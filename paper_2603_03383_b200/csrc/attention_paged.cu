@@ -40,7 +40,7 @@ constexpr int PA_QUEUE = 4;               // pieces that are handed out and may 
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
 constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
-constexpr int TILE_COST = 4, ITEM_COST = 4;   // what a piece's start and end take, in quarters of a key tile
+constexpr int TILE_COST = 4, ITEM_COST = 16;   // what a piece's start and end take, in quarters of a key tile
 
 template <int D> struct PaSmem {
     static constexpr int HALVES = D / 64;
@@ -58,7 +58,8 @@ enum {
     PB_FULL = 0, PB_FREE = 10, PB_CLEAN = 20, PB_QFULL = 30, PB_QFREE = 32, PB_SREADY = 34, PB_PREADY = 36, PB_ODONE = 38, PB_FINAL = 40,
     PB_PIECE = 41,                         // [3 queues][PA_QUEUE]: pairs; single tiles of either half of the CTA
     PB_TAKEN = PB_PIECE + 3 * PA_QUEUE,
-    PB_COUNT = PB_TAKEN + 3 * PA_QUEUE
+    PB_TURN = PB_TAKEN + 3 * PA_QUEUE,     // [2] an issuing warp's turn at the tensor core
+    PB_COUNT = PB_TURN + 2
 };
 constexpr uint32_t PA_OFF_MISC = PB_COUNT * 8, PA_OFF_QUEUE = (PA_OFF_MISC + 40 + 15) / 16 * 16;
 static_assert(PA_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1024, "barrier region");
@@ -311,6 +312,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             ptx::mbar_init(bar(PB_SREADY + s), 1);
             ptx::mbar_init(bar(PB_PREADY + s), 8);
             ptx::mbar_init(bar(PB_ODONE + s), 1);
+            ptx::mbar_init(bar(PB_TURN + s), 1);
         }
         ptx::mbar_init(bar(PB_FINAL), 2);
         for (int q = 0; q < 3; ++q)
@@ -351,6 +353,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         s.b = a.x; s.g = a.y; s.tile0 = a.z; s.t0 = a.w; s.t1 = c.x; s.L = c.y; s.slot = c.z; s.whole = c.w;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(PB_TAKEN + at));
+        __syncwarp();
         return s.t1 > 0;
     };
 
@@ -451,7 +454,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         const bool leader = ptx::elect_one();
         const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_RING, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_RING, SM::HALF);
         const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * D;
-        int entry = 0, n_p = 0, n_q = 0;
+        int entry = 0, n_p = 0, n_q = 0, n_turn = 0;
         uint32_t cleaned = 0;            // parity of each stage's next cleaning
         auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
@@ -469,11 +472,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     auto pass = [&](int e, int stage) {
                         if (!wait(PB_FULL + stage, (e / SM::STAGES) & 1)) return false;
                         if (lane == 0) ptx::mbar_arrive(bar(PB_FREE + stage));
+                        __syncwarp();
                         return true;
                     };
                     return (!v || pass(ve, v_stage)) && (!k || pass(ke, k_stage));
                 }
                 auto k_there = [&]() { return wait(PB_FULL + k_stage, (ke / SM::STAGES) & 1) && (kt != ks.t0 || wait(PB_QFULL + s, n_q++ & 1)); };
+                // Pairs take turns: the products of a row tile go to the tensor core in one run.  Mixed with the other tile's, both tiles' scores
+                // would come when all are done, both softmaxes would then run at once, and the tensor core wait for both.
+                auto begin_run = [&]() {
+                    if (NL == 2) return true;
+                    const int turn = n_turn++;
+                    return s == 0 && turn == 0 ? true : wait(PB_TURN + s, (turn + s - 1) & 1);
+                };
+                auto end_run = [&]() {
+                    if (NL == 1 && lane == 0) ptx::mbar_arrive(bar(PB_TURN + (s ^ 1)));
+                    __syncwarp();
+                };
                 // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be)
                 const bool ahead = v && k && kt != ks.t0;
                 if (ahead && !k_there()) return false;
@@ -481,16 +496,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     // (first that it has landed: only then is the stage's cleaning before this one known to be over)
                     if (!wait(PB_FULL + v_stage, (ve / SM::STAGES) & 1) || (last_v && !wait(PB_CLEAN + v_stage, clean_parity))) return false;
                     if (!wait(PB_PREADY + s, n_p++ & 1)) return false;
+                    if (!begin_run()) return false;
                     ptx::tc_fence_after();
                     const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
 #pragma unroll
                     for (int kk = 0; kk < PA_KEYS / 16; ++kk)
                         ptx::mma_ts_elect(t_o, t_s + (kk / 4) * 64 + (kk % 4) * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
                     if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(PB_ODONE + s), leader);
+                    if (!ahead) end_run();
                 }
                 if (k) {
                     if (!ahead) {
-                        if (!k_there()) return false;
+                        if (!k_there() || !begin_run()) return false;
                         ptx::tc_fence_after();
                     }
                     const uint32_t dk = dk0 + (uint32_t)k_stage * (SM::TILE >> 4);
@@ -501,6 +518,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     }
                     ptx::tc_commit_elect(bar(PB_SREADY + s), leader);
                     if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(PB_QFREE + s), leader);
+                    end_run();
                 }
                 if (v) ptx::tc_commit_elect(bar(PB_FREE + v_stage), leader);
                 if (k) ptx::tc_commit_elect(bar(PB_FREE + k_stage), leader);
