@@ -380,43 +380,44 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         int n_q[2] = {0, 0};
         const int boxes = PA_KEYS / p.page_rows, box = lane % boxes, half = lane / boxes;
         const uint32_t q_bytes = (uint32_t)(p.npc * p.G) * 128u * SM::HALVES;
-        // this lane's page of a key tile, and the row in it; no page: copied as zeros
-        auto find = [&](const PaPiece &s, int t, int *row) {
-            const int off = t * PA_KEYS + box * p.page_rows, key = off + (s.b < 0 ? 0 : p.shared);
-            *row = key & ((1 << p.pages.page_shift) - 1);
-            int page = p.pages.n_pages;
-            if (half < SM::HALVES && off < s.L + (s.b < 0 ? 0 : p.T)) {
-                const int id = p.pages.table[(int64_t)max(s.b, 0) * p.pages.max_pages + (key >> p.pages.page_shift)];
-                if (id >= 0 && id < p.pages.n_pages) page = id;
-            }
-            return page;
+        // This lane's entry of the table for a key tile, requested here and looked at where the tile is: nothing waits for it meanwhile.
+        // (Where there is no page, or the table names none, zeros are copied.)
+        auto find = [&](const PaPiece &s, int t) {
+            const int key = t * PA_KEYS + box * p.page_rows;
+            int id = -1;
+            if (half < SM::HALVES && key < s.L + (s.b < 0 ? 0 : p.T))
+                asm volatile("ld.global.s32 %0, [%1];" : "=r"(id)
+                             : "l"(p.pages.table + (int64_t)max(s.b, 0) * p.pages.max_pages + ((key + (s.b < 0 ? 0 : p.shared)) >> p.pages.page_shift)));
+            return id;
         };
-        auto load = [&](const CUtensorMap *map, int page, int row, int g) {
+        auto row_in_page = [&](const PaPiece &s, int t) {
+            return (t * PA_KEYS + box * p.page_rows + (s.b < 0 ? 0 : p.shared)) & ((1 << p.pages.page_shift) - 1);
+        };
+        auto load = [&](const CUtensorMap *map, int id, int row, int g) {
             if (entry >= SM::STAGES && !wait(PB_FREE + stage, (turns - 1) & 1)) return false;
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar(PB_FULL + stage), SM::TILE);
             __syncwarp();
             if (half < SM::HALVES)
                 ptx::tma_load_4d(sbase + SM::OFF_RING + stage * SM::TILE + half * SM::HALF + box * p.page_rows * 128, map, bar(PB_FULL + stage),
-                                 half * 64, row, g, page);
+                                 half * 64, row, g, id >= 0 && id < p.pages.n_pages ? id : p.pages.n_pages);
             ++entry;
             if (++stage == SM::STAGES) { stage = 0; ++turns; }
             return true;
         };
         auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
-            int v_page[NL] = {}, v_row[NL] = {}, k_page[NL] = {}, k_row[NL] = {}, n[NL] = {};
+            int v_id[NL] = {}, k_id[NL] = {}, n[NL] = {};
             auto next = [&](int l, PaPiece &s) {
                 if (!hand_out(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
-                k_page[l] = find(s, s.t0, &k_row[l]);
+                k_id[l] = find(s, s.t0);
                 return true;
             };
             return for_rounds<NL>(next, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
-                if (v && !load(&v_map, v_page[l], v_row[l], vs.g)) return false;
+                if (v && !load(&v_map, v_id[l], row_in_page(vs, vt), vs.g)) return false;
                 if (!k) return true;
-                if (!load(&k_map, k_page[l], k_row[l], ks.g)) return false;
-                v_page[l] = k_page[l];
-                v_row[l] = k_row[l];
-                if (kt + 1 < ks.t1) k_page[l] = find(ks, kt + 1, &k_row[l]);     // on its way while others are requested
+                if (!load(&k_map, k_id[l], row_in_page(ks, kt), ks.g)) return false;
+                v_id[l] = k_id[l];
+                if (kt + 1 < ks.t1) k_id[l] = find(ks, kt + 1);
                 if (kt == ks.t0)
                     for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) {
                         if (n_q[s] && !wait(PB_QFREE + s, (n_q[s] - 1) & 1)) return false;
@@ -545,26 +546,28 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 };
                 if (v && !landed()) return false;
                 if (v && is_last(vs, vt)) {
-                    const int first = max(0, vs.L - vt * PA_KEYS), end = vs.L + p.T - vt * PA_KEYS;
+                    // rows of the tree are looked through, those behind them on their page cleared (the pages behind are copied as zeros)
+                    const int first = max(0, vs.L - vt * PA_KEYS), end = min(vs.L + p.T - vt * PA_KEYS, PA_KEYS);
+                    const int clear = (end + p.page_rows - 1) / p.page_rows * p.page_rows;
                     bool odd = false;
 #pragma unroll
                     for (int h = 0; h < SM::HALVES; ++h) {
                         uint4 *x = reinterpret_cast<uint4 *>(gbase + SM::OFF_RING + stage * SM::TILE + h * SM::HALF);
-                        for (int e = first * 8 + lane; e < PA_KEYS * 8; e += 32) {
-                            if (e / 8 >= end) {
-                                x[e] = make_uint4(0u, 0u, 0u, 0u);
-                                continue;
-                            }
+                        for (int e = end * 8 + lane; e < clear * 8; e += 32) x[e] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 4
+                        for (int e = first * 8 + lane; e < end * 8; e += 32) {
                             const uint4 u = x[e];
+                            // an exponent of all ones anywhere: the halves of a word side by side
+                            auto ones = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+                            if ((ones(u.x) | ones(u.y) | ones(u.z) | ones(u.w)) == 0u) continue;
                             uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                            bool here = false;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                if (nonfinite16(w[i])) { w[i] &= 0xffff0000u; here = true; }
-                                if (nonfinite16(w[i] >> 16)) { w[i] &= 0xffffu; here = true; }
+                                if (nonfinite16(w[i])) w[i] &= 0xffff0000u;
+                                if (nonfinite16(w[i] >> 16)) w[i] &= 0xffffu;
                             }
-                            if (here) x[e] = make_uint4(w[0], w[1], w[2], w[3]);
-                            odd = odd || here;
+                            x[e] = make_uint4(w[0], w[1], w[2], w[3]);
+                            odd = true;
                         }
                     }
                     if (__any_sync(0xffffffffu, odd) && lane == 0)
@@ -616,8 +619,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
                 const bool some = __any_sync(0xffffffffu, mine);
                 // visibility of the tree rows as 32-bit words; the rows in front of them are visible to every node, those behind to none
-                const uint32_t *anc = reinterpret_cast<const uint32_t *>(p.anc) + (mine && pc.b >= 0 ? node * 4 : 0);
-                auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w < 4 && mine && pc.b >= 0 ? anc[w] : 0u; };
+                uint4 anc = make_uint4(0u, 0u, 0u, 0u);
+                if (mine && pc.b >= 0) anc = reinterpret_cast<const uint4 *>(p.anc)[node];
+                auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w == 0 ? anc.x : w == 1 ? anc.y : w == 2 ? anc.z : w == 3 ? anc.w : 0u; };
                 float m_used = -INFINITY, l = 0.f;
                 for (int t = pc.t0; t < pc.t1; ++t) {
                     if (!wait(PB_SREADY + s, n_s++ & 1)) { ok = false; break; }
