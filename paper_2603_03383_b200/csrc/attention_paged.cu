@@ -762,22 +762,34 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------- their combination
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the pieces s of a row's two items (the prefix' and the sequence's own), in the order
-// of the keys whoever worked them off.  16 neighbouring threads look at a row's maxima side by side; then a thread takes 8 columns of a
-// row, neighbouring threads neighbouring rows, as the slots are laid out.
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the pieces s of a row's two items (the prefix' and the sequence's own).  A thread takes
+// 8 columns of a row, neighbouring threads neighbouring rows, as the slots are laid out, and four pieces at a time, their
+// (max, sum) and their columns requested together: the kernel is a chain of loads from L2.  SPLIT > 1: that many threads share a row's columns,
+// each every SPLIT-th group of four pieces, and meet in shared memory; the order of the additions depends on the pieces alone.
 struct PaSource {
     const float *o;       // slot of the first piece, at the row
     const float2 *ml;
     int n, rows;
 };
+struct PaSum {
+    float m, l, acc[8];
+    __device__ __forceinline__ void add(float m2, float l2, const float (&a)[8]) {
+        const float m_new = max_nan(m, m2);
+        const float w = m == -INFINITY ? 0.f : ex2(m - m_new), w2 = m2 == -INFINITY ? 0.f : ex2(m2 - m_new);
+        m = m_new;
+        l = fmaf(w2, l2, w * l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(w2, a[e], w * acc[e]);
+    }
+};
 
-template <int D>
+template <int D, int SPLIT>
 __global__ void __launch_bounds__(256)
 paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
-    constexpr int CHUNKS = D / 8, ROWS = 256 / CHUNKS;
+    constexpr int CHUNKS = D / 8, ROWS = 256 / (CHUNKS * SPLIT);
     __shared__ PaSource src[2][ROWS];
     __shared__ int64_t out_at[ROWS];
-    __shared__ float top[ROWS];
+    __shared__ PaSum sums[SPLIT > 1 ? 256 : 1];
     let_next_start();
     const int tid = threadIdx.x, per_seq = p.T * p.G;
     int b = p.B, g = 0, node = 0, head = 0;
@@ -785,65 +797,76 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
         const int r = (int)blockIdx.x * ROWS + tid, bg = r / per_seq, x = r - bg * per_seq;
         b = bg / p.Hkv; g = bg - b * p.Hkv; node = x / p.G; head = x - node * p.G;
     }
+    // row tile and row in it -> phase, item and row of the slot
+    auto place = [&](int n, bool prefix, int *item, int *row) -> const PaPhase & {
+        const int tile = n / p.npc, per = prefix ? p.phase[0].prefix_per_head : p.phase[0].seq_per_head;
+        const int k = tile / 2 < per ? 0 : 1;
+        const PaPhase &f = p.phase[k];
+        *row = (k ? 0 : (tile & 1) * 128) + (n - tile * p.npc) * p.G + head;
+        const int i = k ? g : g * per + tile / 2;
+        *item = prefix ? i : f.prefix_items + b * f.seq_items + i;
+        return f;
+    };
     previous_done();
     if (tid < ROWS) {
         int64_t at = -1;
-        src[0][tid].n = src[1][tid].n = 0;
-        if (b < p.B && seq_tiles(p, p.seq_lens[b])) {
-            // row tile and row in it -> phase, item and row of the slot
-            auto find = [&](int n, bool prefix) {
-                const int tile = n / p.npc, per = prefix ? p.phase[0].prefix_per_head : p.phase[0].seq_per_head;
-                const int k = tile / 2 < per ? 0 : 1;
-                const PaPhase &f = p.phase[k];
-                const int row = (k ? 0 : (tile & 1) * 128) + (n - tile * p.npc) * p.G + head;
-                const int i = k ? g : g * per + tile / 2, item = prefix ? i : f.prefix_items + b * f.seq_items + i;
-                const int2 span = f.span[item];
+        PaSource s0 = {}, s1 = {};
+        if (b < p.B) {
+            int item0 = 0, row0 = 0, item1, row1;
+            const PaPhase &f0 = place(b * p.T + node, true, &item0, &row0), &f1 = place(node, false, &item1, &row1);
+            const int len = p.seq_lens[b];
+            int2 span0 = make_int2(0, -1);
+            if (p.shared) span0 = f0.span[item0];
+            const int2 span1 = f1.span[item1];           // (of a sequence that is left out: not looked at)
+            auto source = [&](const PaPhase &f, int item, int row, int2 span) {
                 const size_t slot = (size_t)item + span.x;
-                PaSource s;
-                s.o = f.o + (slot * CHUNKS * f.rows + row) * 8;
-                s.ml = f.ml + slot * f.rows + row;
-                s.n = span.y - span.x + 1;
-                s.rows = f.rows;
-                return s;
+                return PaSource{f.o + (slot * CHUNKS * f.rows + row) * 8, f.ml + slot * f.rows + row, span.y - span.x + 1, f.rows};
             };
-            if (p.shared) src[0][tid] = find(b * p.T + node, true);
-            src[1][tid] = find(node, false);
-            // a single piece was written out by the kernel before
-            if (p.shared || src[1][tid].n > 1) at = (((int64_t)b * p.T + node) * p.Hq + g * p.G + head) * D;
+            if (seq_tiles(p, len)) {
+                if (p.shared) s0 = source(f0, item0, row0, span0);
+                s1 = source(f1, item1, row1, span1);
+                // a single piece was written out by the kernel before
+                if (p.shared || s1.n > 1) at = (((int64_t)b * p.T + node) * p.Hq + g * p.G + head) * D;
+            }
         }
+        src[0][tid] = s0;
+        src[1][tid] = s1;
         out_at[tid] = at;
     }
     __syncthreads();
-    {
-        const int row = tid / CHUNKS;
-        float m = -INFINITY;
+    const int row = tid % ROWS, chunk = tid / ROWS % CHUNKS, part = tid / (ROWS * CHUNKS);
+    PaSum sum = {-INFINITY, 0.f, {}};
+    if (out_at[row] >= 0) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            for (int i = tid % CHUNKS; i < src[k][row].n; i += CHUNKS) m = max_nan(m, src[k][row].ml[(size_t)i * src[k][row].rows].x);
+        for (int k = 0; k < 2; ++k) {
+            const PaSource s = src[k][row];
+            for (int i0 = part * 4; i0 < s.n; i0 += SPLIT * 4) {
+                float2 ml[4];
+                float4 a[4], c[4];
 #pragma unroll
-        for (int o = CHUNKS / 2; o; o /= 2) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (tid % CHUNKS == 0) top[row] = m;
-    }
-    __syncthreads();
-    const int row = tid % ROWS, chunk = tid / ROWS;
-    if (out_at[row] < 0) return;
-    const float m = top[row];
-    float acc[8] = {}, l = 0.f;
+                for (int u = 0; u < 4; ++u) {
+                    const int i = min(i0 + u, s.n - 1);
+                    const float4 *o = reinterpret_cast<const float4 *>(s.o + ((size_t)i * CHUNKS + chunk) * s.rows * 8);
+                    ml[u] = s.ml[(size_t)i * s.rows];
+                    a[u] = o[0];
+                    c[u] = o[1];
+                }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const PaSource s = src[k][row];
-#pragma unroll 4
-        for (int i = 0; i < s.n; ++i) {
-            const float2 ml = s.ml[(size_t)i * s.rows];
-            const float4 *o = reinterpret_cast<const float4 *>(s.o + ((size_t)i * CHUNKS + chunk) * s.rows * 8);
-            const float4 a = o[0], c = o[1];
-            const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
-            l = fmaf(w, ml.y, l);
-            acc[0] = fmaf(w, a.x, acc[0]); acc[1] = fmaf(w, a.y, acc[1]); acc[2] = fmaf(w, a.z, acc[2]); acc[3] = fmaf(w, a.w, acc[3]);
-            acc[4] = fmaf(w, c.x, acc[4]); acc[5] = fmaf(w, c.y, acc[5]); acc[6] = fmaf(w, c.z, acc[6]); acc[7] = fmaf(w, c.w, acc[7]);
+                for (int u = 0; u < 4; ++u)
+                    if (i0 + u < s.n) sum.add(ml[u].x, ml[u].y, {a[u].x, a[u].y, a[u].z, a[u].w, c[u].x, c[u].y, c[u].z, c[u].w});
+            }
         }
     }
-    const float inv = 1.f / l;
+    if (SPLIT > 1) {
+        sums[tid] = sum;
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int k = 1; k < SPLIT; ++k) sum.add(sums[tid + k * ROWS * CHUNKS].m, sums[tid + k * ROWS * CHUNKS].l, sums[tid + k * ROWS * CHUNKS].acc);
+    }
+    if (out_at[row] < 0) return;
+    const float inv = 1.f / sum.l;
+    const float *acc = sum.acc;
     *reinterpret_cast<uint4 *>(p.out + out_at[row] + chunk * 8) = make_uint4(pack2_bf16(acc[0] * inv, acc[1] * inv), pack2_bf16(acc[2] * inv, acc[3] * inv),
                                                                             pack2_bf16(acc[4] * inv, acc[5] * inv), pack2_bf16(acc[6] * inv, acc[7] * inv));
 }
@@ -900,8 +923,12 @@ static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtens
     }
     MTV_CUDA_CHECK(launch_dependent(paged_attn_kernel<D>, dim3(sm_count()), PA_THREADS, PaSmem<D>::TOTAL, stream, q, k, v, p));
     const int64_t rows = (int64_t)p.B * p.Hkv * p.T * p.G;
-    const int per_block = 256 / (D / 8);
-    MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D>, dim3((unsigned)((rows + per_block - 1) / per_block)), 256, 0, stream, p));
+    // Few rows (decoding): their pieces are many, and a thread for each would leave SMs empty.
+    constexpr int PER = 256 / (D / 8);
+    if (rows < 4L * PER * sm_count())
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 4>, dim3((unsigned)((rows + PER / 4 - 1) / (PER / 4))), 256, 0, stream, p));
+    else
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 1>, dim3((unsigned)((rows + PER - 1) / PER)), 256, 0, stream, p));
     return MTV_OK;
 }
 
