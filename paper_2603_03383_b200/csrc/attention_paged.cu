@@ -5,9 +5,10 @@
 // divide 128; the others idle).  Behind the shared prefix the nodes of all sequences follow one another, and a tile takes them as they
 // come: every shared key is loaded and multiplied once per tile, whoever the rows belong to.  Behind it a tile holds nodes of one
 // sequence.  An ITEM is a KV head's keys (the prefix, or one sequence's own) for two row tiles, or for the one that is left over where
-// their number is odd; its keys come in tiles of 128.  Items of two row tiles and items of one are worked off one kind
-// after the other (the PHASES of the kernel), each laid out on a line on which a key tile counts TILE_COST and the start and end of an item
-// ITEM_COST, and each line is cut into equal runs, one per worker.  A worker's PIECE of an item leaves O (fp32, unnormalised) and the running
+// their number is odd; its keys come in tiles of 128.  Items of two row tiles and items of one (the PHASES of the kernel) are each laid
+// out on a line on which a key tile counts TILE_COST and the start and end of an item ITEM_COST; the CTAs are divided between the two
+// by what they take (not one after the other on all: the prefix of a decoding batch would be cut into 148 pieces of four key tiles, whose partial
+// results and cold starts took longer than its products), and each line is cut into equal runs, one per worker.  A worker's PIECE of an item leaves O (fp32, unnormalised) and the running
 // (max, sum) of its rows in the workspace, and the second kernel joins the pieces; an item that is one worker's alone and has no prefix
 // beside it is written out directly.
 //
@@ -20,8 +21,7 @@
 //                     in order, so S may overwrite the P that the product in front of it reads, and "S is complete" implies that O is
 //                     complete up to the tile before.  (A wait costs an issuing warp a hundred cycles even where there is nothing to wait for,
 //                     and the tensor core has only some two products queued: one warp for both row tiles left it idle a third of the time.)
-//   warp 18           derives the pieces from the lengths, hands them to the other warps, and requests their Q, K and V (a box per page);
-//                     reports the sequences' status at the end
+//   warp 18           derives the pieces from the lengths, hands them to the other warps, and requests their Q, K and V (a box per page)
 //   warp 19           clears V rows behind the last key (their weight is 0, but 0 * NaN is not) and takes non-finite values of the tree's
 //                     V rows out (they are given to the rows that see them at the end)
 //
@@ -40,7 +40,10 @@ constexpr int PA_QUEUE = 4;               // pieces that are handed out and may 
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
 constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
-constexpr int TILE_COST = 4, ITEM_COST = 16;   // what a piece's start and end take, in quarters of a key tile
+constexpr int TILE_COST = 4;              // a key tile on a line
+__host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }   // what the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles
+__host__ __device__ constexpr int PHASE_COST(int single) { return single ? 4 : 7; }   // and what a quarter of a key tile takes a CTA, one against the other: pairs are bound by the tensor core and
+                                          // its waits (3.9 k cycles a key tile at D = 128), single row tiles by their K and V (2.2 k, two at a time)
 
 template <int D> struct PaSmem {
     static constexpr int HALVES = D / 64;
@@ -68,17 +71,17 @@ struct PaPhase {
     int prefix_items, seq_items;       // items of the prefix, and of each sequence
     int prefix_per_head, seq_per_head;
     int prefix_tile0, seq_tile0;       // row tile of a head's first item (0 where an item is a pair)
-    int workers, rows;                 // at most; rows of a slot
+    int rows;                          // of a slot
     float *o;                          // [slots][D / 8][rows][8]
     float2 *ml;                        // [slots][rows]
     int2 *span;                        // [items]: first and last worker that has a piece of it
 };
 struct PaParams {
     PagedRef pages;
-    PaPhase phase[2];                  // pairs of row tiles, single row tiles
+    PaPhase phase[3];                  // pairs of row tiles, single row tiles, thin ones
     const int32_t *seq_lens;
     const uint64_t *anc;               // [T][2]
-    const __nv_bfloat16 *v;
+    const __nv_bfloat16 *q, *k, *v;
     __nv_bfloat16 *out;
     int32_t *status, *dev_error;
     float scale_log2;
@@ -87,13 +90,13 @@ struct PaParams {
 
 // ---------------------------------------------------------------------------------------- the division of the work
 __device__ __forceinline__ int key_tiles(int keys) { return (keys + PA_KEYS - 1) / PA_KEYS; }
-__device__ __forceinline__ int item_cost(int tiles) { return tiles ? tiles * TILE_COST + ITEM_COST : 0; }
+__device__ __forceinline__ int item_cost(int tiles, int ends) { return tiles ? tiles * TILE_COST + ends : 0; }
 // own key tiles of a sequence; 0: it is left out
 __device__ __forceinline__ int seq_tiles(const PaParams &p, int L) {
     return p.pages.fits(L, p.T) && L >= p.shared ? key_tiles(L - p.shared + p.T) : 0;
 }
 // tiles of an item in front of position y of its stretch of the line
-__device__ __forceinline__ int cut_at(int y, int tiles) { return y <= ITEM_COST ? 0 : min((y - ITEM_COST + TILE_COST / 2) / TILE_COST, tiles); }
+__device__ __forceinline__ int cut_at(int y, int tiles, int ends) { return y <= ends ? 0 : min((y - ends + TILE_COST / 2) / TILE_COST, tiles); }
 
 struct __align__(16) PaPiece {
     int b;              // -1: the prefix
@@ -110,7 +113,7 @@ __device__ __forceinline__ bool is_last(const PaPiece &s, int t) { return s.b >=
 // A worker's run of a phase's line (lines are shorter than 2^31: checked by the host).
 struct PaWalk {
     int x0, x1, S;      // the run, and the position of the next item
-    int b, idx, tiles, L, worker;
+    int b, idx, tiles, L, worker, ends;
     __device__ __forceinline__ void load(const PaParams &p) {
         if (b < 0) {
             L = p.shared;
@@ -129,9 +132,9 @@ struct PaWalk {
                 load(p);
                 continue;
             }
-            s.t0 = cut_at(x0 - S, tiles);
-            s.t1 = cut_at(x1 - S, tiles);
-            S += item_cost(tiles);
+            s.t0 = cut_at(x0 - S, tiles, ends);
+            s.t1 = cut_at(x1 - S, tiles, ends);
+            S += item_cost(tiles, ends);
             const int i = idx++;
             if (s.t0 >= s.t1) continue;
             const int per = b < 0 ? f.prefix_per_head : f.seq_per_head, item = b < 0 ? i : f.prefix_items + b * f.seq_items + i;
@@ -151,36 +154,58 @@ struct PaWalk {
 };
 // The runs of the workers of a CTA (pairs; single tiles of its halves) and the items they begin in.  One warp.
 __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], int cta, int n_cta, int lane) {
-    auto cost_of = [&](int b) { return b < p.B ? item_cost(seq_tiles(p, p.seq_lens[b])) : 0; };
-    const int own0 = cost_of(lane);      // cost of an item of this lane's sequence
-    int total = own0;
-    for (int b0 = 32; b0 < p.B; b0 += 32) total += cost_of(b0 + lane);
-    total = __reduce_add_sync(0xffffffffu, total);
-    const int cost = item_cost(key_tiles(p.shared));
+    auto tiles_of = [&](int b) { return b < p.B ? seq_tiles(p, p.seq_lens[b]) : 0; };
+    const int own0 = tiles_of(lane);
+    int tiles = own0, seqs = own0 > 0;   // key tiles of an item of every sequence that is not left out, and their number
+    for (int b0 = 32; b0 < p.B; b0 += 32) {
+        const int t = tiles_of(b0 + lane);
+        tiles += t;
+        seqs += t > 0;
+    }
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
+    seqs = __reduce_add_sync(0xffffffffu, seqs);
+    int prefix[2], length[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+        prefix[f] = item_cost(key_tiles(p.shared), ITEM_COST(f)) * p.phase[f].prefix_items;
+        length[f] = prefix[f] + (tiles * TILE_COST + seqs * ITEM_COST(f)) * p.phase[f].seq_items;
+    }
+    // the first CTAs take the pairs, the others the single row tiles
+    int n_pairs = n_cta;
+    if (length[1]) {
+        const float a = (float)length[0] * PHASE_COST(0), b = (float)length[1] * PHASE_COST(1);
+        n_pairs = length[0] ? max(1, min(n_cta - 1, __float2int_rn(n_cta * (a / (a + b))))) : 0;
+    }
     int y[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        const PaPhase &f = p.phase[k > 0];
-        const int prefix = cost * f.prefix_items, length = prefix + total * f.seq_items;
-        w[k].worker = k == 2 ? cta + n_cta : cta;
+        const int f = k > 0, cost = item_cost(key_tiles(p.shared), ITEM_COST(f));
+        const int workers = f ? 2 * (n_cta - n_pairs) : n_pairs, worker = k == 0 ? cta : k == 1 ? cta - n_pairs : cta + n_cta - 2 * n_pairs;
+        const bool on = f ? cta >= n_pairs : cta < n_pairs;
+        w[k].worker = worker;
+        w[k].ends = ITEM_COST(f);
         // none shorter than a key tile, so that no worker in the middle of an item is left without a tile
-        const int run = max((length + f.workers - 1) / f.workers, TILE_COST);
-        w[k].x0 = (int)min((int64_t)length, (int64_t)run * w[k].worker);
-        w[k].x1 = (int)min((int64_t)length, (int64_t)w[k].x0 + run);
+        const int run = on ? max((length[f] + workers - 1) / workers, TILE_COST) : 0;
+        w[k].x0 = on ? (int)min((int64_t)length[f], (int64_t)run * worker) : 0;
+        w[k].x1 = (int)min((int64_t)length[f], (int64_t)w[k].x0 + run);
         w[k].b = -1;
         w[k].idx = 0;
         w[k].S = w[k].x0 == w[k].x1 ? w[k].x1 : 0;
         y[k] = -1;
-        if (w[k].x0 < prefix) {
-            w[k].idx = w[k].x0 / cost;
-            w[k].S = w[k].idx * cost;
-        } else if (w[k].x0 < w[k].x1) {
-            y[k] = w[k].x0 - prefix;
+        if (w[k].x0 < w[k].x1) {
+            if (w[k].x0 < prefix[f]) {
+                w[k].idx = w[k].x0 / cost;
+                w[k].S = w[k].idx * cost;
+            } else {
+                y[k] = w[k].x0 - prefix[f];
+            }
         }
     }
-    int before = 0;
+    int before_tiles = 0, before_seqs = 0;
     for (int b0 = 0; b0 < p.B && (y[0] >= 0 || y[1] >= 0 || y[2] >= 0); b0 += 32) {
-        const int own = b0 ? cost_of(b0 + lane) : own0;
+        const int own = b0 ? tiles_of(b0 + lane) : own0;
+        const uint32_t some = __ballot_sync(0xffffffffu, own > 0);
+        const int n = __popc(some & (0xffffffffu >> (31 - lane)));
         int c = own;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -190,16 +215,18 @@ __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], i
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
             const PaPhase &f = p.phase[k > 0];
-            const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * f.seq_items > y[k]);
+            const int ends = ITEM_COST(k > 0), up_to = ((before_tiles + c) * TILE_COST + (before_seqs + n) * ends) * f.seq_items;
+            const uint32_t behind = __ballot_sync(0xffffffffu, up_to > y[k]);
             if (y[k] < 0 || !behind) continue;
             const int at = __ffs((int)behind) - 1;
-            const int each = __shfl_sync(0xffffffffu, own, at), first = (before + __shfl_sync(0xffffffffu, c, at) - each) * f.seq_items;
+            const int each = item_cost(__shfl_sync(0xffffffffu, own, at), ends), first = __shfl_sync(0xffffffffu, up_to, at) - each * f.seq_items;
             w[k].b = b0 + at;
             w[k].idx = (y[k] - first) / each;
             w[k].S = w[k].x0 - y[k] + first + w[k].idx * each;
             y[k] = -1;
         }
-        before += __shfl_sync(0xffffffffu, c, 31);
+        before_tiles += __shfl_sync(0xffffffffu, c, 31);
+        before_seqs += __popc(some);
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k)
@@ -438,16 +465,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             for (int e = max(0, entry - SM::STAGES); e < entry; ++e) ptx::mbar_wait(bar(PB_FULL + e % SM::STAGES), (e / SM::STAGES) & 1);
             for (int s = 0; s < 2; ++s)
                 if (n_q[s]) ptx::mbar_wait(bar(PB_QFULL + s), (n_q[s] - 1) & 1);
-        }
-        // which sequences can be attended to
-        if (p.status && cta < p.B) {
-            const int prefix = p.pages.check(0, 0, p.shared, lane);
-            for (int b = cta; b < p.B; b += n_cta) {
-                const int L = p.seq_lens[b];
-                int code = seq_tiles(p, L) ? p.pages.check(b, p.shared, L - p.shared + p.T, lane) : MTV_ERR_CAPACITY;
-                if (code == MTV_OK) code = prefix;
-                if (lane == 0) p.status[b] = code;
-            }
         }
     } else if (warp == PA_MMA_WARP || warp == PA_MMA_WARP + 1) {
         // ------------------------------------------------------------ products of row tile s
@@ -761,6 +778,293 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     if (warp == PA_MMA_WARP) ptx::tmem_dealloc(tmem, 512);
 }
 
+// ---------------------------------------------------------------------------------------- thin items
+// At most 16 query rows against a KV head's keys (plain decoding; the smallest trees): nothing but the bytes of K and V counts, and a row tile of
+// 128 would be nearly empty, its ring full of tiles that wait for each other's scores.  So these items go to warps of their own: mma.sync
+// with 16 rows, K and V straight from global memory into the operand registers, no shared memory in between.  A contraction's order
+// is free as long as both operands have it, and so is the order of O's columns: a thread takes 16-byte chunks of K as two products' B operands, and 32
+// bytes of a V row as its column in 16 products, two keys' values side by side by a byte permutation.
+// A CTA of four warps walks a run of the line of all thin items, 16 keys to a warp at a time; while a warp computes on 16 keys, V of them and K
+// of its next ones are on the way (8 KB a warp, two CTAs to an SM).  At a piece's end the warps join in shared memory.
+constexpr int TH_ROWS = 16, TH_WARPS = 4, TH_KEYS = 16, TH_STEP = TH_WARPS * TH_KEYS;
+constexpr int TH_ENDS = 3;                // what an item's start and end take, in steps of 64 keys
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ int thin_steps(int keys) { return (keys + TH_STEP - 1) / TH_STEP; }
+
+template <int D>
+__global__ void __launch_bounds__(TH_WARPS * 32, 2)
+paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
+    constexpr int C = D / 32;              // 32-column parts of a row
+    constexpr int J = D / 8;               // products of 8 columns of O
+    __shared__ float o_x[TH_WARPS][TH_ROWS][D + 4];
+    __shared__ float2 ml_x[TH_WARPS][TH_ROWS];
+    __shared__ int start[5];               // x0, x1, S, b, idx
+    let_next_start();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r0 = lane / 4, quad = lane % 4;
+    const PaPhase &ph = p.phase[2];
+    const int worker = blockIdx.x, workers = gridDim.x;
+    previous_done();
+    auto cost_of = [&](int b) {
+        const int L = b < p.B ? p.seq_lens[b] : -1;
+        return L >= 0 && p.pages.fits(L, p.T) && L >= p.shared ? thin_steps(L - p.shared + p.T) + TH_ENDS : 0;
+    };
+    if (warp == 0) {
+        const int own0 = cost_of(lane);
+        int total = own0;
+        for (int b0 = 32; b0 < p.B; b0 += 32) total += cost_of(b0 + lane);
+        total = __reduce_add_sync(0xffffffffu, total);
+        const int each = thin_steps(p.shared) + TH_ENDS, prefix = ph.prefix_items * each, length = prefix + total * ph.seq_items;
+        const int run = max((length + workers - 1) / workers, 1), x0 = (int)min((int64_t)length, (int64_t)run * worker), x1 = (int)min((int64_t)length, (int64_t)x0 + run);
+        int b = -1, idx = 0, S = x1;
+        if (x0 < x1 && x0 < prefix) {
+            idx = x0 / each;
+            S = idx * each;
+        } else if (x0 < x1) {
+            const int y = x0 - prefix;
+            int before = 0;
+            for (int b0 = 0; b0 < p.B; b0 += 32) {
+                const int own = b0 ? cost_of(b0 + lane) : own0;
+                int c = own;
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const int x = __shfl_up_sync(0xffffffffu, c, o);
+                    if (lane >= o) c += x;
+                }
+                const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * ph.seq_items > y);
+                if (behind) {
+                    const int at = __ffs((int)behind) - 1, cost = __shfl_sync(0xffffffffu, own, at);
+                    const int first = (before + __shfl_sync(0xffffffffu, c, at) - cost) * ph.seq_items;
+                    b = b0 + at;
+                    idx = (y - first) / cost;
+                    S = prefix + first + idx * cost;
+                    break;
+                }
+                before += __shfl_sync(0xffffffffu, c, 31);
+            }
+        }
+        if (lane == 0) { start[0] = x0; start[1] = x1; start[2] = S; start[3] = b; start[4] = idx; }
+    }
+    __syncthreads();
+    const int x0 = start[0], x1 = start[1];
+    int S = start[2], b = start[3], idx = start[4];
+    int L = 0, cost = 0;                   // keys of the item (prefix: the shared ones; else its own in front of the tree)
+    auto load_item = [&]() {
+        if (b < 0) {
+            L = p.shared;
+            cost = thin_steps(p.shared) + TH_ENDS;
+        } else {
+            cost = cost_of(b);
+            L = p.seq_lens[b] - p.shared;
+        }
+    };
+    if (x0 < x1) load_item();
+    while (S < x1) {
+        if (idx >= (b < 0 ? ph.prefix_items : ph.seq_items) || cost == 0) {
+            if (++b >= p.B) break;
+            idx = 0;
+            load_item();
+            continue;
+        }
+        const int steps = cost - TH_ENDS;
+        const int t0 = max(0, min(x0 - S - TH_ENDS, steps)), t1 = max(0, min(x1 - S - TH_ENDS, steps));
+        S += cost;
+        const int g = idx++;
+        if (t0 >= t1) continue;
+        const int item = b < 0 ? g : ph.prefix_items + b * ph.seq_items + g;
+        const bool own = b >= 0;
+        const int n_keys = L + (own ? p.T : 0), key0 = own ? p.shared : 0, rows = (own ? p.T : p.B * p.T) * p.G;
+        if (threadIdx.x == 0) {
+            if (t0 == 0) ph.span[item].x = worker;
+            if (t1 == steps) ph.span[item].y = worker;
+        }
+        // ---- the query rows as A operands: columns c * 32 + quad * 8 + [0, 4) and [4, 8) of rows r0 and r0 + 8
+        uint32_t qa[C][2][4];
+        uint32_t see[2];                   // tree rows that are visible to rows r0 and r0 + 8 (at most 16 nodes)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = r0 + 8 * h, n = r / p.G;
+            const bool is = r < rows;
+            const __nv_bfloat16 *src = p.q + (((size_t)(own ? b * p.T : 0) + n) * p.Hq + g * p.G + (r - n * p.G)) * D + quad * 8;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const uint4 u = is ? *reinterpret_cast<const uint4 *>(src + c * 32) : make_uint4(0u, 0u, 0u, 0u);
+                qa[c][0][h] = u.x; qa[c][0][h + 2] = u.y;
+                qa[c][1][h] = u.z; qa[c][1][h + 2] = u.w;
+            }
+            see[h] = is && own ? (uint32_t)p.anc[n * 2] : 0u;
+        }
+        float o[J][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        // ---- this warp's blocks of 16 keys: key (t * TH_WARPS + warp) * 16
+        const int32_t *table = p.pages.table + (int64_t)max(b, 0) * p.pages.max_pages;
+        auto block_key = [&](int t) { return (t * TH_WARPS + warp) * TH_KEYS; };
+        auto page_of = [&](int t) { return t < t1 && block_key(t) < n_keys ? table[(block_key(t) + key0) >> p.pages.page_shift] : -1; };
+        auto row_at = [&](int t, int id) {     // element offset of the block's first row; < 0: there is none
+            return id < 0 || id >= p.pages.n_pages ? -1ll
+                   : (long long)id * p.pages.stride_page + (long long)((block_key(t) + key0) & ((1 << p.pages.page_shift) - 1)) * p.pages.stride_t +
+                         g * p.pages.stride_h;
+        };
+        uint4 kx[2][C];                    // keys r0 and r0 + 8 of the block
+        auto load_k = [&](long long at) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    kx[h][c] = at >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p.k + at + (r0 + 8 * h) * p.pages.stride_t + c * 32 + quad * 8)) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        int id = page_of(t0), id_next = page_of(t0 + 1);
+        long long at = row_at(t0, id);
+        load_k(at);
+        for (int t = t0; t < t1; ++t) {
+            const int first = block_key(t);
+            if (first >= n_keys) break;    // (the item's last step: no keys for this warp)
+            // V of keys 2 quad, 2 quad + 1 and the same + 8: columns r0 * (D / 8) + [0, D / 8)
+            uint32_t vx[4][J / 2];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int key = 2 * quad + (k & 1) + 8 * (k >> 1);
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.v + at + key * p.pages.stride_t + r0 * J);
+                const bool is = at >= 0 && first + key < n_keys;     // rows behind the last key may hold anything
+#pragma unroll
+                for (int c = 0; c < J / 8; ++c) {
+                    const uint4 u = is ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
+                    vx[k][c * 4] = u.x; vx[k][c * 4 + 1] = u.y; vx[k][c * 4 + 2] = u.z; vx[k][c * 4 + 3] = u.w;
+                }
+            }
+            // ---- scores of keys [0, 8) and [8, 16): c0, c1 row r0, c2, c3 row r0 + 8, keys 2 quad and 2 quad + 1
+            float sc[2][4] = {};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    mma16816(sc[h], qa[c][0], kx[h][c].x, kx[h][c].y);
+                    mma16816(sc[h], qa[c][1], kx[h][c].z, kx[h][c].w);
+                }
+            const long long at_now = at;
+            id = id_next;
+            id_next = page_of(t + 2);
+            at = row_at(t + 1, id);
+            if (t + 1 < t1) load_k(at);    // on its way during the rest
+            const bool edge = first + TH_KEYS > L;
+            if (edge) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int a = first + 8 * h + 2 * quad + (e & 1) - L;
+                        if (a >= 0 && (!own || a >= p.T || !(see[e >> 1] >> a & 1u))) sc[h][e] = -INFINITY;
+                    }
+            }
+            float mx[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                mx[h] = max_nan(max_nan(sc[0][2 * h], sc[0][2 * h + 1]), max_nan(sc[1][2 * h], sc[1][2 * h + 1]));
+                mx[h] = max_nan(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
+                mx[h] = max_nan(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2)) * p.scale_log2;
+                if (mx[h] == INFINITY) mx[h] = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+            }
+            if (__any_sync(0xffffffffu, !(mx[0] <= m[0] + 8.f) || !(mx[1] <= m[1] + 8.f))) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float m_new = mx[h] <= m[h] ? m[h] : mx[h];
+                    const float w = m[h] == -INFINITY ? 0.f : ex2(m[h] - m_new);
+                    m[h] = m_new;
+                    l[h] *= w;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) { o[j][2 * h] *= w; o[j][2 * h + 1] *= w; }
+                }
+            }
+            const float me[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+            uint32_t pa[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float w0 = ex2(fmaf(sc[h][2 * r], p.scale_log2, -me[r])), w1 = ex2(fmaf(sc[h][2 * r + 1], p.scale_log2, -me[r]));
+                    l[r] += w0 + w1;
+                    pa[h * 2 + r] = pack2_bf16(w0, w1);
+                }
+            bool odd = false;
+            if (edge && own) {
+                // values of the tree's rows that are not finite are left out here and given below to the rows that see them
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int e = 0; e < J / 2; ++e) {
+                        if (nonfinite16(vx[k][e])) { vx[k][e] &= 0xffff0000u; odd = true; }
+                        if (nonfinite16(vx[k][e] >> 16)) { vx[k][e] &= 0xffffu; odd = true; }
+                    }
+                odd = __any_sync(0xffffffffu, odd);
+            }
+#pragma unroll
+            for (int j = 0; j < J; j += 2) {
+                mma16816(o[j], pa, __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x5410), __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x5410));
+                mma16816(o[j + 1], pa, __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x7632), __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x7632));
+            }
+            if (odd && at_now >= 0)
+                for (int k = 0; k < TH_KEYS; ++k) {
+                    const int a = first + k - L;
+                    if (a >= p.T) break;
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint16_t x = *reinterpret_cast<const uint16_t *>(p.v + at_now + k * p.pages.stride_t + (2 * quad + (e & 1)) * J + j);
+                            // (the shared keys and those in front of the tree are seen by all)
+                            if (nonfinite16(x) && (a < 0 || (see[e >> 1] >> a & 1u))) o[j][e] += __uint_as_float((uint32_t)x << 16);
+                        }
+                }
+        }
+        // ---- the four warps' shares of a row are joined: O[row][column (2 quad + (e & 1)) * J + j]
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            if (quad == 0) ml_x[warp][r0 + 8 * h] = make_float2(m[h], l[h]);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                o_x[warp][r0 + 8 * h][2 * quad * J + j] = o[j][2 * h];
+                o_x[warp][r0 + 8 * h][(2 * quad + 1) * J + j] = o[j][2 * h + 1];
+            }
+        }
+        __syncthreads();
+        const bool direct = p.shared == 0 && t1 - t0 == steps;      // the item's only piece
+        const size_t slot = (size_t)item + worker;
+        for (int e = threadIdx.x; e < rows * (D / 8); e += TH_WARPS * 32) {
+            const int row = e % rows, chunk = e / rows;
+            float mm = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < TH_WARPS; ++w) mm = max_nan(mm, ml_x[w][row].x);
+            float acc[8] = {}, ll = 0.f;
+#pragma unroll
+            for (int w = 0; w < TH_WARPS; ++w) {
+                const float2 ml = ml_x[w][row];
+                const float x = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
+                ll = fmaf(x, ml.y, ll);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] = fmaf(x, o_x[w][row][chunk * 8 + k], acc[k]);
+            }
+            if (direct) {
+                const float inv = 1.f / ll;
+                const int n = row / p.G;
+                *reinterpret_cast<uint4 *>(p.out + (((size_t)b * p.T + n) * p.Hq + g * p.G + row - n * p.G) * D + chunk * 8) =
+                    make_uint4(pack2_bf16(acc[0] * inv, acc[1] * inv), pack2_bf16(acc[2] * inv, acc[3] * inv), pack2_bf16(acc[4] * inv, acc[5] * inv),
+                               pack2_bf16(acc[6] * inv, acc[7] * inv));
+            } else {
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(acc[k]);
+                ptx::st_global_32(ph.o + ((slot * (D / 8) + chunk) * TH_ROWS + row) * 8, w);
+                if (chunk == 0) ph.ml[slot * TH_ROWS + row] = make_float2(ll == 0.f ? -INFINITY : mm, ll);
+            }
+        }
+        __syncthreads();                   // before the next piece's shares
+    }
+}
+
 // ---------------------------------------------------------------------------------------- their combination
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the pieces s of a row's two items (the prefix' and the sequence's own).  A thread takes
 // 8 columns of a row, neighbouring threads neighbouring rows, as the slots are laid out, and four pieces at a time, their
@@ -799,15 +1103,26 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
     }
     // row tile and row in it -> phase, item and row of the slot
     auto place = [&](int n, bool prefix, int *item, int *row) -> const PaPhase & {
+        const bool thin = prefix ? p.phase[2].prefix_items : p.phase[2].seq_items;
         const int tile = n / p.npc, per = prefix ? p.phase[0].prefix_per_head : p.phase[0].seq_per_head;
-        const int k = tile / 2 < per ? 0 : 1;
+        const int k = thin ? 2 : tile / 2 < per ? 0 : 1;
         const PaPhase &f = p.phase[k];
-        *row = (k ? 0 : (tile & 1) * 128) + (n - tile * p.npc) * p.G + head;
+        *row = thin ? n * p.G + head : (k ? 0 : (tile & 1) * 128) + (n - tile * p.npc) * p.G + head;
         const int i = k ? g : g * per + tile / 2;
         *item = prefix ? i : f.prefix_items + b * f.seq_items + i;
         return f;
     };
     previous_done();
+    // which sequences can be attended to, a warp each
+    if (p.status && (int)blockIdx.x * 8 < p.B) {
+        const int b2 = (int)blockIdx.x * 8 + tid / 32, lane = tid % 32;
+        if (b2 < p.B) {
+            const int len = p.seq_lens[b2];
+            int code = seq_tiles(p, len) ? p.pages.check(b2, p.shared, len - p.shared + p.T, lane) : MTV_ERR_CAPACITY;
+            if (code == MTV_OK) code = p.pages.check(0, 0, p.shared, lane);
+            if (lane == 0) p.status[b2] = code;
+        }
+    }
     if (tid < ROWS) {
         int64_t at = -1;
         PaSource s0 = {}, s1 = {};
@@ -873,22 +1188,23 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
 
 // ---------------------------------------------------------------------------------------- host
 // The phases of a call and the layout of its workspace; returns the bytes.
-static size_t pa_plan(PaPhase (&ph)[2], int T, int B, int G, int Hkv, int D, int shared, char *ws) {
+static size_t pa_plan(PaPhase (&ph)[3], int T, int B, int G, int Hkv, int D, int shared, char *ws) {
     const int npc = 128 / G, sms = sm_count();
-    const int prefix_tiles = shared ? (B * T + npc - 1) / npc : 0, seq_tiles = (T + npc - 1) / npc;
+    // at most 16 rows: thin items (measured for plain decoding, 64 sequences of 4 rows a KV head: 37 us, and 60 as single row tiles)
+    const bool thin_seq = T * G <= TH_ROWS, thin_prefix = shared && B * T * G <= TH_ROWS;
+    const int prefix_tiles = shared && !thin_prefix ? (B * T + npc - 1) / npc : 0, seq_tiles = thin_seq ? 0 : (T + npc - 1) / npc;
     size_t at = 0;
-    for (int f = 0; f < 2; ++f) {
+    for (int f = 0; f < 3; ++f) {
         PaPhase &x = ph[f];
-        x.prefix_per_head = f ? prefix_tiles % 2 : prefix_tiles / 2;
-        x.seq_per_head = f ? seq_tiles % 2 : seq_tiles / 2;
+        x.prefix_per_head = f == 2 ? thin_prefix : f ? prefix_tiles % 2 : prefix_tiles / 2;
+        x.seq_per_head = f == 2 ? thin_seq : f ? seq_tiles % 2 : seq_tiles / 2;
         x.prefix_items = Hkv * x.prefix_per_head;
         x.seq_items = Hkv * x.seq_per_head;
         x.prefix_tile0 = f ? prefix_tiles - 1 : 0;
         x.seq_tile0 = f ? seq_tiles - 1 : 0;
-        x.workers = f ? 2 * sms : sms;
-        x.rows = f ? 128 : 256;
+        x.rows = f == 2 ? TH_ROWS : f ? 128 : 256;
         const size_t items = (size_t)x.prefix_items + (size_t)B * x.seq_items;
-        const size_t slots = items ? items + x.workers : 0;     // a piece's slot: its item's number plus its worker's
+        const size_t slots = items ? items + (f ? 2 : 1) * sms : 0;     // a piece's slot: its item's number plus its worker's
         x.o = reinterpret_cast<float *>(ws + at);
         at += align_up(slots * x.rows * D * sizeof(float), 256);
         x.ml = reinterpret_cast<float2 *>(ws + at);
@@ -903,10 +1219,11 @@ static bool pa_sizes_ok(const mtv_tree *tree, int B, int Hq, int Hkv, int D, int
     return tree && B >= 1 && B <= PA_MAX_B && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= 8 && (D == 64 || D == 128) && shared >= 0 &&
            (int64_t)Hq * B * tree->T <= 1 << 28;
 }
-// Lines of either phase stay below 2^31, whatever the lengths.
-static bool pa_lines_ok(const PaPhase (&ph)[2], int B, int shared, int64_t slots) {
+// All lines stay below 2^31, whatever the lengths.
+static bool pa_lines_ok(const PaPhase (&ph)[3], int B, int shared, int64_t slots) {
     for (const PaPhase &f : ph) {
-        const int64_t prefix = (shared / PA_KEYS + 1) * TILE_COST + ITEM_COST, own = (slots / PA_KEYS + 2) * TILE_COST + ITEM_COST;
+        // (a thin item's steps are of 64 keys and count one)
+        const int64_t ends = ITEM_COST(0), prefix = (shared / PA_KEYS + 1) * TILE_COST + ends, own = (slots / PA_KEYS + 2) * TILE_COST + ends;
         if (own * B > 0x7fffffff || prefix > 0x7fffffff) return false;
         if ((double)prefix * f.prefix_items + (double)own * B * f.seq_items > 2147000000.0) return false;
     }
@@ -921,7 +1238,11 @@ static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtens
         MTV_CUDA_CHECK(cudaFuncSetAttribute(paged_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PaSmem<D>::TOTAL));
         if (done) *done = true;
     }
-    MTV_CUDA_CHECK(launch_dependent(paged_attn_kernel<D>, dim3(sm_count()), PA_THREADS, PaSmem<D>::TOTAL, stream, q, k, v, p));
+    const PaPhase &thin = p.phase[2];
+    if (p.phase[0].prefix_items + p.phase[0].seq_items + p.phase[1].prefix_items + p.phase[1].seq_items)
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_kernel<D>, dim3(sm_count()), PA_THREADS, PaSmem<D>::TOTAL, stream, q, k, v, p));
+    if (thin.prefix_items + thin.seq_items)
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_thin_kernel<D>, dim3(2 * sm_count()), TH_WARPS * 32, 0, stream, p));
     const int64_t rows = (int64_t)p.B * p.Hkv * p.T * p.G;
     // Few rows (decoding): their pieces are many, and a thread for each would leave SMs empty.
     constexpr int PER = 256 / (D / 8);
@@ -937,7 +1258,7 @@ static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtens
 extern "C" size_t tree_attention_paged_workspace_bytes(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int shared_len) {
     using namespace mtv;
     if (!pa_sizes_ok(tree, B, Hq, Hkv, D, shared_len)) return 0;
-    PaPhase ph[2];
+    PaPhase ph[3];
     return pa_plan(ph, tree->T, B, Hq / Hkv, Hkv, D, shared_len, nullptr);
 }
 
@@ -962,6 +1283,8 @@ extern "C" int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq
     p.npc = 128 / p.G;
     p.page_rows = pool->page_size < PA_KEYS ? pool->page_size : PA_KEYS;
     p.seq_lens = seq_lens; p.anc = tree->d_anc;
+    p.q = reinterpret_cast<const __nv_bfloat16 *>(q);
+    p.k = reinterpret_cast<const __nv_bfloat16 *>(k_pool);
     p.v = reinterpret_cast<const __nv_bfloat16 *>(v_pool);
     p.out = reinterpret_cast<__nv_bfloat16 *>(out);
     p.status = status; p.dev_error = tree->d_error;

@@ -69,6 +69,13 @@ def check(tree, tb, Hq, Hkv, D, page, shared, lens, seed=1, tokens_outside=False
     (5, 128, 5, 5, 128, 16, 160, [161, 161, 161]),       # groups of one
     (1, 1, 4, 1, 64, 16, 0, [9000] + [1] * 300 + [5000] + [3] * 200),      # long pieces beside many short ones
     (1, 1, 2, 2, 128, 32, 32, [40 + i % 50 for i in range(150)] + [6000]),
+    # at most 16 query rows a KV head: of a sequence, and of all behind the prefix (2 x 8, 4 x 4)
+    (2, 2, 8, 1, 128, 16, 0, [0, 5, 14, 15, 16, 63, 64, 500]),
+    (3, 16, 2, 2, 64, 32, 64, [64, 80, 1001]),
+    (3, 4, 16, 4, 128, 64, 128, [128, 129, 2047]),
+    (2, 3, 10, 2, 128, 16, 16, [17, 300]),
+    (1, 1, 8, 1, 64, 16, 160, [160, 333]),
+    (1, 1, 16, 4, 128, 128, 2048, [2048, 2100, 2049, 5000]),
 ])
 def test_against_the_oracle(K, T, Hq, Hkv, D, page, shared, lens):
     tb, tree = make_tree("rank_prior", K, (), T) if T > 1 else make_tree("cartesian", 1, (1,))
@@ -84,7 +91,7 @@ def _tree(K, T):
     return make_tree("rank_prior", K, (), T)
 
 
-@pytest.mark.parametrize("D,T,G", [(128, 64, 4), (64, 1, 8), (128, 20, 3)])
+@pytest.mark.parametrize("D,T,G", [(128, 64, 4), (64, 1, 8), (128, 20, 3), (128, 4, 4)])
 @pytest.mark.parametrize("size", [1.0, 30.0, 300.0])
 def test_scores_that_grow_along_the_keys(D, T, G, size):
     """Keys that get longer: the running maximum of most rows rises from tile to tile, by up to hundreds, so that the reference has to
@@ -108,7 +115,7 @@ def test_scores_that_grow_along_the_keys(D, T, G, size):
     assert ((out.double() - want).abs() / (bound(want, absolute) + slop)).max().item() <= 1.0
 
 
-@pytest.mark.parametrize("T", [1, 29, 64])
+@pytest.mark.parametrize("T", [1, 4, 29, 64])
 @pytest.mark.parametrize("D", [64, 128])
 def test_non_finite_rows_reach_those_who_see_them(D, T):
     """NaN and infinities in K and V rows of single nodes and behind the last node: nodes that do not see them have the results of a cache
@@ -122,7 +129,7 @@ def test_non_finite_rows_reach_those_who_see_them(D, T):
     clean, _ = want_of(q, kp, vp, t, lens, tb["mask"])
     mask = torch.tensor(tb["mask"], dtype=torch.bool)
     at = lambda b, s: (int(t[b, s // page]), s % page)  # noqa: E731
-    bad_v = {} if T == 1 else {0: (5, float("nan")), 1: (T - 1, float("inf")), 2: (T // 2, float("-inf"))}
+    bad_v = {} if T == 1 else {0: (min(5, T - 1), float("nan")), 1: (T - 1, float("inf")), 2: (T // 2, float("-inf"))}
     for b, L in enumerate(lens):
         for s in range(L + T, L + T + 30):       # behind the last node
             pg, r = at(b, s)
@@ -147,20 +154,21 @@ def test_non_finite_rows_reach_those_who_see_them(D, T):
         assert (out[b][fine] - want[fine]).abs().max().item() <= 2e-2
 
 
+@pytest.mark.parametrize("T", [64, 3])
 @pytest.mark.parametrize("where", ["q", "k", "k_inf"])
-def test_non_finite_scores(where):
+def test_non_finite_scores(where, T):
     """A NaN in a query row makes that row NaN; a NaN or an infinity in a prefix key every row of its head that has a finite query."""
-    tb, tree = _tree(4, 64)
+    tb, tree = _tree(4, T)
     g = torch.Generator().manual_seed(13)
     shared, lens, page, Hkv, G, D = 128, [400, 200], 16, 2, 4, 128
     for col in (0, 6, 12, 13, 14, 15, 70, 127):              # columns of either exponential
-        t, n_pages = table(g, 2, 400 - shared + 64, page, shared)
+        t, n_pages = table(g, 2, 400 - shared + T, page, shared)
         kp, vp = pools(g, 2, n_pages, Hkv, page, D)
-        q = torch.randn(2, 64, Hkv * G, D, generator=g).to(torch.bfloat16)
-        want = torch.zeros(2, 64, Hkv * G, dtype=torch.bool)
+        q = torch.randn(2, T, Hkv * G, D, generator=g).to(torch.bfloat16)
+        want = torch.zeros(2, T, Hkv * G, dtype=torch.bool)
         if where == "q":
-            q[1, 9, 5, col] = float("nan")
-            want[1, 9, 5] = True
+            q[1, T - 2, 5, col] = float("nan")
+            want[1, T - 2, 5] = True
         else:
             s = 128 + 128 + col if where == "k" else 128 + col      # sequence 0 alone, second or first own tile
             pg, r = int(t[0, s // page]), s % page
