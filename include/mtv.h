@@ -407,7 +407,7 @@ int keys_merge_shards(int n, int n_shards, int v_slab, const unsigned long long 
  *   page_table     device [B][max_pages] int32: slot s of sequence b is row s % page_size of page page_table[b][s / page_size];
  *                  entries behind a sequence's last slot are never followed
  * page_size: a power of two from 16 to 65536; strides multiples of 8 and at least D; pool base addresses 16-byte aligned;
- * max_pages * page_size below 2^31 - 256.  Sequences may share pages that a call only reads; two sequences of a call that
+ * max_pages * page_size below 2^31 - 256; D is 64 or 128, heads at most 4096.  Sequences may share pages that a call only reads; two sequences of a call that
  * write rows of the same page race.
  * status[b] of the calls below: MTV_OK; MTV_ERR_CAPACITY if seq_lens[b] is negative or the rows do not fit max_pages;
  * MTV_ERR_BOUNDS if the table names no page of the pool where the call needs one (checked in every build).

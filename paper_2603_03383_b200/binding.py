@@ -396,7 +396,7 @@ def mtv_verify_step_host(tree, dev: StepArgs, host: StepArgs, stream=None):
 def pool_layout(pool: torch.Tensor) -> PoolLayout:
     """Layout of a pool tensor [n_pages][Hkv][page_size][D] of any strides with the columns innermost (a pool whose pages hold
     [page_size][Hkv][D] is passed as its transposed view)."""
-    assert pool.dim() == 4 and pool.stride(3) == 1
+    assert pool.dim() == 4 and pool.stride(3) == 1 and pool.dtype == torch.bfloat16
     sp, sh, st = pool.stride()[:3]
     return PoolLayout(sp, sh, st, pool.shape[2], pool.shape[0])
 

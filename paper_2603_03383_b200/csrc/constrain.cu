@@ -41,33 +41,46 @@ struct ConstrainParams {
     int T, V, words, n_bias, n_masks, rows_per_block;
 };
 
+// bits 0-3 -> the sign bits of bytes 0-3
+__device__ __forceinline__ uint32_t signs_of(uint32_t bits) { return ((bits & 0xfu) * 0x00204081u & 0x01010101u) << 7; }
+// every byte of the result: the sign of the byte of x that its digit of the selector names (8 + byte), eight times.  (__byte_perm leaves the digits'
+// top bit out.)
+__device__ __forceinline__ uint32_t spread(uint32_t x, uint32_t selector) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %1, %2;" : "=r"(r) : "r"(x), "r"(selector));
+    return r;
+}
+// where a bit is 0: -inf
+__device__ __forceinline__ uint32_t keep(uint32_t x, uint32_t mask, uint32_t hidden) { return (x & mask) | (hidden & ~mask); }
+
 template <typename E> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
     static constexpr int VEC = 8;
     static __device__ __forceinline__ float get(const __nv_bfloat16 *p) { return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16); }
     static __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
-    static __device__ __forceinline__ float at(const uint4 &u, int e) {
-        const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
-        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    static __device__ __forceinline__ uint4 masked(const uint4 &u, uint32_t bits) {
+        const uint32_t a = signs_of(bits), b = signs_of(bits >> 4), hidden = 0xff80ff80u;
+        return make_uint4(keep(u.x, spread(a, 0x9988u), hidden), keep(u.y, spread(a, 0xbbaau), hidden),
+                          keep(u.z, spread(b, 0x9988u), hidden), keep(u.w, spread(b, 0xbbaau), hidden));
     }
-    // what is not in `bits` becomes -inf
-    static __device__ __forceinline__ uint4 masked(uint4 u, uint32_t bits) {
-        uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (!(bits >> (2 * k) & 1)) w[k] = (w[k] & 0xffff0000u) | 0xff80u;
-            if (!(bits >> (2 * k + 1) & 1)) w[k] = (w[k] & 0xffffu) | 0xff800000u;
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+    // largest value of a vector; NaN counts for nothing
+    static __device__ __forceinline__ float top(const uint4 &u) {
+        const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&u);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
     }
 };
 template <> struct Elem<float> {
     static constexpr int VEC = 4;
     static __device__ __forceinline__ float get(const float *p) { return *p; }
     static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
-    static __device__ __forceinline__ float at(const uint4 &u, int e) { return __uint_as_float(e == 0 ? u.x : e == 1 ? u.y : e == 2 ? u.z : u.w); }
-    static __device__ __forceinline__ uint4 masked(uint4 u, uint32_t bits) {
-        return make_uint4(bits & 1 ? u.x : 0xff800000u, bits & 2 ? u.y : 0xff800000u, bits & 4 ? u.z : 0xff800000u, bits & 8 ? u.w : 0xff800000u);
+    static __device__ __forceinline__ uint4 masked(const uint4 &u, uint32_t bits) {
+        const uint32_t a = signs_of(bits), hidden = 0xff800000u;
+        return make_uint4(keep(u.x, spread(a, 0x8888u), hidden), keep(u.y, spread(a, 0x9999u), hidden),
+                          keep(u.z, spread(a, 0xaaaau), hidden), keep(u.w, spread(a, 0xbbbbu), hidden));
+    }
+    static __device__ __forceinline__ float top(const uint4 &u) {
+        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
     }
 };
 
@@ -155,28 +168,36 @@ constrain_kernel(const ConstrainParams p) {
         }
     __syncthreads();
     const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
-    // ---- rows: a warp per unit of 1024 tokens
-    for (int u = warp; u < n_rows * CN_SUBS; u += CN_WARPS) {
-        const int r = u / CN_SUBS, s = u % CN_SUBS, base = slab + s * CN_UNIT;
-        const int n_tok = min(CN_UNIT, p.V - base);
-        if (n_tok <= 0) continue;
-        const size_t row = (size_t)b * p.T + row0 + r;
-        const E *in = static_cast<const E *>(p.logits) + (int64_t)row * p.ld_in + base;
-        E *out = WRITE ? static_cast<E *>(p.out) + (int64_t)row * p.ld_out + base : nullptr;
-        int m = p.mask_of ? p.mask_of[row] : -1;
+    // ---- rows: a warp per unit of 1024 tokens.  A unit's mask is requested while the one before is worked on.
+    auto mask_word = [&](int u) -> uint32_t {
+        const int r = u / CN_SUBS, base = slab + u % CN_SUBS * CN_UNIT;
+        if (r >= n_rows || base + lane * 32 >= p.V) return 0u;
+        int m = p.mask_of ? p.mask_of[(size_t)b * p.T + row0 + r] : -1;
         if (m >= p.n_masks) {
             if (lane == 0) atomicExch(p.dev_error, MTV_ERR_BOUNDS);
             m = -1;
         }
-        uint32_t allowed = 0u;
-        if (lane * 32 < n_tok) {
-            allowed = m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + lane] : 0xffffffffu;
-            if (n_tok - lane * 32 < 32) allowed &= (1u << (n_tok - lane * 32)) - 1u;
-        }
-        int here = lane < CN_PATH ? path[r][lane] - base : -1;       // this lane's token of the path, where it lies in this unit
-        if (here < 0 || here >= n_tok) here = -1;
+        uint32_t w = m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + lane] : 0xffffffffu;
+        const int left = p.V - base - lane * 32;
+        if (left < 32) w &= (1u << left) - 1u;
+        return w;
+    };
+    uint32_t next = mask_word(warp);
+    for (int u = warp; u < n_rows * CN_SUBS; u += CN_WARPS) {
+        const int r = u / CN_SUBS, s = u % CN_SUBS, base = slab + s * CN_UNIT;
+        const int n_tok = min(CN_UNIT, p.V - base);
+        const uint32_t allowed = next;
+        next = mask_word(u + CN_WARPS);
+        // (nothing allowed: the argmax need not look at the logits)
+        if (n_tok <= 0 || (!WRITE && !__any_sync(0xffffffffu, allowed != 0u))) continue;
+        const size_t row = (size_t)b * p.T + row0 + r;
+        const E *in = static_cast<const E *>(p.logits) + (int64_t)row * p.ld_in + base;
+        E *out = WRITE ? static_cast<E *>(p.out) + (int64_t)row * p.ld_out + base : nullptr;
+        int here = lane < CN_PATH ? path[r][lane] : -1;       // this lane's token of the path, where it lies in this unit
+        here = here >= base && here - base < n_tok ? here - base : -1;
+        const uint32_t on_path = __ballot_sync(0xffffffffu, here >= 0);
         uint32_t dense = allowed & ~listed[s][lane];
-        for (uint32_t some = __ballot_sync(0xffffffffu, here >= 0); some; some &= some - 1) {
+        for (uint32_t some = on_path; some; some &= some - 1) {
             const int at = __shfl_sync(0xffffffffu, here, __ffs((int)some) - 1);
             if (lane == at / 32) dense &= ~(1u << (at % 32));
         }
@@ -188,57 +209,56 @@ constrain_kernel(const ConstrainParams p) {
         const int off = (int)((uintptr_t)in / sizeof(E) % VEC);
         const bool out_vec = WRITE && (int)((uintptr_t)out / sizeof(E) % VEC) == off;
         const int n_vec = (off + n_tok + VEC - 1) / VEC;
-        float best = -INFINITY;
-        int at = -1;
-        bool low = false;        // an allowed -inf was met
+        constexpr uint32_t ALL = (1u << VEC) - 1u;
+        auto whole = [&](int j) { return j * VEC >= off && (j + 1) * VEC - off <= n_tok; };
+        auto bits_of = [&](int j) {
+            const int t0 = j * VEC - off;
+            return __funnelshift_r(words[t0 >> 5], words[(t0 >> 5) + 1], t0 & 31) & ALL;
+        };
+        // the largest of the tokens taken one by one and the first that has it; the largest of the vectors and the first vector that has it
+        float best = -INFINITY, best_v = -INFINITY;
+        int at = -1, at_v = -1;
         auto one = [&](int t, float x) {
             if (x > best || (x == best && t < at)) { best = x; at = t; }
-            low = low || x == -INFINITY;
         };
-        auto vec_of = [&](int j, const uint4 &x) {
-            const int t0 = j * VEC - off;
-            const uint32_t bits = __funnelshift_r(words[t0 >> 5], words[(t0 >> 5) + 1], t0 & 31);
-            if (WRITE) {
-                const uint4 y = El::masked(x, bits);
-                if (out_vec) {
-                    *reinterpret_cast<uint4 *>(out + t0) = y;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) out[t0 + e] = reinterpret_cast<const E *>(&y)[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float v = El::at(x, e);
-                    if (bits >> e & 1) {
-                        if (v > best) { best = v; at = t0 + e; }
-                        low = low || v == -INFINITY;
-                    }
-                }
-            }
-        };
-        auto whole = [&](int j) { return j * VEC >= off && (j + 1) * VEC - off <= n_tok; };
         for (int j0 = lane; j0 < n_vec; j0 += 32 * 4) {
             uint4 x[4];
+            uint32_t bits[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (j0 + 32 * k < n_vec && whole(j0 + 32 * k)) x[k] = *reinterpret_cast<const uint4 *>(in + ((j0 + 32 * k) * VEC - off));
+            for (int k = 0; k < 4; ++k) {
+                const int j = j0 + 32 * k;
+                bits[k] = j < n_vec && whole(j) ? bits_of(j) : 0u;
+                if (bits[k]) x[k] = *reinterpret_cast<const uint4 *>(in + (j * VEC - off));
+                else x[k] = make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int j = j0 + 32 * k;
                 if (j >= n_vec) continue;
-                if (whole(j)) {
-                    vec_of(j, x[k]);
-                } else {
+                if (!whole(j)) {
                     for (int t = max(0, j * VEC - off); t < min(n_tok, (j + 1) * VEC - off); ++t) {
-                        const bool on = words[t >> 5] >> (t & 31) & 1;
+                        const bool is = words[t >> 5] >> (t & 31) & 1;
                         if (WRITE) {
-                            if (on) out[t] = in[t];
+                            if (is) out[t] = in[t];
                             else El::put(out + t, -INFINITY);
-                        } else if (on) {
+                        } else if (is) {
                             one(t, El::get(in + t));
                         }
                     }
+                    continue;
+                }
+                const uint4 y = El::masked(x[k], bits[k]);
+                if (WRITE) {
+                    const int t0 = j * VEC - off;
+                    if (out_vec) {
+                        *reinterpret_cast<uint4 *>(out + t0) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) out[t0 + e] = reinterpret_cast<const E *>(&y)[e];
+                    }
+                } else {
+                    const float v = El::top(y);
+                    if (v > best_v) { best_v = v; at_v = j; }     // strictly: the first vector stays
                 }
             }
         }
@@ -246,7 +266,8 @@ constrain_kernel(const ConstrainParams p) {
         // ---- listed tokens, then those of the path that are in no list
         auto special = [&](int t, uint32_t counted, float bias) {
             int c = (int)(counted & ~CN_PROMPT);
-            for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
+            if (on_path)
+                for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
             const float x = pen.apply(El::get(in + t), c, c > 0 || counted & CN_PROMPT, bias);
             if (WRITE) El::put(out + t, x);
             else one(t, x);
@@ -261,31 +282,42 @@ constrain_kernel(const ConstrainParams p) {
             if (first) special(here, 0u, 0.f);
         }
         if (!WRITE) {
-            // -inf alone: the first allowed one (its value is in no comparison above)
-            const bool any = __any_sync(0xffffffffu, at >= 0);
-            if (any || __any_sync(0xffffffffu, low)) {
-                if (!any) {
-                    for (int t = lane; t < n_tok && at < 0; t += 32)
-                        if (allowed_of[warp][t / 32] >> (t % 32) & 1) {
-                            int c = 0, bit = listed[s][t / 32] >> (t % 32) & 1;
-                            float x = El::get(in + t);
-                            for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
-                            if (bit || c) {
-                                float bias = 0.f;
-                                uint32_t counted = 0u;
-                                for (int e = 0; bit && e < n_list[s]; ++e)
-                                    if (list_at[s][e] == t) { bias = list_bias[s][e]; counted = list_count[s][e]; }
-                                c += (int)(counted & ~CN_PROMPT);
-                                x = pen.apply(x, c, c > 0 || counted & CN_PROMPT, bias);
-                            }
-                            if (x == -INFINITY) at = t;
-                        }
+            const float mine = fmaxf(best, best_v);
+            const uint32_t image = value_image(mine);         // (of -inf where this lane has nothing)
+            const uint32_t top = __reduce_max_sync(0xffffffffu, image);
+            uint32_t first = 0xffffffffu;
+            if (top != value_image(-INFINITY)) {
+                if (image == top) {
+                    if (best == mine) first = (uint32_t)at;
+                    if (best_v == mine) {
+                        // the first element of that vector that has the value
+                        const int t0 = at_v * VEC - off;
+                        const uint32_t bits = bits_of(at_v);
+                        for (int e = 0; e < VEC; ++e)
+                            if ((bits >> e & 1u) && El::get(in + t0 + e) == mine) { first = min(first, (uint32_t)(t0 + e)); break; }
+                    }
                 }
-                const uint32_t image = at >= 0 ? value_image(best) : 0u;
-                const uint32_t top = __reduce_max_sync(0xffffffffu, image);
-                const uint32_t first = __reduce_min_sync(0xffffffffu, at >= 0 && image == top ? (uint32_t)(base + at) : 0xffffffffu);
-                if (lane == 0) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - first));
+            } else {
+                // nothing but -inf and NaN: the first allowed -inf
+                for (int t = lane; t < n_tok && first == 0xffffffffu; t += 32)
+                    if (allowed_of[warp][t / 32] >> (t % 32) & 1) {
+                        int c = 0;
+                        const bool in_list = listed[s][t / 32] >> (t % 32) & 1;
+                        float x = El::get(in + t);
+                        for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
+                        if (in_list || c) {
+                            float bias = 0.f;
+                            uint32_t counted = 0u;
+                            for (int e = 0; in_list && e < n_list[s]; ++e)
+                                if (list_at[s][e] == t) { bias = list_bias[s][e]; counted = list_count[s][e]; }
+                            c += (int)(counted & ~CN_PROMPT);
+                            x = pen.apply(x, c, c > 0 || counted & CN_PROMPT, bias);
+                        }
+                        if (x == -INFINITY) first = (uint32_t)t;
+                    }
             }
+            first = __reduce_min_sync(0xffffffffu, first);
+            if (lane == 0 && first != 0xffffffffu) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - ((uint32_t)base + first)));
         }
         __syncwarp();       // before the next unit's bits
     }

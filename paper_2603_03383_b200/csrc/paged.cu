@@ -6,6 +6,7 @@
 namespace mtv {
 
 constexpr int PAGED_THREADS = 256;
+constexpr int PAGED_MAX_HEADS = 4096;
 constexpr int APPEND_ROWS = 4;       // rows of a block: with half a head's columns 64 (32), all its threads have an angle to work out
 
 // (x[d], x[d + D/2]) -> (x[d] cos - x[d + D/2] sin, x[d + D/2] cos + x[d] sin) for 8 columns, in fp32, rounded once to bf16
@@ -144,7 +145,8 @@ static int launch_append(AppendParams &p, cudaStream_t stream) {
     p.row_blocks = (p.n_rows + APPEND_ROWS - 1) / APPEND_ROWS;
     // enough blocks to fill the device a few times over, as many layers per block as that leaves
     long per = (long)p.row_blocks * p.n_layers / (6L * sm_count());
-    per = per < 1 ? 1 : per > p.n_layers ? p.n_layers : per;
+    per = per < 1 ? 1 : per > 64 ? 64 : per;
+    if (per > p.n_layers) per = p.n_layers;
     p.layers_per_block = (int)per;
     const int report = p.status || !p.row_blocks ? (p.B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32) : 0;
     MTV_CUDA_CHECK(launch_dependent(kv_append_rope_paged_kernel, dim3(p.row_blocks + report, (unsigned)((p.n_layers + per - 1) / per)),
@@ -156,8 +158,8 @@ static int append_args(AppendParams &p, int B, int Hq, int Hkv, int D, int n_lay
                        const mtv_bf16 *v_new, mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool,
                        const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta, int32_t *status) {
     if (!q || !q_out || !k_new || !v_new || !k_pools || !v_pools || !seq_lens) return MTV_ERR_INVALID_ARG;
-    if (B < 1 || Hq < 1 || Hkv < 1 || n_layers < 1 || !(rope_theta >= 0.f)) return MTV_ERR_INVALID_ARG;
-    if ((D != 64 && D != 128) || n_layers > 65535) return MTV_ERR_UNSUPPORTED_SHAPE;
+    if (B < 1 || Hq < 1 || Hkv < 1 || n_layers < 1 || !(rope_theta >= 0.f && rope_theta < INFINITY)) return MTV_ERR_INVALID_ARG;
+    if ((D != 64 && D != 128) || n_layers > 65535 || Hq > PAGED_MAX_HEADS || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
     const int rc = paged_ref(p.pages, pool, page_table, max_pages, D);
     if (rc != MTV_OK) return rc;
     p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.D = D; p.n_layers = n_layers;
@@ -306,7 +308,7 @@ extern "C" int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv,
     MTV_RANGE("kv_compact_accepted_paged");
     if (!tree || !k_pools || !v_pools || !seq_lens || !new_lens || !accept_len || !acc_nodes || B < 1 || Hkv < 1 || n_layers < 1)
         return MTV_ERR_INVALID_ARG;
-    if ((D != 64 && D != 128) || B > 65535) return MTV_ERR_UNSUPPORTED_SHAPE;
+    if ((D != 64 && D != 128) || B > 65535 || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
     CompactParams p = {};
     const int rc = paged_ref(p.pages, pool, page_table, max_pages, D);
     if (rc != MTV_OK) return rc;

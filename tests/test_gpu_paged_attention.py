@@ -177,3 +177,126 @@ def test_non_finite_scores(where, T):
             want[0, :, G:] = True
         out = run(tree, q, kp, vp, t, lens, shared)
         assert torch.equal(torch.isnan(out).all(-1), want) and torch.equal(torch.isnan(out).any(-1), want), col
+
+
+def sequences_of(t, n_pages, page, Hkv, D, lens, shared, T, Hq, seed=21):
+    g = torch.Generator().manual_seed(seed)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    return kp, vp, torch.randn(len(lens), T, Hq, D, generator=g).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,page,shared,lens", [
+    (64, 32, 8, 128, 64, 256, [256, 383, 900]), (29, 8, 2, 64, 16, 48, [700, 49]), (1, 8, 2, 128, 16, 32, [33, 32, 400]), (4, 4, 1, 64, 16, 0, [77]),
+])
+def test_pages_with_the_heads_inside(T, Hq, Hkv, D, page, shared, lens):
+    tb, tree = _tree(4, T)
+    check(tree, tb, Hq, Hkv, D, page, shared, lens, tokens_outside=True)
+    check(tree, tb, Hq, Hkv, D, page, shared, lens, scale=0.3)
+
+
+@pytest.mark.parametrize("T,G", [(64, 4), (20, 3), (1, 4), (4, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_sequences_that_cannot_be(D, T, G):
+    """Lengths that do not fit or end inside the prefix: out stays as it was.  A page that is not there: BOUNDS, and the other sequences have
+    what they would have alone.  Table entries behind the last slot are never followed."""
+    tb, tree = _tree(4, T)
+    page, shared, Hkv = 16, 64, 2
+    lens = [130, 63, -1, 300, 400, 210, 416 - T, 417 - T]
+    g = torch.Generator().manual_seed(5)
+    t, n_pages = table(g, len(lens), 416 - shared, page, shared)
+    kp, vp, q = sequences_of(t, n_pages, page, Hkv, D, lens, shared, T, Hkv * G)
+    assert t.shape[1] * page == 416
+    bad = t.clone()
+    bad[3, 100 // page] = n_pages
+    bad[0, -(-(130 + T) // page):] = -1
+    bad[5, (210 + T - 1) // page] = -3
+    status = torch.full((len(lens),), 5, dtype=torch.int32, device=DEV)
+    out = run(tree, q, kp, vp, bad, lens, shared, status=status)
+    cap = -6
+    assert status.tolist() == [0, cap, cap, -7, cap if 400 + T > 416 else 0, -7, 0, cap]
+    ok = [b for b in range(len(lens)) if status[b] == 0]
+    want, absolute = want_of(q[ok], kp, vp, t[ok], [lens[b] for b in ok], tb["mask"])
+    assert ((out[ok].double() - want).abs() / bound(want, absolute)).max().item() <= 1.0
+    for b in range(len(lens)):
+        if status[b] == cap:
+            assert (out[b] == 7.0).all()
+    bad = t.clone()
+    bad[0, 1] = n_pages + 5                      # a page of the prefix: it is missing for all
+    run(tree, q, kp, vp, bad, lens, shared, status=status)
+    assert all(s in (-7, cap) for s in status.tolist()[:1])
+
+
+@pytest.mark.parametrize("T", [64, 1])
+def test_two_streams_and_a_graph(T):
+    """Calls with workspaces of their own on two streams at once, and two graphs over one workspace replayed in turn, with other lengths and
+    pages than at their capture."""
+    tb, tree = _tree(4, T)
+    Hq, Hkv, D, page, shared = 16, 4, 128, 16, 96
+    lens = [[96, 500, 1000], [700, 97, 333]]
+    g = torch.Generator().manual_seed(5)
+    t, n_pages = table(g, 3, 1000 + T - shared, page, shared)
+    kp, vp, q = sequences_of(t, n_pages, page, Hkv, D, lens[0], shared, T, Hq)
+    kd, vd, td, qd = kp.to(DEV), vp.to(DEV), t.to(DEV), [q.to(DEV), q.flip(0).to(DEV)]
+    ld = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in lens]
+    n = binding.paged_workspace_bytes(tree, 3, Hq, Hkv, D, shared)
+    ws = [torch.full((n,), 0xff, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs = [torch.zeros_like(x) for x in qd]
+    want = [want_of(x.cpu(), kp, vp, t, ls, tb["mask"]) for x, ls in zip(qd, lens)]
+
+    def right(order=(0, 1)):
+        torch.cuda.synchronize()
+        for i, j in enumerate(order):
+            assert ((outs[i].cpu().double() - want[j][0]).abs() / bound(*want[j])).max().item() <= 1.0
+    call = lambda i, w, stream=None: binding.tree_verify_attention_paged(tree, qd[i], kd, vd, td, ld[i], outs[i], ws[w], shared_len=shared, stream=stream)  # noqa: E731
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for i in range(2):
+            call(i, i, streams[i])
+    right()
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=streams[0]):
+            call(i, 0, streams[0])
+    ws[0].fill_(0xff)
+    for swapped in (False, True):
+        if swapped:
+            ld[0].copy_(torch.tensor(lens[1])), ld[1].copy_(torch.tensor(lens[0]))
+            a, b = qd[0].clone(), qd[1].clone()
+            qd[0].copy_(b), qd[1].copy_(a)
+        for o in outs:
+            o.fill_(9.0)
+        for _ in range(3):
+            graphs[0].replay()
+            graphs[1].replay()
+        right((1, 0) if swapped else (0, 1))
+    assert binding.mtv_device_error(tree) == 0
+
+
+def test_refusals():
+    tb, tree = _tree(4, 20)
+    page, Hkv, Hq, D, lens = 16, 2, 4, 64, [70, 80]
+    g = torch.Generator().manual_seed(5)
+    t, n_pages = table(g, 2, 100, page)
+    kp, vp, q = (x.to(DEV) for x in sequences_of(t, n_pages, page, Hkv, D, lens, 0, 20, Hq))
+    td, ld, out = t.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), torch.full_like(q, 7.0)
+    n = binding.paged_workspace_bytes(tree, 2, Hq, Hkv, D)
+    ws = torch.zeros(n + 512, dtype=torch.uint8, device=DEV)
+    ws = ws[-ws.data_ptr() % 256:]
+
+    def code(q=q, out=out, ws=ws[:n], shared=0, scale=0.0):
+        with pytest.raises(binding.MtvError) as e:
+            binding.tree_verify_attention_paged(tree, q, kp, vp, td, ld, out, ws, shared_len=shared, scale=scale)
+        return e.value.code
+    assert code(ws=ws[:n - 1]) == -3 and code(ws=ws[16:n + 16]) in (-1, -3)
+    assert code(shared=8) == -1 and code(shared=-16) == -1 and code(shared=16 * (t.shape[1] + 1)) == -1
+    for s in (-1.0, float("nan"), float("inf")):
+        assert code(scale=s) == -1
+    off = torch.zeros(q.numel() + 8, dtype=torch.bfloat16, device=DEV)[1:1 + q.numel()].view(q.shape)
+    assert code(q=off) == -1 and code(out=off) == -1
+    wide = torch.zeros(2, 20, 5, D, dtype=torch.bfloat16, device=DEV)
+    assert code(q=wide, out=torch.zeros_like(wide)) in (-1, -2)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all() and binding.mtv_device_error(tree) == 0
