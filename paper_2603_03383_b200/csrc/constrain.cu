@@ -17,10 +17,11 @@
 
 namespace mtv {
 
-constexpr int CN_THREADS = 128, CN_WARPS = CN_THREADS / 32;
-constexpr int CN_UNIT = 1024, CN_WORDS = CN_UNIT / 32;
-constexpr int CN_SUBS = 2, CN_SLAB = CN_SUBS * CN_UNIT;
+constexpr int CN_THREADS = 256, CN_WARPS = CN_THREADS / 32;
+constexpr int CN_SLAB = 2048, CN_WORDS = CN_SLAB / 32, CN_PER = CN_WORDS / 32;
+constexpr int CN_ROWS = 32;          // most rows of a block
 constexpr int CN_PATH = MTV_MAX_K + 1;
+constexpr int CN_BLOCKS = 8;
 constexpr int CN_MAX_BIAS = 4096;
 constexpr uint32_t CN_PROMPT = 0x80000000u;
 
@@ -38,7 +39,7 @@ struct ConstrainParams {
     const int32_t *tree_tok;         // [B][T] or null
     const uint64_t *anc;             // [T][2]
     int32_t *dev_error;
-    int T, V, words, n_bias, n_masks, rows_per_block;
+    int B, T, V, words, n_bias, n_masks, rows_per_block, groups;
 };
 
 // bits 0-3 -> the sign bits of bytes 0-3
@@ -105,222 +106,270 @@ __global__ void __launch_bounds__(CN_THREADS)
 constrain_kernel(const ConstrainParams p) {
     using El = Elem<E>;
     constexpr int VEC = El::VEC;
-    __shared__ uint32_t listed[CN_SUBS][CN_WORDS], biased[CN_SUBS][CN_WORDS], allowed_of[CN_WARPS][CN_WORDS + 1], dense_of[CN_WARPS][CN_WORDS + 1];
-    __shared__ uint32_t list_count[CN_SUBS][CN_UNIT];
-    __shared__ float list_bias[CN_SUBS][CN_UNIT];
-    __shared__ uint16_t list_at[CN_SUBS][CN_UNIT];
-    __shared__ int n_list[CN_SUBS];
-    __shared__ int32_t path[MTV_MAX_T][CN_PATH];
+    __shared__ uint32_t listed[CN_WORDS], biased[CN_WORDS], bits_of_warp[CN_WARPS][CN_WORDS + 1];
+    __shared__ uint32_t list_count[CN_SLAB];
+    __shared__ float list_bias[CN_SLAB];
+    __shared__ uint16_t list_at[CN_SLAB];
+    __shared__ int n_listed;
+    __shared__ int32_t path[CN_ROWS][CN_PATH];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const int b = blockIdx.z, slab = (int)blockIdx.x * CN_SLAB, row0 = (int)blockIdx.y * p.rows_per_block;
-    const int n_rows = min(p.rows_per_block, p.T - row0);
+    // slabs are the slowest: vocabularies give their frequent tokens low numbers, and the slabs with long lists start first
+    const int group = (int)blockIdx.x % p.groups, b = (int)blockIdx.x / p.groups % p.B, base = (int)blockIdx.x / p.groups / p.B * CN_SLAB;
+    const int row0 = group * p.rows_per_block, n_rows = min(p.rows_per_block, p.T - row0), n_tok = min(CN_SLAB, p.V - base);
     let_next_start();
     previous_done();
-    // ---- the slab's counted and biased tokens, and the path of every row
-    if (tid < CN_SUBS * CN_WORDS) {
-        const int w = slab / 32 + tid;
-        listed[tid / CN_WORDS][tid % CN_WORDS] = p.seen && w < p.words ? p.seen[(size_t)b * p.words + w] : 0u;
-        biased[tid / CN_WORDS][tid % CN_WORDS] = 0u;
-    }
-    if (tid < CN_WARPS) allowed_of[tid][CN_WORDS] = dense_of[tid][CN_WORDS] = 0u;
-    for (int r = tid; r < n_rows; r += CN_THREADS) {
-        int n = 0;
-        if (p.tree_tok)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                for (uint64_t bits = p.anc[(row0 + r) * 2 + h]; bits && n < CN_PATH; bits &= bits - 1)
-                    path[r][n++] = p.tree_tok[(size_t)b * p.T + h * 64 + __ffsll((long long)bits) - 1];
-        while (n < CN_PATH) path[r][n++] = -1;
-    }
-    __syncthreads();
-    for (int k = tid; k < p.n_bias; k += CN_THREADS) {
-        const int v = p.bias_ids[(size_t)b * p.n_bias + k];
-        if (v >= slab && v - slab < CN_SLAB && v < p.V) {
-            const int at = v - slab;
-            atomicOr(&listed[at / CN_UNIT][at % CN_UNIT / 32], 1u << (at % 32));
-            atomicOr(&biased[at / CN_UNIT][at % CN_UNIT / 32], 1u << (at % 32));
-        }
-    }
-    __syncthreads();
-    if (warp < CN_SUBS) {
-        uint32_t w = listed[warp][lane];
-        const int mine = __popc(w);
-        int before = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int x = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane >= o) before += x;
-        }
-        if (lane == 31) n_list[warp] = before;
-        before -= mine;
-        for (; w; w &= w - 1) list_at[warp][before++] = (uint16_t)(lane * 32 + __ffs((int)w) - 1);
-    }
-    __syncthreads();
-    for (int s = 0; s < CN_SUBS; ++s)
-        for (int e = tid; e < n_list[s]; e += CN_THREADS) {
-            const int at = list_at[s][e], v = slab + s * CN_UNIT + at;
-            float sum = 0.f;
-            if (biased[s][at / 32] >> (at % 32) & 1)
-                for (int k = 0; k < p.n_bias; ++k)          // a token that is named more than once: in the list's order
-                    if (p.bias_ids[(size_t)b * p.n_bias + k] == v) sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + k]);
-            list_bias[s][e] = sum;
-            list_count[s][e] = p.counts && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
-        }
-    __syncthreads();
-    const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
-    // ---- rows: a warp per unit of 1024 tokens.  A unit's mask is requested while the one before is worked on.
-    auto mask_word = [&](int u) -> uint32_t {
-        const int r = u / CN_SUBS, base = slab + u % CN_SUBS * CN_UNIT;
-        if (r >= n_rows || base + lane * 32 >= p.V) return 0u;
-        int m = p.mask_of ? p.mask_of[(size_t)b * p.T + row0 + r] : -1;
+    // the words of a row's mask: bit t % 32 of word t / 32 for the slab's token t, word i * 32 + lane here
+    auto mask_words = [&](int r, uint32_t (&w)[CN_PER]) {
+        int m = r < n_rows && p.mask_of ? p.mask_of[(size_t)b * p.T + row0 + r] : -1;
         if (m >= p.n_masks) {
             if (lane == 0) atomicExch(p.dev_error, MTV_ERR_BOUNDS);
             m = -1;
         }
-        uint32_t w = m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + lane] : 0xffffffffu;
-        const int left = p.V - base - lane * 32;
-        if (left < 32) w &= (1u << left) - 1u;
-        return w;
+#pragma unroll
+        for (int i = 0; i < CN_PER; ++i) {
+            const int at = (i * 32 + lane) * 32, left = n_tok - at;
+            w[i] = left <= 0 ? 0u : m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + i * 32 + lane] : 0xffffffffu;
+            if (left > 0 && left < 32) w[i] &= (1u << left) - 1u;
+        }
     };
-    uint32_t next = mask_word(warp);
-    for (int u = warp; u < n_rows * CN_SUBS; u += CN_WARPS) {
-        const int r = u / CN_SUBS, s = u % CN_SUBS, base = slab + s * CN_UNIT;
-        const int n_tok = min(CN_UNIT, p.V - base);
-        const uint32_t allowed = next;
-        next = mask_word(u + CN_WARPS);
+    uint32_t next[CN_PER];
+    mask_words(warp, next);
+    const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
+    // ---- the slab's counted and biased tokens, and the path of every row
+    for (int i = tid; i < CN_WORDS; i += CN_THREADS) {
+        const int w = base / 32 + i;
+        listed[i] = p.seen && w < p.words ? p.seen[(size_t)b * p.words + w] : 0u;
+        biased[i] = 0u;
+    }
+    for (int e = tid; e < n_rows * CN_PATH; e += CN_THREADS) {
+        const int r = e / CN_PATH;
+        int k = e - r * CN_PATH, node = -1;
+        if (p.tree_tok) {                                   // the k-th node of the path
+            uint64_t lo = p.anc[(row0 + r) * 2], hi = p.anc[(row0 + r) * 2 + 1];
+            for (; k > 0 && (lo | hi); --k) {
+                if (lo) lo &= lo - 1;
+                else hi &= hi - 1;
+            }
+            node = lo ? __ffsll((long long)lo) - 1 : hi ? 63 + __ffsll((long long)hi) : -1;
+        }
+        path[r][e - r * CN_PATH] = node >= 0 ? p.tree_tok[(size_t)b * p.T + node] : -1;
+    }
+    __syncthreads();
+    for (int k = tid; k < p.n_bias; k += CN_THREADS) {
+        const int at = p.bias_ids[(size_t)b * p.n_bias + k] - base;
+        if (at >= 0 && at < n_tok) {
+            atomicOr(&listed[at / 32], 1u << (at % 32));
+            atomicOr(&biased[at / 32], 1u << (at % 32));
+        }
+    }
+    if (p.n_bias) __syncthreads();
+    if (warp == 0) {
+        int start = 0;
+#pragma unroll
+        for (int i = 0; i < CN_PER; ++i) {
+            uint32_t w = listed[i * 32 + lane];
+            const int mine = __popc(w);
+            int before = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int x = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += x;
+            }
+            const int all = __shfl_sync(0xffffffffu, before, 31);
+            before += start - mine;
+            for (; w; w &= w - 1) list_at[before++] = (uint16_t)((i * 32 + lane) * 32 + __ffs((int)w) - 1);
+            start += all;
+        }
+        if (lane == 0) n_listed = start;
+    }
+    __syncthreads();
+    for (int e = tid; e < n_listed; e += CN_THREADS) {
+        const int at = list_at[e], v = base + at;
+        float sum = 0.f;
+        if (biased[at / 32] >> (at % 32) & 1)
+#pragma unroll 8
+            for (int k = 0; k < p.n_bias; ++k)          // a token that is named more than once: in the list's order
+                if (p.bias_ids[(size_t)b * p.n_bias + k] == v) sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + k]);
+        list_bias[e] = sum;
+        list_count[e] = p.counts && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
+    }
+    __syncthreads();
+    // ---- a warp per row; its mask is requested while the row before is worked on
+    uint32_t *words = bits_of_warp[warp];
+    for (int r = warp; r < n_rows; r += CN_WARPS) {
+        uint32_t allowed[CN_PER], any = 0u;
+#pragma unroll
+        for (int i = 0; i < CN_PER; ++i) any |= allowed[i] = next[i];
+        mask_words(r + CN_WARPS, next);
         // (nothing allowed: the argmax need not look at the logits)
-        if (n_tok <= 0 || (!WRITE && !__any_sync(0xffffffffu, allowed != 0u))) continue;
+        if (!WRITE && !__any_sync(0xffffffffu, any != 0u)) continue;
         const size_t row = (size_t)b * p.T + row0 + r;
         const E *in = static_cast<const E *>(p.logits) + (int64_t)row * p.ld_in + base;
         E *out = WRITE ? static_cast<E *>(p.out) + (int64_t)row * p.ld_out + base : nullptr;
-        int here = lane < CN_PATH ? path[r][lane] : -1;       // this lane's token of the path, where it lies in this unit
+        int here = lane < CN_PATH ? path[r][lane] : -1;       // this lane's token of the path, where it lies in this slab
         here = here >= base && here - base < n_tok ? here - base : -1;
         const uint32_t on_path = __ballot_sync(0xffffffffu, here >= 0);
-        uint32_t dense = allowed & ~listed[s][lane];
-        for (uint32_t some = on_path; some; some &= some - 1) {
-            const int at = __shfl_sync(0xffffffffu, here, __ffs((int)some) - 1);
-            if (lane == at / 32) dense &= ~(1u << (at % 32));
-        }
-        allowed_of[warp][lane] = allowed;
-        dense_of[warp][lane] = dense;
-        __syncwarp();
-        const uint32_t *words = WRITE ? allowed_of[warp] : dense_of[warp];
-        // the vectors of the row's addresses: vector j holds tokens [j * VEC - off, (j + 1) * VEC - off) of the unit
+        // The vectors of the row's addresses: vector j holds tokens [j * VEC - off, (j + 1) * VEC - off); bit j * VEC + e of the words belongs to its
+        // element e.
         const int off = (int)((uintptr_t)in / sizeof(E) % VEC);
-        const bool out_vec = WRITE && (int)((uintptr_t)out / sizeof(E) % VEC) == off;
-        const int n_vec = (off + n_tok + VEC - 1) / VEC;
-        constexpr uint32_t ALL = (1u << VEC) - 1u;
-        auto whole = [&](int j) { return j * VEC >= off && (j + 1) * VEC - off <= n_tok; };
-        auto bits_of = [&](int j) {
-            const int t0 = j * VEC - off;
-            return __funnelshift_r(words[t0 >> 5], words[(t0 >> 5) + 1], t0 & 31) & ALL;
+        auto set_words = [&](const uint32_t (&w)[CN_PER]) {
+            __syncwarp();
+            uint32_t carry = 0u;
+#pragma unroll
+            for (int i = 0; i < CN_PER; ++i) {
+                uint32_t below = __shfl_up_sync(0xffffffffu, w[i], 1);
+                if (lane == 0) below = carry;
+                words[i * 32 + lane] = __funnelshift_l(below, w[i], off);
+                carry = __shfl_sync(0xffffffffu, w[i], 31);
+            }
+            if (lane == 0) words[CN_WORDS] = __funnelshift_l(carry, 0u, off);
+            __syncwarp();
         };
+        if (WRITE) {
+            set_words(allowed);
+        } else {
+            uint32_t dense[CN_PER];
+#pragma unroll
+            for (int i = 0; i < CN_PER; ++i) dense[i] = allowed[i] & ~listed[i * 32 + lane];
+            for (uint32_t some = on_path; some; some &= some - 1) {
+                const int at = __shfl_sync(0xffffffffu, here, __ffs((int)some) - 1);
+#pragma unroll
+                for (int i = 0; i < CN_PER; ++i)
+                    if (at / 32 == i * 32 + lane) dense[i] &= ~(1u << (at % 32));
+            }
+            set_words(dense);
+        }
+        auto bits_of = [&](int j) {
+            const uint32_t x = reinterpret_cast<const uint8_t *>(words)[j * VEC / 8];
+            return VEC == 8 ? x : x >> (j % 2 * 4) & 0xfu;
+        };
+        auto bit_of = [&](int t) { return words[(t + off) >> 5] >> ((t + off) & 31) & 1u; };
         // the largest of the tokens taken one by one and the first that has it; the largest of the vectors and the first vector that has it
         float best = -INFINITY, best_v = -INFINITY;
         int at = -1, at_v = -1;
         auto one = [&](int t, float x) {
             if (x > best || (x == best && t < at)) { best = x; at = t; }
         };
-        for (int j0 = lane; j0 < n_vec; j0 += 32 * 4) {
-            uint4 x[4];
-            uint32_t bits[4];
+        // ---- whole vectors
+        const int j_lo = off > 0, j_hi = (off + n_tok) / VEC;
+        const bool out_vec = WRITE && (int)((uintptr_t)out / sizeof(E) % VEC) == off;
+        constexpr int DEEP = 4;
+        for (int j0 = j_lo + lane; j0 < j_hi; j0 += 32 * DEEP) {
+            uint4 x[DEEP];
+            uint32_t bits[DEEP];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < DEEP; ++k) {
                 const int j = j0 + 32 * k;
-                bits[k] = j < n_vec && whole(j) ? bits_of(j) : 0u;
+                bits[k] = j < j_hi ? bits_of(j) : 0u;
+                x[k] = make_uint4(0u, 0u, 0u, 0u);
                 if (bits[k]) x[k] = *reinterpret_cast<const uint4 *>(in + (j * VEC - off));
-                else x[k] = make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int j = j0 + 32 * k;
-                if (j >= n_vec) continue;
-                if (!whole(j)) {
-                    for (int t = max(0, j * VEC - off); t < min(n_tok, (j + 1) * VEC - off); ++t) {
-                        const bool is = words[t >> 5] >> (t & 31) & 1;
-                        if (WRITE) {
-                            if (is) out[t] = in[t];
-                            else El::put(out + t, -INFINITY);
-                        } else if (is) {
-                            one(t, El::get(in + t));
-                        }
-                    }
-                    continue;
-                }
+            for (int k = 0; k < DEEP; ++k) {
+                const int j = j0 + 32 * k, t0 = j * VEC - off;
                 const uint4 y = El::masked(x[k], bits[k]);
-                if (WRITE) {
-                    const int t0 = j * VEC - off;
+                if (!WRITE) {
+                    const float v = El::top(y);
+                    if (v > best_v) { best_v = v; at_v = j; }     // strictly: the first vector stays
+                } else if (j < j_hi) {
                     if (out_vec) {
                         *reinterpret_cast<uint4 *>(out + t0) = y;
                     } else {
 #pragma unroll
                         for (int e = 0; e < VEC; ++e) out[t0 + e] = reinterpret_cast<const E *>(&y)[e];
                     }
-                } else {
-                    const float v = El::top(y);
-                    if (v > best_v) { best_v = v; at_v = j; }     // strictly: the first vector stays
                 }
             }
         }
-        __syncwarp();
+        // ---- the tokens of the two vectors that the row shares with others
+        {
+            const int head = min(n_tok, j_lo * VEC - off), tail = max(head, j_hi * VEC - off);
+            const int t = lane < VEC ? lane : tail + lane - VEC;
+            if (lane < VEC ? t < head : t < n_tok && lane < 2 * VEC) {
+                const bool is = bit_of(t);
+                if (!WRITE) {
+                    if (is) one(t, El::get(in + t));
+                } else if (is) {
+                    out[t] = in[t];
+                } else {
+                    El::put(out + t, -INFINITY);
+                }
+            }
+        }
         // ---- listed tokens, then those of the path that are in no list
+        if (WRITE) __syncwarp();
+        else set_words(allowed);
         auto special = [&](int t, uint32_t counted, float bias) {
             int c = (int)(counted & ~CN_PROMPT);
             if (on_path)
                 for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
-            const float x = pen.apply(El::get(in + t), c, c > 0 || counted & CN_PROMPT, bias);
+            return pen.apply(El::get(in + t), c, c > 0 || counted & CN_PROMPT, bias);
+        };
+        for (int e = lane; e < n_listed; e += 32) {
+            const int t = list_at[e];
+            if (!bit_of(t)) continue;
+            const float x = special(t, list_count[e], list_bias[e]);
             if (WRITE) El::put(out + t, x);
             else one(t, x);
-        };
-        for (int e = lane; e < n_list[s]; e += 32) {
-            const int t = list_at[s][e];
-            if (allowed_of[warp][t / 32] >> (t % 32) & 1) special(t, list_count[s][e], list_bias[s][e]);
         }
-        if (here >= 0 && (allowed_of[warp][here / 32] >> (here % 32) & 1) && !(listed[s][here / 32] >> (here % 32) & 1)) {
+        if (here >= 0 && bit_of(here) && !(listed[here / 32] >> (here % 32) & 1)) {
             bool first = true;          // the same token twice on a path: once
             for (int k = 0; k < lane; ++k) first = first && path[r][k] != base + here;
-            if (first) special(here, 0u, 0.f);
-        }
-        if (!WRITE) {
-            const float mine = fmaxf(best, best_v);
-            const uint32_t image = value_image(mine);         // (of -inf where this lane has nothing)
-            const uint32_t top = __reduce_max_sync(0xffffffffu, image);
-            uint32_t first = 0xffffffffu;
-            if (top != value_image(-INFINITY)) {
-                if (image == top) {
-                    if (best == mine) first = (uint32_t)at;
-                    if (best_v == mine) {
-                        // the first element of that vector that has the value
-                        const int t0 = at_v * VEC - off;
-                        const uint32_t bits = bits_of(at_v);
-                        for (int e = 0; e < VEC; ++e)
-                            if ((bits >> e & 1u) && El::get(in + t0 + e) == mine) { first = min(first, (uint32_t)(t0 + e)); break; }
-                    }
-                }
-            } else {
-                // nothing but -inf and NaN: the first allowed -inf
-                for (int t = lane; t < n_tok && first == 0xffffffffu; t += 32)
-                    if (allowed_of[warp][t / 32] >> (t % 32) & 1) {
-                        int c = 0;
-                        const bool in_list = listed[s][t / 32] >> (t % 32) & 1;
-                        float x = El::get(in + t);
-                        for (int k = 0; k < CN_PATH; ++k) c += path[r][k] == base + t;
-                        if (in_list || c) {
-                            float bias = 0.f;
-                            uint32_t counted = 0u;
-                            for (int e = 0; in_list && e < n_list[s]; ++e)
-                                if (list_at[s][e] == t) { bias = list_bias[s][e]; counted = list_count[s][e]; }
-                            c += (int)(counted & ~CN_PROMPT);
-                            x = pen.apply(x, c, c > 0 || counted & CN_PROMPT, bias);
-                        }
-                        if (x == -INFINITY) first = (uint32_t)t;
-                    }
+            if (first) {
+                const float x = special(here, 0u, 0.f);
+                if (WRITE) El::put(out + here, x);
+                else one(here, x);
             }
-            first = __reduce_min_sync(0xffffffffu, first);
-            if (lane == 0 && first != 0xffffffffu) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - ((uint32_t)base + first)));
         }
-        __syncwarp();       // before the next unit's bits
+        if (WRITE) continue;
+        // ---- the row's largest value in this slab, and the first token that has it
+        const float mine = fmaxf(best, best_v);
+        const uint32_t image = value_image(mine);         // (of -inf where this lane has nothing)
+        const uint32_t top = __reduce_max_sync(0xffffffffu, image);
+        uint32_t first = 0xffffffffu;
+        if (top != value_image(-INFINITY)) {
+            if (image == top) {
+                if (best == mine) first = (uint32_t)at;
+                if (best_v == mine) {
+                    const int t0 = at_v * VEC - off;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(in + t0);
+#pragma unroll
+                    for (int e = VEC - 1; e >= 0; --e)
+                        if (El::get(reinterpret_cast<const E *>(&x) + e) == mine && bit_of(t0 + e) && !(listed[(t0 + e) / 32] >> ((t0 + e) % 32) & 1)) {
+                            bool alone = true;
+                            if (on_path)
+                                for (int k = 0; k < CN_PATH; ++k) alone = alone && path[r][k] != base + t0 + e;
+                            if (alone) first = min(first, (uint32_t)(t0 + e));
+                        }
+                }
+            }
+        } else {
+            // nothing but -inf and NaN: the first allowed -inf
+            for (int t = lane; t < n_tok && first == 0xffffffffu; t += 32)
+                if (bit_of(t)) {
+                    float x = El::get(in + t), bias = 0.f;
+                    uint32_t counted = 0u;
+                    const bool in_list = listed[t / 32] >> (t % 32) & 1;
+                    bool walked = false;
+                    for (int k = 0; k < CN_PATH; ++k) walked = walked || path[r][k] == base + t;
+                    for (int e = 0; in_list && e < n_listed; ++e)
+                        if (list_at[e] == t) { bias = list_bias[e]; counted = list_count[e]; }
+                    if (in_list || walked) x = special(t, counted, bias);
+                    if (x == -INFINITY) first = (uint32_t)t;
+                }
+        }
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0 && first != 0xffffffffu) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - ((uint32_t)base + first)));
     }
+}
+
+// The keys' zeros: a kernel, so that the one behind it is launched while it runs.
+__global__ void __launch_bounds__(256)
+clear_keys_kernel(int n, unsigned long long *keys) {
+    let_next_start();
+    previous_done();
+    const int i = (int)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) keys[i] = 0ull;
 }
 
 // ---------------------------------------------------------------------------------------- counts
@@ -359,13 +408,14 @@ static int constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void
     p.mask = rules->mask; p.mask_of = rules->n_masks > 0 ? rules->mask_of : nullptr; p.n_masks = rules->n_masks;
     p.tree_tok = tree_tok; p.anc = tree->d_anc; p.dev_error = tree->d_error;
     p.T = tree->T; p.V = V; p.words = (V + 31) / 32;
-    // every block lists its slab's tokens anew: as many rows to a block as leave about eight blocks per SM
-    const int slabs = (V + CN_SLAB - 1) / CN_SLAB;
-    long groups = (8L * sm_count() + (long)slabs * B - 1) / ((long)slabs * B);
-    groups = groups < 1 ? 1 : groups > p.T ? p.T : groups;
-    p.rows_per_block = (p.T + (int)groups - 1) / (int)groups;
-    const dim3 grid(slabs, (p.T + p.rows_per_block - 1) / p.rows_per_block, B);
-    if (keys) MTV_CUDA_CHECK(cudaMemsetAsync(keys, 0, (size_t)B * p.T * sizeof *keys, stream));
+    // A row per warp at least; every block lists its slab's tokens anew, so more where that still leaves a few blocks per SM.
+    const int64_t slabs = (V + CN_SLAB - 1) / CN_SLAB;
+    int per = CN_WARPS;
+    while (per < CN_ROWS && slabs * B * ((p.T + 2 * per - 1) / (2 * per)) >= CN_BLOCKS * sm_count()) per *= 2;
+    p.B = B; p.rows_per_block = per; p.groups = (p.T + per - 1) / per;
+    if (slabs * B * p.groups > 0x7fffffff) return MTV_ERR_UNSUPPORTED_SHAPE;
+    const dim3 grid((unsigned)(slabs * B * p.groups));
+    if (keys) MTV_CUDA_CHECK(launch_dependent(clear_keys_kernel, dim3((B * p.T + 255) / 256), 256, 0, stream, B * p.T, keys));
     auto kernel = dtype == MTV_LOGITS_BF16 ? (keys ? constrain_kernel<__nv_bfloat16, false> : constrain_kernel<__nv_bfloat16, true>)
                                            : (keys ? constrain_kernel<float, false> : constrain_kernel<float, true>);
     MTV_CUDA_CHECK(launch_dependent(kernel, grid, CN_THREADS, 0, stream, p));
