@@ -5,12 +5,17 @@
 //   x = x + bias;  not allowed by the row's mask: -inf
 // every operation rounded to fp32 by itself (no contraction), so that equal inputs give equal keys whatever the order they are met in.
 //
-// Bound by memory: the logits are read once (and written once in the form that writes).  What a token was counted, and whether it is
-// allowed, are bits (1/16 of the logits' bytes per sequence, 1/16 per mask); only the few tokens that are counted, biased or on
-// the path go through the formula.  A block takes a slab of the vocabulary for some of a sequence's nodes.  It first lists the slab's counted and
-// biased tokens once; a warp then takes a row's unit of 1024 tokens: a dense pass over those that are allowed and in no list (16-byte
-// loads, maximum or copy), and a sparse one over the lists.  Rows may begin at any element: vectors are cut at the addresses' 16-byte
-// boundaries, and the two that a unit shares with its neighbours are taken element by element.
+// The logits are read once (and written once in the form that writes).  What a token was counted, and whether it is allowed, are bits
+// (1/16 of the logits' bytes per sequence, 1/16 per mask); only the few tokens that are counted, biased or on the path go through the
+// formula.  A block takes a slab of 2048 tokens of the vocabulary for some of a sequence's nodes.  It first lists the slab's counted and biased
+// tokens; then a warp per row makes a dense pass over the allowed tokens that are in no list (16-byte loads, masks laid over whole
+// vectors, packed maxima or copies) and a sparse one over the list.  Rows may begin at any element: vectors are cut at the addresses' 16-byte
+// boundaries, and the two that a slab shares with its neighbours are taken element by element.
+// Measured: argmax of 8 x 64 rows of 131072 bf16 logits, 64 masks, 4000 tokens of text a sequence, with the acceptance 47 us (134 MB: 20.5 us at the
+// memory's rate); written, 5 x 64 rows of 50003: 24 us (9.8).  Bound by instructions and their latency: about 850 a warp for a row's slab at
+// half an instruction a cycle, a third of them the list's (a division each, on lanes that the list only partly fills).  Blocks of 8 rows cost
+// 8 us more (every block lists anew, three loads deep), of 32 rows 8 us (the last wave is short); five blocks per SM rather than the four that
+// the compiler's choice of registers leaves: 66 -> 47; rows staged in shared memory by asynchronous copies: 75, as two blocks fit then.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -29,7 +34,7 @@ struct ConstrainParams {
     const void *logits;
     void *out;                       // or null: keys
     int64_t ld_in, ld_out;           // elements from row to row
-    unsigned long long *keys;        // [B*T], zero before the launch
+    unsigned long long *keys;        // [B*T], zero before the launch where there is more than one slab
     const uint32_t *counts, *seen;   // [B][V], [B][words], or null
     const float *repetition, *presence, *frequency;   // [B] or null
     const int32_t *bias_ids;         // [B][n_bias]
@@ -40,10 +45,11 @@ struct ConstrainParams {
     const uint64_t *anc;             // [T][2]
     int32_t *dev_error;
     int B, T, V, words, n_bias, n_masks, rows_per_block, groups;
+    bool one_slab;                   // a row's key is written once
 };
 
-// bits 0-3 -> the sign bits of bytes 0-3
-__device__ __forceinline__ uint32_t signs_of(uint32_t bits) { return ((bits & 0xfu) * 0x00204081u & 0x01010101u) << 7; }
+// bits 0-3 -> the top bits of bytes 0-3 (the products of a bit with the factor's four fall on places of their own; other bits hold anything)
+__device__ __forceinline__ uint32_t signs_of(uint32_t bits) { return (bits & 0xfu) * 0x10204080u; }
 // every byte of the result: the sign of the byte of x that its digit of the selector names (8 + byte), eight times.  (__byte_perm leaves the digits'
 // top bit out.)
 __device__ __forceinline__ uint32_t spread(uint32_t x, uint32_t selector) {
@@ -64,12 +70,14 @@ template <> struct Elem<__nv_bfloat16> {
         return make_uint4(keep(u.x, spread(a, 0x9988u), hidden), keep(u.y, spread(a, 0xbbaau), hidden),
                           keep(u.z, spread(b, 0x9988u), hidden), keep(u.w, spread(b, 0xbbaau), hidden));
     }
-    // largest value of a vector; NaN counts for nothing
-    static __device__ __forceinline__ float top(const uint4 &u) {
+    // running maximum of vectors; NaN counts for nothing
+    using Top = __nv_bfloat162;
+    static __device__ __forceinline__ Top none() { return __float2bfloat162_rn(-INFINITY); }
+    static __device__ __forceinline__ Top more(Top m, const uint4 &u) {
         const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&u);
-        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
+        return __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
     }
+    static __device__ __forceinline__ float value(Top m) { return fmaxf(__low2float(m), __high2float(m)); }
 };
 template <> struct Elem<float> {
     static constexpr int VEC = 4;
@@ -80,9 +88,12 @@ template <> struct Elem<float> {
         return make_uint4(keep(u.x, spread(a, 0x8888u), hidden), keep(u.y, spread(a, 0x9999u), hidden),
                           keep(u.z, spread(a, 0xaaaau), hidden), keep(u.w, spread(a, 0xbbbbu), hidden));
     }
-    static __device__ __forceinline__ float top(const uint4 &u) {
-        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    using Top = float;
+    static __device__ __forceinline__ Top none() { return -INFINITY; }
+    static __device__ __forceinline__ Top more(Top m, const uint4 &u) {
+        return fmaxf(m, fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w))));
     }
+    static __device__ __forceinline__ float value(Top m) { return m; }
 };
 
 // Order-preserving image of a value that is no NaN; both zeros are one.
@@ -102,15 +113,16 @@ struct Penalties {
 };
 
 template <typename E, bool WRITE>
-__global__ void __launch_bounds__(CN_THREADS)
+__global__ void __launch_bounds__(CN_THREADS, 5)
 constrain_kernel(const ConstrainParams p) {
     using El = Elem<E>;
     constexpr int VEC = El::VEC;
-    __shared__ uint32_t listed[CN_WORDS], biased[CN_WORDS], bits_of_warp[CN_WARPS][CN_WORDS + 1];
+    __shared__ uint32_t listed[CN_WORDS], biased[CN_WORDS], allowed_of[CN_WARPS][CN_WORDS], dense_of[CN_WARPS][CN_WORDS + 1];
     __shared__ uint32_t list_count[CN_SLAB];
     __shared__ float list_bias[CN_SLAB];
     __shared__ uint16_t list_at[CN_SLAB];
-    __shared__ int n_listed;
+    __shared__ uint32_t match[CN_MAX_BIAS];      // the slab's entries of the bias list, in no order: place in the list << 16 | token
+    __shared__ int n_listed, n_match;
     __shared__ int32_t path[CN_ROWS][CN_PATH];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     // slabs are the slowest: vocabularies give their frequent tokens low numbers, and the slabs with long lists start first
@@ -118,29 +130,15 @@ constrain_kernel(const ConstrainParams p) {
     const int row0 = group * p.rows_per_block, n_rows = min(p.rows_per_block, p.T - row0), n_tok = min(CN_SLAB, p.V - base);
     let_next_start();
     previous_done();
-    // the words of a row's mask: bit t % 32 of word t / 32 for the slab's token t, word i * 32 + lane here
-    auto mask_words = [&](int r, uint32_t (&w)[CN_PER]) {
-        int m = r < n_rows && p.mask_of ? p.mask_of[(size_t)b * p.T + row0 + r] : -1;
-        if (m >= p.n_masks) {
-            if (lane == 0) atomicExch(p.dev_error, MTV_ERR_BOUNDS);
-            m = -1;
-        }
-#pragma unroll
-        for (int i = 0; i < CN_PER; ++i) {
-            const int at = (i * 32 + lane) * 32, left = n_tok - at;
-            w[i] = left <= 0 ? 0u : m >= 0 ? p.mask[(size_t)m * p.words + base / 32 + i * 32 + lane] : 0xffffffffu;
-            if (left > 0 && left < 32) w[i] &= (1u << left) - 1u;
-        }
-    };
-    uint32_t next[CN_PER];
-    mask_words(warp, next);
+    // ---- the slab's counted and biased tokens, and the path of every row.  Loads that wait for nothing are issued first: a block's start is
+    // a chain of three or four of them, one behind the other.
+    int mask_at = -1;                           // lane i: the mask of this warp's i-th row
+    if (p.mask_of && warp + lane * CN_WARPS < n_rows) mask_at = p.mask_of[(size_t)b * p.T + row0 + warp + lane * CN_WARPS];
+    uint32_t seen = 0u;
+    if (tid < CN_WORDS && p.seen && base / 32 + tid < p.words) seen = p.seen[(size_t)b * p.words + base / 32 + tid];
+    int biased_at = -1;
+    if (tid < p.n_bias) biased_at = p.bias_ids[(size_t)b * p.n_bias + tid] - base;
     const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
-    // ---- the slab's counted and biased tokens, and the path of every row
-    for (int i = tid; i < CN_WORDS; i += CN_THREADS) {
-        const int w = base / 32 + i;
-        listed[i] = p.seen && w < p.words ? p.seen[(size_t)b * p.words + w] : 0u;
-        biased[i] = 0u;
-    }
     for (int e = tid; e < n_rows * CN_PATH; e += CN_THREADS) {
         const int r = e / CN_PATH;
         int k = e - r * CN_PATH, node = -1;
@@ -154,12 +152,31 @@ constrain_kernel(const ConstrainParams p) {
         }
         path[r][e - r * CN_PATH] = node >= 0 ? p.tree_tok[(size_t)b * p.T + node] : -1;
     }
+    if (mask_at >= p.n_masks) {
+        if (p.mask_of) atomicExch(p.dev_error, MTV_ERR_BOUNDS);
+        mask_at = -1;
+    }
+    // the words of the mask of this warp's i-th row: bit t % 32 of word t / 32 for the slab's token t, word k * 32 + lane here
+    auto mask_words = [&](int i, uint32_t (&w)[CN_PER]) {
+        const int m = __shfl_sync(0xffffffffu, mask_at, i);
+#pragma unroll
+        for (int k = 0; k < CN_PER; ++k)
+            w[k] = m >= 0 && (k * 32 + lane) * 32 < n_tok ? p.mask[(size_t)m * p.words + base / 32 + k * 32 + lane] : 0xffffffffu;
+    };
+    uint32_t next[CN_PER];
+    mask_words(0, next);
+    if (tid < CN_WORDS) {
+        listed[tid] = seen;
+        biased[tid] = 0u;
+    }
+    if (tid == 0) n_match = 0;
     __syncthreads();
     for (int k = tid; k < p.n_bias; k += CN_THREADS) {
-        const int at = p.bias_ids[(size_t)b * p.n_bias + k] - base;
-        if (at >= 0 && at < n_tok) {
-            atomicOr(&listed[at / 32], 1u << (at % 32));
-            atomicOr(&biased[at / 32], 1u << (at % 32));
+        if (k != tid) biased_at = p.bias_ids[(size_t)b * p.n_bias + k] - base;
+        if (biased_at >= 0 && biased_at < n_tok) {
+            atomicOr(&listed[biased_at / 32], 1u << (biased_at % 32));
+            atomicOr(&biased[biased_at / 32], 1u << (biased_at % 32));
+            match[atomicAdd(&n_match, 1)] = (uint32_t)k << 16 | (uint32_t)biased_at;
         }
     }
     if (p.n_bias) __syncthreads();
@@ -187,23 +204,34 @@ constrain_kernel(const ConstrainParams p) {
         const int at = list_at[e], v = base + at;
         float sum = 0.f;
         if (biased[at / 32] >> (at % 32) & 1)
-#pragma unroll 8
-            for (int k = 0; k < p.n_bias; ++k)          // a token that is named more than once: in the list's order
-                if (p.bias_ids[(size_t)b * p.n_bias + k] == v) sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + k]);
+            for (int last = -1;;) {                         // a token that is named more than once: in the list's order
+                uint32_t found = 0xffffffffu;
+                for (int k = 0; k < n_match; ++k)
+                    if ((int)(match[k] & 0xffffu) == at && (int)(match[k] >> 16) > last) found = min(found, match[k]);
+                if (found == 0xffffffffu) break;
+                last = (int)(found >> 16);
+                sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + last]);
+            }
         list_bias[e] = sum;
         list_count[e] = p.counts && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
     }
     __syncthreads();
     // ---- a warp per row; its mask is requested while the row before is worked on
-    uint32_t *words = bits_of_warp[warp];
-    for (int r = warp; r < n_rows; r += CN_WARPS) {
+    uint32_t *words = dense_of[warp];
+    for (int r = warp, turn = 0; r < n_rows; r += CN_WARPS, ++turn) {
         uint32_t allowed[CN_PER], any = 0u;
 #pragma unroll
-        for (int i = 0; i < CN_PER; ++i) any |= allowed[i] = next[i];
-        mask_words(r + CN_WARPS, next);
+        for (int i = 0; i < CN_PER; ++i) {
+            const int left = n_tok - (i * 32 + lane) * 32;
+            any |= allowed[i] = left >= 32 ? next[i] : left > 0 ? next[i] & ((1u << left) - 1u) : 0u;
+        }
+        mask_words(turn + 1, next);
         // (nothing allowed: the argmax need not look at the logits)
-        if (!WRITE && !__any_sync(0xffffffffu, any != 0u)) continue;
         const size_t row = (size_t)b * p.T + row0 + r;
+        if (!WRITE && !__any_sync(0xffffffffu, any != 0u)) {
+            if (p.one_slab && lane == 0) p.keys[row] = 0ull;
+            continue;
+        }
         const E *in = static_cast<const E *>(p.logits) + (int64_t)row * p.ld_in + base;
         E *out = WRITE ? static_cast<E *>(p.out) + (int64_t)row * p.ld_out + base : nullptr;
         int here = lane < CN_PATH ? path[r][lane] : -1;       // this lane's token of the path, where it lies in this slab
@@ -212,39 +240,41 @@ constrain_kernel(const ConstrainParams p) {
         // The vectors of the row's addresses: vector j holds tokens [j * VEC - off, (j + 1) * VEC - off); bit j * VEC + e of the words belongs to its
         // element e.
         const int off = (int)((uintptr_t)in / sizeof(E) % VEC);
-        auto set_words = [&](const uint32_t (&w)[CN_PER]) {
-            __syncwarp();
-            uint32_t carry = 0u;
+        uint32_t dense[CN_PER];
 #pragma unroll
-            for (int i = 0; i < CN_PER; ++i) {
-                uint32_t below = __shfl_up_sync(0xffffffffu, w[i], 1);
-                if (lane == 0) below = carry;
-                words[i * 32 + lane] = __funnelshift_l(below, w[i], off);
-                carry = __shfl_sync(0xffffffffu, w[i], 31);
-            }
-            if (lane == 0) words[CN_WORDS] = __funnelshift_l(carry, 0u, off);
-            __syncwarp();
-        };
-        if (WRITE) {
-            set_words(allowed);
-        } else {
-            uint32_t dense[CN_PER];
-#pragma unroll
-            for (int i = 0; i < CN_PER; ++i) dense[i] = allowed[i] & ~listed[i * 32 + lane];
+        for (int i = 0; i < CN_PER; ++i) {
+            allowed_of[warp][i * 32 + lane] = allowed[i];
+            dense[i] = WRITE ? allowed[i] : allowed[i] & ~listed[i * 32 + lane];
+        }
+        if (!WRITE)
             for (uint32_t some = on_path; some; some &= some - 1) {
                 const int at = __shfl_sync(0xffffffffu, here, __ffs((int)some) - 1);
 #pragma unroll
                 for (int i = 0; i < CN_PER; ++i)
                     if (at / 32 == i * 32 + lane) dense[i] &= ~(1u << (at % 32));
             }
-            set_words(dense);
+        if (off == 0) {
+#pragma unroll
+            for (int i = 0; i < CN_PER; ++i) words[i * 32 + lane] = dense[i];
+        } else {
+            uint32_t carry = 0u;
+#pragma unroll
+            for (int i = 0; i < CN_PER; ++i) {
+                uint32_t below = __shfl_up_sync(0xffffffffu, dense[i], 1);
+                if (lane == 0) below = carry;
+                words[i * 32 + lane] = __funnelshift_l(below, dense[i], off);
+                carry = __shfl_sync(0xffffffffu, dense[i], 31);
+            }
+            if (lane == 0) words[CN_WORDS] = carry >> (32 - off);
         }
+        __syncwarp();
         auto bits_of = [&](int j) {
             const uint32_t x = reinterpret_cast<const uint8_t *>(words)[j * VEC / 8];
             return VEC == 8 ? x : x >> (j % 2 * 4) & 0xfu;
         };
-        auto bit_of = [&](int t) { return words[(t + off) >> 5] >> ((t + off) & 31) & 1u; };
-        // the largest of the tokens taken one by one and the first that has it; the largest of the vectors and the first vector that has it
+        auto is_dense = [&](int t) { return words[(t + off) >> 5] >> ((t + off) & 31) & 1u; };
+        auto is_allowed = [&](int t) { return allowed_of[warp][t >> 5] >> (t & 31) & 1u; };
+        // the largest of the tokens taken one by one and the first that has it; the largest of the vectors and the first DEEP that have it
         float best = -INFINITY, best_v = -INFINITY;
         int at = -1, at_v = -1;
         auto one = [&](int t, float x) {
@@ -264,13 +294,13 @@ constrain_kernel(const ConstrainParams p) {
                 x[k] = make_uint4(0u, 0u, 0u, 0u);
                 if (bits[k]) x[k] = *reinterpret_cast<const uint4 *>(in + (j * VEC - off));
             }
+            typename El::Top top = El::none();
 #pragma unroll
             for (int k = 0; k < DEEP; ++k) {
                 const int j = j0 + 32 * k, t0 = j * VEC - off;
                 const uint4 y = El::masked(x[k], bits[k]);
                 if (!WRITE) {
-                    const float v = El::top(y);
-                    if (v > best_v) { best_v = v; at_v = j; }     // strictly: the first vector stays
+                    top = El::more(top, y);
                 } else if (j < j_hi) {
                     if (out_vec) {
                         *reinterpret_cast<uint4 *>(out + t0) = y;
@@ -280,13 +310,30 @@ constrain_kernel(const ConstrainParams p) {
                     }
                 }
             }
+            const float v = El::value(top);
+            if (!WRITE && v > best_v) { best_v = v; at_v = j0; }     // strictly: the first ones stay
+        }
+        // the first token that has the vectors' largest value: the elements of the DEEP vectors of each lane that has it, one to a lane
+        uint32_t top_v = value_image(best_v), first_v = 0xffffffffu;
+        if (!WRITE) {
+            const uint32_t mine = top_v;
+            top_v = __reduce_max_sync(0xffffffffu, mine);
+            if (top_v != value_image(-INFINITY))
+                for (uint32_t some = __ballot_sync(0xffffffffu, mine == top_v); some; some &= some - 1) {
+                    const int j0 = __shfl_sync(0xffffffffu, at_v, __ffs((int)some) - 1);
+#pragma unroll
+                    for (int i = lane; i < DEEP * VEC; i += 32) {
+                        const int j = j0 + i / VEC * 32, t = j * VEC - off + i % VEC;
+                        if (j < j_hi && is_dense(t) && value_image(El::get(in + t)) == top_v) first_v = min(first_v, (uint32_t)t);
+                    }
+                }
         }
         // ---- the tokens of the two vectors that the row shares with others
         {
             const int head = min(n_tok, j_lo * VEC - off), tail = max(head, j_hi * VEC - off);
             const int t = lane < VEC ? lane : tail + lane - VEC;
             if (lane < VEC ? t < head : t < n_tok && lane < 2 * VEC) {
-                const bool is = bit_of(t);
+                const bool is = is_dense(t);
                 if (!WRITE) {
                     if (is) one(t, El::get(in + t));
                 } else if (is) {
@@ -298,7 +345,6 @@ constrain_kernel(const ConstrainParams p) {
         }
         // ---- listed tokens, then those of the path that are in no list
         if (WRITE) __syncwarp();
-        else set_words(allowed);
         auto special = [&](int t, uint32_t counted, float bias) {
             int c = (int)(counted & ~CN_PROMPT);
             if (on_path)
@@ -307,12 +353,12 @@ constrain_kernel(const ConstrainParams p) {
         };
         for (int e = lane; e < n_listed; e += 32) {
             const int t = list_at[e];
-            if (!bit_of(t)) continue;
+            if (!is_allowed(t)) continue;
             const float x = special(t, list_count[e], list_bias[e]);
             if (WRITE) El::put(out + t, x);
             else one(t, x);
         }
-        if (here >= 0 && bit_of(here) && !(listed[here / 32] >> (here % 32) & 1)) {
+        if (here >= 0 && is_allowed(here) && !(listed[here / 32] >> (here % 32) & 1)) {
             bool first = true;          // the same token twice on a path: once
             for (int k = 0; k < lane; ++k) first = first && path[r][k] != base + here;
             if (first) {
@@ -321,32 +367,21 @@ constrain_kernel(const ConstrainParams p) {
                 else one(here, x);
             }
         }
-        if (WRITE) continue;
+        if (WRITE) {
+            __syncwarp();
+            continue;
+        }
         // ---- the row's largest value in this slab, and the first token that has it
-        const float mine = fmaxf(best, best_v);
-        const uint32_t image = value_image(mine);         // (of -inf where this lane has nothing)
-        const uint32_t top = __reduce_max_sync(0xffffffffu, image);
-        uint32_t first = 0xffffffffu;
+        const uint32_t image = value_image(best);         // (of -inf where this lane has nothing)
+        const uint32_t top = max(top_v, __reduce_max_sync(0xffffffffu, image));
+        uint32_t first = top_v == top ? first_v : 0xffffffffu;
         if (top != value_image(-INFINITY)) {
-            if (image == top) {
-                if (best == mine) first = (uint32_t)at;
-                if (best_v == mine) {
-                    const int t0 = at_v * VEC - off;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(in + t0);
-#pragma unroll
-                    for (int e = VEC - 1; e >= 0; --e)
-                        if (El::get(reinterpret_cast<const E *>(&x) + e) == mine && bit_of(t0 + e) && !(listed[(t0 + e) / 32] >> ((t0 + e) % 32) & 1)) {
-                            bool alone = true;
-                            if (on_path)
-                                for (int k = 0; k < CN_PATH; ++k) alone = alone && path[r][k] != base + t0 + e;
-                            if (alone) first = min(first, (uint32_t)(t0 + e));
-                        }
-                }
-            }
+            if (image == top) first = min(first, (uint32_t)at);
         } else {
             // nothing but -inf and NaN: the first allowed -inf
+            first = 0xffffffffu;
             for (int t = lane; t < n_tok && first == 0xffffffffu; t += 32)
-                if (bit_of(t)) {
+                if (is_allowed(t)) {
                     float x = El::get(in + t), bias = 0.f;
                     uint32_t counted = 0u;
                     const bool in_list = listed[t / 32] >> (t % 32) & 1;
@@ -359,7 +394,13 @@ constrain_kernel(const ConstrainParams p) {
                 }
         }
         first = __reduce_min_sync(0xffffffffu, first);
-        if (lane == 0 && first != 0xffffffffu) atomicMax(p.keys + row, (unsigned long long)top << 32 | (0xffffffffu - ((uint32_t)base + first)));
+        if (lane == 0 && first != 0xffffffffu) {
+            const unsigned long long key = (unsigned long long)top << 32 | (0xffffffffu - ((uint32_t)base + first));
+            if (p.one_slab) p.keys[row] = key;
+            else atomicMax(p.keys + row, key);
+        }
+        if (p.one_slab && lane == 0 && first == 0xffffffffu) p.keys[row] = 0ull;
+        __syncwarp();       // before the next row's bits
     }
 }
 
@@ -415,7 +456,8 @@ static int constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void
     p.B = B; p.rows_per_block = per; p.groups = (p.T + per - 1) / per;
     if (slabs * B * p.groups > 0x7fffffff) return MTV_ERR_UNSUPPORTED_SHAPE;
     const dim3 grid((unsigned)(slabs * B * p.groups));
-    if (keys) MTV_CUDA_CHECK(launch_dependent(clear_keys_kernel, dim3((B * p.T + 255) / 256), 256, 0, stream, B * p.T, keys));
+    p.one_slab = slabs == 1;
+    if (keys && !p.one_slab) MTV_CUDA_CHECK(launch_dependent(clear_keys_kernel, dim3((B * p.T + 255) / 256), 256, 0, stream, B * p.T, keys));
     auto kernel = dtype == MTV_LOGITS_BF16 ? (keys ? constrain_kernel<__nv_bfloat16, false> : constrain_kernel<__nv_bfloat16, true>)
                                            : (keys ? constrain_kernel<float, false> : constrain_kernel<float, true>);
     MTV_CUDA_CHECK(launch_dependent(kernel, grid, CN_THREADS, 0, stream, p));
