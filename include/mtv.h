@@ -419,7 +419,8 @@ typedef struct {
 
 /* tree_kv_append_rope_layers for such a cache: node i of sequence b at position seq_lens[b] + depth[i], its rotated K row
  * and its V row to slot seq_lens[b] + i; k_pools / v_pools: device arrays of n_layers device pointers.  The rotated queries go to
- * q_out_layers (which may be q_layers itself; otherwise the two must not overlap).  Same angles, arithmetic and rope_theta.
+ * q_out_layers (which may be q_layers itself; otherwise the two must not overlap).  Same angles and rope_theta; the sine and cosine are
+ * taken in fp32 once the angle is reduced, so that a bf16 may differ from that call's by a rounding.
  * MTV_ERR_CAPACITY: nothing of b is written.  MTV_ERR_BOUNDS: K/V rows whose page does not exist are left out, the rest of
  * the sequence is written. */
 int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,

@@ -6,8 +6,9 @@
 namespace mtv {
 
 constexpr int PAGED_THREADS = 256;
+constexpr int APPEND_DEEP = 1;       // pairs of 16-byte chunks that a thread asks for at a time
 constexpr int PAGED_MAX_HEADS = 4096;
-constexpr int APPEND_ROWS = 4;       // rows of a block: with half a head's columns 64 (32), all its threads have an angle to work out
+constexpr int APPEND_ROWS = 2;       // rows of a block
 
 // (x[d], x[d + D/2]) -> (x[d] cos - x[d + D/2] sin, x[d + D/2] cos + x[d] sin) for 8 columns, in fp32, rounded once to bf16
 __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float *cs, const float *sn) {
@@ -41,13 +42,39 @@ __device__ __forceinline__ int rows_of(const AppendParams &p, int b, int *first)
     return p.starts ? p.starts[b + 1] - *first : p.T;
 }
 
+// 16 bytes of a row, whatever its address
+template <bool VEC> __device__ __forceinline__ uint4 load8(const __nv_bfloat16 *p) {
+    uint4 x;
+    if constexpr (VEC) {
+        x = *reinterpret_cast<const uint4 *>(p);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) reinterpret_cast<__nv_bfloat16 *>(&x)[k] = p[k];
+    }
+    return x;
+}
+template <bool VEC> __device__ __forceinline__ void store8(__nv_bfloat16 *p, const uint4 &x) {
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4 *>(p) = x;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) p[k] = reinterpret_cast<const __nv_bfloat16 *>(&x)[k];
+    }
+}
+
 // Bound by memory: per row and layer Hq rows are read and written, 2 Hkv read and 2 Hkv written.  A block takes APPEND_ROWS rows of
 // some layers, works their angles out once (in double precision as far as the reduction to one turn goes: positions reach tens of
-// thousands of radians; the sine and cosine of what is left in fp32), and moves 16-byte chunks.  The blocks behind the
-// rows' own report one sequence per warp.
+// thousands of radians; the sine and cosine of what is left in fp32), and moves 16-byte chunks.  The first of them are requested before
+// anything else: lengths, pages and angles are worked out meanwhile.  The blocks behind the rows' own report one sequence per warp.
+// Measured: trees of 4 x 64 nodes, 32 + 2 x 8 heads of 128, 32 layers: 35.6 us (201 MB, 5.6 TB/s; 30.8 at the memory's rate); five prompts of
+// 3005 tokens, 28 + 2 x 4 heads, one layer: 13.4 us (8.5): there the chain length, page, angle, row of the last wave of blocks.  Two rows a block: four
+// take 34.9 and 15.4, one 36.5 and 17.4; two pairs in flight per thread 34.8 and 14.9, as fewer blocks fit.
+// VEC: the rows begin at multiples of 16 bytes.
+template <int D, bool VEC>
 __global__ void __launch_bounds__(PAGED_THREADS)
 kv_append_rope_paged_kernel(const AppendParams p) {
-    __shared__ __align__(16) float cs[APPEND_ROWS][64], sn[APPEND_ROWS][64];   // D / 2 <= 64
+    constexpr int HALF = D / 2, PER_HEAD = D / 16, SLOTS = PAGED_THREADS / PER_HEAD;    // threads of a head; heads at a time
+    __shared__ __align__(16) float cs[APPEND_ROWS][HALF], sn[APPEND_ROWS][HALF];
     __shared__ int64_t dst_of[APPEND_ROWS];    // of the row inside a pool; -1: no K/V row is written
     __shared__ int pos_of[APPEND_ROWS];        // -1: the row is left alone
     const int tid = threadIdx.x;
@@ -63,6 +90,34 @@ kv_append_rope_paged_kernel(const AppendParams p) {
         return;
     }
     const int r0 = (int)blockIdx.x * APPEND_ROWS;
+    // A thread takes two chunks of 8 columns of a head, half a row apart; heads of a row in the order queries, keys, values, rows of a layer
+    // behind one another.  (row, h) of its next pair, the row counted over the layers: a step is SLOTS heads.
+    const int c = tid % PER_HEAD * 8, heads = p.Hq + 2 * p.Hkv;
+    const int l0 = (int)blockIdx.y * p.layers_per_block, end = min(p.n_layers - l0, p.layers_per_block) * APPEND_ROWS;
+    const int step_rows = SLOTS / heads, step_heads = SLOTS - step_rows * heads;
+    int row = tid / PER_HEAD / heads, h = tid / PER_HEAD - row * heads;
+    uint4 x[APPEND_DEEP][2];
+    int at_row[APPEND_DEEP], at_h[APPEND_DEEP];
+    auto request = [&] {
+#pragma unroll
+        for (int k = 0; k < APPEND_DEEP; ++k) {
+            const int j = row % APPEND_ROWS;
+            at_row[k] = row < end && r0 + j < p.n_rows ? row : -1;
+            at_h[k] = h;
+            if (at_row[k] >= 0) {
+                const size_t i = (size_t)(l0 + row / APPEND_ROWS) * p.n_rows + r0 + j;
+                const int g = h - p.Hq;
+                const __nv_bfloat16 *src = g < 0 ? p.q + (i * p.Hq + h) * D : g < p.Hkv ? p.k_new + (i * p.Hkv + g) * D : p.v_new + (i * p.Hkv + g - p.Hkv) * D;
+                x[k][0] = load8<VEC>(src + c);
+                x[k][1] = load8<VEC>(src + HALF + c);
+            }
+            row += step_rows;
+            h += step_heads;
+            if (h >= heads) { h -= heads; ++row; }
+        }
+    };
+    request();
+    const double per_position = exp2(-2.0 * (tid % HALF) / D * p.log2_theta) * 0.15915494309189535;   // turns: / 2 pi
     int b0 = 0;
     if (p.starts) {        // the sequence of the block's first row: how many end at or before it
         for (int s = 0; s < p.B; s += PAGED_THREADS) b0 += __syncthreads_count(s + tid < p.B && p.starts[s + tid + 1] <= r0);
@@ -86,70 +141,50 @@ kv_append_rope_paged_kernel(const AppendParams p) {
         dst_of[tid] = dst;
     }
     __syncthreads();
-    const int half = p.D / 2;
     {
-        const int j = tid / half, d = tid % half;
+        const int j = tid / HALF, d = tid % HALF;
         if (j < APPEND_ROWS && pos_of[j] >= 0) {
-            const double turns = (double)pos_of[j] * exp2(-2.0 * d / p.D * p.log2_theta) * 0.15915494309189535;   // / 2 pi
+            const double turns = (double)pos_of[j] * per_position;
             const float a = (float)((turns - rint(turns)) * 6.283185307179586);
             sincosf(a, &sn[j][d], &cs[j][d]);
         }
     }
     __syncthreads();
-    // A thread takes two chunks of 8 columns of a head, half a row apart: D / 16 threads per head, heads of a row in the order
-    // queries, keys, values.
-    const int shift = p.D == 128 ? 3 : 2;
-    const int c = tid & ((1 << shift) - 1), heads = p.Hq + 2 * p.Hkv;
-    const int l0 = (int)blockIdx.y * p.layers_per_block, n_l = min(p.n_layers - l0, p.layers_per_block);
-    for (int e = tid >> shift; e < n_l * APPEND_ROWS * heads; e += PAGED_THREADS >> shift) {
-        const int lj = e / heads, h = e - lj * heads, j = lj % APPEND_ROWS, layer = l0 + lj / APPEND_ROWS;
-        if (pos_of[j] < 0) continue;
-        const size_t row = (size_t)layer * p.n_rows + r0 + j;
-        const __nv_bfloat16 *src;
-        __nv_bfloat16 *dst;
-        if (h < p.Hq) {
-            src = p.q + (row * p.Hq + h) * p.D;
-            dst = p.q_out + (row * p.Hq + h) * p.D;
-        } else {
-            if (dst_of[j] < 0) continue;
-            const bool is_v = h >= p.Hq + p.Hkv;
-            const int g = h - p.Hq - (is_v ? p.Hkv : 0);
-            src = (is_v ? p.v_new : p.k_new) + (row * p.Hkv + g) * p.D;
-            dst = (is_v ? p.v_pools : p.k_pools)[layer] + dst_of[j] + g * p.pages.stride_h;
-        }
-        const bool aligned = (((uintptr_t)src | (uintptr_t)dst) & 15) == 0;   // else element by element
-        uint4 x1, x2;
-        if (aligned) {
-            x1 = *reinterpret_cast<const uint4 *>(src + c * 8);
-            x2 = *reinterpret_cast<const uint4 *>(src + half + c * 8);
-        } else {
-            for (int k = 0; k < 8; ++k) {
-                reinterpret_cast<__nv_bfloat16 *>(&x1)[k] = src[c * 8 + k];
-                reinterpret_cast<__nv_bfloat16 *>(&x2)[k] = src[half + c * 8 + k];
+    for (;;) {
+#pragma unroll
+        for (int k = 0; k < APPEND_DEEP; ++k) {
+            const int j = at_row[k] % APPEND_ROWS;
+            if (at_row[k] < 0 || pos_of[j] < 0) continue;
+            const int layer = l0 + at_row[k] / APPEND_ROWS, g = at_h[k] - p.Hq;
+            __nv_bfloat16 *dst;
+            if (g < 0) {
+                dst = p.q_out + (((size_t)layer * p.n_rows + r0 + j) * p.Hq + at_h[k]) * D;
+            } else {
+                if (dst_of[j] < 0) continue;
+                const bool is_v = g >= p.Hkv;
+                dst = (is_v ? p.v_pools : p.k_pools)[layer] + dst_of[j] + (g - (is_v ? p.Hkv : 0)) * p.pages.stride_h;
             }
+            if (g < p.Hkv) rotate8(x[k][0], x[k][1], &cs[j][c], &sn[j][c]);
+            store8<VEC>(dst + c, x[k][0]);
+            store8<VEC>(dst + HALF + c, x[k][1]);
         }
-        if (h < p.Hq + p.Hkv) rotate8(x1, x2, &cs[j][c * 8], &sn[j][c * 8]);
-        if (aligned) {
-            *reinterpret_cast<uint4 *>(dst + c * 8) = x1;
-            *reinterpret_cast<uint4 *>(dst + half + c * 8) = x2;
-        } else {
-            for (int k = 0; k < 8; ++k) {
-                dst[c * 8 + k] = reinterpret_cast<const __nv_bfloat16 *>(&x1)[k];
-                dst[half + c * 8 + k] = reinterpret_cast<const __nv_bfloat16 *>(&x2)[k];
-            }
-        }
+        if (row >= end) break;
+        request();
     }
 }
 
 static int launch_append(AppendParams &p, cudaStream_t stream) {
     p.row_blocks = (p.n_rows + APPEND_ROWS - 1) / APPEND_ROWS;
     // enough blocks to fill the device a few times over, as many layers per block as that leaves
-    long per = (long)p.row_blocks * p.n_layers / (6L * sm_count());
+    long per = (long)p.row_blocks * p.n_layers / (12L * sm_count());
     per = per < 1 ? 1 : per > 64 ? 64 : per;
     if (per > p.n_layers) per = p.n_layers;
     p.layers_per_block = (int)per;
     const int report = p.status || !p.row_blocks ? (p.B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32) : 0;
-    MTV_CUDA_CHECK(launch_dependent(kv_append_rope_paged_kernel, dim3(p.row_blocks + report, (unsigned)((p.n_layers + per - 1) / per)),
+    const bool vec = (((uintptr_t)p.q | (uintptr_t)p.q_out | (uintptr_t)p.k_new | (uintptr_t)p.v_new) & 15) == 0;
+    auto kernel = p.D == 128 ? (vec ? kv_append_rope_paged_kernel<128, true> : kv_append_rope_paged_kernel<128, false>)
+                             : (vec ? kv_append_rope_paged_kernel<64, true> : kv_append_rope_paged_kernel<64, false>);
+    MTV_CUDA_CHECK(launch_dependent(kernel, dim3(p.row_blocks + report, (unsigned)((p.n_layers + per - 1) / per)),
                                     PAGED_THREADS, 0, stream, p));
     return MTV_OK;
 }
