@@ -452,8 +452,10 @@ int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int
  * are joined.  shared_len: a multiple of page_size (0: nothing is shared), at most every seq_lens[b]
  * and max_pages * page_size.
  * A tree of its root alone is plain decoding of one token per sequence.
- * Same formula, types and rounding as tree_verify_attention; scale == 0 means 1/sqrt(D), negative scales are refused.
- * q, out [B][T][Hq][D] contiguous, 16-byte aligned.  B <= 1024.  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such
+ * Same formula, types and rounding as tree_verify_attention; scale == 0 means 1/sqrt(D); scales that are negative, NaN or above 1e30 are
+ * refused (MTV_ERR_INVALID_ARG).
+ * q, out [B][T][Hq][D] contiguous, 16-byte aligned, not overlapping.  B <= 1024, Hq * B * T <= 2^28; MTV_ERR_UNSUPPORTED_SHAPE also where
+ * shared_len and B * max_pages * page_size, taken for every tile of 128 query rows, pass what 32 bits count (some 10^10 keys).  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such
  * a sequence is left as it was.  MTV_ERR_BOUNDS: keys on pages that do not exist count as zero rows, out[b] is of no use.
  * NaN or infinities in the K/V rows of nodes that a node does not see, and in rows behind the last node, do not reach its output.
  * ws: tree_attention_paged_workspace_bytes, device, 256-byte aligned; nothing in it outlives the call.  Calls that share a
@@ -504,7 +506,7 @@ int logits_constrain(const mtv_tree_t *tree, int B, int V, int dtype, const void
                      int64_t stride_out, const mtv_logit_rules *rules, const int32_t *tree_tok, void *stream);
 
 /* The argmax of the same values, never stored: keys [B*T] for tree_accept_keys, in the form of lm_head_argmax (compared in fp32;
- * ties: lowest v; NaN is never chosen).  A row that has no token left (its mask allows none) gets the key 0: its argmax reads -1,
+ * ties: lowest v; NaN is never chosen).  A row that has no token left (its mask allows none, or only NaN) gets the key 0: its argmax reads -1,
  * which no drafted token equals, and next_root is -1 if the acceptance ends there. */
 int constrained_argmax_keys(const mtv_tree_t *tree, int B, int V, int dtype, const void *logits, int64_t stride_in,
                             const mtv_logit_rules *rules, const int32_t *tree_tok, unsigned long long *keys, void *stream);

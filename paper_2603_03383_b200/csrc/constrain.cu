@@ -137,7 +137,8 @@ constrain_kernel(const ConstrainParams p) {
     uint32_t seen = 0u;
     if (tid < CN_WORDS && p.seen && base / 32 + tid < p.words) seen = p.seen[(size_t)b * p.words + base / 32 + tid];
     int biased_at = -1;
-    if (tid < p.n_bias) biased_at = p.bias_ids[(size_t)b * p.n_bias + tid] - base;
+    auto bias_at = [&](int k) { return (int)((uint32_t)p.bias_ids[(size_t)b * p.n_bias + k] - (uint32_t)base); };   // any number may stand there
+    if (tid < p.n_bias) biased_at = bias_at(tid);
     const Penalties pen = {p.repetition ? p.repetition[b] : 1.f, p.presence ? p.presence[b] : 0.f, p.frequency ? p.frequency[b] : 0.f};
     for (int e = tid; e < n_rows * CN_PATH; e += CN_THREADS) {
         const int r = e / CN_PATH;
@@ -172,7 +173,7 @@ constrain_kernel(const ConstrainParams p) {
     if (tid == 0) n_match = 0;
     __syncthreads();
     for (int k = tid; k < p.n_bias; k += CN_THREADS) {
-        if (k != tid) biased_at = p.bias_ids[(size_t)b * p.n_bias + k] - base;
+        if (k != tid) biased_at = bias_at(k);
         if (biased_at >= 0 && biased_at < n_tok) {
             atomicOr(&listed[biased_at / 32], 1u << (biased_at % 32));
             atomicOr(&biased[biased_at / 32], 1u << (biased_at % 32));

@@ -69,6 +69,8 @@ def check(tree, tb, Hq, Hkv, D, page, shared, lens, seed=1, tokens_outside=False
     (5, 128, 5, 5, 128, 16, 160, [161, 161, 161]),       # groups of one
     (1, 1, 4, 1, 64, 16, 0, [9000] + [1] * 300 + [5000] + [3] * 200),      # long pieces beside many short ones
     (1, 1, 2, 2, 128, 32, 32, [40 + i % 50 for i in range(150)] + [6000]),
+    (1, 1, 2, 1, 64, 16, 32, [32 + 7 * i % 40 for i in range(1024)]),          # the largest batch
+    (2, 3, 64, 64, 64, 16, 0, [3, 100]),                                        # many KV heads
     # at most 16 query rows a KV head: of a sequence, and of all behind the prefix (2 x 8, 4 x 4)
     (2, 2, 8, 1, 128, 16, 0, [0, 5, 14, 15, 16, 63, 64, 500]),
     (3, 16, 2, 2, 64, 32, 64, [64, 80, 1001]),
