@@ -457,6 +457,7 @@ int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int
  * q, out [B][T][Hq][D] contiguous, 16-byte aligned, not overlapping.  B <= 1024, Hq * B * T <= 2^28; MTV_ERR_UNSUPPORTED_SHAPE also where
  * shared_len and B * max_pages * page_size, taken for every tile of 128 query rows, pass what 32 bits count (some 10^10 keys).  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such
  * a sequence is left as it was.  MTV_ERR_BOUNDS: keys on pages that do not exist count as zero rows, out[b] is of no use.
+ * A bounded wait that runs out (MTV_ERR_TIMEOUT, the tree's device error word) leaves rows of out as they were or of no use.
  * NaN or infinities in the K/V rows of nodes that a node does not see, and in rows behind the last node, do not reach its output.
  * ws: tree_attention_paged_workspace_bytes, device, 256-byte aligned; nothing in it outlives the call.  Calls that share a
  * workspace must not overlap on the device; calls that share a tree may. */

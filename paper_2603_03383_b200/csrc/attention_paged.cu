@@ -36,6 +36,7 @@
 // 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 34.6 us for 6.3 us of bytes; start, first tile and joining are two thirds of it.
 #include "attn_common.cuh"
 #include "paged_common.cuh"
+#include "paged_plan.cuh"
 
 namespace mtv {
 
@@ -72,15 +73,6 @@ enum {
 constexpr uint32_t PA_OFF_MISC = PB_COUNT * 8, PA_OFF_QUEUE = (PA_OFF_MISC + 40 + 15) / 16 * 16;
 static_assert(PA_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1024, "barrier region");
 
-struct PaPhase {
-    int prefix_items, seq_items;       // items of the prefix, and of each sequence
-    int prefix_per_head, seq_per_head;
-    int prefix_tile0, seq_tile0;       // row tile of a head's first item (0 where an item is a pair)
-    int rows;                          // of a slot
-    float *o;                          // [slots][D / 8][rows][8]
-    float2 *ml;                        // [slots][rows]
-    int2 *span;                        // [items]: first and last worker that has a piece of it
-};
 struct PaParams {
     PagedRef pages;
     PaPhase phase[3];                  // pairs of row tiles, single row tiles, thin ones
@@ -793,7 +785,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 // of its next ones are on the way (8 KB a warp, two CTAs to an SM).  At a piece's end the warps join in shared memory.
 // Measured: 64 single tokens, 8 KV heads of 128, 100 to 1000 keys each: 149 MB in 37 us = 4.0 TB/s.  Bound by the bytes in flight, 64 KB an SM;
 // 221 registers a thread leave no third CTA (with spills: 89 us instead of 61 in one comparison), and more or shorter pieces change nothing (62, 60).
-constexpr int TH_ROWS = 16, TH_WARPS = 4, TH_KEYS = 16, TH_STEP = TH_WARPS * TH_KEYS;
+constexpr int TH_WARPS = 4, TH_KEYS = 16, TH_STEP = TH_WARPS * TH_KEYS;
 constexpr int TH_ENDS = 3;                // what an item's start and end take, in steps of 64 keys
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -1144,7 +1136,7 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
                 const size_t slot = (size_t)item + span.x;
                 return PaSource{f.o + (slot * CHUNKS * f.rows + row) * 8, f.ml + slot * f.rows + row, span.y - span.x + 1, f.rows};
             };
-            if (seq_tiles(p, len)) {
+            if (seq_tiles(p, len) && (!p.shared || pa_span_ok(f0, span0)) && pa_span_ok(f1, span1)) {
                 if (p.shared) s0 = source(f0, item0, row0, span0);
                 s1 = source(f1, item1, row1, span1);
                 // a single piece was written out by the kernel before
@@ -1194,34 +1186,6 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
 }
 
 // ---------------------------------------------------------------------------------------- host
-// The phases of a call and the layout of its workspace; returns the bytes.
-static size_t pa_plan(PaPhase (&ph)[3], int T, int B, int G, int Hkv, int D, int shared, char *ws) {
-    const int npc = 128 / G, sms = sm_count();
-    // at most 16 rows: thin items (64 single tokens of 4 rows a KV head behind 8192 shared keys: the whole call 77 us, and 94 as row tiles)
-    const bool thin_seq = T * G <= TH_ROWS, thin_prefix = shared && B * T * G <= TH_ROWS;
-    const int prefix_tiles = shared && !thin_prefix ? (B * T + npc - 1) / npc : 0, seq_tiles = thin_seq ? 0 : (T + npc - 1) / npc;
-    size_t at = 0;
-    for (int f = 0; f < 3; ++f) {
-        PaPhase &x = ph[f];
-        x.prefix_per_head = f == 2 ? thin_prefix : f ? prefix_tiles % 2 : prefix_tiles / 2;
-        x.seq_per_head = f == 2 ? thin_seq : f ? seq_tiles % 2 : seq_tiles / 2;
-        x.prefix_items = Hkv * x.prefix_per_head;
-        x.seq_items = Hkv * x.seq_per_head;
-        x.prefix_tile0 = f ? prefix_tiles - 1 : 0;
-        x.seq_tile0 = f ? seq_tiles - 1 : 0;
-        x.rows = f == 2 ? TH_ROWS : f ? 128 : 256;
-        const size_t items = (size_t)x.prefix_items + (size_t)B * x.seq_items;
-        const size_t slots = items ? items + (f ? 2 : 1) * sms : 0;     // a piece's slot: its item's number plus its worker's
-        x.o = reinterpret_cast<float *>(ws + at);
-        at += align_up(slots * x.rows * D * sizeof(float), 256);
-        x.ml = reinterpret_cast<float2 *>(ws + at);
-        at += align_up(slots * x.rows * sizeof(float2), 256);
-        x.span = reinterpret_cast<int2 *>(ws + at);
-        at += align_up(items * sizeof(int2), 256);
-    }
-    return at;
-}
-
 static bool pa_sizes_ok(const mtv_tree *tree, int B, int Hq, int Hkv, int D, int shared) {
     return tree && B >= 1 && B <= PA_MAX_B && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= 8 && (D == 64 || D == 128) && shared >= 0 &&
            (int64_t)Hq * B * tree->T <= 1 << 28;
@@ -1267,7 +1231,7 @@ extern "C" size_t tree_attention_paged_workspace_bytes(const mtv_tree_t *tree, i
     using namespace mtv;
     if (!pa_sizes_ok(tree, B, Hq, Hkv, D, shared_len)) return 0;
     PaPhase ph[3];
-    return pa_plan(ph, tree->T, B, Hq / Hkv, Hkv, D, shared_len, nullptr);
+    return pa_plan(ph, sm_count(), tree->T, B, Hq / Hkv, Hkv, D, shared_len, nullptr);
 }
 
 extern "C" int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, const mtv_bf16 *q, const mtv_bf16 *k_pool,
@@ -1286,7 +1250,7 @@ extern "C" int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq
         return MTV_ERR_INVALID_ARG;
     p.T = tree->T; p.B = B; p.G = Hq / Hkv; p.Hq = Hq; p.Hkv = Hkv;
     p.shared = shared_len;
-    if (ws_bytes < pa_plan(p.phase, p.T, B, p.G, Hkv, D, shared_len, static_cast<char *>(ws))) return MTV_ERR_WORKSPACE;
+    if (ws_bytes < pa_plan(p.phase, sm_count(), p.T, B, p.G, Hkv, D, shared_len, static_cast<char *>(ws))) return MTV_ERR_WORKSPACE;
     if (!pa_lines_ok(p.phase, B, shared_len, (int64_t)max_pages * pool->page_size)) return MTV_ERR_UNSUPPORTED_SHAPE;
     p.npc = 128 / p.G;
     p.page_rows = pool->page_size < PA_KEYS ? pool->page_size : PA_KEYS;
