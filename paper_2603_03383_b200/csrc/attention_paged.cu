@@ -46,6 +46,12 @@ constexpr int PA_QUEUE = 4;               // pieces that are handed out and may 
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
 constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
+// P goes to the second product as bf16, whose rounding is the largest error beside the output's own (relative 2-norm against 64 bits, N(0, 1) inputs:
+// .0023 with it, .00166 without).  As in tree_verify_attention, head size 64 has a second bf16 term, what the rounding of the first left, in every tile
+// (three trees of 128 nodes, 16 / 2 heads of 64, 4096 shared keys: 31.2 us without, 35.3 with), and so have thin items, whose products cost nothing beside
+// their bytes.  At head size 128 a row tile has one term (its products are a third of the time there: 16384 shared keys 179 us, 238 with two in every tile,
+// 192 in four of a piece; one-layer calls of tree_verify_attention are at .0027).
+template <int D> constexpr bool TWO_TERMS = D == 64;
 constexpr int TILE_COST = 4;              // a key tile on a line
 __host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }   // what the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles
 __host__ __device__ constexpr int PHASE_COST(int single) { return single ? 4 : 7; }   // and what a quarter of a key tile takes a CTA, one against the other: pairs are bound by the tensor core and
@@ -277,6 +283,11 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// What the rounding of two values to bf16 pairs left, as bf16 pairs.
+__device__ __forceinline__ uint32_t rounded_off(float2 p, uint32_t w) {
+    const float2 r = __fadd2_rn(p, make_float2(-__uint_as_float(w << 16), -__uint_as_float(w & 0xffff0000u)));
+    return pack2_bf16(r.x, r.y);
+}
 __device__ __forceinline__ bool nonfinite16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
 
 // The two warps that hold the same rows: whether any of their threads says so.
@@ -309,6 +320,10 @@ __global__ void __launch_bounds__(PA_THREADS, 1)
 paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                   const __grid_constant__ PaParams p) {
     using SM = PaSmem<D>;
+    constexpr bool TWO = TWO_TERMS<D>;
+    // tensor-memory columns of a half of the keys (64 scores): P, keys 0-31 at 0-15 and 32-63 at 32-47 with their second terms behind them, or all at 0-31;
+    // and what the threads of a row exchange, where second terms go, or behind P
+    constexpr int X_COL = TWO ? 16 : 40;
     extern __shared__ unsigned char smem_raw[];
     let_next_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -516,7 +531,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
 #pragma unroll
                     for (int kk = 0; kk < PA_KEYS / 16; ++kk)
-                        ptx::mma_ts_elect(t_o, t_s + (kk / 4) * 64 + (kk % 4) * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
+                        ptx::mma_ts_elect(t_o, t_s + (TWO ? kk / 2 * 32 + kk % 2 * 8 : kk / 4 * 64 + kk % 4 * 8), dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
+                    if (TWO) {
+#pragma unroll
+                        for (int kk = 0; kk < PA_KEYS / 16; ++kk)
+                            ptx::mma_ts_elect(t_o, t_s + kk / 2 * 32 + 16 + kk % 2 * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, true, leader);
+                    }
                     if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(PB_ODONE + s), leader);
                     if (!ahead) end_run();
                 }
@@ -607,14 +627,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         // ------------------------------------------------------------ softmax: thread (row, hf) of row tile s: columns [64 hf, 64 hf + 64)
         const int s = warp >> 3, hf = (warp >> 2) & 1, qd = warp & 3, row = qd * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
-        const uint32_t t_s = lane_base + s * 128 + hf * 64;      // this half's scores; P over their first 32 columns, what is exchanged behind
+        const uint32_t t_s = lane_base + s * 128 + hf * 64;      // this half's scores, and P over them
         const uint32_t t_x = lane_base + s * 128 + (hf ^ 1) * 64;
         const uint32_t t_o = lane_base + 256 + s * D + hf * (D / 2);
         const int pair_bar = 2 + s * 4 + qd;
         const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
         const bool in_tile = node_in_tile < p.npc;
         const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
-        // what the other half of the row has: both put theirs behind their P's place, where nothing is any more
+        // what the other half of the row has: both put theirs where nothing is any more
         auto exchange = [&](int col, float v) {
             tmem_put(t_s + col, v);
             ptx::tmem_st_wait();
@@ -641,9 +661,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     if (!wait(PB_SREADY + s, n_s++ & 1)) { ok = false; break; }
                     ptx::tc_fence_after();
                     if (some) {
-                        uint32_t pk[32];
+                        uint32_t pk[32], rest[TWO ? 32 : 1];     // bf16 pairs; what their rounding left
                         float2 la, lb;
-                        for (bool move = t == pc.t0;;) {
+                        bool move = t == pc.t0;
+                        for (;;) {
                             uint32_t sr[64];
                             ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
                             ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
@@ -666,7 +687,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 #pragma unroll
                                     for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
                                 float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * p.scale_log2;
-                                mxs = max_nan(mxs, exchange(40, mxs));
+                                mxs = max_nan(mxs, exchange(X_COL, mxs));
                                 if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
                                 const float m_new = mxs <= m_used ? m_used : mxs;            // (a NaN is taken over)
                                 const bool need = m_new != m_used && m_used != -INFINITY && mine;
@@ -695,7 +716,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                                 const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
                                 const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
                                 float2 p01, p23;
-                                if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                if (!TWO && e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                    // (with second terms the other pipes have more to do: 35.3 us without polynomials, 36.5 with, in the example above)
                                     px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
                                     p01 = exp2_poly2(x01);
                                     p23 = exp2_poly2(x23);
@@ -707,6 +729,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                                 lb = __fadd2_rn(lb, p23);
                                 pk[e] = pack2_bf16(p01.x, p01.y);
                                 pk[e + 1] = pack2_bf16(p23.x, p23.y);
+                                if constexpr (TWO) {
+                                    rest[e] = rounded_off(p01, pk[e]);
+                                    rest[e + 1] = rounded_off(p23, pk[e + 1]);
+                                }
                             }
                             if (move) break;
                             // a sum that is too large, infinite or NaN, and a row that has met no visible key yet
@@ -714,9 +740,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                             if (!any_of_rows(pair_bar, mine && ask)) break;
                             move = true;
                         }
-                        ptx::tmem_st32(t_s, pk);
                         l += (la.x + la.y) + (lb.x + lb.y);
-                        if (t == pc.t1 - 1) l += exchange(41, l);       // the row's sum; S is another tile's behind this one's P
+                        const bool last = t == pc.t1 - 1;
+                        if constexpr (TWO) {
+                            if (last) l += exchange(X_COL + 1, l);      // the row's sum
+                            // (second terms go over what was exchanged when the other half has read it)
+                            if (move || last) asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                ptx::tmem_st16(t_s + h * 32, *reinterpret_cast<uint32_t(*)[16]>(&pk[h * 16]));
+                                ptx::tmem_st16(t_s + h * 32 + 16, *reinterpret_cast<uint32_t(*)[16]>(&rest[h * 16]));
+                            }
+                        } else {
+                            ptx::tmem_st32(t_s, pk);
+                            if (last) l += exchange(X_COL + 1, l);      // S is another tile's behind this one's P
+                        }
                         ptx::tmem_st_wait();
                     }
                     ptx::tc_fence_before();
@@ -977,7 +1015,7 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
                 }
             }
             const float me[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-            uint32_t pa[4];
+            uint32_t pa[4], rest[4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -985,6 +1023,7 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
                     const float w0 = ex2(fmaf(sc[h][2 * r], p.scale_log2, -me[r])), w1 = ex2(fmaf(sc[h][2 * r + 1], p.scale_log2, -me[r]));
                     l[r] += w0 + w1;
                     pa[h * 2 + r] = pack2_bf16(w0, w1);
+                    rest[h * 2 + r] = rounded_off(make_float2(w0, w1), pa[h * 2 + r]);
                 }
             bool odd = false;
             if (edge && own) {
@@ -1000,8 +1039,12 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
             }
 #pragma unroll
             for (int j = 0; j < J; j += 2) {
-                mma16816(o[j], pa, __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x5410), __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x5410));
-                mma16816(o[j + 1], pa, __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x7632), __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x7632));
+                const uint32_t a0 = __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x5410), a1 = __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x5410);
+                const uint32_t b0 = __byte_perm(vx[0][j / 2], vx[1][j / 2], 0x7632), b1 = __byte_perm(vx[2][j / 2], vx[3][j / 2], 0x7632);
+                mma16816(o[j], pa, a0, a1);
+                mma16816(o[j + 1], pa, b0, b1);
+                mma16816(o[j], rest, a0, a1);
+                mma16816(o[j + 1], rest, b0, b1);
             }
             if (odd && at_now >= 0)
                 for (int k = 0; k < TH_KEYS; ++k) {

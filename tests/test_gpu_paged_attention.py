@@ -302,3 +302,32 @@ def test_refusals():
     assert code(q=wide, out=torch.zeros_like(wide)) in (-1, -2)
     torch.cuda.synchronize()
     assert (out == 7.0).all() and binding.mtv_device_error(tree) == 0
+
+
+@pytest.mark.parametrize("K,T,Hq,Hkv,D,page,shared,lens", [
+    (1, 1, 8, 1, 64, 16, 0, [3, 9, 40, 700]),             # at most 16 rows a KV head, of a sequence and of all behind the prefix
+    (1, 1, 16, 2, 128, 64, 0, [3, 9, 40, 700]),
+    (1, 1, 16, 4, 128, 64, 128, [130, 128, 900]),
+    (2, 2, 8, 1, 128, 16, 0, [0, 5, 14, 63, 500]),
+    (3, 4, 16, 4, 64, 32, 32, [32, 47, 333]),
+    (3, 29, 8, 2, 64, 16, 0, [128, 5]),                   # row tiles of head size 64
+    (4, 64, 32, 8, 64, 32, 256, [256, 383, 900]),
+    (4, 64, 32, 8, 64, 32, 4096, [4100, 5000]),
+    (4, 65, 6, 1, 64, 128, 384, [384, 400]),
+    (5, 128, 16, 2, 64, 32, 0, [5, 3000]),
+    (1, 1, 32, 8, 64, 64, 1024, [1024 + 17 * i for i in range(40)]),
+])
+def test_weights_in_two_terms(K, T, Hq, Hkv, D, page, shared, lens):
+    """Where weights have two bf16 terms their own rounding stays out of the result: two bf16 terms leave at most 2^-16 of a weight.  The exponentials are good to 7.5e-5,
+    above and below the fraction, the scores as in bound(); beside them there is the output's rounding alone."""
+    tb, tree = _tree(K, T)
+    g = torch.Generator().manual_seed(23)
+    B = len(lens)
+    t, n_pages = table(g, B, max(lens) - shared + T, page, shared)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    q = torch.randn(B, T, Hq, D, generator=g).to(torch.bfloat16)
+    out = run(tree, q, kp, vp, t, lens, shared)
+    want, absolute = want_of(q, kp, vp, t, lens, tb["mask"])
+    most = EPS * want.abs() + (1 + EPS) * (2.0 ** -16 + 2 * 7.5e-5 + 1e-4) * absolute + 1e-30
+    worst = ((out.double() - want).abs() / most).max().item()
+    assert worst <= 1.0, worst
