@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(CN_THREADS, 5)
 constrain_kernel(const ConstrainParams p) {
     using El = Elem<E>;
     constexpr int VEC = El::VEC;
-    __shared__ uint32_t listed[CN_WORDS], biased[CN_WORDS], allowed_of[CN_WARPS][CN_WORDS], dense_of[CN_WARPS][CN_WORDS + 1];
+    __shared__ uint32_t listed[CN_WORDS], biased[CN_WORDS], known[CN_WORDS], allowed_of[CN_WARPS][CN_WORDS], dense_of[CN_WARPS][CN_WORDS + 1];
     __shared__ uint32_t list_count[CN_SLAB];
     __shared__ float list_bias[CN_SLAB];
     __shared__ uint16_t list_at[CN_SLAB];
@@ -167,7 +167,7 @@ constrain_kernel(const ConstrainParams p) {
     uint32_t next[CN_PER];
     mask_words(0, next);
     if (tid < CN_WORDS) {
-        listed[tid] = seen;
+        listed[tid] = known[tid] = seen;
         biased[tid] = 0u;
     }
     if (tid == 0) n_match = 0;
@@ -214,7 +214,8 @@ constrain_kernel(const ConstrainParams p) {
                 sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + last]);
             }
         list_bias[e] = sum;
-        list_count[e] = p.counts && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
+        // (a count whose bit in `seen` is 0 may be an earlier sequence's)
+        list_count[e] = known[at / 32] >> (at % 32) & 1u && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;
     }
     __syncthreads();
     // ---- a warp per row; its mask is requested while the row before is worked on

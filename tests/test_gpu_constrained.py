@@ -227,3 +227,24 @@ def test_counts(B, V, n, prompt):
     assert torch.equal(seen.cpu(), _rules.packed(want != 0))
     binding.token_counts_add(tokens[:, :0].to(DEV), counts, seen)          # nothing to add
     assert torch.equal(counts.cpu().long(), want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("V", [900, 5003])
+def test_counts_whose_seen_bit_is_not_set(dtype, V):
+    """A token whose bit in `seen` is 0 counts as never seen whatever its count says, biased or not, on the path or not."""
+    tb, tree, x, r, tok, paths = case(3, 29, 2, V, dtype, 400, 200, 3)
+    g = torch.Generator().manual_seed(1)
+    cleared = torch.rand(2, V, generator=g) < 0.5
+    cleared[1] = True                               # a sequence that begins anew by clearing its words
+    cleared[:, tok[0, 1]] = True
+    r["seen"] = _rules.packed((r["counts"] != 0) & ~cleared)
+    plain = dict(r, counts=torch.where(cleared, 0, r["counts"]))
+    assert (cleared & (r["counts"] != 0)).gather(1, r["bias_ids"].long().clamp(0, V - 1)).any()
+    want, _ = _rules.constrained(x, plain, tok, paths, torch.float32)
+    out, keys = torch.empty_like(x, device=DEV), torch.empty(2 * tree.T, dtype=torch.int64, device=DEV)
+    binding.logits_constrain(tree, x.to(DEV), out, on_device(r), tok.to(DEV))
+    binding.constrained_argmax_keys(tree, x.to(DEV), keys, on_device(r), tok.to(DEV))
+    assert torch.equal(bits(out.cpu() + 0.0), bits(want.to(dtype) + 0.0))
+    key, _, top = _rules.keys_of(want)
+    assert torch.equal(keys.cpu(), torch.where(top == -INF, 0, key))
