@@ -475,9 +475,9 @@ int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, 
  * from the root to i (root and i included), seen = c > 0 or v in b's prompt:
  *   x = logits[b][i][v] as fp32
  *   seen:   x = x > 0 ? x / repetition[b] : x * repetition[b]
- *           x = x - frequency[b] * c
- *   c > 0:  x = x - presence[b]
- *           x = x + bias                 (the sum of v's entries in b's list, in the list's order)
+ *   c > 0:  x = x - frequency[b] * c
+ *           x = x - presence[b]
+ *   then    x = x + bias                 (the sum of v's entries in b's list, in the list's order)
  *   bit v of the row's mask is 0:  -inf  (whatever the logit holds)
  * each operation rounded to fp32 by itself.
  * All pointers device; NULL fields leave their part out.  words = ceil(V / 32); bit v % 32 of word v / 32 stands for token v.

@@ -1,7 +1,7 @@
 // Penalties for repeated tokens, biases and grammar masks on the base model's logits at the tree's nodes, in front of the acceptance
 // (Section 3.2; the paper accepts on the plain argmax).  For row (b, i) and token v, with c = occurrences of v in sequence b's generated
 // text and on the path from the root to node i, seen = c > 0 or v in the prompt:
-//   x = logit;  seen: x = x > 0 ? x / repetition : x * repetition;  x = x - frequency * c;  c > 0: x = x - presence;
+//   x = logit;  seen: x = x > 0 ? x / repetition : x * repetition;  c > 0: x = x - frequency * c, x = x - presence;
 //   x = x + bias;  not allowed by the row's mask: -inf
 // every operation rounded to fp32 by itself (no contraction), so that equal inputs give equal keys whatever the order they are met in.
 //
@@ -106,8 +106,7 @@ struct Penalties {
     float r, p, f;
     __device__ __forceinline__ float apply(float x, int c, bool seen, float bias) const {
         if (seen) x = x > 0.f ? __fdiv_rn(x, r) : __fmul_rn(x, r);
-        x = __fsub_rn(x, __fmul_rn(f, (float)c));
-        if (c > 0) x = __fsub_rn(x, p);
+        if (c > 0) x = __fsub_rn(__fsub_rn(x, __fmul_rn(f, (float)c)), p);
         return __fadd_rn(x, bias);
     }
 };

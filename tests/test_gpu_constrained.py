@@ -248,3 +248,22 @@ def test_counts_whose_seen_bit_is_not_set(dtype, V):
     assert torch.equal(bits(out.cpu() + 0.0), bits(want.to(dtype) + 0.0))
     key, _, top = _rules.keys_of(want)
     assert torch.equal(keys.cpu(), torch.where(top == -INF, 0, key))
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+def test_an_infinite_frequency_penalty(dtype):
+    """It takes what was generated, on the path too, out of the choice, and nothing else: not what is only in the prompt, nor what is only biased."""
+    tb, tree, x, r, tok, paths = case(3, 29, 2, 1100, dtype, 300, 100, 0)
+    r["frequency"][:] = 0.0
+    want, _ = _rules.constrained(x, r, tok, paths, torch.float32)
+    generated = ((r["counts"].long() & 0x7fffffff) > 0)[:, None].repeat(1, tree.T, 1)
+    for b in range(2):
+        for i, p in enumerate(paths):
+            generated[b, i, tok[b, p].long()] = True
+    want = torch.where(generated, -INF, want)
+    r["frequency"][:] = INF
+    out, keys = torch.empty_like(x, device=DEV), torch.empty(2 * tree.T, dtype=torch.int64, device=DEV)
+    binding.logits_constrain(tree, x.to(DEV), out, on_device(r), tok.to(DEV))
+    binding.constrained_argmax_keys(tree, x.to(DEV), keys, on_device(r), tok.to(DEV))
+    assert torch.equal(bits(out.cpu() + 0.0), bits(want.to(dtype) + 0.0))
+    assert torch.equal(keys.cpu(), _rules.keys_of(want)[0])
