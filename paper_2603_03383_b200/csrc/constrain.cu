@@ -27,7 +27,7 @@ constexpr int CN_SLAB = 2048, CN_WORDS = CN_SLAB / 32, CN_PER = CN_WORDS / 32;
 constexpr int CN_ROWS = 32;          // most rows of a block
 constexpr int CN_PATH = MTV_MAX_K + 1;
 constexpr int CN_BLOCKS = 8;
-constexpr int CN_MAX_BIAS = 4096;
+constexpr int CN_MAX_BIAS = 4096;    // a power of two
 constexpr uint32_t CN_PROMPT = 0x80000000u;
 
 struct ConstrainParams {
@@ -111,6 +111,37 @@ struct Penalties {
     }
 };
 
+// n <= 32 words ascending, by one warp; n of them, with room for the next power of two, by the block: a bitonic sort.
+__device__ __forceinline__ void sort_warp(uint32_t *w, int n, int lane) {
+    uint32_t x = lane < n ? w[lane] : 0xffffffffu;
+#pragma unroll
+    for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+        for (int j = k / 2; j > 0; j /= 2) {
+            const uint32_t y = __shfl_xor_sync(0xffffffffu, x, j);
+            x = ((lane & j) == 0) == ((lane & k) == 0) ? min(x, y) : max(x, y);
+        }
+    if (lane < n) w[lane] = x;
+}
+__device__ __noinline__ void sort_block(uint32_t *w, int n, int tid) {
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += CN_THREADS) w[i] = 0xffffffffu;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int i = tid; i < size / 2; i += CN_THREADS) {
+                const int a = 2 * i - (i & (j - 1));
+                const uint32_t x = w[a], y = w[a + j];
+                if ((x > y) == ((a & k) == 0)) {
+                    w[a] = y;
+                    w[a + j] = x;
+                }
+            }
+            __syncthreads();
+        }
+}
+
 template <typename E, bool WRITE>
 __global__ void __launch_bounds__(CN_THREADS, 5)
 constrain_kernel(const ConstrainParams p) {
@@ -120,7 +151,7 @@ constrain_kernel(const ConstrainParams p) {
     __shared__ uint32_t list_count[CN_SLAB];
     __shared__ float list_bias[CN_SLAB];
     __shared__ uint16_t list_at[CN_SLAB];
-    __shared__ uint32_t match[CN_MAX_BIAS];      // the slab's entries of the bias list, in no order: place in the list << 16 | token
+    __shared__ uint32_t match[CN_MAX_BIAS];      // the slab's entries of the bias list: token << 16 | place in the list; sorted before they are used
     __shared__ int n_listed, n_match;
     __shared__ int32_t path[CN_ROWS][CN_PATH];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -176,7 +207,7 @@ constrain_kernel(const ConstrainParams p) {
         if (biased_at >= 0 && biased_at < n_tok) {
             atomicOr(&listed[biased_at / 32], 1u << (biased_at % 32));
             atomicOr(&biased[biased_at / 32], 1u << (biased_at % 32));
-            match[atomicAdd(&n_match, 1)] = (uint32_t)k << 16 | (uint32_t)biased_at;
+            match[atomicAdd(&n_match, 1)] = (uint32_t)biased_at << 16 | (uint32_t)k;
         }
     }
     if (p.n_bias) __syncthreads();
@@ -199,19 +230,35 @@ constrain_kernel(const ConstrainParams p) {
         }
         if (lane == 0) n_listed = start;
     }
+    if (warp == 1 && n_match > 1 && n_match <= 32) sort_warp(match, n_match, lane);
     __syncthreads();
+    if (n_match > 32) sort_block(match, n_match, tid);
     for (int e = tid; e < n_listed; e += CN_THREADS) {
         const int at = list_at[e], v = base + at;
         float sum = 0.f;
-        if (biased[at / 32] >> (at % 32) & 1)
-            for (int last = -1;;) {                         // a token that is named more than once: in the list's order
-                uint32_t found = 0xffffffffu;
-                for (int k = 0; k < n_match; ++k)
-                    if ((int)(match[k] & 0xffffu) == at && (int)(match[k] >> 16) > last) found = min(found, match[k]);
-                if (found == 0xffffffffu) break;
-                last = (int)(found >> 16);
-                sum = __fadd_rn(sum, p.bias[(size_t)b * p.n_bias + last]);
+        if (biased[at / 32] >> (at % 32) & 1) {             // its entries lie side by side, in the list's order
+            int lo = 0;
+            for (int hi = n_match; lo < hi;) {
+                const int mid = (lo + hi) / 2;
+                if (match[mid] < (uint32_t)at << 16) lo = mid + 1;
+                else hi = mid;
             }
+            bool more = true;
+            for (; more; lo += 8) {                         // (eight at a time, so that their loads do not wait for one another)
+                float x[8];
+                bool is[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t m = lo + k < n_match ? match[lo + k] : 0xffffffffu;
+                    is[k] = m >> 16 == (uint32_t)at;
+                    x[k] = is[k] ? p.bias[(size_t)b * p.n_bias + (m & 0xffffu)] : 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (is[k]) sum = __fadd_rn(sum, x[k]);
+                more = is[7];
+            }
+        }
         list_bias[e] = sum;
         // (a count whose bit in `seen` is 0 may be an earlier sequence's)
         list_count[e] = known[at / 32] >> (at % 32) & 1u && v < p.V ? p.counts[(size_t)b * p.V + v] : 0u;

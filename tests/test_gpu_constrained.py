@@ -267,3 +267,26 @@ def test_an_infinite_frequency_penalty(dtype):
     binding.constrained_argmax_keys(tree, x.to(DEV), keys, on_device(r), tok.to(DEV))
     assert torch.equal(bits(out.cpu() + 0.0), bits(want.to(dtype) + 0.0))
     assert torch.equal(keys.cpu(), _rules.keys_of(want)[0])
+
+
+@pytest.mark.parametrize("V", [300, 40000])
+def test_one_token_named_by_a_whole_bias_list(V):
+    """4096 entries of one token (a list padded with a valid id): their sum in the list's order, and no slower than a list of many tokens
+    by more than its loads.  Adding 4096 values one by one is a chain of some 100 thousand cycles, 60 us; a millisecond bounds a call."""
+    tb, tree, x, r, tok, paths = case(2, 6, 3, V, BF16, 50, 4096, 0)
+    r["bias"] *= 2.0 ** -6
+    r["bias_ids"][0] = 7
+    r["bias_ids"][1, ::2] = V - 1
+    r["bias_ids"][2, 64:] = 0
+    xd, rd, td = x.to(DEV), on_device(r), tok.to(DEV)
+    out, keys = torch.empty_like(xd), torch.empty(3 * tree.T, dtype=torch.int64, device=DEV)
+    want, _ = _rules.constrained(x, r, tok, paths, torch.float32)
+    for _ in range(2):
+        start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        binding.logits_constrain(tree, xd, out, rd, td)
+        binding.constrained_argmax_keys(tree, xd, keys, rd, td)
+        stop.record()
+    assert torch.equal(bits(out.cpu() + 0.0), bits(want.to(BF16) + 0.0))
+    assert torch.equal(keys.cpu(), _rules.keys_of(want)[0])
+    assert start.elapsed_time(stop) < 2.0
