@@ -14,8 +14,8 @@ __device__ __forceinline__ float ex2(float x) {
 }
 // 2^x for two values on the FMA pipes: x = j + f with j the nearest integer (read off the low mantissa bits of
 // x + 1.5 * 2^23) and f in [-0.5, 0.5]; 2^f by a cubic with the smallest largest relative error over that interval (7.5e-5, far
-// below the bf16 rounding of P); 2^j by an add to the exponent field.  x <= 127; it is clamped at -126 (the result then underflows
-// towards zero like ex2's).
+// below the bf16 rounding of P); 2^j by an add to the exponent field.  x <= 127; it is clamped at -126, and what the polynomial gives there,
+// q(0) 2^-126, is taken off: from there down the result is exactly 0, like ex2's, so that a hidden key's V row counts for nothing however large it is.
 __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     const float magic = 12582912.f;
     x.x = fmaxf(x.x, -126.f);
@@ -26,8 +26,9 @@ __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     float2 q = __ffma2_rn(make_float2(0.055171650f, 0.055171650f), f, make_float2(0.24261113f, 0.24261113f));
     q = __ffma2_rn(q, f, make_float2(0.69326097f, 0.69326097f));
     q = __ffma2_rn(q, f, make_float2(0.99992806f, 0.99992806f));
-    return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23)));
+    const float least = __int_as_float(__float_as_int(0.99992806f) - (126 << 23));
+    return __fadd2_rn(make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)),
+                                  __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23))), make_float2(-least, -least));
 }
 __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
     uint32_t r;

@@ -72,3 +72,26 @@ def test_scores_that_are_not_numbers(D, step, bad, row):
     hit = torch.zeros_like(out, dtype=torch.bool)
     hit[2, 1, :, 3 * G:4 * G] = True
     assert out[hit].isnan().all() and out[~hit].isfinite().all()
+
+
+@pytest.mark.parametrize("D,step", [(64, False), (128, False), (128, True)])
+def test_large_values_of_nodes_that_are_not_seen(D, step):
+    """The largest finite V rows in every leaf, the leaves in every column of a tile: they reach the leaves alone."""
+    tb, tree = make_tree("cartesian", 3, (4, 2, 2))
+    n, Hkv = tree.T, 2
+    mask = torch.tensor(tb["mask"], dtype=torch.bool)
+    leaf = mask.sum(0) == 1
+    for L in range(90, 106):
+        g = torch.Generator().manual_seed(L)
+        q = torch.randn(2, 1, n, Hkv * G, D, generator=g).to(torch.bfloat16)
+        ks, vs = ([torch.randn(1, Hkv, L + n + 5, D, generator=g).to(torch.bfloat16) for _ in range(2)] for _ in range(2))
+        lens = torch.tensor([L], dtype=torch.int32)
+        want = [ref.tree_attention(q[l], ks[l], vs[l], lens, tb["mask"]) for l in range(2)]
+        size = [ref.tree_attention(q[l], ks[l], vs[l].abs(), lens, tb["mask"]) for l in range(2)]
+        for v in vs:
+            v[:, :, L:L + n][:, :, leaf] = torch.finfo(torch.bfloat16).max
+        out = _run(tree, q.to(DEV), [k.to(DEV) for k in ks], [v.to(DEV) for v in vs], [L], Hkv, D, L + n + 5, step)
+        for l in range(2):
+            # the output's rounding, the weights' and, where a row's parts are joined, theirs; scores and exponentials 1e-4
+            most = 2.0 ** -8 * want[l].abs() + (2.1 * 2.0 ** -8 + 1e-4) * size[l]
+            assert ((out[l].cpu().double() - want[l]).abs() / most)[:, ~leaf].max().item() <= 1.0

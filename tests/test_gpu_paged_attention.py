@@ -331,3 +331,48 @@ def test_weights_in_two_terms(K, T, Hq, Hkv, D, page, shared, lens):
     most = EPS * want.abs() + (1 + EPS) * (2.0 ** -16 + 2 * 7.5e-5 + 1e-4) * absolute + 1e-30
     worst = ((out.double() - want).abs() / most).max().item()
     assert worst <= 1.0, worst
+
+
+@pytest.mark.parametrize("T", [3, 20, 64, 128])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_values_of_nodes_that_are_not_seen(D, T):
+    """The largest finite V rows in every leaf, the leaves in every column of a tile: they reach the leaves alone."""
+    tb, tree = _tree(4, T)
+    g = torch.Generator().manual_seed(17)
+    mask = torch.tensor(tb["mask"], dtype=torch.bool)
+    leaf = mask.sum(0) == 1                                # nobody else sees it
+    shared, page, Hkv, G = 64, 16, 2, 8
+    lens = [64 + i for i in range(16)] + [190 + 16 * i for i in range(8)]
+    t, n_pages = table(g, len(lens), max(lens) - shared + T, page, shared)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    q = torch.randn(len(lens), T, Hkv * G, D, generator=g).to(torch.bfloat16)
+    want, absolute = want_of(q, kp, vp, t, lens, tb["mask"])
+    for b, L in enumerate(lens):
+        for i in leaf.nonzero()[:, 0].tolist():
+            vp[int(t[b, (L + i) // page]), :, (L + i) % page] = torch.finfo(torch.bfloat16).max * (-1) ** (i + b)
+    out = run(tree, q, kp, vp, t, lens, shared)
+    assert ((out.double() - want).abs() / bound(want, absolute))[:, ~leaf].max().item() <= 1.0
+
+
+@pytest.mark.parametrize("T,G", [(1, 4), (20, 8), (64, 8)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_that_vanish(D, T, G):
+    """A visible key whose score is 300 below the others' (a weight of 2^-430) adds nothing, whatever its V row and its column."""
+    tb, tree = _tree(4, T)
+    g = torch.Generator().manual_seed(19)
+    shared, page, Hkv = 0, 16, 2
+    lens = [300 + i for i in range(16)]
+    t, n_pages = table(g, len(lens), max(lens) + T, page, shared)
+    kp, vp = pools(g, 2, n_pages, Hkv, page, D)
+    kp[..., 0] = 0
+    q = torch.randn(len(lens), T, Hkv * G, D, generator=g).to(torch.bfloat16)
+    q[..., 0] = 16.0
+    clean = vp.clone()
+    for b, L in enumerate(lens):
+        for s in (5 + b, 130 + b, L - 1):
+            pg, r = int(t[b, s // page]), s % page
+            kp[pg, :, r, 0] = -300.0 * D ** 0.5 / 16
+            clean[pg, :, r], vp[pg, :, r] = 0.0, torch.finfo(torch.bfloat16).max
+    want, absolute = want_of(q, kp, clean, t, lens, tb["mask"])
+    out = run(tree, q, kp, vp, t, lens, shared)
+    assert ((out.double() - want).abs() / bound(want, absolute)).max().item() <= 1.0
