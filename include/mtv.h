@@ -432,7 +432,8 @@ int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, in
 /* The same for runs of consecutive tokens (prompts, chunks of them, single tokens): rows row_starts[b] .. row_starts[b+1] - 1 of
  * q_layers, q_out_layers [n_layers][n_rows][Hq][D] and k_new_layers, v_new_layers [n_layers][n_rows][Hkv][D] belong to sequence b, the i-th
  * of them at slot and position seq_lens[b] + i.  row_starts: device [B+1], ascending; a sequence may have no rows.  Rows outside
- * [row_starts[0], row_starts[B]) are padding and left as they are.  n_rows may be 0.  seq_lens is not changed. */
+ * [row_starts[0], row_starts[B]) are padding and left as they are.  n_rows may be 0 (the rows' pointers
+ * may then be NULL).  seq_lens is not changed. */
 int kv_append_rope_paged(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
                          const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, mtv_bf16 *const *k_pools,
                          mtv_bf16 *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,

@@ -191,8 +191,9 @@ static int launch_append(AppendParams &p, cudaStream_t stream) {
 
 static int append_args(AppendParams &p, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q, mtv_bf16 *q_out, const mtv_bf16 *k_new,
                        const mtv_bf16 *v_new, mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool,
-                       const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta, int32_t *status) {
-    if (!q || !q_out || !k_new || !v_new || !k_pools || !v_pools || !seq_lens) return MTV_ERR_INVALID_ARG;
+                       const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta, int32_t *status, bool no_rows) {
+    if (!k_pools || !v_pools || !seq_lens) return MTV_ERR_INVALID_ARG;
+    if (!no_rows && (!q || !q_out || !k_new || !v_new)) return MTV_ERR_INVALID_ARG;
     if (B < 1 || Hq < 1 || Hkv < 1 || n_layers < 1 || !(rope_theta >= 0.f && rope_theta < INFINITY)) return MTV_ERR_INVALID_ARG;
     if ((D != 64 && D != 128) || n_layers > 65535 || Hq > PAGED_MAX_HEADS || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
     const int rc = paged_ref(p.pages, pool, page_table, max_pages, D);
@@ -309,7 +310,7 @@ extern "C" int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, 
     if (!tree || !tree->on_device) return MTV_ERR_INVALID_ARG;
     AppendParams p = {};
     const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, k_pools, v_pools, pool, page_table,
-                               max_pages, seq_lens, rope_theta, status);
+                               max_pages, seq_lens, rope_theta, status, false);
     if (rc != MTV_OK) return rc;
     if (B > (1 << 30) / tree->T) return MTV_ERR_UNSUPPORTED_SHAPE;
     p.T = tree->T;
@@ -328,7 +329,7 @@ extern "C" int kv_append_rope_paged(int B, int n_rows, int Hq, int Hkv, int D, i
     if (n_rows > 1 << 30) return MTV_ERR_UNSUPPORTED_SHAPE;
     AppendParams p = {};
     const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, k_pools, v_pools, pool, page_table,
-                               max_pages, seq_lens, rope_theta, status);
+                               max_pages, seq_lens, rope_theta, status, n_rows == 0);
     if (rc != MTV_OK) return rc;
     p.n_rows = n_rows;
     p.starts = row_starts;

@@ -284,3 +284,18 @@ def test_compaction_that_cannot_be(in_place):
     for pg, r, x in moved:
         k0[pg, :, r] = x
     assert torch.equal(kp[0].cpu(), k0)
+
+
+def test_no_rows_in_empty_tensors():
+    """Tensors without rows have no address: the call reports the lengths all the same."""
+    g = torch.Generator().manual_seed(8)
+    t, n_pages = table(g, 3, 32, 16)
+    kp, vp = (pools(g, 2, n_pages, 2, 16, 64, False, DEV) for _ in range(2))
+    before = [x.clone() for x in kp + vp]
+    q, k = torch.empty(2, 0, 4, 64, dtype=BF16, device=DEV), torch.empty(2, 0, 2, 64, dtype=BF16, device=DEV)
+    assert q.data_ptr() == 0
+    status = i32([5] * 3)
+    binding.kv_append_rope_paged(q, q, k, k, binding.cache_pointer_array(kp, DEV), binding.cache_pointer_array(vp, DEV), binding.pool_layout(kp[0]),
+                                 t.to(DEV), i32([0, 33, -1]), i32([0, 0, 0, 0]), status=status)
+    assert status.tolist() == [0, CAPACITY, CAPACITY]
+    assert all(torch.equal(x, y) for x, y in zip(before, kp + vp))

@@ -103,3 +103,12 @@ def test_layouts_that_the_wrappers_refuse():
     for p in (pool[..., ::2], pool.half(), pool[0]):
         with pytest.raises((binding.MtvError, AssertionError)):
             binding.pool_layout(p)
+
+
+def test_rows_without_an_address():
+    """Only a call without rows may leave their pointers out; what else it lacks is refused before a device is touched."""
+    none = dict(q=None, q_out=None, k=None, v=None)
+    assert rows(**none) == INVALID and rows(n_rows=1, **none) == INVALID
+    for kw in (dict(kp=None), dict(table=None), dict(lens=None), dict(starts=None), dict(B=0), dict(D=96), dict(theta=-1.0)):
+        assert rows(n_rows=0, **none, **kw) in (INVALID, SHAPE)
+        assert rows(n_rows=0, **kw) == rows(n_rows=0, **none, **kw)
