@@ -393,42 +393,99 @@ def mtv_verify_step_host(tree, dev: StepArgs, host: StepArgs, stream=None):
 
 
 # ------------------------------------------------------------------------------------- caches in pages
+# What these calls and those of the next section are given is looked at before its address goes over: a kernel that reads int64 as int32, or
+# past the end of a tensor, reports nothing.  A refusal names the argument.  (pysrc/tensors.cpp looks at all tensors of a call in one step; a set of
+# rules is looked at when it is made.)
+_BF16, _I32, _I64, _F32, _ANY, _OPTIONAL, _STRIDED, _LIKE_PREVIOUS = 0, 1, 2, 3, 4, 16, 32, 64
+_MAYBE_I32 = _I32 | _OPTIONAL
+_tensors = None
+
+
+def _refuse(where, name):
+    raise MtvError(-1, "%s: %s" % (where, name))
+
+
+def _look(where, names, *args):
+    """args: (tensor, kind, elements at least) one after another, see pysrc/tensors.cpp -> (device, address, address, ...)."""
+    global _tensors
+    if _tensors is None:
+        from . import _tensors as loaded        # (missing: run build.py)
+        _tensors = loaded
+    found = _tensors.addresses(*args)
+    if type(found) is int:
+        _refuse(where, names[found])
+    # the library launches on the current device
+    if found[0] < 0 or found[0] != torch._C._cuda_getDevice():
+        _refuse(where, "tensors that are not on the current CUDA device")
+    return found
+
+
 def pool_layout(pool: torch.Tensor) -> PoolLayout:
     """Layout of a pool tensor [n_pages][Hkv][page_size][D] of any strides with the columns innermost (a pool whose pages hold
     [page_size][Hkv][D] is passed as its transposed view)."""
-    assert pool.dim() == 4 and pool.stride(3) == 1 and pool.dtype == torch.bfloat16
+    if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype is not torch.bfloat16:
+        _refuse("pool_layout", "pool")
     sp, sh, st = pool.stride()[:3]
     return PoolLayout(sp, sh, st, pool.shape[2], pool.shape[0])
+
+
+_APPEND = ("q_layers", "q_out_layers", "k_new_layers", "v_new_layers", "k_ptrs", "v_ptrs", "page_table", "seq_lens", "status", "row_starts")
 
 
 def tree_kv_append_rope_paged(tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table,
                               seq_lens, rope_theta=0.0, status=None, stream=None):
     """q_layers, q_out_layers [n_layers][B][T][Hq][D], k_new_layers / v_new_layers [n_layers][B][T][Hkv][D]; k_ptrs / v_ptrs: device
     arrays of the layers' pools (cache_pointer_array); page_table [B][max_pages]."""
-    n_layers, B, T, Hq, D = q_layers.shape
-    _check(lib().tree_kv_append_rope_paged(tree.handle, B, Hq, k_new_layers.shape[3], D, n_layers, _ptr(q_layers), _ptr(q_out_layers),
-                                           _ptr(k_new_layers), _ptr(v_new_layers), _ptr(k_ptrs), _ptr(v_ptrs), pool,
-                                           _ptr(page_table), page_table.shape[1], _ptr(seq_lens), rope_theta, _ptr(status),
-                                           _stream(stream)), "tree_kv_append_rope_paged")
+    where, shape = "tree_kv_append_rope_paged", q_layers.shape
+    if len(shape) != 5 or shape[2] != tree.T:
+        _refuse(where, "q_layers")
+    n_layers, B, T, Hq, D = shape
+    if k_new_layers.dim() != 5 or page_table.dim() != 2:
+        _refuse(where, "k_new_layers" if page_table.dim() == 2 else "page_table")
+    Hkv, max_pages = k_new_layers.shape[3], page_table.shape[1]
+    if k_new_layers.shape != (n_layers, B, T, Hkv, D):
+        _refuse(where, "k_new_layers")
+    rows = n_layers * B * T * D
+    _, q, q_out, k, v, kp, vp, table, lens, st = _look(
+        where, _APPEND, q_layers, _BF16, rows * Hq, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
+        v_new_layers, _BF16 | _LIKE_PREVIOUS, -1, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, B * max_pages, seq_lens, _I32, B,
+        status, _MAYBE_I32, B)
+    _check(lib().tree_kv_append_rope_paged(tree.handle, B, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, rope_theta, st,
+                                           _stream(stream)), where)
 
 
 def kv_append_rope_paged(q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table, seq_lens,
                          row_starts, rope_theta=0.0, status=None, stream=None):
     """q_layers, q_out_layers [n_layers][n_rows][Hq][D], k_new_layers / v_new_layers [n_layers][n_rows][Hkv][D]; row_starts [B+1]."""
-    n_layers, n_rows, Hq, D = q_layers.shape
-    _check(lib().kv_append_rope_paged(page_table.shape[0], n_rows, Hq, k_new_layers.shape[2], D, n_layers, _ptr(q_layers), _ptr(q_out_layers),
-                                      _ptr(k_new_layers), _ptr(v_new_layers), _ptr(k_ptrs), _ptr(v_ptrs), pool,
-                                      _ptr(page_table), page_table.shape[1], _ptr(seq_lens), _ptr(row_starts), rope_theta,
-                                      _ptr(status), _stream(stream)), "kv_append_rope_paged")
+    where = "kv_append_rope_paged"
+    for t, dim, name in ((q_layers, 4, "q_layers"), (k_new_layers, 4, "k_new_layers"), (page_table, 2, "page_table")):
+        if t.dim() != dim:
+            _refuse(where, name)
+    (n_layers, n_rows, Hq, D), (B, max_pages), Hkv = q_layers.shape, page_table.shape, k_new_layers.shape[2]
+    if k_new_layers.shape != (n_layers, n_rows, Hkv, D):
+        _refuse(where, "k_new_layers")
+    _, q, q_out, k, v, kp, vp, table, lens, st, starts = _look(
+        where, _APPEND, q_layers, _BF16, -1, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1, v_new_layers, _BF16 | _LIKE_PREVIOUS, -1,
+        k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B, status, _MAYBE_I32, B, row_starts, _I32, B + 1)
+    _check(lib().kv_append_rope_paged(B, n_rows, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, starts, rope_theta, st,
+                                      _stream(stream)), where)
+
+
+_COMPACT = ("k_ptrs", "v_ptrs", "page_table", "seq_lens", "new_lens", "accept_len", "acc_nodes", "status")
 
 
 def kv_compact_accepted_paged(tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool: PoolLayout, page_table, seq_lens, new_lens, accept_len,
                               acc_nodes, status=None, stream=None):
-    """new_lens may be seq_lens itself."""
+    """new_lens may be seq_lens itself; accept_len [B], acc_nodes [B][K + 1]."""
+    where = "kv_compact_accepted_paged"
+    if page_table.dim() != 2:
+        _refuse(where, "page_table")
     B, max_pages = page_table.shape
-    _check(lib().kv_compact_accepted_paged(tree.handle, B, Hkv, D, n_layers, _ptr(k_ptrs), _ptr(v_ptrs), pool,
-                                           _ptr(page_table), max_pages, _ptr(seq_lens), _ptr(new_lens), _ptr(accept_len),
-                                           _ptr(acc_nodes), _ptr(status), _stream(stream)), "kv_compact_accepted_paged")
+    _, kp, vp, table, lens, new, n, nodes, st = _look(
+        where, _COMPACT, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B, new_lens, _I32, B, accept_len, _I32, B,
+        acc_nodes, _I32, B * (tree.K + 1), status, _MAYBE_I32, B)
+    _check(lib().kv_compact_accepted_paged(tree.handle, B, Hkv, D, n_layers, kp, vp, pool, table, max_pages, lens, new, n, nodes, st, _stream(stream)),
+           where)
 
 
 def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
@@ -436,16 +493,28 @@ def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
     return lib().tree_attention_paged_workspace_bytes(tree.handle, B, Hq, Hkv, D, shared_len)
 
 
+_ATTENTION = ("q", "out", "k_pool", "v_pool", "page_table", "seq_lens", "status", "ws")
+
+
 def tree_verify_attention_paged(tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len=0, scale=0.0, status=None,
                                 stream=None):
     """q, out [B][T][Hq][D]; k_pool, v_pool [n_pages][Hkv][page_size][D] (see pool_layout), the same strides."""
-    B, T, Hq, D = q.shape
-    pool = pool_layout(k_pool)
-    assert v_pool.shape == k_pool.shape and v_pool.stride() == k_pool.stride()
-    _check(lib().tree_verify_attention_paged(tree.handle, B, Hq, k_pool.shape[1], D, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
-                                             pool, page_table.data_ptr(), page_table.shape[1], shared_len,
-                                             seq_lens.data_ptr(), scale, out.data_ptr(), _ptr(status), ws.data_ptr(), ws.nbytes,
-                                             _stream(stream)), "tree_verify_attention_paged")
+    where, shape, pools, strides = "tree_verify_attention_paged", q.shape, k_pool.shape, k_pool.stride()
+    if len(shape) != 4 or shape[1] != tree.T:
+        _refuse(where, "q")
+    B, T, Hq, D = shape
+    if len(pools) != 4 or pools[3] != D or strides[3] != 1:
+        _refuse(where, "k_pool")
+    if v_pool.stride() != strides:
+        _refuse(where, "v_pool")
+    if page_table.dim() != 2:
+        _refuse(where, "page_table")
+    max_pages = page_table.shape[1]
+    _, q_at, out_at, k, v, table, lens, st, ws_at = _look(
+        where, _ATTENTION, q, _BF16, -1, out, _BF16 | _LIKE_PREVIOUS, -1, k_pool, _BF16 | _STRIDED, -1, v_pool, _BF16 | _STRIDED | _LIKE_PREVIOUS, -1,
+        page_table, _I32, B * max_pages, seq_lens, _I32, B, status, _MAYBE_I32, B, ws, _ANY, -1)
+    _check(lib().tree_verify_attention_paged(tree.handle, B, Hq, pools[1], D, q_at, k, v, PoolLayout(strides[0], strides[1], strides[2], pools[2], pools[0]),
+                                             table, max_pages, shared_len, lens, scale, out_at, st, ws_at, ws.nbytes, _stream(stream)), where)
 
 
 # ------------------------------------------------------------------------------------- constrained decoding
@@ -453,10 +522,32 @@ def logit_rules(counts=None, seen=None, repetition=None, presence=None, frequenc
                 mask_of=None) -> LogitRules:
     """counts [B][V], seen [B][words], repetition / presence / frequency [B] fp32, bias_ids / bias [B][n], mask [n_masks][words],
     mask_of [B][T]; words of 32 tokens in int32 storage (see include/mtv.h).  The tensors have to outlive the rules' use."""
-    r = LogitRules(*[_ptr(t) for t in (counts, seen, repetition, presence, frequency, bias_ids, bias, mask, mask_of)])
+    tensors = (counts, seen, repetition, presence, frequency, bias_ids, bias, mask, mask_of)
+    names = [n for n, _ in LogitRules._fields_]
+    i32, f32 = (torch.int32, torch.uint32), (torch.float32,)
+    # what the rules ask of a call: at most B sequences, V tokens in W words, T nodes, one device
+    asks, devs = {}, set()
+    for t, name, types, dims in zip(tensors, names, (i32, i32, f32, f32, f32, i32, f32, i32, i32), ("BV", "BW", "B", "B", "B", "Bn", "Bn", "mW", "BT")):
+        if t is None:
+            continue
+        if t.dtype not in types or t.dim() != len(dims) or not t.is_contiguous():
+            _refuse("logit_rules", name)
+        for d, size in zip(dims, t.shape):
+            if asks.setdefault(d, size) != size and d != "B":
+                _refuse("logit_rules", name)
+            asks[d] = min(asks[d], size)
+        devs.add(t.get_device())
+    if (bias_ids is None) != (bias is None):
+        _refuse("logit_rules", "bias_ids" if bias_ids is None else "bias")
+    if "V" in asks and asks.get("W", (asks["V"] + 31) // 32) != (asks["V"] + 31) // 32:
+        _refuse("logit_rules", "mask" if seen is None else "seen")
+    if len(devs) > 1:
+        _refuse("logit_rules", "tensors of several devices")
+    r = LogitRules(*[_ptr(t) for t in tensors])
     r.n_bias = 0 if bias_ids is None else bias_ids.shape[-1]
     r.n_masks = 0 if mask is None else mask.shape[0]
-    r.tensors = (counts, seen, repetition, presence, frequency, bias_ids, bias, mask, mask_of)
+    r.tensors = tensors
+    r.asks = tuple(asks.get(d) for d in "BVWT") + (devs.pop() if devs else None,)
     return r
 
 
@@ -465,6 +556,8 @@ _LOGIT_TYPES = {torch.bfloat16: 0, torch.float32: 1}
 
 def _logit_rows(x, where):
     """(type, row stride) of logits [B][T][V] with rows at even distances; anything else is refused."""
+    if x.dim() != 3:
+        raise MtvError(-1, where)
     B, T, V = x.shape
     sb, st, sv = x.stride()
     if (V > 1 and sv != 1) or (B > 1 and T > 1 and sb != T * st) or x.dtype not in _LOGIT_TYPES:
@@ -472,30 +565,48 @@ def _logit_rows(x, where):
     return _LOGIT_TYPES[x.dtype], st if T > 1 else sb if B > 1 else V
 
 
+def _constrained_rows(tree, logits, rules, where):
+    """(B, V, type, row stride) of a constrained call; rules of other sizes or of another device are refused."""
+    dtype, stride = _logit_rows(logits, where)
+    B, T, V = logits.shape
+    if T != tree.T:
+        _refuse(where, "logits")
+    b, v, w, t, device = getattr(rules, "asks", (None,) * 5)
+    if ((b is not None and b < B) or (v is not None and v != V) or (w is not None and w != (V + 31) // 32) or (t is not None and t != T) or
+            (device is not None and device != logits.get_device())):
+        _refuse(where, "rules")
+    return B, V, dtype, stride
+
+
 def logits_constrain(tree, logits, out, rules: LogitRules, tree_tok=None, stream=None):
     """logits, out [B][T][V], bf16 or fp32, rows evenly spaced; out may be logits."""
-    B, T, V = logits.shape
-    dtype, stride = _logit_rows(logits, "logits_constrain")
-    dtype_out, stride_out = _logit_rows(out, "logits_constrain")
-    if out.shape != logits.shape or dtype_out != dtype:
-        raise MtvError(-1, "logits_constrain")
-    _check(lib().logits_constrain(tree.handle, B, V, dtype, _ptr(logits), stride, _ptr(out), stride_out, rules, _ptr(tree_tok),
-                                  _stream(stream)), "logits_constrain")
+    where = "logits_constrain"
+    B, V, dtype, stride = _constrained_rows(tree, logits, rules, where)
+    dtype_out, stride_out = _logit_rows(out, where)
+    kind = _F32 if dtype else _BF16
+    _, x, y, tok = _look(where, ("logits", "out", "tree_tok"), logits, kind | _STRIDED, -1, out, kind | _STRIDED | _LIKE_PREVIOUS, -1,
+                         tree_tok, _MAYBE_I32, B * tree.T)
+    _check(lib().logits_constrain(tree.handle, B, V, dtype, x, stride, y, stride_out, rules, tok, _stream(stream)), where)
 
 
 def constrained_argmax_keys(tree, logits, keys, rules: LogitRules, tree_tok=None, stream=None):
     """logits [B][T][V], bf16 or fp32, rows evenly spaced -> keys [B*T] (int64 storage of the uint64 keys)."""
-    B, T, V = logits.shape
-    dtype, stride = _logit_rows(logits, "constrained_argmax_keys")
-    _check(lib().constrained_argmax_keys(tree.handle, B, V, dtype, _ptr(logits), stride, rules, _ptr(tree_tok), _ptr(keys),
-                                         _stream(stream)), "constrained_argmax_keys")
+    where = "constrained_argmax_keys"
+    B, V, dtype, stride = _constrained_rows(tree, logits, rules, where)
+    _, x, tok, keys_at = _look(where, ("logits", "tree_tok", "keys"), logits, (_F32 if dtype else _BF16) | _STRIDED, -1,
+                               tree_tok, _MAYBE_I32, B * tree.T, keys, _I64, B * tree.T)
+    _check(lib().constrained_argmax_keys(tree.handle, B, V, dtype, x, stride, rules, tok, keys_at, _stream(stream)), where)
 
 
 def token_counts_add(tokens, counts, seen, lens=None, prompt=False, stream=None):
     """tokens [B][n] -> counts [B][V], seen [B][words]."""
-    B, n = tokens.shape
-    _check(lib().token_counts_add(B, counts.shape[1], n, _ptr(tokens), _ptr(lens), 1 if prompt else 0, _ptr(counts), _ptr(seen),
-                                  _stream(stream)), "token_counts_add")
+    where = "token_counts_add"
+    if tokens.dim() != 2 or counts.dim() != 2:
+        _refuse(where, "tokens" if tokens.dim() != 2 else "counts")
+    (B, n), V = tokens.shape, counts.shape[1]
+    _, tok, ls, c, s = _look(where, ("tokens", "lens", "counts", "seen"), tokens, _I32, -1, lens, _MAYBE_I32, B, counts, _I32, B * V,
+                             seen, _I32, B * ((V + 31) // 32))
+    _check(lib().token_counts_add(B, V, n, tok, ls, 1 if prompt else 0, c, s, _stream(stream)), where)
 
 
 KERNELS = ["heads_resblock", "heads_vocab_topk", "heads_merge", "attn_partial", "attn_combine",
