@@ -453,9 +453,9 @@ int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int
  * are joined.  shared_len: a multiple of page_size (0: nothing is shared), at most every seq_lens[b]
  * and max_pages * page_size.
  * A tree of its root alone is plain decoding of one token per sequence.
- * Same formula and types as tree_verify_attention, weights rounded as there: to two bf16 terms (2^-16 of a weight) at D = 64, and at either head size
- * where a KV head has at most 16 query rows; else to one (2^-8) at D = 128, whatever the length.  An infinity in V that a node sees makes its output
- * infinite or NaN.  scale == 0 means 1/sqrt(D); scales that are negative, NaN or above 1e30 are
+ * Same formula and types as tree_verify_attention.  Weights are rounded to two bf16 terms (2^-16 of a weight) at D = 64, as there, and at either head size
+ * where a KV head has at most 16 query rows; else, at D = 128, to one (2^-8), where tree_verify_attention has a second one for some of the keys in some
+ * calls.  An infinity in V that a node sees makes its output infinite or NaN.  scale == 0 means 1/sqrt(D); scales that are negative, NaN or above 1e30 are
  * refused (MTV_ERR_INVALID_ARG).
  * q, out [B][T][Hq][D] contiguous, 16-byte aligned, not overlapping.  B <= 1024, Hq * B * T <= 2^28; MTV_ERR_UNSUPPORTED_SHAPE also where
  * shared_len and B * max_pages * page_size, taken for every tile of 128 query rows, pass what 32 bits count (some 10^10 keys).  status[b] = MTV_ERR_CAPACITY also if seq_lens[b] < shared_len; out of such

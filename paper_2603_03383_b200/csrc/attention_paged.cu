@@ -30,10 +30,11 @@
 // tile forms no maximum; a vote of the two threads of a row says that neither needs the reference moved, and only otherwise they take
 // the scores again, exchange their maxima (through tensor memory) and rescale O.
 //
-// Measured, whole calls: trees of 64 nodes of 8 sequences, 32 / 8 heads of 128, 16384 shared keys and up to 2048 of their own (136 GFLOP in
-// tiles): 153 us, 164 alone under a profiler with the tensor pipe at 50 %: a pair of key tiles takes some 3.9 k cycles of the 2.05 k that its
+// Measured, whole calls: trees of 64 nodes of 8 sequences, 32 / 8 heads of 128, 16384 shared keys and up to 2048 of their own (147 GFLOP):
+// 178 us (one card of several took 153), the tensor pipe at 50 %: a pair of key tiles takes some 3.9 k cycles of the 2.05 k that its
 // products need; the rest is the chain scores -> exponentials -> weights -> product of each row tile, which its one other row tile does not hide.
-// 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 34.6 us for 6.3 us of bytes; start, first tile and joining are two thirds of it.
+// 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 33 to 37 us for 6.4 us of bytes; start, first tile and joining are two thirds of it.
+// All 20 warps have 96 registers; the softmax warps spill (160 bytes stored, 204 loaded a thread at D = 128, 144 and 244 at D = 64).
 #include "attn_common.cuh"
 #include "paged_common.cuh"
 #include "paged_plan.cuh"
@@ -50,12 +51,12 @@ constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
 // .0023 with it, .00166 without).  As in tree_verify_attention, head size 64 has a second bf16 term, what the rounding of the first left, in every tile
 // (three trees of 128 nodes, 16 / 2 heads of 64, 4096 shared keys: 31.2 us without, 35.3 with), and so have thin items, whose products cost nothing beside
 // their bytes.  At head size 128 a row tile has one term (its products are a third of the time there: 16384 shared keys 179 us, 238 with two in every tile,
-// 192 in four of a piece; one-layer calls of tree_verify_attention are at .0027).
+// 192 in four of a piece; one-layer calls of tree_verify_attention are at .0027, short ones at .0017).
 template <int D> constexpr bool TWO_TERMS = D == 64;
 constexpr int TILE_COST = 4;              // a key tile on a line
 __host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }   // what the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles
 __host__ __device__ constexpr int PHASE_COST(int single) { return single ? 4 : 7; }   // and what a quarter of a key tile takes a CTA, one against the other: pairs are bound by the tensor core and
-                                          // its waits (3.9 k cycles a key tile at D = 128), single row tiles by their K and V (2.2 k, two at a time)
+                                          // its waits (3.9 k cycles a key tile at D = 128), single row tiles by their K and V (2.2 k, two at a time); measured at D = 128, taken at D = 64 too
 
 template <int D> struct PaSmem {
     static constexpr int HALVES = D / 64;
@@ -821,8 +822,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 // bytes of a V row as its column in 16 products, two keys' values side by side by a byte permutation.
 // A CTA of four warps walks a run of the line of all thin items, 16 keys to a warp at a time; while a warp computes on 16 keys, V of them and K
 // of its next ones are on the way (8 KB a warp, two CTAs to an SM).  At a piece's end the warps join in shared memory.
-// Measured: 64 single tokens, 8 KV heads of 128, 100 to 1000 keys each: 149 MB in 37 us = 4.0 TB/s.  Bound by the bytes in flight, 64 KB an SM;
-// 221 registers a thread leave no third CTA (with spills: 89 us instead of 61 in one comparison), and more or shorter pieces change nothing (62, 60).
+// Measured: 64 single tokens, 8 KV heads of 128, 100 to 1000 keys each: 149 MB in 37 us = 4.0 TB/s.  Bound by the bytes in flight, 64 KB an SM
+// (V of a block is requested in the iteration that uses it, only K is ahead); 218 registers a thread leave no third CTA (with spills: 89 us instead of 61 in one comparison), and more or shorter pieces change nothing (62, 60).
 constexpr int TH_WARPS = 4, TH_KEYS = 16, TH_STEP = TH_WARPS * TH_KEYS;
 constexpr int TH_ENDS = 3;                // what an item's start and end take, in steps of 64 keys
 
@@ -1258,8 +1259,8 @@ static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtens
     if (thin.prefix_items + thin.seq_items)
         MTV_CUDA_CHECK(launch_dependent(paged_attn_thin_kernel<D>, dim3(2 * sm_count()), TH_WARPS * 32, 0, stream, p));
     const int64_t rows = (int64_t)p.B * p.Hkv * p.T * p.G;
-    // Fewer blocks than SMs with a thread per row and chunk (decoding: few rows, each of many pieces): four threads share one.  Whole calls, D = 128: 2048 rows
-    // (128 blocks) 77 us so and 86 with one thread; 5684 rows (356 blocks) 37.9 and 34.6; 16384 rows 167 and 153.
+    // Fewer blocks than SMs with a thread per row and chunk (decoding: few rows, each of many pieces): four threads share one.  Whole calls on one card, D = 128
+    // (D = 64 goes by the same rule, not measured): 2048 rows (128 blocks) 77 us so and 86 with one thread; 5684 rows (356 blocks) 37.9 and 34.6; 16384 rows 167 and 153.
     constexpr int PER = 256 / (D / 8);
     if (rows < (int64_t)PER * sm_count())
         MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 4>, dim3((unsigned)((rows + PER / 4 - 1) / (PER / 4))), 256, 0, stream, p));

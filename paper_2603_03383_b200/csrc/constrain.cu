@@ -11,9 +11,12 @@
 // tokens; then a warp per row makes a dense pass over the allowed tokens that are in no list (16-byte loads, masks laid over whole
 // vectors, packed maxima or copies) and a sparse one over the list.  Rows may begin at any element: vectors are cut at the addresses' 16-byte
 // boundaries, and the two that a slab shares with its neighbours are taken element by element.
-// Measured: argmax of 8 x 64 rows of 131072 bf16 logits, 64 masks, 4000 tokens of text a sequence, with the acceptance 47 us (134 MB: 20.5 us at the
-// memory's rate); written, 5 x 64 rows of 50003: 24 us (9.8).  Bound by instructions and their latency: about 900 a warp for a row's slab at
-// 0.63 an instruction a cycle and scheduler, a third of them the list's (a division each, on lanes that the list only partly fills).  Blocks of 8 rows cost
+// A slab's entries of the bias list are sorted by token and place, so that a token's entries are summed in the list's order in one go: up to 32 by a warp
+// beside the listing, more by the block (4096 entries of one token, 4 x 64 rows of 40000: 0.18 ms; of 2000 tokens in one slab: 0.07).
+// Measured: argmax of 8 x 64 rows of 131072 bf16 logits, 64 masks, 4000 tokens of text a sequence, with the acceptance 49 us (134 MB: 21 us at the
+// memory's rate); written, 5 x 64 rows of 50003: 25 us (9.9).  Bound by instructions and their latency: about 950 a warp for a row's slab at
+// 0.63 an instruction a cycle and scheduler, a third of them the list's (a division each, on lanes that the list only partly fills; it is gone through for
+// every row, though few listed tokens can be the maximum); written, 1000 blocks on 740 places are 1.35 waves, and the kernel spills (40 bytes a thread).  Blocks of 8 rows cost
 // 8 us more (every block lists anew, three loads deep), of 32 rows 8 us (the last wave is short); five blocks per SM rather than the four that
 // the compiler's choice of registers leaves: 66 -> 47; rows staged in shared memory by asynchronous copies: 75, as two blocks fit then.
 #include <cuda_bf16.h>

@@ -66,8 +66,8 @@ template <bool VEC> __device__ __forceinline__ void store8(__nv_bfloat16 *p, con
 // some layers, works their angles out once (in double precision as far as the reduction to one turn goes: positions reach tens of
 // thousands of radians; the sine and cosine of what is left in fp32), and moves 16-byte chunks.  The first of them are requested before
 // anything else: lengths, pages and angles are worked out meanwhile.  The blocks behind the rows' own report one sequence per warp.
-// Measured: trees of 4 x 64 nodes, 32 + 2 x 8 heads of 128, 32 layers: 35.6 us (201 MB, 5.6 TB/s; 30.8 at the memory's rate); five prompts of
-// 3005 tokens, 28 + 2 x 4 heads, one layer: 13.4 us (8.5): there the chain length, page, angle, row of the last wave of blocks.  Two rows a block: four
+// Measured: trees of 4 x 64 nodes, 32 + 2 x 8 heads of 128, 32 layers: 35.7 us (201 MB, 5.6 TB/s; 31.1 at the memory's rate); five prompts of
+// 3005 tokens, 28 + 2 x 4 heads, one layer: 13.5 us (8.6): 1503 blocks are 1.7 waves, and each begins with the chain length, page, angle.  Two rows a block: four
 // take 34.9 and 15.4, one 36.5 and 17.4; two pairs in flight per thread 34.8 and 14.9, as fewer blocks fit.
 // VEC: the rows begin at multiples of 16 bytes.
 template <int D, bool VEC>
