@@ -116,7 +116,7 @@ def test_attention(tree):
     for name, good in attend_args().items():
         for bad in wrong(name, good):
             if name == "ws" and bad.is_contiguous() or name == "page_table" and bad.is_contiguous() and bad.dtype is I32:
-                continue                                    # (its size is the library's to judge)
+                continue                                    # (the library looks at its size)
             if name == "q" and bad.dtype is BF16 and bad.shape[-1] < D:
                 continue
             assert any(n in refused(call, dict(attend_args(), **{name: bad})) for n in ([name, "v_pool"] if name == "k_pool" else [name])), (name, bad.dtype)
