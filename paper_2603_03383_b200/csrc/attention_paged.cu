@@ -35,17 +35,12 @@
 // products need; the rest is the chain scores -> exponentials -> weights -> product of each row tile, which its one other row tile does not hide.
 // 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 33 to 37 us for 6.4 us of bytes; start, first tile and joining are two thirds of it.
 // All 20 warps have 96 registers; the softmax warps spill (160 bytes stored, 204 loaded a thread at D = 128, 144 and 244 at D = 64).
-#include "attn_common.cuh"
-#include "paged_common.cuh"
-#include "paged_plan.cuh"
+#include "paged_attn.cuh"
 
 namespace mtv {
 
 constexpr int PA_THREADS = 640;
 constexpr int PA_MMA_WARP = 16, PA_TMA_WARP = 18, PA_CLEAN_WARP = 19;
-constexpr int PA_QUEUE = 4;               // pieces that are handed out and may not have been taken by all
-constexpr int PA_KEYS = 128;              // keys of a tile
-constexpr int PA_MAX_B = 1024;
 constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
 // P goes to the second product as bf16, whose rounding is the largest error beside the output's own (relative 2-norm against 64 bits, N(0, 1) inputs:
 // .0023 with it, .00166 without).  As in tree_verify_attention, head size 64 has a second bf16 term, what the rounding of the first left, in every tile
@@ -53,8 +48,6 @@ constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
 // their bytes.  At head size 128 a row tile has one term (its products are a third of the time there: 16384 shared keys 179 us, 238 with two in every tile,
 // 192 in four of a piece; one-layer calls of tree_verify_attention are at .0027, short ones at .0017).
 template <int D> constexpr bool TWO_TERMS = D == 64;
-constexpr int TILE_COST = 4;              // a key tile on a line
-__host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }   // what the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles
 __host__ __device__ constexpr int PHASE_COST(int single) { return single ? 4 : 7; }   // and what a quarter of a key tile takes a CTA, one against the other: pairs are bound by the tensor core and
                                           // its waits (3.9 k cycles a key tile at D = 128), single row tiles by their K and V (2.2 k, two at a time); measured at D = 128, taken at D = 64 too
 
@@ -80,210 +73,6 @@ enum {
 constexpr uint32_t PA_OFF_MISC = PB_COUNT * 8, PA_OFF_QUEUE = (PA_OFF_MISC + 40 + 15) / 16 * 16;
 static_assert(PA_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1024, "barrier region");
 
-struct PaParams {
-    PagedRef pages;
-    PaPhase phase[3];                  // pairs of row tiles, single row tiles, thin ones
-    const int32_t *seq_lens;
-    const uint64_t *anc;               // [T][2]
-    const __nv_bfloat16 *q, *k, *v;
-    __nv_bfloat16 *out;
-    int32_t *status, *dev_error;
-    float scale_log2;
-    int B, T, G, Hq, Hkv, shared, npc, page_rows;
-};
-
-// ---------------------------------------------------------------------------------------- the division of the work
-__device__ __forceinline__ int key_tiles(int keys) { return (keys + PA_KEYS - 1) / PA_KEYS; }
-__device__ __forceinline__ int item_cost(int tiles, int ends) { return tiles ? tiles * TILE_COST + ends : 0; }
-// own key tiles of a sequence; 0: it is left out
-__device__ __forceinline__ int seq_tiles(const PaParams &p, int L) {
-    return p.pages.fits(L, p.T) && L >= p.shared ? key_tiles(L - p.shared + p.T) : 0;
-}
-// tiles of an item in front of position y of its stretch of the line
-__device__ __forceinline__ int cut_at(int y, int tiles, int ends) { return y <= ends ? 0 : min((y - ends + TILE_COST / 2) / TILE_COST, tiles); }
-
-struct __align__(16) PaPiece {
-    int b;              // -1: the prefix
-    int g, tile0;       // KV head, first row tile
-    int t0, t1;         // key tiles; t1 = 0: no more pieces
-    int L;              // keys in front of the tree, without the shared ones (prefix: the shared ones)
-    int slot;
-    int whole;          // the item's only piece
-};
-static_assert(sizeof(PaPiece) == 32, "two 16-byte words");
-// The tile needs more than its copy: it holds rows of the tree, or rows behind them.
-__device__ __forceinline__ bool is_last(const PaPiece &s, int t) { return s.b >= 0 && (t + 1) * PA_KEYS > s.L; }
-
-// A worker's run of a phase's line (lines are shorter than 2^31: checked by the host).
-struct PaWalk {
-    int x0, x1, S;      // the run, and the position of the next item
-    int b, idx, tiles, L, worker, ends;
-    __device__ __forceinline__ void load(const PaParams &p) {
-        if (b < 0) {
-            L = p.shared;
-            tiles = key_tiles(L);
-        } else {
-            const int len = p.seq_lens[b];
-            tiles = seq_tiles(p, len);
-            L = len - p.shared;
-        }
-    }
-    __device__ __forceinline__ bool next(const PaParams &p, const PaPhase &f, PaPiece &s) {
-        while (S < x1) {
-            if (idx >= (b < 0 ? f.prefix_items : f.seq_items) || tiles == 0) {
-                if (++b >= p.B) return false;
-                idx = 0;
-                load(p);
-                continue;
-            }
-            s.t0 = cut_at(x0 - S, tiles, ends);
-            s.t1 = cut_at(x1 - S, tiles, ends);
-            S += item_cost(tiles, ends);
-            const int i = idx++;
-            if (s.t0 >= s.t1) continue;
-            const int per = b < 0 ? f.prefix_per_head : f.seq_per_head, item = b < 0 ? i : f.prefix_items + b * f.seq_items + i;
-            s.b = b; s.L = L;
-            s.g = i / per;
-            s.tile0 = (b < 0 ? f.prefix_tile0 : f.seq_tile0) + 2 * (i - s.g * per);
-            s.slot = item + worker;
-            s.whole = s.t0 == 0 && s.t1 == tiles;
-            if (threadIdx.x % 32 == 0) {
-                if (s.t0 == 0) f.span[item].x = worker;
-                if (s.t1 == tiles) f.span[item].y = worker;
-            }
-            return true;
-        }
-        return false;
-    }
-};
-// The runs of the workers of a CTA (pairs; single tiles of its halves) and the items they begin in.  One warp.
-__device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], int cta, int n_cta, int lane) {
-    auto tiles_of = [&](int b) { return b < p.B ? seq_tiles(p, p.seq_lens[b]) : 0; };
-    const int own0 = tiles_of(lane);
-    int tiles = own0, seqs = own0 > 0;   // key tiles of an item of every sequence that is not left out, and their number
-    for (int b0 = 32; b0 < p.B; b0 += 32) {
-        const int t = tiles_of(b0 + lane);
-        tiles += t;
-        seqs += t > 0;
-    }
-    tiles = __reduce_add_sync(0xffffffffu, tiles);
-    seqs = __reduce_add_sync(0xffffffffu, seqs);
-    int prefix[2], length[2];
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-        prefix[f] = item_cost(key_tiles(p.shared), ITEM_COST(f)) * p.phase[f].prefix_items;
-        length[f] = prefix[f] + (tiles * TILE_COST + seqs * ITEM_COST(f)) * p.phase[f].seq_items;
-    }
-    // the first CTAs take the pairs, the others the single row tiles
-    int n_pairs = n_cta;
-    if (length[1]) {
-        const float a = (float)length[0] * PHASE_COST(0), b = (float)length[1] * PHASE_COST(1);
-        n_pairs = length[0] ? max(1, min(n_cta - 1, __float2int_rn(n_cta * (a / (a + b))))) : 0;
-    }
-    int y[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        const int f = k > 0, cost = item_cost(key_tiles(p.shared), ITEM_COST(f));
-        const int workers = f ? 2 * (n_cta - n_pairs) : n_pairs, worker = k == 0 ? cta : k == 1 ? cta - n_pairs : cta + n_cta - 2 * n_pairs;
-        const bool on = f ? cta >= n_pairs : cta < n_pairs;
-        w[k].worker = worker;
-        w[k].ends = ITEM_COST(f);
-        // none shorter than a key tile, so that no worker in the middle of an item is left without a tile
-        const int run = on ? max((length[f] + workers - 1) / workers, TILE_COST) : 0;
-        w[k].x0 = on ? (int)min((int64_t)length[f], (int64_t)run * worker) : 0;
-        w[k].x1 = (int)min((int64_t)length[f], (int64_t)w[k].x0 + run);
-        w[k].b = -1;
-        w[k].idx = 0;
-        w[k].S = w[k].x0 == w[k].x1 ? w[k].x1 : 0;
-        y[k] = -1;
-        if (w[k].x0 < w[k].x1) {
-            if (w[k].x0 < prefix[f]) {
-                w[k].idx = w[k].x0 / cost;
-                w[k].S = w[k].idx * cost;
-            } else {
-                y[k] = w[k].x0 - prefix[f];
-            }
-        }
-    }
-    int before_tiles = 0, before_seqs = 0;
-    for (int b0 = 0; b0 < p.B && (y[0] >= 0 || y[1] >= 0 || y[2] >= 0); b0 += 32) {
-        const int own = b0 ? tiles_of(b0 + lane) : own0;
-        const uint32_t some = __ballot_sync(0xffffffffu, own > 0);
-        const int n = __popc(some & (0xffffffffu >> (31 - lane)));
-        int c = own;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int x = __shfl_up_sync(0xffffffffu, c, o);
-            if (lane >= o) c += x;
-        }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            const PaPhase &f = p.phase[k > 0];
-            const int ends = ITEM_COST(k > 0), up_to = ((before_tiles + c) * TILE_COST + (before_seqs + n) * ends) * f.seq_items;
-            const uint32_t behind = __ballot_sync(0xffffffffu, up_to > y[k]);
-            if (y[k] < 0 || !behind) continue;
-            const int at = __ffs((int)behind) - 1;
-            const int each = item_cost(__shfl_sync(0xffffffffu, own, at), ends), first = __shfl_sync(0xffffffffu, up_to, at) - each * f.seq_items;
-            w[k].b = b0 + at;
-            w[k].idx = (y[k] - first) / each;
-            w[k].S = w[k].x0 - y[k] + first + w[k].idx * each;
-            y[k] = -1;
-        }
-        before_tiles += __shfl_sync(0xffffffffu, c, 31);
-        before_seqs += __popc(some);
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-        if (w[k].x0 < w[k].x1) w[k].load(p);
-}
-
-// All of a phase's key tiles in the order in which the ring holds them: a round takes, list after list, V of the tile before and K of the
-// tile after.  next(list, piece) -> whether there is one; f(list, piece and tile of V or none, piece and tile of K or none) -> whether to go on.
-template <int NL, typename N, typename F>
-__device__ __forceinline__ bool for_rounds(N &&next, F &&f) {
-    PaPiece cur[NL], old[NL];
-    int t[NL], old_t[NL];
-    bool live[NL], pend[NL];
-#pragma unroll
-    for (int l = 0; l < NL; ++l) {
-        live[l] = next(l, cur[l]);
-        t[l] = cur[l].t0;
-        pend[l] = false;
-        old[l] = cur[l];
-        old_t[l] = 0;
-    }
-    for (;;) {
-        bool any = false;
-#pragma unroll
-        for (int l = 0; l < NL; ++l) {
-            if (!live[l] && !pend[l]) continue;
-            any = true;
-            if (!f(l, pend[l], old[l], old_t[l], live[l], cur[l], t[l])) return false;
-            pend[l] = live[l];
-            if (live[l]) {
-                old[l] = cur[l];
-                old_t[l] = t[l];
-                if (++t[l] == cur[l].t1) {
-                    live[l] = next(l, cur[l]);
-                    t[l] = cur[l].t0;
-                }
-            }
-        }
-        if (!any) return true;
-    }
-}
-
-// maximum that a NaN wins
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
 // What the rounding of two values to bf16 pairs left, as bf16 pairs.
 __device__ __forceinline__ uint32_t rounded_off(float2 p, uint32_t w) {
     const float2 r = __fadd2_rn(p, make_float2(-__uint_as_float(w << 16), -__uint_as_float(w & 0xffff0000u)));
@@ -291,28 +80,6 @@ __device__ __forceinline__ uint32_t rounded_off(float2 p, uint32_t w) {
 }
 __device__ __forceinline__ bool nonfinite16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
 
-// The two warps that hold the same rows: whether any of their threads says so.
-__device__ __forceinline__ bool any_of_rows(int barrier, bool mine) {
-    uint32_t r;
-    asm volatile(
-        "{\n"
-        ".reg .pred p, q;\n"
-        "setp.ne.u32 p, %1, 0;\n"
-        "barrier.cta.red.or.pred q, %2, 64, p;\n"
-        "selp.u32 %0, 1, 0, q;\n"
-        "}\n"
-        : "=r"(r) : "r"((uint32_t)mine), "r"(barrier) : "memory");
-    return r != 0;
-}
-__device__ __forceinline__ void tmem_put(uint32_t taddr, float v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
-}
-__device__ __forceinline__ float tmem_get(uint32_t taddr) {
-    float v;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n"
-                 "tcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(taddr) : "memory");
-    return v;
-}
 __device__ __forceinline__ void pa_cta_sync() { asm volatile("bar.sync 1, %0;" ::"n"(PA_THREADS) : "memory"); }
 
 // ---------------------------------------------------------------------------------------- pieces
@@ -400,7 +167,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     if (warp == PA_TMA_WARP) {
         // ------------------------------------------------------------ pieces; Q, K and V
         PaWalk w[3];
-        begin_walks(p, w, cta, n_cta, lane);
+        begin_walks(p, w, cta, n_cta, lane, PHASE_COST(0), PHASE_COST(1));
         // One piece more for a queue, or its end: a piece without tiles.  (There is room, or will be without this warp's doing: the queries
         // of a piece are only requested when the scores of the one before are complete, so this warp is never three pieces ahead.)
         auto hand_out = [&](int q, int n, PaPiece &s) {
@@ -831,7 +598,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ int thin_steps(int keys) { return (keys + TH_STEP - 1) / TH_STEP; }
 
 template <int D>
 __global__ void __launch_bounds__(TH_WARPS * 32, 2)
@@ -846,46 +612,8 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
     const PaPhase &ph = p.phase[2];
     const int worker = blockIdx.x, workers = gridDim.x;
     previous_done();
-    auto cost_of = [&](int b) {
-        const int L = b < p.B ? p.seq_lens[b] : -1;
-        return L >= 0 && p.pages.fits(L, p.T) && L >= p.shared ? thin_steps(L - p.shared + p.T) + TH_ENDS : 0;
-    };
-    if (warp == 0) {
-        const int own0 = cost_of(lane);
-        int total = own0;
-        for (int b0 = 32; b0 < p.B; b0 += 32) total += cost_of(b0 + lane);
-        total = __reduce_add_sync(0xffffffffu, total);
-        const int each = thin_steps(p.shared) + TH_ENDS, prefix = ph.prefix_items * each, length = prefix + total * ph.seq_items;
-        const int run = max((length + workers - 1) / workers, 1), x0 = (int)min((int64_t)length, (int64_t)run * worker), x1 = (int)min((int64_t)length, (int64_t)x0 + run);
-        int b = -1, idx = 0, S = x1;
-        if (x0 < x1 && x0 < prefix) {
-            idx = x0 / each;
-            S = idx * each;
-        } else if (x0 < x1) {
-            const int y = x0 - prefix;
-            int before = 0;
-            for (int b0 = 0; b0 < p.B; b0 += 32) {
-                const int own = b0 ? cost_of(b0 + lane) : own0;
-                int c = own;
-#pragma unroll
-                for (int o = 1; o < 32; o *= 2) {
-                    const int x = __shfl_up_sync(0xffffffffu, c, o);
-                    if (lane >= o) c += x;
-                }
-                const uint32_t behind = __ballot_sync(0xffffffffu, (before + c) * ph.seq_items > y);
-                if (behind) {
-                    const int at = __ffs((int)behind) - 1, cost = __shfl_sync(0xffffffffu, own, at);
-                    const int first = (before + __shfl_sync(0xffffffffu, c, at) - cost) * ph.seq_items;
-                    b = b0 + at;
-                    idx = (y - first) / cost;
-                    S = prefix + first + idx * cost;
-                    break;
-                }
-                before += __shfl_sync(0xffffffffu, c, 31);
-            }
-        }
-        if (lane == 0) { start[0] = x0; start[1] = x1; start[2] = S; start[3] = b; start[4] = idx; }
-    }
+    using Line = ThinLine<TH_STEP, TH_ENDS>;
+    if (warp == 0) Line::begin(p, worker, workers, lane, start);
     __syncthreads();
     const int x0 = start[0], x1 = start[1];
     int S = start[2], b = start[3], idx = start[4];
@@ -893,9 +621,9 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
     auto load_item = [&]() {
         if (b < 0) {
             L = p.shared;
-            cost = thin_steps(p.shared) + TH_ENDS;
+            cost = Line::steps(p.shared) + TH_ENDS;
         } else {
-            cost = cost_of(b);
+            cost = Line::cost_of(p, b);
             L = p.seq_lens[b] - p.shared;
         }
     };
@@ -1230,12 +958,12 @@ paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
 }
 
 // ---------------------------------------------------------------------------------------- host
-static bool pa_sizes_ok(const mtv_tree *tree, int B, int Hq, int Hkv, int D, int shared) {
+bool pa_sizes_ok(const mtv_tree *tree, int B, int Hq, int Hkv, int D, int shared) {
     return tree && B >= 1 && B <= PA_MAX_B && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= 8 && (D == 64 || D == 128) && shared >= 0 &&
            (int64_t)Hq * B * tree->T <= 1 << 28;
 }
 // All lines stay below 2^31, whatever the lengths.
-static bool pa_lines_ok(const PaPhase (&ph)[3], int B, int shared, int64_t slots) {
+bool pa_lines_ok(const PaPhase (&ph)[3], int B, int shared, int64_t slots) {
     for (const PaPhase &f : ph) {
         // (a thin item's steps are of 64 keys and count one)
         const int64_t ends = ITEM_COST(0), prefix = (shared / PA_KEYS + 1) * TILE_COST + ends, own = (slots / PA_KEYS + 2) * TILE_COST + ends;
@@ -1244,6 +972,20 @@ static bool pa_lines_ok(const PaPhase (&ph)[3], int B, int shared, int64_t slots
     }
     return true;
 }
+
+template <int D>
+static int launch_combine(const PaParams &p, cudaStream_t stream) {
+    const int64_t rows = (int64_t)p.B * p.Hkv * p.T * p.G;
+    // Fewer blocks than SMs with a thread per row and chunk (decoding: few rows, each of many pieces): four threads share one.  Whole calls on one card, D = 128
+    // (D = 64 goes by the same rule, not measured): 2048 rows (128 blocks) 77 us so and 86 with one thread; 5684 rows (356 blocks) 37.9 and 34.6; 16384 rows 167 and 153.
+    constexpr int PER = 256 / (D / 8);
+    if (rows < (int64_t)PER * sm_count())
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 4>, dim3((unsigned)((rows + PER / 4 - 1) / (PER / 4))), 256, 0, stream, p));
+    else
+        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 1>, dim3((unsigned)((rows + PER - 1) / PER)), 256, 0, stream, p));
+    return MTV_OK;
+}
+int pa_combine(const PaParams &p, int D, cudaStream_t stream) { return D == 128 ? launch_combine<128>(p, stream) : launch_combine<64>(p, stream); }
 
 template <int D>
 static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const PaParams &p, cudaStream_t stream) {
@@ -1258,15 +1000,7 @@ static int launch_paged(const CUtensorMap &q, const CUtensorMap &k, const CUtens
         MTV_CUDA_CHECK(launch_dependent(paged_attn_kernel<D>, dim3(sm_count()), PA_THREADS, PaSmem<D>::TOTAL, stream, q, k, v, p));
     if (thin.prefix_items + thin.seq_items)
         MTV_CUDA_CHECK(launch_dependent(paged_attn_thin_kernel<D>, dim3(2 * sm_count()), TH_WARPS * 32, 0, stream, p));
-    const int64_t rows = (int64_t)p.B * p.Hkv * p.T * p.G;
-    // Fewer blocks than SMs with a thread per row and chunk (decoding: few rows, each of many pieces): four threads share one.  Whole calls on one card, D = 128
-    // (D = 64 goes by the same rule, not measured): 2048 rows (128 blocks) 77 us so and 86 with one thread; 5684 rows (356 blocks) 37.9 and 34.6; 16384 rows 167 and 153.
-    constexpr int PER = 256 / (D / 8);
-    if (rows < (int64_t)PER * sm_count())
-        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 4>, dim3((unsigned)((rows + PER / 4 - 1) / (PER / 4))), 256, 0, stream, p));
-    else
-        MTV_CUDA_CHECK(launch_dependent(paged_attn_combine_kernel<D, 1>, dim3((unsigned)((rows + PER - 1) / PER)), 256, 0, stream, p));
-    return MTV_OK;
+    return pa_combine(p, D, stream);
 }
 
 }  // namespace mtv
