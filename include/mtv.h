@@ -19,6 +19,8 @@
  * and the same step for a program that keeps K and V in pages and decodes under constraints:
  *   tree_kv_append_rope_paged, kv_append_rope_paged, tree_verify_attention_paged (a prefix that the batch
  *                          shares is attended to once for all), kv_compact_accepted_paged
+ *   the same calls with the suffix _fp8, and kv_read_paged_fp8
+ *                          such a cache in 8 bits: quantised as it is written, read by the attention as it is
  *   logits_constrain, constrained_argmax_keys, token_counts_add
  *                          penalties for repeated tokens, biases and grammar masks in front of the acceptance
  *
@@ -469,6 +471,54 @@ int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, 
                                 const mtv_bf16 *v_pool, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
                                 int shared_len, const int32_t *seq_lens, float scale, mtv_bf16 *out, int32_t *status,
                                 void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The same cache in 8 bits (the paper's is bf16): half the bytes for a sequence's keys, and for what the attention reads.
+ *   pools          uint8_t, e4m3 codes (1 sign, 4 exponent, 3 fraction bits; largest value 448; no infinities), in the layout above with strides
+ *                  counted in elements, which are bytes here: multiples of 16 and at least D
+ *   k_scale, v_scale   device fp32 [n_layers][Hkv] (the attention takes one layer's [Hkv]), positive and finite: a code c of head g stands for
+ *                  c * scale[g].  Scales of a head that differ from call to call give rows that stand for other values: keep them with the cache.
+ *   a value x is stored as the code nearest to x * (1 / scale) (in fp32; ties to the even code); beyond 448, infinities too, as +-448; NaN as NaN
+ * Everything else — page tables, lengths, limits, errors and status — is as in the calls without the suffix.
+ */
+
+/* tree_kv_append_rope_paged, kv_append_rope_paged: K rows are rotated in fp32 and rounded once, to the code; V rows are rounded as they
+ * come; the rotated queries stay bf16. */
+int tree_kv_append_rope_paged_fp8(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,
+                                  mtv_bf16 *q_out_layers, const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers,
+                                  uint8_t *const *k_pools, uint8_t *const *v_pools, const mtv_pool_layout *pool,
+                                  const int32_t *page_table, int max_pages, const int32_t *seq_lens, const float *k_scale, const float *v_scale,
+                                  float rope_theta, int32_t *status, void *stream);
+int kv_append_rope_paged_fp8(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
+                             const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, uint8_t *const *k_pools,
+                             uint8_t *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                             const int32_t *seq_lens, const int32_t *row_starts, const float *k_scale, const float *v_scale, float rope_theta,
+                             int32_t *status, void *stream);
+
+/* Rows of such a cache as bf16 (a prefix for a prefill of the program's own, a cache that goes elsewhere): row row_starts[b] + i of k_out_layers,
+ * v_out_layers [n_layers][n_rows][Hkv][D] is slot first[b] + i of sequence b, its codes times the scale in fp32, rounded once.  first: device [B] or NULL (0);
+ * row_starts: device [B+1], ascending; rows outside [row_starts[0], row_starts[B]) are left as they are.  Outputs 16-byte aligned; n_rows may be 0
+ * (they may then be NULL).  status[b] as for the appending, of slots first[b] to first[b] + rows - 1: MTV_ERR_CAPACITY (nothing of b is
+ * written) or MTV_ERR_BOUNDS (rows whose page does not exist are left as they are). */
+int kv_read_paged_fp8(int B, int n_rows, int Hkv, int D, int n_layers, const uint8_t *const *k_pools, const uint8_t *const *v_pools,
+                      const mtv_pool_layout *pool, const int32_t *page_table, int max_pages, const int32_t *first, const int32_t *row_starts,
+                      const float *k_scale, const float *v_scale, mtv_bf16 *k_out_layers, mtv_bf16 *v_out_layers, int32_t *status, void *stream);
+
+/* kv_compact_accepted_paged: codes move, scales have no part in it. */
+int kv_compact_accepted_paged_fp8(const mtv_tree_t *tree, int B, int Hkv, int D, int n_layers, uint8_t *const *k_pools,
+                                  uint8_t *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                                  const int32_t *seq_lens, int32_t *new_lens, const int32_t *accept_len, const int32_t *acc_nodes,
+                                  int32_t *status, void *stream);
+
+/* tree_verify_attention_paged over such a cache: the scores are scale * k_scale[g] * <q, codes of k>, the result v_scale[g] times the weighted sum of V's
+ * codes.  fp16 products (codes are numbers of fp16; a query row is multiplied by the power of two that brings its largest value to [256, 512), in
+ * which values below 2^-25 of it lose bits), fp32 sums and softmax, weights rounded to fp16 (2^-11 of a weight, and 2^-33 of the
+ * row's largest at least).  NaN in q, or in a K or V row that a node sees, makes its output NaN; so does an infinity in q.
+ * Workspace: tree_attention_paged_workspace_bytes. */
+int tree_verify_attention_paged_fp8(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, const mtv_bf16 *q, const uint8_t *k_pool,
+                                    const uint8_t *v_pool, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                                    int shared_len, const int32_t *seq_lens, const float *k_scale, const float *v_scale, float scale,
+                                    mtv_bf16 *out, int32_t *status, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
  * Constrained decoding: what a serving program lays over the base model's logits before a token is chosen (the paper chooses by

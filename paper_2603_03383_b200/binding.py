@@ -34,7 +34,8 @@ EXPORTS = ["tree_build_static", "tree_gen_cartesian", "tree_gen_rank_prior", "tr
            "mtv_verify_steps", "mtv_debug_bounds_enabled", "heads_merge_shards", "attn_interleave_shards",
            "keys_merge_shards", "node_argmax_keys", "tree_kv_append_rope_paged", "kv_append_rope_paged",
            "kv_compact_accepted_paged", "tree_attention_paged_workspace_bytes", "tree_verify_attention_paged",
-           "logits_constrain", "constrained_argmax_keys", "token_counts_add"]
+           "logits_constrain", "constrained_argmax_keys", "token_counts_add", "tree_kv_append_rope_paged_fp8",
+           "kv_append_rope_paged_fp8", "kv_read_paged_fp8", "kv_compact_accepted_paged_fp8", "tree_verify_attention_paged_fp8"]
 
 
 class MtvError(RuntimeError):
@@ -140,6 +141,12 @@ def lib():
         L.tree_attention_paged_workspace_bytes.restype = sz
         L.tree_verify_attention_paged.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, pool, vp, i32, i32, vp, C.c_float, vp, vp,
                                                   vp, sz, vp]
+        L.tree_kv_append_rope_paged_fp8.argtypes = [vp, i32, i32, i32, i32, i32] + [vp] * 6 + [pool, vp, i32, vp, vp, vp, C.c_float, vp, vp]
+        L.kv_append_rope_paged_fp8.argtypes = [i32] * 6 + [vp] * 6 + [pool, vp, i32] + [vp] * 4 + [C.c_float, vp, vp]
+        L.kv_read_paged_fp8.argtypes = [i32] * 5 + [vp, vp, pool, vp, i32] + [vp] * 8
+        L.kv_compact_accepted_paged_fp8.argtypes = L.kv_compact_accepted_paged.argtypes
+        L.tree_verify_attention_paged_fp8.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, pool, vp, i32, i32, vp, vp, vp, C.c_float, vp, vp,
+                                                      vp, sz, vp]
         rules = C.POINTER(LogitRules)
         L.logits_constrain.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, rules, vp, vp]
         L.constrained_argmax_keys.argtypes = [vp, i32, i32, i32, vp, i64, rules, vp, vp, vp]
@@ -396,7 +403,7 @@ def mtv_verify_step_host(tree, dev: StepArgs, host: StepArgs, stream=None):
 # What these calls and those of the next section are given is looked at before its address goes over: a kernel that reads int64 as int32, or
 # past the end of a tensor, reports nothing.  A refusal names the argument.  (pysrc/tensors.cpp looks at all tensors of a call in one step; a set of
 # rules is looked at when it is made.)
-_BF16, _I32, _I64, _F32, _ANY, _OPTIONAL, _STRIDED, _LIKE_PREVIOUS = 0, 1, 2, 3, 4, 16, 32, 64
+_BF16, _I32, _I64, _F32, _ANY, _FP8, _OPTIONAL, _STRIDED, _LIKE_PREVIOUS = 0, 1, 2, 3, 4, 5, 16, 32, 64
 _MAYBE_I32 = _I32 | _OPTIONAL
 _tensors = None
 
@@ -422,21 +429,33 @@ def _look(where, names, *args):
 
 def pool_layout(pool: torch.Tensor) -> PoolLayout:
     """Layout of a pool tensor [n_pages][Hkv][page_size][D] of any strides with the columns innermost (a pool whose pages hold
-    [page_size][Hkv][D] is passed as its transposed view)."""
-    if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype is not torch.bfloat16:
+    [page_size][Hkv][D] is passed as its transposed view): bf16, or the codes of the calls with the suffix _fp8 (float8_e4m3fn)."""
+    if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
         _refuse("pool_layout", "pool")
     sp, sh, st = pool.stride()[:3]
-    return PoolLayout(sp, sh, st, pool.shape[2], pool.shape[0])
+    layout = PoolLayout(sp, sh, st, pool.shape[2], pool.shape[0])
+    layout.dtype = pool.dtype
+    return layout
 
 
-_APPEND = ("q_layers", "q_out_layers", "k_new_layers", "v_new_layers", "k_ptrs", "v_ptrs", "page_table", "seq_lens", "status", "row_starts")
+def _layout_of(pool, dtype, where):
+    """Strides are counted in elements: a layout that was made of another type's pool is refused."""
+    if getattr(pool, "dtype", dtype) is not dtype:
+        _refuse(where, "pool")
 
 
-def tree_kv_append_rope_paged(tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table,
-                              seq_lens, rope_theta=0.0, status=None, stream=None):
-    """q_layers, q_out_layers [n_layers][B][T][Hq][D], k_new_layers / v_new_layers [n_layers][B][T][Hkv][D]; k_ptrs / v_ptrs: device
-    arrays of the layers' pools (cache_pointer_array); page_table [B][max_pages]."""
-    where, shape = "tree_kv_append_rope_paged", q_layers.shape
+_APPEND = ("q_layers", "q_out_layers", "k_new_layers", "v_new_layers", "k_ptrs", "v_ptrs", "page_table", "seq_lens", "status")
+_SCALES = ("k_scale", "v_scale")
+
+
+def _scales(scales, n):
+    """The two scales' part of a look, for calls that have them."""
+    return (scales[0], _F32, n, scales[1], _F32, n) if scales else ()
+
+
+def _append_tree(where, call, dtype, scales, tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool, page_table, seq_lens,
+                 rope_theta, status, stream):
+    shape = q_layers.shape
     if len(shape) != 5 or shape[2] != tree.T:
         _refuse(where, "q_layers")
     n_layers, B, T, Hq, D = shape
@@ -445,47 +464,106 @@ def tree_kv_append_rope_paged(tree, q_layers, q_out_layers, k_new_layers, v_new_
     Hkv, max_pages = k_new_layers.shape[3], page_table.shape[1]
     if k_new_layers.shape != (n_layers, B, T, Hkv, D):
         _refuse(where, "k_new_layers")
+    _layout_of(pool, dtype, where)
     rows = n_layers * B * T * D
-    _, q, q_out, k, v, kp, vp, table, lens, st = _look(
-        where, _APPEND, q_layers, _BF16, rows * Hq, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
+    _, q, q_out, k, v, kp, vp, table, lens, st, *sc = _look(
+        where, _APPEND + _SCALES, q_layers, _BF16, rows * Hq, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
         v_new_layers, _BF16 | _LIKE_PREVIOUS, -1, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, B * max_pages, seq_lens, _I32, B,
-        status, _MAYBE_I32, B)
-    _check(lib().tree_kv_append_rope_paged(tree.handle, B, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, rope_theta, st,
-                                           _stream(stream)), where)
+        status, _MAYBE_I32, B, *_scales(scales, n_layers * Hkv))
+    _check(call(tree.handle, B, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, *sc, rope_theta, st, _stream(stream)), where)
 
 
-def kv_append_rope_paged(q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table, seq_lens,
-                         row_starts, rope_theta=0.0, status=None, stream=None):
-    """q_layers, q_out_layers [n_layers][n_rows][Hq][D], k_new_layers / v_new_layers [n_layers][n_rows][Hkv][D]; row_starts [B+1]."""
-    where = "kv_append_rope_paged"
+def _append_rows(where, call, dtype, scales, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool, page_table, seq_lens, row_starts,
+                 rope_theta, status, stream):
     for t, dim, name in ((q_layers, 4, "q_layers"), (k_new_layers, 4, "k_new_layers"), (page_table, 2, "page_table")):
         if t.dim() != dim:
             _refuse(where, name)
     (n_layers, n_rows, Hq, D), (B, max_pages), Hkv = q_layers.shape, page_table.shape, k_new_layers.shape[2]
     if k_new_layers.shape != (n_layers, n_rows, Hkv, D):
         _refuse(where, "k_new_layers")
-    _, q, q_out, k, v, kp, vp, table, lens, st, starts = _look(
-        where, _APPEND, q_layers, _BF16, -1, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1, v_new_layers, _BF16 | _LIKE_PREVIOUS, -1,
-        k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B, status, _MAYBE_I32, B, row_starts, _I32, B + 1)
-    _check(lib().kv_append_rope_paged(B, n_rows, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, starts, rope_theta, st,
-                                      _stream(stream)), where)
+    _layout_of(pool, dtype, where)
+    _, q, q_out, k, v, kp, vp, table, lens, st, *sc, starts = _look(
+        where, _APPEND + (_SCALES if scales else ()) + ("row_starts",), q_layers, _BF16, -1, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
+        v_new_layers, _BF16 | _LIKE_PREVIOUS, -1, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B,
+        status, _MAYBE_I32, B, *_scales(scales, n_layers * Hkv), row_starts, _I32, B + 1)
+    _check(call(B, n_rows, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, starts, *sc, rope_theta, st, _stream(stream)), where)
+
+
+def tree_kv_append_rope_paged(tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table,
+                              seq_lens, rope_theta=0.0, status=None, stream=None):
+    """q_layers, q_out_layers [n_layers][B][T][Hq][D], k_new_layers / v_new_layers [n_layers][B][T][Hkv][D]; k_ptrs / v_ptrs: device
+    arrays of the layers' pools (cache_pointer_array); page_table [B][max_pages]."""
+    _append_tree("tree_kv_append_rope_paged", lib().tree_kv_append_rope_paged, torch.bfloat16, (), tree, q_layers, q_out_layers, k_new_layers,
+                 v_new_layers, k_ptrs, v_ptrs, pool, page_table, seq_lens, rope_theta, status, stream)
+
+
+def kv_append_rope_paged(q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table, seq_lens,
+                         row_starts, rope_theta=0.0, status=None, stream=None):
+    """q_layers, q_out_layers [n_layers][n_rows][Hq][D], k_new_layers / v_new_layers [n_layers][n_rows][Hkv][D]; row_starts [B+1]."""
+    _append_rows("kv_append_rope_paged", lib().kv_append_rope_paged, torch.bfloat16, (), q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs,
+                 v_ptrs, pool, page_table, seq_lens, row_starts, rope_theta, status, stream)
+
+
+def tree_kv_append_rope_paged_fp8(tree, q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table,
+                                  seq_lens, k_scale, v_scale, rope_theta=0.0, status=None, stream=None):
+    """tree_kv_append_rope_paged into pools of e4m3 codes; k_scale, v_scale [n_layers][Hkv] fp32."""
+    _append_tree("tree_kv_append_rope_paged_fp8", lib().tree_kv_append_rope_paged_fp8, torch.float8_e4m3fn, (k_scale, v_scale), tree, q_layers,
+                 q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool, page_table, seq_lens, rope_theta, status, stream)
+
+
+def kv_append_rope_paged_fp8(q_layers, q_out_layers, k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool: PoolLayout, page_table, seq_lens,
+                             row_starts, k_scale, v_scale, rope_theta=0.0, status=None, stream=None):
+    """kv_append_rope_paged into pools of e4m3 codes; k_scale, v_scale [n_layers][Hkv] fp32."""
+    _append_rows("kv_append_rope_paged_fp8", lib().kv_append_rope_paged_fp8, torch.float8_e4m3fn, (k_scale, v_scale), q_layers, q_out_layers,
+                 k_new_layers, v_new_layers, k_ptrs, v_ptrs, pool, page_table, seq_lens, row_starts, rope_theta, status, stream)
+
+
+_READ = ("k_ptrs", "v_ptrs", "page_table", "first", "row_starts", "k_scale", "v_scale", "k_out_layers", "v_out_layers", "status")
+
+
+def kv_read_paged_fp8(k_ptrs, v_ptrs, pool: PoolLayout, page_table, row_starts, k_scale, v_scale, k_out_layers, v_out_layers, first=None,
+                      status=None, stream=None):
+    """k_out_layers, v_out_layers [n_layers][n_rows][Hkv][D] bf16; row_starts [B+1], first [B] (None: from slot 0)."""
+    where = "kv_read_paged_fp8"
+    if k_out_layers.dim() != 4:
+        _refuse(where, "k_out_layers")
+    if page_table.dim() != 2:
+        _refuse(where, "page_table")
+    (n_layers, n_rows, Hkv, D), (B, max_pages) = k_out_layers.shape, page_table.shape
+    _layout_of(pool, torch.float8_e4m3fn, where)
+    _, kp, vp, table, at, starts, ks, vs, k, v, st = _look(
+        where, _READ, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, first, _MAYBE_I32, B, row_starts, _I32, B + 1,
+        k_scale, _F32, n_layers * Hkv, v_scale, _F32, n_layers * Hkv, k_out_layers, _BF16, -1, v_out_layers, _BF16 | _LIKE_PREVIOUS, -1,
+        status, _MAYBE_I32, B)
+    _check(lib().kv_read_paged_fp8(B, n_rows, Hkv, D, n_layers, kp, vp, pool, table, max_pages, at, starts, ks, vs, k, v, st, _stream(stream)), where)
 
 
 _COMPACT = ("k_ptrs", "v_ptrs", "page_table", "seq_lens", "new_lens", "accept_len", "acc_nodes", "status")
 
 
-def kv_compact_accepted_paged(tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool: PoolLayout, page_table, seq_lens, new_lens, accept_len,
-                              acc_nodes, status=None, stream=None):
-    """new_lens may be seq_lens itself; accept_len [B], acc_nodes [B][K + 1]."""
-    where = "kv_compact_accepted_paged"
+def _compact(where, call, dtype, tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool, page_table, seq_lens, new_lens, accept_len, acc_nodes, status, stream):
     if page_table.dim() != 2:
         _refuse(where, "page_table")
     B, max_pages = page_table.shape
+    _layout_of(pool, dtype, where)
     _, kp, vp, table, lens, new, n, nodes, st = _look(
         where, _COMPACT, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B, new_lens, _I32, B, accept_len, _I32, B,
         acc_nodes, _I32, B * (tree.K + 1), status, _MAYBE_I32, B)
-    _check(lib().kv_compact_accepted_paged(tree.handle, B, Hkv, D, n_layers, kp, vp, pool, table, max_pages, lens, new, n, nodes, st, _stream(stream)),
-           where)
+    _check(call(tree.handle, B, Hkv, D, n_layers, kp, vp, pool, table, max_pages, lens, new, n, nodes, st, _stream(stream)), where)
+
+
+def kv_compact_accepted_paged(tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool: PoolLayout, page_table, seq_lens, new_lens, accept_len,
+                              acc_nodes, status=None, stream=None):
+    """new_lens may be seq_lens itself; accept_len [B], acc_nodes [B][K + 1]."""
+    _compact("kv_compact_accepted_paged", lib().kv_compact_accepted_paged, torch.bfloat16, tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool, page_table,
+             seq_lens, new_lens, accept_len, acc_nodes, status, stream)
+
+
+def kv_compact_accepted_paged_fp8(tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool: PoolLayout, page_table, seq_lens, new_lens, accept_len,
+                                  acc_nodes, status=None, stream=None):
+    """kv_compact_accepted_paged of pools of e4m3 codes."""
+    _compact("kv_compact_accepted_paged_fp8", lib().kv_compact_accepted_paged_fp8, torch.float8_e4m3fn, tree, k_ptrs, v_ptrs, n_layers, Hkv, D, pool,
+             page_table, seq_lens, new_lens, accept_len, acc_nodes, status, stream)
 
 
 def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
@@ -496,10 +574,8 @@ def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
 _ATTENTION = ("q", "out", "k_pool", "v_pool", "page_table", "seq_lens", "status", "ws")
 
 
-def tree_verify_attention_paged(tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len=0, scale=0.0, status=None,
-                                stream=None):
-    """q, out [B][T][Hq][D]; k_pool, v_pool [n_pages][Hkv][page_size][D] (see pool_layout), the same strides."""
-    where, shape, pools, strides = "tree_verify_attention_paged", q.shape, k_pool.shape, k_pool.stride()
+def _attention(where, call, kind, scales, tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len, scale, status, stream):
+    shape, pools, strides = q.shape, k_pool.shape, k_pool.stride()
     if len(shape) != 4 or shape[1] != tree.T:
         _refuse(where, "q")
     B, T, Hq, D = shape
@@ -510,11 +586,26 @@ def tree_verify_attention_paged(tree, q, k_pool, v_pool, page_table, seq_lens, o
     if page_table.dim() != 2:
         _refuse(where, "page_table")
     max_pages = page_table.shape[1]
-    _, q_at, out_at, k, v, table, lens, st, ws_at = _look(
-        where, _ATTENTION, q, _BF16, -1, out, _BF16 | _LIKE_PREVIOUS, -1, k_pool, _BF16 | _STRIDED, -1, v_pool, _BF16 | _STRIDED | _LIKE_PREVIOUS, -1,
-        page_table, _I32, B * max_pages, seq_lens, _I32, B, status, _MAYBE_I32, B, ws, _ANY, -1)
-    _check(lib().tree_verify_attention_paged(tree.handle, B, Hq, pools[1], D, q_at, k, v, PoolLayout(strides[0], strides[1], strides[2], pools[2], pools[0]),
-                                             table, max_pages, shared_len, lens, scale, out_at, st, ws_at, ws.nbytes, _stream(stream)), where)
+    _, q_at, out_at, k, v, table, lens, st, ws_at, *sc = _look(
+        where, _ATTENTION + _SCALES, q, _BF16, -1, out, _BF16 | _LIKE_PREVIOUS, -1, k_pool, kind | _STRIDED, -1,
+        v_pool, kind | _STRIDED | _LIKE_PREVIOUS, -1, page_table, _I32, B * max_pages, seq_lens, _I32, B, status, _MAYBE_I32, B, ws, _ANY, -1,
+        *_scales(scales, pools[1]))
+    _check(call(tree.handle, B, Hq, pools[1], D, q_at, k, v, PoolLayout(strides[0], strides[1], strides[2], pools[2], pools[0]), table, max_pages,
+                shared_len, lens, *sc, scale, out_at, st, ws_at, ws.nbytes, _stream(stream)), where)
+
+
+def tree_verify_attention_paged(tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len=0, scale=0.0, status=None,
+                                stream=None):
+    """q, out [B][T][Hq][D]; k_pool, v_pool [n_pages][Hkv][page_size][D] (see pool_layout), the same strides."""
+    _attention("tree_verify_attention_paged", lib().tree_verify_attention_paged, _BF16, (), tree, q, k_pool, v_pool, page_table, seq_lens, out, ws,
+               shared_len, scale, status, stream)
+
+
+def tree_verify_attention_paged_fp8(tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, k_scale, v_scale, shared_len=0, scale=0.0,
+                                    status=None, stream=None):
+    """tree_verify_attention_paged over pools of e4m3 codes (float8_e4m3fn); k_scale, v_scale [Hkv] fp32, the layer's."""
+    _attention("tree_verify_attention_paged_fp8", lib().tree_verify_attention_paged_fp8, _FP8, (k_scale, v_scale), tree, q, k_pool, v_pool, page_table,
+               seq_lens, out, ws, shared_len, scale, status, stream)
 
 
 # ------------------------------------------------------------------------------------- constrained decoding

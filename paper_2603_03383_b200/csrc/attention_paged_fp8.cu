@@ -1,0 +1,996 @@
+// Tree attention over pages of e4m3 codes (Section 3.2 / Fig. 2(b); the paper's cache is bf16): the division into items, pieces and phases, the joining
+// and the workspace are those of the bf16 cache (attention_paged.cu, paged_attn.cuh); here stands what the codes change.
+//   s_ij = (scale k_scale) <q_i, K8_j>,  out_i = v_scale sum_j softmax(s_i)_j V8_j
+//
+// Every code is a number of fp16, so the products are fp16 x fp16 -> fp32 on the tensor cores, without a loss in K and V, and the scales are left to the
+// softmax' factor and to the end.  Nothing else than codes is read from memory; they become fp16 tiles in shared memory, one conversion instruction for
+// two codes.  (The tensor cores' own 8-bit products would want the queries and the weights in 8 bits, or as two terms of 8 bits at twice
+// the products, which is the time of one in fp16: the conversion costs warps that have nothing else to do.)
+//   q   bf16 has a wider range than fp16: a row is multiplied by the power of two that brings its largest value to [256, 512), and its factor of
+//       the scores divided by it.  8 bits of a bf16 then fit whatever is above 2^-25 of the largest.
+//   P   weights are fp16, 2^SHIFT at the reference (the maximum of a piece's first tile) and below 2^16: they lose bits below 2^(-14 - SHIFT) of the
+//       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.
+//
+// One persistent CTA per SM, two row tiles in flight, each with its scores, weights and accumulator in tensor memory and eight softmax warps:
+//   warps 0-7 / 8-15  softmax of row tile 0 / 1; in front of a piece they turn its queries into fp16
+//   warps 16-19       codes -> fp16 tiles (128 keys, 128-byte swizzle); rows behind the last key become zeros (their weight is 0, but 0 * NaN is not),
+//                     NaN codes of the tree's V rows too (they are given to the rows that see them at the end)
+//   warps 20, 21      issue the products of row tile 0 / 1
+//   warp 22           derives the pieces, requests Q and the codes (a box per page)
+// Codes and tiles have a ring each.  A CTA of pairs shares K and V between its row tiles and is bound by the softmax and the products: four tiles,
+// two stages of codes (D = 128); one of single row tiles is bound by its bytes: three tiles, four stages of codes.
+// The softmax warpgroups have 96 registers, the others 48 (768 threads of 80 at the launch).
+#include <limits.h>
+
+#include "fp8.cuh"
+#include "paged_attn.cuh"
+
+namespace mtv {
+
+constexpr int P8_THREADS = 768;
+constexpr int P8_CONV_WARP = 16, P8_CONV_WARPS = 4, P8_MMA_WARP = 20, P8_TMA_WARP = 22;
+constexpr int P8_REGS_FEWER = 48, P8_REGS_MORE = 96;
+static_assert(4 * P8_REGS_MORE + 2 * P8_REGS_FEWER <= 6 * 80, "registers of the warpgroups against those of the launch");
+constexpr float P8_SHIFT = 8.f;
+constexpr float P8_LIMIT = 15.99f;        // weights stay below 2^16, which fp16 ends at
+
+template <int D> struct P8Smem {
+    static constexpr int HALVES = D / 64;
+    static constexpr uint32_t HALF = 128 * 128;          // 128 rows of 64 columns, 128-byte swizzle
+    static constexpr uint32_t TILE = HALVES * HALF, CODES = 128 * D;
+    // stages with one list of key tiles (pairs) and with two (single row tiles)
+    __host__ __device__ static constexpr int tiles(int lists) { return (lists == 1 ? 4 : 3) * (3 - HALVES); }
+    __host__ __device__ static constexpr int codes(int lists) { return lists == 1 ? (D == 128 ? 2 : 8) : (D == 128 ? 4 : 12); }
+    static constexpr int MAX_TILES = tiles(1), MAX_CODES = codes(2);
+    static constexpr uint32_t RING = tiles(1) * TILE + codes(1) * CODES;
+    static_assert(RING == tiles(2) * TILE + codes(2) * CODES, "one region for either");
+    static constexpr uint32_t OFF_RING = 2 * TILE, OFF_BAR = OFF_RING + RING, TOTAL = 1024 + OFF_BAR + 1280;
+    static_assert(TOTAL <= 227 * 1024, "shared memory budget");
+    static constexpr uint32_t IDESC = (1u << 4) | (128u >> 4) << 24;                             // fp16 x fp16 -> fp32, M = 128
+    static constexpr uint32_t IDESC_QK = IDESC | (128u >> 3) << 17;                               // N = 128 keys
+    static constexpr uint32_t IDESC_PV = IDESC | (uint32_t)(D >> 3) << 17 | 1u << 16;             // N = D columns, B (= V) N-major
+};
+
+enum {
+    P8_CFULL = 0, P8_CFREE = 12, P8_FULL = 24, P8_FREE = 32, P8_QFULL = 40, P8_QREADY = 42, P8_QFREE = 44, P8_SREADY = 46, P8_PREADY = 48, P8_ODONE = 50,
+    P8_FINAL = 52,
+    P8_PIECE = 53,                         // [3 queues][PA_QUEUE]: pairs; single tiles of either half of the CTA
+    P8_TAKEN = P8_PIECE + 3 * PA_QUEUE,
+    P8_TURN = P8_TAKEN + 3 * PA_QUEUE,     // [2] an issuing warp's turn at the tensor core
+    P8_COUNT = P8_TURN + 2
+};
+constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 40 + 15) / 16 * 16;
+static_assert(P8_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1280, "barrier region");
+static_assert(P8Smem<64>::MAX_TILES <= 8 && P8Smem<64>::MAX_CODES <= 12 && P8Smem<128>::MAX_TILES <= 8 && P8Smem<128>::MAX_CODES <= 12, "barriers of the rings");
+
+constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
+
+// What the issuing warps and the converting ones want of a piece (their registers are few).
+struct P8Tiles { int t0, t1; };
+struct P8Rows {
+    int t0, t1;
+    int L;              // keys in front of the tree; more than there can be where it is not the piece's (the prefix)
+};
+
+struct P8Params {
+    PaParams a;                            // (its k and v are not used)
+    const uint8_t *k, *v;
+    const float *k_scale, *v_scale;        // [Hkv]
+};
+
+// The power of two that brings a row of bf16 queries whose largest absolute value has these bits (as fp32) to [256, 512), and its reciprocal.
+__device__ __forceinline__ float2 row_factor(uint32_t largest) {
+    const int e = (int)(largest >> 23);
+    if (largest == 0u || e == 255) return make_float2(1.f, 1.f);
+    const int k = min(135 - e, 126);
+    return make_float2(__int_as_float((127 + k) << 23), __int_as_float((127 - k) << 23));
+}
+__device__ __forceinline__ uint32_t larger_bits(uint32_t m, uint32_t pair) { return max(m, max(pair << 16, pair & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t abs2_bf16(uint32_t pair) { return pair & 0x7fff7fffu; }
+__device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor) {
+    return pack2_f16(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
+}
+
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P8_REGS_FEWER)); }
+
+// ---------------------------------------------------------------------------------------- pieces
+template <int D>
+__global__ void __launch_bounds__(P8_THREADS, 1)
+paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                   const __grid_constant__ P8Params pp) {
+    using SM = P8Smem<D>;
+    constexpr int X_COL = 40;              // of a half's tensor-memory columns, behind P: what the threads of a row exchange
+    const PaParams &p = pp.a;
+    extern __shared__ unsigned char smem_raw[];
+    let_next_start();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u, sbase = raw + pad;
+    unsigned char *gbase = smem_raw + pad;
+    const uint32_t bars = sbase + SM::OFF_BAR;
+    auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + SM::OFF_BAR + P8_OFF_MISC);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 4);
+    volatile int *bad = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 8);   // [2][4]: 1 + the last piece with NaN in V
+    int4 *queue = reinterpret_cast<int4 *>(gbase + SM::OFF_BAR + P8_OFF_QUEUE);                    // [3][PA_QUEUE] pieces
+
+    if (warp == P8_TMA_WARP && lane == 0) {
+        ptx::prefetch_tensormap(&q_map);
+        ptx::prefetch_tensormap(&k_map);
+        ptx::prefetch_tensormap(&v_map);
+        for (int s = 0; s < SM::MAX_CODES; ++s) {
+            ptx::mbar_init(bar(P8_CFULL + s), 1);
+            ptx::mbar_init(bar(P8_CFREE + s), P8_CONV_WARPS);
+        }
+        for (int s = 0; s < SM::MAX_TILES; ++s) {
+            ptx::mbar_init(bar(P8_FULL + s), P8_CONV_WARPS);
+            ptx::mbar_init(bar(P8_FREE + s), 2);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(bar(P8_QFULL + s), 1);
+            ptx::mbar_init(bar(P8_QREADY + s), 8);
+            ptx::mbar_init(bar(P8_QFREE + s), 1);
+            ptx::mbar_init(bar(P8_SREADY + s), 1);
+            ptx::mbar_init(bar(P8_PREADY + s), 8);
+            ptx::mbar_init(bar(P8_ODONE + s), 1);
+            ptx::mbar_init(bar(P8_TURN + s), 1);
+        }
+        ptx::mbar_init(bar(P8_FINAL), 2);
+        for (int q = 0; q < 3; ++q)
+            for (int i = 0; i < PA_QUEUE; ++i) {
+                ptx::mbar_init(bar(P8_PIECE + q * PA_QUEUE + i), 1);
+                ptx::mbar_init(bar(P8_TAKEN + q * PA_QUEUE + i), 2 + P8_CONV_WARPS + (q ? 8 : 16));
+            }
+        ptx::fence_mbar_init();
+        *abort_flag = 0;
+        for (int k = 0; k < 8; ++k) bad[k] = 0;
+    }
+    if (warp == P8_MMA_WARP) {
+        ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    previous_done();
+    const int n_cta = gridDim.x, cta = blockIdx.x;
+    const uint32_t tmem = *tmem_slot;
+    auto give_up = [&]() {
+        *abort_flag = 1;
+        atomicExch(p.dev_error, MTV_ERR_TIMEOUT);
+    };
+    // a whole warp waits; the same answer for all lanes
+    auto wait = [&](int b, uint32_t parity) {
+        const bool ok = ptx::mbar_wait(bar(b), parity);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if (lane == 0) give_up();
+        return false;
+    };
+    // the n-th piece of a queue; none (or nothing to be had): false
+    auto take = [&](int q, int n, PaPiece &s) {
+        const int at = q * PA_QUEUE + n % PA_QUEUE;
+        if (__any_sync(0xffffffffu, *abort_flag) || !wait(P8_PIECE + at, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
+        const int4 a = queue[at * 2], c = queue[at * 2 + 1];
+        s.b = a.x; s.g = a.y; s.tile0 = a.z; s.t0 = a.w; s.t1 = c.x; s.L = c.y; s.slot = c.z; s.whole = c.w;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(P8_TAKEN + at));
+        __syncwarp();
+        return s.t1 > 0;
+    };
+
+    // (in the branches themselves: where they met again the compiler would count on the smaller number)
+    if (warp == P8_TMA_WARP) {
+        fewer_registers();
+        // ------------------------------------------------------------ pieces; Q and the codes of K and V
+        PaWalk w[3];
+        begin_walks(p, w, cta, n_cta, lane, P8_COST_PAIRS, P8_COST_SINGLE);
+        // One piece more for a queue, or its end: a piece without tiles.  (There is room, or will be without this warp's doing: the queries
+        // of a piece are only requested when the scores of the one before are complete, so this warp is never three pieces ahead.)
+        auto hand_out = [&](int q, int n, PaPiece &s) {
+            const int at = q * PA_QUEUE + n % PA_QUEUE;
+            const bool any = w[q].next(p, p.phase[q > 0], s);
+            if (!any) s = PaPiece{};
+            if (n >= PA_QUEUE && !wait(P8_TAKEN + at, (n / PA_QUEUE - 1) & 1)) { s.t0 = s.t1 = 0; return false; }
+            if (lane == 0) {
+                queue[at * 2] = make_int4(s.b, s.g, s.tile0, s.t0);
+                queue[at * 2 + 1] = make_int4(s.t1, s.L, s.slot, s.whole);
+                ptx::mbar_arrive(bar(P8_PIECE + at));
+            }
+            __syncwarp();
+            return any;
+        };
+        int n_q[2] = {0, 0};
+        const int boxes = PA_KEYS / p.page_rows;
+        const uint32_t q_bytes = (uint32_t)(p.npc * p.G) * 128u * SM::HALVES;
+        // This lane's entry of the table for a key tile, requested here and looked at where the tile is: nothing waits for it meanwhile.
+        // (Where there is no page, or the table names none, zeros are copied.)
+        auto find = [&](const PaPiece &s, int t) {
+            const int key = t * PA_KEYS + lane * p.page_rows;
+            int id = -1;
+            if (lane < boxes && key < s.L + (s.b < 0 ? 0 : p.T))
+                asm volatile("ld.global.s32 %0, [%1];" : "=r"(id)
+                             : "l"(p.pages.table + (int64_t)max(s.b, 0) * p.pages.max_pages + ((key + (s.b < 0 ? 0 : p.shared)) >> p.pages.page_shift)));
+            return id;
+        };
+        auto row_in_page = [&](const PaPiece &s, int t) {
+            return (t * PA_KEYS + lane * p.page_rows + (s.b < 0 ? 0 : p.shared)) & ((1 << p.pages.page_shift) - 1);
+        };
+        // (a CTA has pieces of one phase alone, so both begin at the rings' first stages)
+        auto phase = [&](auto lists) {
+            constexpr int NL = decltype(lists)::value, STAGES = SM::codes(NL);
+            constexpr uint32_t OFF_CODES = SM::OFF_RING + SM::tiles(NL) * SM::TILE;
+            int entry = 0, stage = 0, turns = 0;
+            auto load = [&](const CUtensorMap *map, int id, int row, int g) {
+                if (entry >= STAGES && !wait(P8_CFREE + stage, (turns - 1) & 1)) return false;
+                if (lane == 0) ptx::mbar_arrive_expect_tx(bar(P8_CFULL + stage), SM::CODES);
+                __syncwarp();
+                if (lane < boxes)
+                    ptx::tma_load_4d(sbase + OFF_CODES + stage * SM::CODES + lane * p.page_rows * D, map, bar(P8_CFULL + stage), 0, row, g,
+                                     id >= 0 && id < p.pages.n_pages ? id : p.pages.n_pages);
+                ++entry;
+                if (++stage == STAGES) { stage = 0; ++turns; }
+                return true;
+            };
+            int v_id[NL] = {}, k_id[NL] = {}, n[NL] = {};
+            auto next = [&](int l, PaPiece &s) {
+                if (!hand_out(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
+                k_id[l] = find(s, s.t0);
+                return true;
+            };
+            const bool ok = for_rounds<NL>(next, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+                if (v && !load(&v_map, v_id[l], row_in_page(vs, vt), vs.g)) return false;
+                if (!k) return true;
+                if (!load(&k_map, k_id[l], row_in_page(ks, kt), ks.g)) return false;
+                v_id[l] = k_id[l];
+                if (kt + 1 < ks.t1) k_id[l] = find(ks, kt + 1);
+                if (kt == ks.t0)
+                    for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) {
+                        if (n_q[s] && !wait(P8_QFREE + s, (n_q[s] - 1) & 1)) return false;
+                        ++n_q[s];
+                        if (lane == 0) {
+                            ptx::mbar_arrive_expect_tx(bar(P8_QFULL + s), q_bytes);
+                            for (int h = 0; h < SM::HALVES; ++h)
+                                ptx::tma_load_4d(sbase + s * SM::TILE + h * SM::HALF, &q_map, bar(P8_QFULL + s), h * 64, ks.g * p.G,
+                                                 max(ks.b, 0) * p.T + (ks.tile0 + (NL == 1 ? s : 0)) * p.npc, 0);
+                        }
+                        __syncwarp();
+                    }
+                return true;
+            });
+            if (ok && !*abort_flag) return true;
+            // copies in flight get a bounded chance to land before the CTA can exit
+            for (int e = max(0, entry - STAGES); e < entry; ++e) ptx::mbar_wait(bar(P8_CFULL + e % STAGES), (e / STAGES) & 1);
+            for (int s = 0; s < 2; ++s)
+                if (n_q[s]) ptx::mbar_wait(bar(P8_QFULL + s), (n_q[s] - 1) & 1);
+            return false;
+        };
+        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+    } else if (warp >= P8_CONV_WARP && warp < P8_CONV_WARP + P8_CONV_WARPS) {
+        // ------------------------------------------------------------ codes -> fp16
+        fewer_registers();
+        const int tid = (warp - P8_CONV_WARP) * 32 + lane;
+        constexpr int PER_ROW = D / 16;                        // 16 codes at a time
+        constexpr int TIMES = 128 * PER_ROW / (P8_CONV_WARPS * 32);
+        // chunk (row, c) of 16 codes: two chunks of 8 fp16.  Lanes of the second half of a row store them the other way round, so that the eight lanes
+        // of a row reach eight different groups of banks.
+        const int c = tid % PER_ROW, row0 = tid / PER_ROW, half = c / 4, first_c = 2 * (c % 4) + (D == 128 ? half : 0);
+        constexpr int ROWS = P8_CONV_WARPS * 32 / PER_ROW;     // from one of a thread's chunks to its next; a multiple of 8
+        static_assert(ROWS % 8 == 0, "the swizzle of a thread's chunks is the same");
+        const uint32_t to_a = half * SM::HALF + row0 * 128 + ((first_c ^ (row0 & 7)) << 4), to_b = half * SM::HALF + row0 * 128 + ((first_c ^ 1 ^ (row0 & 7)) << 4);
+        const bool swapped = first_c & 1;
+        int n_piece[2] = {0, 0};
+        auto phase = [&](auto lists) {
+            constexpr int NL = decltype(lists)::value, STAGES = SM::tiles(NL), CODES = SM::codes(NL);
+            const unsigned char *codes = gbase + SM::OFF_RING + STAGES * SM::TILE + tid * 16;
+            unsigned char *tiles = gbase + SM::OFF_RING;
+            int n[NL] = {}, stage = 0, turns = 0, from = 0, from_turns = 0;
+            // first, end: rows whose NaN codes become 0, and behind which all do; the whole tile as it is: end = 128, first = 128.
+            auto convert = [&](int first, int end, bool *odd) {
+                if (!wait(P8_CFULL + from, from_turns & 1)) return false;
+                if (turns && !wait(P8_FREE + stage, (turns - 1) & 1)) return false;
+                const uint4 *src = reinterpret_cast<const uint4 *>(codes + from * SM::CODES);
+                unsigned char *dst = tiles + stage * SM::TILE;
+#pragma unroll
+                for (int i0 = 0; i0 < TIMES; i0 += 4) {
+                    uint4 u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] = src[(i0 + i) * (P8_CONV_WARPS * 32)];
+                    if (first < 128 || end < 128) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int row = row0 + (i0 + i) * ROWS;
+                            if (row >= end) {
+                                u[i] = make_uint4(0u, 0u, 0u, 0u);
+                            } else if (row >= first) {
+                                const uint32_t nx = nan_codes(u[i].x), ny = nan_codes(u[i].y), nz = nan_codes(u[i].z), nw = nan_codes(u[i].w);
+                                if (nx | ny | nz | nw) {
+                                    u[i] = make_uint4(without(u[i].x, nx), without(u[i].y, ny), without(u[i].z, nz), without(u[i].w, nw));
+                                    *odd = true;
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 lo = make_uint4(f16x2_lo(u[i].x), f16x2_hi(u[i].x), f16x2_lo(u[i].y), f16x2_hi(u[i].y));
+                        const uint4 hi = make_uint4(f16x2_lo(u[i].z), f16x2_hi(u[i].z), f16x2_lo(u[i].w), f16x2_hi(u[i].w));
+                        *reinterpret_cast<uint4 *>(dst + to_a + (i0 + i) * ROWS * 128) = swapped ? hi : lo;
+                        *reinterpret_cast<uint4 *>(dst + to_b + (i0 + i) * ROWS * 128) = swapped ? lo : hi;
+                    }
+                }
+                return true;
+            };
+            auto pass = [&]() {
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    ptx::mbar_arrive(bar(P8_FULL + stage));
+                    ptx::mbar_arrive(bar(P8_CFREE + from));
+                }
+                __syncwarp();
+                if (++stage == STAGES) { stage = 0; ++turns; }
+                if (++from == CODES) { from = 0; ++from_turns; }
+            };
+            return for_rounds<NL, P8Rows>([&](int l, P8Rows &s) {
+                PaPiece pc;
+                const bool any = take(NL == 1 ? 0 : 1 + l, n[l]++, pc);
+                s = {pc.t0, pc.t1, pc.b < 0 ? INT_MAX : pc.L};
+                return any;
+            }, [&](int l, bool v, const P8Rows &vs, int vt, bool k, const P8Rows &ks, int kt) {
+                if (v) {
+                    bool odd = false;
+                    const bool last = (vt + 1) * PA_KEYS > vs.L;
+                    if (!convert(last ? max(0, vs.L - vt * PA_KEYS) : 128, last ? min(vs.L + p.T - vt * PA_KEYS, PA_KEYS) : 128, &odd)) return false;
+                    if (last && __any_sync(0xffffffffu, odd) && lane == 0)
+                        for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) bad[s * 4 + (n_piece[s] & 3)] = n_piece[s] + 1;
+                    pass();
+                    if (vt == vs.t1 - 1)
+                        for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) ++n_piece[s];
+                }
+                if (k) {
+                    if (!convert(128, 128, nullptr)) return false;
+                    pass();
+                }
+                return true;
+            });
+        };
+        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+    } else if (warp == P8_MMA_WARP || warp == P8_MMA_WARP + 1) {
+        // ------------------------------------------------------------ products of row tile s
+        fewer_registers();
+        const int s = warp - P8_MMA_WARP;
+        const bool leader = ptx::elect_one();
+        const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_RING, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_RING, SM::HALF);
+        const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * D;
+        int n_p = 0, n_q = 0, n_turn = 0;
+        auto phase = [&](auto lists) {
+            constexpr int NL = decltype(lists)::value, STAGES = SM::tiles(NL);
+            int n[NL] = {}, entry = 0;
+            return for_rounds<NL, P8Tiles>([&](int l, P8Tiles &x) {
+                PaPiece pc;
+                const bool any = take(NL == 1 ? 0 : 1 + l, n[l]++, pc);
+                x = {pc.t0, pc.t1};
+                return any;
+            }, [&](int l, bool v, const P8Tiles &vs, int vt, bool k, const P8Tiles &ks, int kt) {
+                const int ve = entry, ke = entry + (v ? 1 : 0);
+                entry = ke + (k ? 1 : 0);
+                const int v_stage = ve % STAGES, k_stage = ke % STAGES;
+                if (NL == 2 && l != s) {
+                    // the other tile's: waited for and handed back all the same, so that this warp is never a turn of the ring ahead or
+                    // late (a parity wait cannot tell a phase from the one two before or behind)
+                    auto pass = [&](int e, int stage) {
+                        if (!wait(P8_FULL + stage, (e / STAGES) & 1)) return false;
+                        if (lane == 0) ptx::mbar_arrive(bar(P8_FREE + stage));
+                        __syncwarp();
+                        return true;
+                    };
+                    return (!v || pass(ve, v_stage)) && (!k || pass(ke, k_stage));
+                }
+                auto k_there = [&]() { return wait(P8_FULL + k_stage, (ke / STAGES) & 1) && (kt != ks.t0 || wait(P8_QREADY + s, n_q++ & 1)); };
+                // Pairs take turns: the products of a row tile go to the tensor core in one run.  Mixed with the other tile's, both tiles' scores
+                // would come when all are done, both softmaxes would then run at once, and the tensor core wait for both.
+                auto begin_run = [&]() {
+                    if (NL == 2) return true;
+                    const int turn = n_turn++;
+                    return s == 0 && turn == 0 ? true : wait(P8_TURN + s, (turn + s - 1) & 1);
+                };
+                auto end_run = [&]() {
+                    if (NL == 1 && lane == 0) ptx::mbar_arrive(bar(P8_TURN + (s ^ 1)));
+                    __syncwarp();
+                };
+                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be)
+                const bool ahead = v && k && kt != ks.t0;
+                if (ahead && !k_there()) return false;
+                if (v) {
+                    if (!wait(P8_FULL + v_stage, (ve / STAGES) & 1) || !wait(P8_PREADY + s, n_p++ & 1) || !begin_run()) return false;
+                    ptx::tc_fence_after();
+                    const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < PA_KEYS / 16; ++kk)
+                        ptx::mma_ts_elect(t_o, t_s + kk / 4 * 64 + kk % 4 * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
+                    if (vt == vs.t1 - 1) ptx::tc_commit_elect(bar(P8_ODONE + s), leader);
+                    if (!ahead) end_run();
+                }
+                if (k) {
+                    if (!ahead) {
+                        if (!k_there() || !begin_run()) return false;
+                        ptx::tc_fence_after();
+                    }
+                    const uint32_t dk = dk0 + (uint32_t)k_stage * (SM::TILE >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t o = ((kk / 4) * SM::HALF + (kk % 4) * 32) >> 4;
+                        ptx::mma_ss_elect(t_s, dq + o, dk + o, ptx::DESC_HI, SM::IDESC_QK, kk > 0, leader);
+                    }
+                    ptx::tc_commit_elect(bar(P8_SREADY + s), leader);
+                    if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(P8_QFREE + s), leader);
+                    end_run();
+                }
+                if (v) ptx::tc_commit_elect(bar(P8_FREE + v_stage), leader);
+                if (k) ptx::tc_commit_elect(bar(P8_FREE + k_stage), leader);
+                return true;
+            });
+        };
+        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+        // what was issued is complete, and has signalled, before the CTA can exit
+        ptx::tc_commit_elect(bar(P8_FINAL), leader);
+        ptx::mbar_wait(bar(P8_FINAL), 0);
+    } else if (warp < P8_CONV_WARP) {
+        // ------------------------------------------------------------ softmax: thread (row, hf) of row tile s: columns [64 hf, 64 hf + 64)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P8_REGS_MORE));
+        const int s = warp >> 3, hf = (warp >> 2) & 1, qd = warp & 3, row = qd * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
+        const uint32_t t_s = lane_base + s * 128 + hf * 64;      // this half's scores, and P over them
+        const uint32_t t_x = lane_base + s * 128 + (hf ^ 1) * 64;
+        const uint32_t t_o = lane_base + 256 + s * D + hf * (D / 2);
+        const int pair_bar = 2 + s * 4 + qd;
+        const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
+        const bool in_tile = node_in_tile < p.npc;
+        // what the other half of the row has: both put theirs where nothing is any more
+        auto exchange = [&](int col, float v) {
+            tmem_put(t_s + col, v);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            ptx::tc_fence_after();
+            return tmem_get(t_x + col);
+        };
+        int n_s = 0, n_piece = 0;
+        bool ok = true;
+        for (int f = 0; f < 2 && ok; ++f) {
+            const PaPhase &ph = p.phase[f];
+            PaPiece pc;
+            for (int n = 0; ok && take(f ? 1 + s : 0, n, pc); ++n) {
+                const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
+                const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
+                const bool some = __any_sync(0xffffffffu, mine);
+                // ---- the queries: each thread of a row takes half of its columns
+                if (!wait(P8_QFULL + s, n_piece & 1)) { ok = false; break; }
+                float sc;
+                {
+                    constexpr int CHUNKS = D / 16;
+                    unsigned char *q = gbase + s * SM::TILE + (D == 128 ? hf * SM::HALF : 0) + row * 128;
+                    const int c0 = D == 128 ? 0 : hf * CHUNKS;
+                    uint32_t most = 0u;
+#pragma unroll 4
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(q + (((c0 + c) ^ (row & 7)) << 4));
+                        most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u.x)), abs2_bf16(u.y)), abs2_bf16(u.z)), abs2_bf16(u.w));
+                    }
+                    most = max(most, __float_as_uint(exchange(X_COL, __uint_as_float(most))));
+                    const float2 factor = row_factor(most);
+#pragma unroll 4
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        uint4 *at = reinterpret_cast<uint4 *>(q + (((c0 + c) ^ (row & 7)) << 4));
+                        const uint4 u = *at;
+                        *at = make_uint4(to_f16(u.x, factor.x), to_f16(u.y, factor.x), to_f16(u.z, factor.x), to_f16(u.w, factor.x));
+                    }
+                    sc = p.scale_log2 * __ldg(pp.k_scale + pc.g) * factor.y;
+                    ptx::tc_fence_before();
+                    ptx::fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar(P8_QREADY + s));
+                }
+                const float2 sc2 = make_float2(sc, sc);
+                // visibility of the tree rows as 32-bit words; the rows in front of them are visible to every node, those behind to none
+                uint4 anc = make_uint4(0u, 0u, 0u, 0u);
+                if (mine && pc.b >= 0) anc = reinterpret_cast<const uint4 *>(p.anc)[node];
+                auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w == 0 ? anc.x : w == 1 ? anc.y : w == 2 ? anc.z : w == 3 ? anc.w : 0u; };
+                float m_used = -INFINITY, l = 0.f;
+                for (int t = pc.t0; t < pc.t1; ++t) {
+                    if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
+                    ptx::tc_fence_after();
+                    if (some) {
+                        uint32_t pk[32];                         // fp16 pairs
+                        float2 la, lb;
+                        bool move = t == pc.t0;
+                        for (;;) {
+                            uint32_t sr[64];
+                            ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                            ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+                            if ((t + 1) * PA_KEYS > pc.L) {
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    const int a0 = t * PA_KEYS + hf * 64 + h * 32 - pc.L;      // tree row of the first column
+                                    const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e)
+                                        if (!((vis >> e) & 1u)) sr[h * 32 + e] = 0xff800000u;   // -inf
+                                }
+                            }
+                            if (move) {
+                                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                                for (int e = 0; e < 64; e += 8)
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
+                                float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * sc;
+                                mxs = max_nan(mxs, exchange(X_COL, mxs));
+                                if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+                                const float m_new = mxs <= m_used ? m_used : mxs;            // (a NaN is taken over)
+                                const bool need = m_new != m_used && m_used != -INFINITY && mine;
+                                if (__any_sync(0xffffffffu, need)) {
+                                    const float alpha = need ? ex2(m_used - m_new) : 1.f;
+#pragma unroll 1
+                                    for (int h = 0; h < D / 32; ++h) {
+                                        uint32_t o[16];
+                                        ptx::tmem_ld16(t_o + h * 16, o);
+                                        ptx::tmem_ld_wait_for16(o);
+#pragma unroll
+                                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                                        ptx::tmem_st16(t_o + h * 16, o);
+                                    }
+                                    l *= alpha;
+                                }
+                                m_used = m_new;
+                            }
+                            const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+                            const float2 nm2 = make_float2(P8_SHIFT - m_eff, P8_SHIFT - m_eff);
+                            la = lb = make_float2(0.f, 0.f);
+                            float px = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const uint32_t *x = sr + 2 * e;
+                                const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
+                                const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
+                                float2 p01, p23;
+                                if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                    px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
+                                    p01 = exp2_poly2(x01);
+                                    p23 = exp2_poly2(x23);
+                                } else {
+                                    p01 = make_float2(ex2(x01.x), ex2(x01.y));
+                                    p23 = make_float2(ex2(x23.x), ex2(x23.y));
+                                }
+                                la = __fadd2_rn(la, p01);
+                                lb = __fadd2_rn(lb, p23);
+                                pk[e] = pack2_f16(p01.x, p01.y);
+                                pk[e + 1] = pack2_f16(p23.x, p23.y);
+                            }
+                            if (move) break;
+                            // a sum that is too large, infinite or NaN (a weight then may be beyond fp16), and a row that has met no visible key yet
+                            const bool ask = !(max_nan(max_nan(la.x, la.y), max_nan(lb.x, lb.y)) < 65504.f) || !(px <= P8_LIMIT) || m_used == -INFINITY;
+                            if (!any_of_rows(pair_bar, mine && ask)) break;
+                            move = true;
+                        }
+                        l += (la.x + la.y) + (lb.x + lb.y);
+                        ptx::tmem_st32(t_s, pk);
+                        if (t == pc.t1 - 1) l += exchange(X_COL + 1, l);      // the row's sum; S is another tile's behind this one's P
+                        ptx::tmem_st_wait();
+                    }
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar(P8_PREADY + s));
+                }
+                if (!ok || !wait(P8_ODONE + s, n_piece & 1)) { ok = false; break; }
+                ptx::tc_fence_after();
+                if (some) {
+                    const bool odd = bad[s * 4 + (n_piece & 3)] == n_piece + 1;
+                    const bool direct = p.shared == 0 && pc.whole;
+                    const float vs = __ldg(pp.v_scale + pc.g), factor = direct ? vs / l : vs;
+                    const int slot_row = f ? row : s * 128 + row;
+                    float *o_out = ph.o + ((size_t)pc.slot * ph.rows * (D / 8) + (size_t)(hf * (D / 16)) * ph.rows + slot_row) * 8;
+                    __nv_bfloat16 *out = p.out + (((size_t)max(pc.b, 0) * p.T + node) * p.Hq + pc.g * p.G + head) * D + hf * (D / 2);
+#pragma unroll 1
+                    for (int h = 0; h < D / 32; ++h) {
+                        uint32_t o[16];
+                        ptx::tmem_ld16(t_o + h * 16, o);
+                        ptx::tmem_ld_wait_for16(o);
+                        if (!mine) continue;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                        if (odd) {
+                            // V codes that the tensor core did not see: NaN with any weight is NaN
+                            for (int a = max(0, pc.t0 * PA_KEYS - pc.L); a < p.T && pc.L + a < pc.t1 * PA_KEYS; ++a) {
+                                if (!(anc_word(a >> 5) >> (a & 31) & 1)) continue;
+                                const int64_t at = p.pages.row(pc.b, p.shared + pc.L + a);
+                                if (at < 0) continue;
+                                const uint8_t *v = pp.v + at + pc.g * p.pages.stride_h + hf * (D / 2) + h * 16;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+                                    if ((v[e] & 0x7fu) == 0x7fu) o[e] = 0x7fffffffu;
+                            }
+                        }
+                        if (direct) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) w[e] = pack2_bf16(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+                            *reinterpret_cast<uint4 *>(out + h * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4 *>(out + h * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                        } else {
+                            ptx::st_global_32(o_out + (size_t)(2 * h) * ph.rows * 8, *reinterpret_cast<const uint32_t(*)[8]>(&o[0]));
+                            ptx::st_global_32(o_out + (size_t)(2 * h + 1) * ph.rows * 8, *reinterpret_cast<const uint32_t(*)[8]>(&o[8]));
+                        }
+                    }
+                    if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(l == 0.f ? -INFINITY : m_used - P8_SHIFT, l);   // (what weighs 1)
+                }
+                ++n_piece;
+            }
+        }
+    } else {
+        fewer_registers();                // (all warps of a warpgroup)
+    }
+    // ---- nobody leaves while the tensor core may still work for the CTA
+    __syncwarp();
+    ptx::tc_fence_before();
+    asm volatile("bar.sync 1, %0;" ::"n"(P8_THREADS) : "memory");
+    ptx::tc_fence_after();
+    if (warp == P8_MMA_WARP) ptx::tmem_dealloc(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------------------- thin items
+// At most 16 query rows against a KV head's keys (plain decoding; the smallest trees): nothing but the bytes counts.  As for the bf16 cache, warps of
+// their own with mma.sync, K and V straight from global memory into registers.  A contraction's order is free as long as both operands have it, and so is
+// the order of O's columns: 16 bytes of a K row are four products' B operands of a thread, converted as they stand; 16 bytes of V rows (8 at D = 64) are
+// its column in 16 products (8), two keys' codes side by side by a byte permutation in front of the conversion.
+// A CTA of four warps walks a run of the line of all thin items, 32 keys to a warp at a time; K of the next keys is requested when the scores are taken,
+// V of them when the products with V are, so that each is on its way during the other's work.  At a piece's end the warps join in shared memory.
+constexpr int T8_WARPS = 4, T8_KEYS = 32, T8_STEP = T8_WARPS * T8_KEYS;
+constexpr int T8_ENDS = 2;                 // what an item's start and end take, in steps of 128 keys
+constexpr float T8_SHIFT = 7.f, T8_SLACK = 8.f;   // weights are 2^SHIFT at the reference, which may be SLACK too small: below 2^16
+
+__device__ __forceinline__ void mma16816_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <int D>
+__global__ void __launch_bounds__(T8_WARPS * 32, 2)
+paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
+    using Line = ThinLine<T8_STEP, T8_ENDS>;
+    constexpr int C = D / 64;              // 64-column parts of a row: 16 bytes of each are a thread's
+    constexpr int J = D / 8, JW = J / 4;   // products of 8 columns of O; words of a V row that are a thread's
+    const PaParams &p = pp.a;
+    __shared__ float o_x[T8_WARPS][TH_ROWS][D + 4];
+    __shared__ float2 ml_x[T8_WARPS][TH_ROWS];
+    __shared__ int start[5];               // x0, x1, S, b, idx
+    let_next_start();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r0 = lane / 4, quad = lane % 4;
+    const PaPhase &ph = p.phase[2];
+    const int worker = blockIdx.x, workers = gridDim.x;
+    previous_done();
+    if (warp == 0) Line::begin(p, worker, workers, lane, start);
+    __syncthreads();
+    const int x0 = start[0], x1 = start[1];
+    int S = start[2], b = start[3], idx = start[4];
+    int L = 0, cost = 0;                   // keys of the item (prefix: the shared ones; else its own in front of the tree)
+    auto load_item = [&]() {
+        if (b < 0) {
+            L = p.shared;
+            cost = Line::steps(p.shared) + T8_ENDS;
+        } else {
+            cost = Line::cost_of(p, b);
+            L = p.seq_lens[b] - p.shared;
+        }
+    };
+    if (x0 < x1) load_item();
+    while (S < x1) {
+        if (idx >= (b < 0 ? ph.prefix_items : ph.seq_items) || cost == 0) {
+            if (++b >= p.B) break;
+            idx = 0;
+            load_item();
+            continue;
+        }
+        const int steps = cost - T8_ENDS;
+        const int t0 = max(0, min(x0 - S - T8_ENDS, steps)), t1 = max(0, min(x1 - S - T8_ENDS, steps));
+        S += cost;
+        const int g = idx++;
+        if (t0 >= t1) continue;
+        const int item = b < 0 ? g : ph.prefix_items + b * ph.seq_items + g;
+        const bool own = b >= 0;
+        const int n_keys = L + (own ? p.T : 0), key0 = own ? p.shared : 0, rows = (own ? p.T : p.B * p.T) * p.G;
+        if (threadIdx.x == 0) {
+            if (t0 == 0) ph.span[item].x = worker;
+            if (t1 == steps) ph.span[item].y = worker;
+        }
+        // ---- this warp's blocks of 32 keys: key (t * T8_WARPS + warp) * 32, in two halves that may lie on two pages
+        const int32_t *table = p.pages.table + (int64_t)max(b, 0) * p.pages.max_pages;
+        auto key_of = [&](int t, int half) { return (t * T8_WARPS + warp) * T8_KEYS + half * 16; };
+        auto page_of = [&](int t, int half) { return t < t1 && key_of(t, half) < n_keys ? table[(key_of(t, half) + key0) >> p.pages.page_shift] : -1; };
+        auto row_at = [&](int t, int half, int id) {     // byte offset of the half's first row; < 0: there is none
+            return id < 0 || id >= p.pages.n_pages ? -1ll
+                   : (long long)id * p.pages.stride_page + (long long)((key_of(t, half) + key0) & ((1 << p.pages.page_shift) - 1)) * p.pages.stride_t +
+                         g * p.pages.stride_h;
+        };
+        uint4 kx[4][C];                    // keys r0 + 8 h of the block
+        uint32_t vx[2][4][JW];             // of half kk: keys 2 quad, 2 quad + 1 and the same + 8; columns r0 * J + [0, J)
+        auto load_k = [&](const long long (&at)[2]) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    kx[h][c] = at[h / 2] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(pp.k + at[h / 2] + (r0 + 8 * (h % 2)) * p.pages.stride_t + c * 64 + quad * 16))
+                                              : make_uint4(0u, 0u, 0u, 0u);
+        };
+        auto load_v = [&](const long long (&at)[2], int t) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int key = 2 * quad + (k & 1) + 8 * (k >> 1);
+                    const uint8_t *src = pp.v + at[kk] + key * p.pages.stride_t + r0 * J;
+                    const bool is = at[kk] >= 0 && key_of(t, kk) + key < n_keys;     // rows behind the last key may hold anything
+                    if constexpr (JW == 4) {
+                        const uint4 u = is ? __ldg(reinterpret_cast<const uint4 *>(src)) : make_uint4(0u, 0u, 0u, 0u);
+                        vx[kk][k][0] = u.x; vx[kk][k][1] = u.y; vx[kk][k][2] = u.z; vx[kk][k][3] = u.w;
+                    } else {
+                        const uint2 u = is ? __ldg(reinterpret_cast<const uint2 *>(src)) : make_uint2(0u, 0u);
+                        vx[kk][k][0] = u.x; vx[kk][k][1] = u.y;
+                    }
+                }
+        };
+        int id_next[2];
+        long long at[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            at[h] = row_at(t0, h, page_of(t0, h));
+            id_next[h] = page_of(t0 + 1, h);
+        }
+        load_k(at);
+        load_v(at, t0);
+        // ---- the query rows as A operands: product (c, i) has columns c * 64 + quad * 16 + 4 i + [0, 2) and [2, 4) of rows r0 and r0 + 8
+        uint32_t qa[C][4][4];
+        uint32_t see[2];                   // tree rows that are visible to rows r0 and r0 + 8 (at most 16 nodes)
+        float sc[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = r0 + 8 * h, n = r / p.G;
+            const bool is = r < rows;
+            const __nv_bfloat16 *src = p.q + (((size_t)(own ? b * p.T : 0) + n) * p.Hq + g * p.G + (r - n * p.G)) * D + quad * 16;
+            uint32_t most = 0u;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const uint4 u = is ? *reinterpret_cast<const uint4 *>(src + c * 64) : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 v = is ? *reinterpret_cast<const uint4 *>(src + c * 64 + 8) : make_uint4(0u, 0u, 0u, 0u);
+                qa[c][0][h] = u.x; qa[c][0][h + 2] = u.y; qa[c][1][h] = u.z; qa[c][1][h + 2] = u.w;
+                qa[c][2][h] = v.x; qa[c][2][h + 2] = v.y; qa[c][3][h] = v.z; qa[c][3][h + 2] = v.w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = larger_bits(larger_bits(most, abs2_bf16(qa[c][i][h])), abs2_bf16(qa[c][i][h + 2]));
+            }
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const float2 factor = row_factor(most);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    qa[c][i][h] = to_f16(qa[c][i][h], factor.x);
+                    qa[c][i][h + 2] = to_f16(qa[c][i][h + 2], factor.x);
+                }
+            sc[h] = p.scale_log2 * __ldg(pp.k_scale + g) * factor.y;
+            see[h] = is && own ? (uint32_t)p.anc[n * 2] : 0u;
+        }
+        float o[J][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        for (int t = t0; t < t1; ++t) {
+            const int first = key_of(t, 0);
+            if (first >= n_keys) break;    // (the item's last step: no keys for this warp)
+            // ---- scores of keys 8 h + [0, 8): c0, c1 row r0, c2, c3 row r0 + 8, keys 8 h + 2 quad and 8 h + 2 quad + 1
+            float x[4][4] = {};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const uint32_t w[4] = {kx[h][c].x, kx[h][c].y, kx[h][c].z, kx[h][c].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma16816_f16(x[h], qa[c][i], f16x2_lo(w[i]), f16x2_hi(w[i]));
+                }
+            const long long at_now[2] = {at[0], at[1]};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                at[h] = row_at(t + 1, h, id_next[h]);
+                id_next[h] = page_of(t + 2, h);
+            }
+            if (t + 1 < t1) load_k(at);
+            const bool edge = first + T8_KEYS > L;
+            if (edge) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int a = first + 8 * h + 2 * quad + (e & 1) - L;
+                        if (a >= 0 && (!own || a >= p.T || !(see[e >> 1] >> a & 1u))) x[h][e] = -INFINITY;
+                    }
+            }
+            float mx[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                mx[r] = max_nan(max3_nan(x[0][2 * r], x[0][2 * r + 1], x[1][2 * r]), max3_nan(x[1][2 * r + 1], x[2][2 * r], x[2][2 * r + 1]));
+                mx[r] = max3_nan(mx[r], x[3][2 * r], x[3][2 * r + 1]);
+                mx[r] = max_nan(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+                mx[r] = max_nan(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2)) * sc[r];
+                if (mx[r] == INFINITY) mx[r] = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+            }
+            if (__any_sync(0xffffffffu, !(mx[0] <= m[0] + T8_SLACK) || !(mx[1] <= m[1] + T8_SLACK))) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float m_new = mx[r] <= m[r] ? m[r] : mx[r];
+                    const float w = m[r] == -INFINITY ? 0.f : ex2(m[r] - m_new);
+                    m[r] = m_new;
+                    l[r] *= w;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) { o[j][2 * r] *= w; o[j][2 * r + 1] *= w; }
+                }
+            }
+            const float me[2] = {m[0] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[0], m[1] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[1]};
+            uint32_t pa[2][4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float w0 = ex2(fmaf(x[h][2 * r], sc[r], me[r])), w1 = ex2(fmaf(x[h][2 * r + 1], sc[r], me[r]));
+                    l[r] += w0 + w1;
+                    pa[h / 2][h % 2 * 2 + r] = pack2_f16(w0, w1);
+                }
+            bool odd = false;
+            if (edge && own) {
+                // NaN codes of the tree's rows are left out here and given below to the rows that see them
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int e = 0; e < JW; ++e) {
+                            const uint32_t nans = nan_codes(vx[kk][k][e]);
+                            if (nans) { vx[kk][k][e] = without(vx[kk][k][e], nans); odd = true; }
+                        }
+                odd = __any_sync(0xffffffffu, odd);
+            }
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int w = 0; w < JW; ++w) {
+                    // keys 2 quad and 2 quad + 1 side by side, columns 4 w + [0, 2) and [2, 4); the same of the keys 8 behind
+                    const uint32_t a = __byte_perm(vx[kk][0][w], vx[kk][1][w], 0x5140), a2 = __byte_perm(vx[kk][0][w], vx[kk][1][w], 0x7362);
+                    const uint32_t c = __byte_perm(vx[kk][2][w], vx[kk][3][w], 0x5140), c2 = __byte_perm(vx[kk][2][w], vx[kk][3][w], 0x7362);
+                    mma16816_f16(o[4 * w], pa[kk], f16x2_lo(a), f16x2_lo(c));
+                    mma16816_f16(o[4 * w + 1], pa[kk], f16x2_hi(a), f16x2_hi(c));
+                    mma16816_f16(o[4 * w + 2], pa[kk], f16x2_lo(a2), f16x2_lo(c2));
+                    mma16816_f16(o[4 * w + 3], pa[kk], f16x2_hi(a2), f16x2_hi(c2));
+                }
+            if (t + 1 < t1) load_v(at, t + 1);
+            if (odd)
+                for (int k = 0; k < T8_KEYS; ++k) {
+                    const int a = first + k - L;
+                    if (a >= p.T) break;
+                    if (at_now[k / 16] < 0) continue;
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint8_t y = pp.v[at_now[k / 16] + k % 16 * p.pages.stride_t + (2 * quad + (e & 1)) * J + j];
+                            // (the shared keys and those in front of the tree are seen by all)
+                            if ((y & 0x7fu) == 0x7fu && (a < 0 || (see[e >> 1] >> a & 1u))) o[j][e] = __int_as_float(0x7fffffff);
+                        }
+                }
+        }
+        // ---- the four warps' shares of a row are joined: O[row][column (2 quad + (e & 1)) * J + j]
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            if (quad == 0) ml_x[warp][r0 + 8 * h] = make_float2(m[h], l[h]);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                o_x[warp][r0 + 8 * h][2 * quad * J + j] = o[j][2 * h];
+                o_x[warp][r0 + 8 * h][(2 * quad + 1) * J + j] = o[j][2 * h + 1];
+            }
+        }
+        __syncthreads();
+        const bool direct = p.shared == 0 && t1 - t0 == steps;      // the item's only piece
+        const size_t slot = (size_t)item + worker;
+        const float vs = __ldg(pp.v_scale + g);
+        for (int e = threadIdx.x; e < rows * (D / 8); e += T8_WARPS * 32) {
+            const int row = e % rows, chunk = e / rows;
+            float mm = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < T8_WARPS; ++w) mm = max_nan(mm, ml_x[w][row].x);
+            float acc[8] = {}, ll = 0.f;
+#pragma unroll
+            for (int w = 0; w < T8_WARPS; ++w) {
+                const float2 ml = ml_x[w][row];
+                const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
+                ll = fmaf(f, ml.y, ll);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] = fmaf(f, o_x[w][row][chunk * 8 + k], acc[k]);
+            }
+            const float factor = direct ? vs / ll : vs;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] *= factor;
+            if (direct) {
+                const int n = row / p.G;
+                *reinterpret_cast<uint4 *>(p.out + (((size_t)b * p.T + n) * p.Hq + g * p.G + row - n * p.G) * D + chunk * 8) =
+                    make_uint4(pack2_bf16(acc[0], acc[1]), pack2_bf16(acc[2], acc[3]), pack2_bf16(acc[4], acc[5]), pack2_bf16(acc[6], acc[7]));
+            } else {
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(acc[k]);
+                ptx::st_global_32(ph.o + ((slot * (D / 8) + chunk) * TH_ROWS + row) * 8, w);
+                if (chunk == 0) ph.ml[slot * TH_ROWS + row] = make_float2(ll == 0.f ? -INFINITY : mm - T8_SHIFT, ll);
+            }
+        }
+        __syncthreads();                   // before the next piece's shares
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host
+template <int D>
+static int launch_paged8(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const P8Params &p, cudaStream_t stream) {
+    static PerDeviceOnce once;
+    bool *done = once.flag();
+    if (!done || !*done) {
+        MTV_CUDA_CHECK(cudaFuncSetAttribute(paged_attn8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, P8Smem<D>::TOTAL));
+        if (done) *done = true;
+    }
+    const PaPhase (&ph)[3] = p.a.phase;
+    if (ph[0].prefix_items + ph[0].seq_items + ph[1].prefix_items + ph[1].seq_items)
+        MTV_CUDA_CHECK(launch_dependent(paged_attn8_kernel<D>, dim3(sm_count()), P8_THREADS, P8Smem<D>::TOTAL, stream, q, k, v, p));
+    if (ph[2].prefix_items + ph[2].seq_items) MTV_CUDA_CHECK(launch_dependent(paged_attn8_thin_kernel<D>, dim3(2 * sm_count()), T8_WARPS * 32, 0, stream, p));
+    return pa_combine(p.a, D, stream);
+}
+
+}  // namespace mtv
+
+extern "C" int tree_verify_attention_paged_fp8(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, const mtv_bf16 *q, const uint8_t *k_pool,
+                                               const uint8_t *v_pool, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                                               int shared_len, const int32_t *seq_lens, const float *k_scale, const float *v_scale, float scale,
+                                               mtv_bf16 *out, int32_t *status, void *ws, size_t ws_bytes, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("tree_verify_attention_paged_fp8");
+    if (!tree || !tree->on_device || !q || !k_pool || !v_pool || !seq_lens || !k_scale || !v_scale || !out || !ws) return MTV_ERR_INVALID_ARG;
+    if (B < 1 || Hq < 1 || Hkv < 1 || shared_len < 0 || !(scale >= 0.f) || scale > 1e30f) return MTV_ERR_INVALID_ARG;
+    if (!pa_sizes_ok(tree, B, Hq, Hkv, D, shared_len)) return MTV_ERR_UNSUPPORTED_SHAPE;
+    P8Params pp = {};
+    PaParams &p = pp.a;
+    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D, 16);
+    if (rc != MTV_OK) return rc;
+    if (shared_len % pool->page_size || shared_len > (int64_t)max_pages * pool->page_size ||
+        (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) || ((uintptr_t)ws & 255))
+        return MTV_ERR_INVALID_ARG;
+    p.T = tree->T; p.B = B; p.G = Hq / Hkv; p.Hq = Hq; p.Hkv = Hkv;
+    p.shared = shared_len;
+    if (ws_bytes < pa_plan(p.phase, sm_count(), p.T, B, p.G, Hkv, D, shared_len, static_cast<char *>(ws))) return MTV_ERR_WORKSPACE;
+    if (!pa_lines_ok(p.phase, B, shared_len, (int64_t)max_pages * pool->page_size)) return MTV_ERR_UNSUPPORTED_SHAPE;
+    p.npc = 128 / p.G;
+    p.page_rows = pool->page_size < PA_KEYS ? pool->page_size : PA_KEYS;
+    p.seq_lens = seq_lens; p.anc = tree->d_anc;
+    p.q = reinterpret_cast<const __nv_bfloat16 *>(q);
+    p.out = reinterpret_cast<__nv_bfloat16 *>(out);
+    p.status = status; p.dev_error = tree->d_error;
+    p.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
+    pp.k = k_pool; pp.v = v_pool; pp.k_scale = k_scale; pp.v_scale = v_scale;
+    CUtensorMap q_map, k_map, v_map;
+    {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)B * p.T, 1};
+        const cuuint64_t str[3] = {(cuuint64_t)D * 2, (cuuint64_t)Hq * D * 2, (cuuint64_t)B * p.T * Hq * D * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)p.npc, 1};
+        if (!encode_map_bf16(&q_map, q, 4, dims, str, box)) return MTV_ERR_CUDA;
+    }
+    {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)pool->page_size, (cuuint64_t)Hkv, (cuuint64_t)pool->n_pages};
+        const cuuint64_t str[3] = {(cuuint64_t)pool->stride_t, (cuuint64_t)pool->stride_h, (cuuint64_t)pool->stride_page};
+        const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)p.page_rows, 1, 1};
+        if (!encode_map_bytes(&k_map, k_pool, 4, dims, str, box) || !encode_map_bytes(&v_map, v_pool, 4, dims, str, box)) return MTV_ERR_CUDA;
+    }
+    return D == 128 ? launch_paged8<128>(q_map, k_map, v_map, pp, (cudaStream_t)stream) : launch_paged8<64>(q_map, k_map, v_map, pp, (cudaStream_t)stream);
+}

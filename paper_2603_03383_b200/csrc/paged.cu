@@ -1,6 +1,9 @@
 // A K/V cache in pages: rows appended with the rotary embedding, and the accepted rows of a step moved to the front of the tree's
 // slots (Section 3.2, "Tensorization of Tree Topology" and "Zero-Copy Retrieval"; the paper's own cache is contiguous).
 // Slot s of sequence b is row s % page of page page_table[b][s / page]; page sizes are powers of two.
+// The rows are bf16, or e4m3 codes with one scale per layer and head: then K rows are rotated in fp32 and rounded once, to the code, and rows
+// can be read back as bf16.
+#include "fp8.cuh"
 #include "paged_common.cuh"
 
 namespace mtv {
@@ -9,6 +12,15 @@ constexpr int PAGED_THREADS = 256;
 constexpr int APPEND_DEEP = 1;       // pairs of 16-byte chunks that a thread asks for at a time
 constexpr int PAGED_MAX_HEADS = 4096;
 constexpr int APPEND_ROWS = 2;       // rows of a block
+
+__device__ __forceinline__ void unpack8(const uint4 &u, float (&x)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[2 * k] = __uint_as_float(w[k] << 16);
+        x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+}
 
 // (x[d], x[d + D/2]) -> (x[d] cos - x[d + D/2] sin, x[d + D/2] cos + x[d] sin) for 8 columns, in fp32, rounded once to bf16
 __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float *cs, const float *sn) {
@@ -25,11 +37,27 @@ __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float *cs, con
     }
 }
 
+// The same times `factor`, rounded once to codes; cs null: nothing is rotated.
+__device__ __forceinline__ void quantise8(const uint4 &a, const uint4 &b, const float *cs, const float *sn, float factor, uint2 &ca, uint2 &cb) {
+    float x[8], y[8];
+    unpack8(a, x);
+    unpack8(b, y);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float c = cs ? cs[k] : 1.f, s = cs ? sn[k] : 0.f, x0 = x[k], y0 = y[k];
+        x[k] = (cs ? x0 * c - y0 * s : x0) * factor;
+        y[k] = (cs ? y0 * c + x0 * s : y0) * factor;
+    }
+    ca = e4m3x8(x);
+    cb = e4m3x8(y);
+}
+
 struct AppendParams {
     int B, T, n_rows, Hq, Hkv, D, n_layers, layers_per_block, row_blocks;
     const __nv_bfloat16 *q, *k_new, *v_new;
     __nv_bfloat16 *q_out;
-    __nv_bfloat16 *const *k_pools, *const *v_pools;
+    void *const *k_pools, *const *v_pools;
+    const float *k_scale, *v_scale;            // [n_layers][Hkv], or null: the pools are bf16
     PagedRef pages;
     const int32_t *seq_lens, *starts, *depth;   // starts: ragged rows, position = slot; or null: T tree nodes per sequence
     double log2_theta;
@@ -69,8 +97,8 @@ template <bool VEC> __device__ __forceinline__ void store8(__nv_bfloat16 *p, con
 // Measured: trees of 4 x 64 nodes, 32 + 2 x 8 heads of 128, 32 layers: 35.7 us (201 MB, 5.6 TB/s; 31.1 at the memory's rate); five prompts of
 // 3005 tokens, 28 + 2 x 4 heads, one layer: 13.5 us (8.6): 1503 blocks are 1.7 waves, and each begins with the chain length, page, angle.  Two rows a block: four
 // take 34.9 and 15.4, one 36.5 and 17.4; two pairs in flight per thread 34.8 and 14.9, as fewer blocks fit.
-// VEC: the rows begin at multiples of 16 bytes.
-template <int D, bool VEC>
+// VEC: the rows begin at multiples of 16 bytes.  FP8: the pools hold codes.
+template <int D, bool VEC, bool FP8>
 __global__ void __launch_bounds__(PAGED_THREADS)
 kv_append_rope_paged_kernel(const AppendParams p) {
     constexpr int HALF = D / 2, PER_HEAD = D / 16, SLOTS = PAGED_THREADS / PER_HEAD;    // threads of a head; heads at a time
@@ -97,6 +125,7 @@ kv_append_rope_paged_kernel(const AppendParams p) {
     const int step_rows = SLOTS / heads, step_heads = SLOTS - step_rows * heads;
     int row = tid / PER_HEAD / heads, h = tid / PER_HEAD - row * heads;
     uint4 x[APPEND_DEEP][2];
+    float scale[APPEND_DEEP];
     int at_row[APPEND_DEEP], at_h[APPEND_DEEP];
     auto request = [&] {
 #pragma unroll
@@ -110,6 +139,7 @@ kv_append_rope_paged_kernel(const AppendParams p) {
                 const __nv_bfloat16 *src = g < 0 ? p.q + (i * p.Hq + h) * D : g < p.Hkv ? p.k_new + (i * p.Hkv + g) * D : p.v_new + (i * p.Hkv + g - p.Hkv) * D;
                 x[k][0] = load8<VEC>(src + c);
                 x[k][1] = load8<VEC>(src + HALF + c);
+                if (FP8 && g >= 0) scale[k] = g < p.Hkv ? p.k_scale[(l0 + row / APPEND_ROWS) * p.Hkv + g] : p.v_scale[(l0 + row / APPEND_ROWS) * p.Hkv + g - p.Hkv];
             }
             row += step_rows;
             h += step_heads;
@@ -162,7 +192,18 @@ kv_append_rope_paged_kernel(const AppendParams p) {
             } else {
                 if (dst_of[j] < 0) continue;
                 const bool is_v = g >= p.Hkv;
-                dst = (is_v ? p.v_pools : p.k_pools)[layer] + dst_of[j] + (g - (is_v ? p.Hkv : 0)) * p.pages.stride_h;
+                const int64_t at = dst_of[j] + (g - (is_v ? p.Hkv : 0)) * p.pages.stride_h;
+                void *pool = (is_v ? p.v_pools : p.k_pools)[layer];
+                if constexpr (FP8) {
+                    uint2 a, b;
+                    const float factor = __frcp_rn(scale[k]);
+                    if (is_v) quantise8(x[k][0], x[k][1], nullptr, nullptr, factor, a, b);
+                    else quantise8(x[k][0], x[k][1], &cs[j][c], &sn[j][c], factor, a, b);
+                    *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + at + c) = a;
+                    *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + at + HALF + c) = b;
+                    continue;
+                }
+                dst = static_cast<__nv_bfloat16 *>(pool) + at;
             }
             if (g < p.Hkv) rotate8(x[k][0], x[k][1], &cs[j][c], &sn[j][c]);
             store8<VEC>(dst + c, x[k][0]);
@@ -173,6 +214,7 @@ kv_append_rope_paged_kernel(const AppendParams p) {
     }
 }
 
+template <bool FP8>
 static int launch_append(AppendParams &p, cudaStream_t stream) {
     p.row_blocks = (p.n_rows + APPEND_ROWS - 1) / APPEND_ROWS;
     // enough blocks to fill the device a few times over, as many layers per block as that leaves
@@ -182,29 +224,29 @@ static int launch_append(AppendParams &p, cudaStream_t stream) {
     p.layers_per_block = (int)per;
     const int report = p.status || !p.row_blocks ? (p.B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32) : 0;
     const bool vec = (((uintptr_t)p.q | (uintptr_t)p.q_out | (uintptr_t)p.k_new | (uintptr_t)p.v_new) & 15) == 0;
-    auto kernel = p.D == 128 ? (vec ? kv_append_rope_paged_kernel<128, true> : kv_append_rope_paged_kernel<128, false>)
-                             : (vec ? kv_append_rope_paged_kernel<64, true> : kv_append_rope_paged_kernel<64, false>);
+    auto kernel = p.D == 128 ? (vec ? kv_append_rope_paged_kernel<128, true, FP8> : kv_append_rope_paged_kernel<128, false, FP8>)
+                             : (vec ? kv_append_rope_paged_kernel<64, true, FP8> : kv_append_rope_paged_kernel<64, false, FP8>);
     MTV_CUDA_CHECK(launch_dependent(kernel, dim3(p.row_blocks + report, (unsigned)((p.n_layers + per - 1) / per)),
                                     PAGED_THREADS, 0, stream, p));
     return MTV_OK;
 }
 
 static int append_args(AppendParams &p, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q, mtv_bf16 *q_out, const mtv_bf16 *k_new,
-                       const mtv_bf16 *v_new, mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool,
+                       const mtv_bf16 *v_new, void *const *k_pools, void *const *v_pools, int code_bytes, const mtv_pool_layout *pool,
                        const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta, int32_t *status, bool no_rows) {
     if (!k_pools || !v_pools || !seq_lens) return MTV_ERR_INVALID_ARG;
     if (!no_rows && (!q || !q_out || !k_new || !v_new)) return MTV_ERR_INVALID_ARG;
     if (B < 1 || Hq < 1 || Hkv < 1 || n_layers < 1 || !(rope_theta >= 0.f && rope_theta < INFINITY)) return MTV_ERR_INVALID_ARG;
     if ((D != 64 && D != 128) || n_layers > 65535 || Hq > PAGED_MAX_HEADS || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
-    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D);
+    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D, 16 / code_bytes);
     if (rc != MTV_OK) return rc;
     p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.D = D; p.n_layers = n_layers;
     p.q = reinterpret_cast<const __nv_bfloat16 *>(q);
     p.q_out = reinterpret_cast<__nv_bfloat16 *>(q_out);
     p.k_new = reinterpret_cast<const __nv_bfloat16 *>(k_new);
     p.v_new = reinterpret_cast<const __nv_bfloat16 *>(v_new);
-    p.k_pools = reinterpret_cast<__nv_bfloat16 *const *>(k_pools);
-    p.v_pools = reinterpret_cast<__nv_bfloat16 *const *>(v_pools);
+    p.k_pools = k_pools;
+    p.v_pools = v_pools;
     p.seq_lens = seq_lens;
     p.log2_theta = log2(rope_theta == 0.f ? 10000.0 : (double)rope_theta);
     p.status = status;
@@ -214,7 +256,7 @@ static int append_args(AppendParams &p, int B, int Hq, int Hkv, int D, int n_lay
 // ---------------------------------------------------------------------------------------- compaction
 struct CompactParams {
     int T, K, Hkv, D;
-    __nv_bfloat16 *const *k_pools, *const *v_pools;
+    char *const *k_pools, *const *v_pools;
     PagedRef pages;
     const int32_t *seq_lens, *accept_len, *acc_nodes;
     int32_t *new_lens, *status;
@@ -239,6 +281,8 @@ __device__ __forceinline__ int compact_check(const CompactParams &p, int b, int 
 // grid = (n_layers, B).  Latency: length and nodes, pages, rows, stores follow one another; a block takes all heads of a layer so that
 // the chain is gone through once.  A source row may be an earlier one's destination (acc_nodes = [0, 2, ..]: j = 1 reads slot 2, j = 2
 // writes it), within a head only: the heads go through in groups whose rows the block's registers hold, all read before any is written.
+// SIZE: bytes of an element.
+template <int SIZE>
 __global__ void __launch_bounds__(PAGED_THREADS)
 kv_compact_paged_kernel(const CompactParams p) {
     constexpr int PER = 4;
@@ -263,21 +307,21 @@ kv_compact_paged_kernel(const CompactParams p) {
     __syncthreads();
     const int n = n_rows;
     if (n <= 0) return;
-    __nv_bfloat16 *const pool[2] = {p.k_pools[layer], p.v_pools[layer]};
-    const int vec = p.D / 8, per_head = 2 * n * vec;                     // 16-byte chunks; at most 256
+    char *const pool[2] = {p.k_pools[layer], p.v_pools[layer]};
+    const int vec = p.D * SIZE / 16, per_head = 2 * n * vec;                     // 16-byte chunks; at most 256
     const int group = PER * PAGED_THREADS / per_head;                    // heads at a time, at least PER
     for (int g0 = 0; g0 < p.Hkv; g0 += group) {
         const int total = min(group, p.Hkv - g0) * per_head;
         uint4 x[PER];
-        __nv_bfloat16 *to[PER];
+        char *to[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int e = tid + k * PAGED_THREADS;
             if (e < total) {
                 const int c = e % vec, j = e / vec % n + 1, v = e / (vec * n) & 1, g = g0 + e / per_head;
-                __nv_bfloat16 *base = (v ? pool[1] : pool[0]) + g * p.pages.stride_h + c * 8;
-                x[k] = *reinterpret_cast<const uint4 *>(base + src_of[j]);
-                to[k] = base + dst_of[j];
+                char *base = (v ? pool[1] : pool[0]) + g * p.pages.stride_h * SIZE + c * 16;
+                x[k] = *reinterpret_cast<const uint4 *>(base + src_of[j] * SIZE);
+                to[k] = base + dst_of[j] * SIZE;
             }
         }
         __syncthreads();
@@ -298,42 +342,164 @@ paged_lens_advance_kernel(int B, const CompactParams p) {
     if (compact_check(p, b, lane, &L, &n) == MTV_OK && lane == 0) p.new_lens[b] = L + n + 1;
 }
 
-}  // namespace mtv
+// ---------------------------------------------------------------------------------------- reading back
+struct ReadParams {
+    int B, n_rows, Hkv, n_layers, layers_per_block, row_blocks;
+    const uint8_t *const *k_pools, *const *v_pools;
+    const float *k_scale, *v_scale;            // [n_layers][Hkv]
+    PagedRef pages;
+    const int32_t *first, *starts;             // first: or null, zeros
+    __nv_bfloat16 *k_out, *v_out;              // [n_layers][n_rows][Hkv][D]
+    int32_t *status;
+};
 
-extern "C" int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,
-                                         mtv_bf16 *q_out_layers, const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers,
-                                         mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool,
-                                         const int32_t *page_table, int max_pages, const int32_t *seq_lens, float rope_theta,
-                                         int32_t *status, void *stream) {
-    using namespace mtv;
-    MTV_RANGE("tree_kv_append_rope_paged");
-    if (!tree || !tree->on_device) return MTV_ERR_INVALID_ARG;
+// Bound by memory: a byte read and two written per value.  A block takes READ_ROWS rows of some layers, finds their pages once, and its threads move
+// 8 codes at a time, READ_DEEP requested together; the blocks behind the rows' own report one sequence per warp.
+constexpr int READ_ROWS = 16, READ_DEEP = 8;
+template <int D>
+__global__ void __launch_bounds__(PAGED_THREADS)
+kv_read_paged_kernel(const ReadParams p) {
+    constexpr int PER_HEAD = D / 8;
+    __shared__ int64_t src_of[READ_ROWS];      // of the row inside a pool; -1: the row is left alone
+    const int tid = threadIdx.x;
+    let_next_start();
+    previous_done();
+    if ((int)blockIdx.x >= p.row_blocks) {
+        const int b = ((int)blockIdx.x - p.row_blocks) * (PAGED_THREADS / 32) + tid / 32;
+        if (!p.status || blockIdx.y || b >= p.B) return;
+        const int code = p.pages.check(b, p.first ? p.first[b] : 0, p.starts[b + 1] - p.starts[b], tid % 32);
+        if (tid % 32 == 0) p.status[b] = code;
+        return;
+    }
+    const int r0 = (int)blockIdx.x * READ_ROWS;
+    int b = 0;                                 // the sequence of the block's first row: how many end at or before it
+    for (int s = 0; s < p.B; s += PAGED_THREADS) b += __syncthreads_count(s + tid < p.B && p.starts[s + tid + 1] <= r0);
+    if (tid < READ_ROWS) {
+        const int r = r0 + tid;
+        int64_t src = -1;
+        while (b < p.B && p.starts[b + 1] <= r) ++b;
+        if (r < p.n_rows && b < p.B) {
+            const int start = p.starts[b], n = p.starts[b + 1] - start, L = p.first ? p.first[b] : 0, i = r - start;
+            if (i >= 0 && p.pages.fits(L, n)) src = p.pages.row(b, L + i);
+        }
+        src_of[tid] = src;
+    }
+    __syncthreads();
+    const int l0 = (int)blockIdx.y * p.layers_per_block, layers = min(p.n_layers - l0, p.layers_per_block);
+    const int per_row = p.Hkv * PER_HEAD, per_layer = 2 * READ_ROWS * per_row;
+    for (int l = l0; l < l0 + layers; ++l) {
+        const uint8_t *const pool[2] = {p.k_pools[l], p.v_pools[l]};
+        for (int e0 = tid; e0 < per_layer; e0 += READ_DEEP * PAGED_THREADS) {
+            uint2 x[READ_DEEP];
+            float scale[READ_DEEP];
+            __nv_bfloat16 *dst[READ_DEEP];
+#pragma unroll
+            for (int k = 0; k < READ_DEEP; ++k) {
+                const int e = e0 + k * PAGED_THREADS;
+                const int v = e >= per_layer / 2, in_pool = v ? e - per_layer / 2 : e, j = in_pool / per_row, in_row = in_pool - j * per_row;
+                const int g = in_row / PER_HEAD, c = in_row % PER_HEAD * 8;
+                dst[k] = nullptr;
+                if (e >= per_layer || src_of[j] < 0) continue;
+                x[k] = __ldg(reinterpret_cast<const uint2 *>((v ? pool[1] : pool[0]) + src_of[j] + g * p.pages.stride_h + c));
+                scale[k] = (v ? p.v_scale : p.k_scale)[l * p.Hkv + g];
+                dst[k] = (v ? p.v_out : p.k_out) + (((size_t)l * p.n_rows + r0 + j) * p.Hkv + g) * D + c;
+            }
+#pragma unroll
+            for (int k = 0; k < READ_DEEP; ++k) {
+                if (!dst[k]) continue;
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t codes = i < 2 ? x[k].x : x[k].y;
+                    const float2 f = f16x2_values(i % 2 ? f16x2_hi(codes) : f16x2_lo(codes));
+                    const __nv_bfloat162 o = __floats2bfloat162_rn(f.x * scale[k], f.y * scale[k]);
+                    w[i] = *reinterpret_cast<const uint32_t *>(&o);
+                }
+                *reinterpret_cast<uint4 *>(dst[k]) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host
+template <bool FP8>
+static int append_tree(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q, mtv_bf16 *q_out, const mtv_bf16 *k_new,
+                       const mtv_bf16 *v_new, void *const *k_pools, void *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table,
+                       int max_pages, const int32_t *seq_lens, const float *k_scale, const float *v_scale, float rope_theta, int32_t *status, void *stream) {
+    if (!tree || !tree->on_device || (FP8 && (!k_scale || !v_scale))) return MTV_ERR_INVALID_ARG;
     AppendParams p = {};
-    const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, k_pools, v_pools, pool, page_table,
-                               max_pages, seq_lens, rope_theta, status, false);
+    const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q, q_out, k_new, v_new, k_pools, v_pools, FP8 ? 1 : 2, pool, page_table, max_pages, seq_lens,
+                               rope_theta, status, false);
     if (rc != MTV_OK) return rc;
     if (B > (1 << 30) / tree->T) return MTV_ERR_UNSUPPORTED_SHAPE;
     p.T = tree->T;
     p.n_rows = B * tree->T;
     p.depth = tree->d_depth;
-    return launch_append(p, (cudaStream_t)stream);
+    p.k_scale = k_scale; p.v_scale = v_scale;
+    return launch_append<FP8>(p, (cudaStream_t)stream);
 }
 
-extern "C" int kv_append_rope_paged(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
-                                    const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, mtv_bf16 *const *k_pools,
-                                    mtv_bf16 *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
-                                    const int32_t *seq_lens, const int32_t *row_starts, float rope_theta, int32_t *status, void *stream) {
-    using namespace mtv;
-    MTV_RANGE("kv_append_rope_paged");
-    if (!row_starts || n_rows < 0) return MTV_ERR_INVALID_ARG;
+template <bool FP8>
+static int append_rows(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q, mtv_bf16 *q_out, const mtv_bf16 *k_new,
+                       const mtv_bf16 *v_new, void *const *k_pools, void *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table,
+                       int max_pages, const int32_t *seq_lens, const int32_t *row_starts, const float *k_scale, const float *v_scale, float rope_theta,
+                       int32_t *status, void *stream) {
+    if (!row_starts || n_rows < 0 || (FP8 && (!k_scale || !v_scale))) return MTV_ERR_INVALID_ARG;
     if (n_rows > 1 << 30) return MTV_ERR_UNSUPPORTED_SHAPE;
     AppendParams p = {};
-    const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, k_pools, v_pools, pool, page_table,
-                               max_pages, seq_lens, rope_theta, status, n_rows == 0);
+    const int rc = append_args(p, B, Hq, Hkv, D, n_layers, q, q_out, k_new, v_new, k_pools, v_pools, FP8 ? 1 : 2, pool, page_table, max_pages, seq_lens,
+                               rope_theta, status, n_rows == 0);
     if (rc != MTV_OK) return rc;
     p.n_rows = n_rows;
     p.starts = row_starts;
-    return launch_append(p, (cudaStream_t)stream);
+    p.k_scale = k_scale; p.v_scale = v_scale;
+    return launch_append<FP8>(p, (cudaStream_t)stream);
+}
+
+template <int SIZE>
+static int compact(const mtv_tree_t *tree, int B, int Hkv, int D, int n_layers, void *const *k_pools, void *const *v_pools, const mtv_pool_layout *pool,
+                   const int32_t *page_table, int max_pages, const int32_t *seq_lens, int32_t *new_lens, const int32_t *accept_len,
+                   const int32_t *acc_nodes, int32_t *status, void *stream) {
+    if (!tree || !k_pools || !v_pools || !seq_lens || !new_lens || !accept_len || !acc_nodes || B < 1 || Hkv < 1 || n_layers < 1)
+        return MTV_ERR_INVALID_ARG;
+    if ((D != 64 && D != 128) || B > 65535 || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
+    CompactParams p = {};
+    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D, 16 / SIZE);
+    if (rc != MTV_OK) return rc;
+    p.T = tree->T; p.K = tree->K; p.Hkv = Hkv; p.D = D;
+    p.k_pools = reinterpret_cast<char *const *>(k_pools);
+    p.v_pools = reinterpret_cast<char *const *>(v_pools);
+    p.seq_lens = seq_lens; p.accept_len = accept_len; p.acc_nodes = acc_nodes;
+    p.new_lens = new_lens; p.status = status;
+    p.in_place = new_lens == seq_lens;
+    cudaStream_t st = (cudaStream_t)stream;
+    MTV_CUDA_CHECK(launch_dependent(kv_compact_paged_kernel<SIZE>, dim3(n_layers, B), PAGED_THREADS, 0, st, p));
+    if (p.in_place)
+        MTV_CUDA_CHECK(launch_dependent(paged_lens_advance_kernel, dim3((B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32)), PAGED_THREADS, 0, st, B, p));
+    return MTV_OK;
+}
+template <typename P> static void *const *untyped(P *const *pools) { return reinterpret_cast<void *const *>(pools); }
+
+}  // namespace mtv
+
+extern "C" int tree_kv_append_rope_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,
+                                         mtv_bf16 *q_out_layers, const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers,
+                                         mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table,
+                                         int max_pages, const int32_t *seq_lens, float rope_theta, int32_t *status, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("tree_kv_append_rope_paged");
+    return append_tree<false>(tree, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, untyped(k_pools), untyped(v_pools), pool,
+                         page_table, max_pages, seq_lens, nullptr, nullptr, rope_theta, status, stream);
+}
+
+extern "C" int kv_append_rope_paged(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
+                                    const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, mtv_bf16 *const *k_pools, mtv_bf16 *const *v_pools,
+                                    const mtv_pool_layout *pool, const int32_t *page_table, int max_pages, const int32_t *seq_lens,
+                                    const int32_t *row_starts, float rope_theta, int32_t *status, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("kv_append_rope_paged");
+    return append_rows<false>(B, n_rows, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, untyped(k_pools), untyped(v_pools), pool,
+                         page_table, max_pages, seq_lens, row_starts, nullptr, nullptr, rope_theta, status, stream);
 }
 
 extern "C" int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv, int D, int n_layers, mtv_bf16 *const *k_pools,
@@ -342,21 +508,67 @@ extern "C" int kv_compact_accepted_paged(const mtv_tree_t *tree, int B, int Hkv,
                                          int32_t *status, void *stream) {
     using namespace mtv;
     MTV_RANGE("kv_compact_accepted_paged");
-    if (!tree || !k_pools || !v_pools || !seq_lens || !new_lens || !accept_len || !acc_nodes || B < 1 || Hkv < 1 || n_layers < 1)
-        return MTV_ERR_INVALID_ARG;
-    if ((D != 64 && D != 128) || B > 65535 || Hkv > PAGED_MAX_HEADS) return MTV_ERR_UNSUPPORTED_SHAPE;
-    CompactParams p = {};
-    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D);
+    return compact<2>(tree, B, Hkv, D, n_layers, untyped(k_pools), untyped(v_pools), pool, page_table, max_pages, seq_lens, new_lens, accept_len, acc_nodes,
+                      status, stream);
+}
+
+extern "C" int tree_kv_append_rope_paged_fp8(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers,
+                                             mtv_bf16 *q_out_layers, const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers,
+                                             uint8_t *const *k_pools, uint8_t *const *v_pools, const mtv_pool_layout *pool,
+                                             const int32_t *page_table, int max_pages, const int32_t *seq_lens, const float *k_scale,
+                                             const float *v_scale, float rope_theta, int32_t *status, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("tree_kv_append_rope_paged_fp8");
+    return append_tree<true>(tree, B, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, untyped(k_pools), untyped(v_pools), pool,
+                        page_table, max_pages, seq_lens, k_scale, v_scale, rope_theta, status, stream);
+}
+
+extern "C" int kv_append_rope_paged_fp8(int B, int n_rows, int Hq, int Hkv, int D, int n_layers, const mtv_bf16 *q_layers, mtv_bf16 *q_out_layers,
+                                        const mtv_bf16 *k_new_layers, const mtv_bf16 *v_new_layers, uint8_t *const *k_pools, uint8_t *const *v_pools,
+                                        const mtv_pool_layout *pool, const int32_t *page_table, int max_pages, const int32_t *seq_lens,
+                                        const int32_t *row_starts, const float *k_scale, const float *v_scale, float rope_theta, int32_t *status,
+                                        void *stream) {
+    using namespace mtv;
+    MTV_RANGE("kv_append_rope_paged_fp8");
+    return append_rows<true>(B, n_rows, Hq, Hkv, D, n_layers, q_layers, q_out_layers, k_new_layers, v_new_layers, untyped(k_pools), untyped(v_pools), pool,
+                        page_table, max_pages, seq_lens, row_starts, k_scale, v_scale, rope_theta, status, stream);
+}
+
+extern "C" int kv_compact_accepted_paged_fp8(const mtv_tree_t *tree, int B, int Hkv, int D, int n_layers, uint8_t *const *k_pools,
+                                             uint8_t *const *v_pools, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,
+                                             const int32_t *seq_lens, int32_t *new_lens, const int32_t *accept_len, const int32_t *acc_nodes,
+                                             int32_t *status, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("kv_compact_accepted_paged_fp8");
+    return compact<1>(tree, B, Hkv, D, n_layers, untyped(k_pools), untyped(v_pools), pool, page_table, max_pages, seq_lens, new_lens, accept_len, acc_nodes,
+                      status, stream);
+}
+
+extern "C" int kv_read_paged_fp8(int B, int n_rows, int Hkv, int D, int n_layers, const uint8_t *const *k_pools, const uint8_t *const *v_pools,
+                                 const mtv_pool_layout *pool, const int32_t *page_table, int max_pages, const int32_t *first,
+                                 const int32_t *row_starts, const float *k_scale, const float *v_scale, mtv_bf16 *k_out_layers,
+                                 mtv_bf16 *v_out_layers, int32_t *status, void *stream) {
+    using namespace mtv;
+    MTV_RANGE("kv_read_paged_fp8");
+    if (!k_pools || !v_pools || !row_starts || !k_scale || !v_scale || B < 1 || n_rows < 0 || Hkv < 1 || n_layers < 1) return MTV_ERR_INVALID_ARG;
+    if (n_rows && (!k_out_layers || !v_out_layers || (((uintptr_t)k_out_layers | (uintptr_t)v_out_layers) & 15))) return MTV_ERR_INVALID_ARG;
+    if ((D != 64 && D != 128) || n_layers > 65535 || Hkv > PAGED_MAX_HEADS || n_rows > 1 << 30) return MTV_ERR_UNSUPPORTED_SHAPE;
+    ReadParams p = {};
+    const int rc = paged_ref(p.pages, pool, page_table, max_pages, D, 16);
     if (rc != MTV_OK) return rc;
-    p.T = tree->T; p.K = tree->K; p.Hkv = Hkv; p.D = D;
-    p.k_pools = reinterpret_cast<__nv_bfloat16 *const *>(k_pools);
-    p.v_pools = reinterpret_cast<__nv_bfloat16 *const *>(v_pools);
-    p.seq_lens = seq_lens; p.accept_len = accept_len; p.acc_nodes = acc_nodes;
-    p.new_lens = new_lens; p.status = status;
-    p.in_place = new_lens == seq_lens;
-    cudaStream_t st = (cudaStream_t)stream;
-    MTV_CUDA_CHECK(launch_dependent(kv_compact_paged_kernel, dim3(n_layers, B), PAGED_THREADS, 0, st, p));
-    if (p.in_place)
-        MTV_CUDA_CHECK(launch_dependent(paged_lens_advance_kernel, dim3((B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32)), PAGED_THREADS, 0, st, B, p));
+    p.B = B; p.n_rows = n_rows; p.Hkv = Hkv; p.n_layers = n_layers;
+    p.k_pools = k_pools; p.v_pools = v_pools; p.k_scale = k_scale; p.v_scale = v_scale;
+    p.first = first; p.starts = row_starts;
+    p.k_out = reinterpret_cast<__nv_bfloat16 *>(k_out_layers);
+    p.v_out = reinterpret_cast<__nv_bfloat16 *>(v_out_layers);
+    p.status = status;
+    p.row_blocks = (n_rows + READ_ROWS - 1) / READ_ROWS;
+    // as in the appending: enough blocks to fill the device a few times over, as many layers per block as that leaves
+    long per = (long)p.row_blocks * n_layers / (12L * sm_count());
+    per = per < 1 ? 1 : per > n_layers ? n_layers : per;
+    p.layers_per_block = (int)per;
+    const int report = status || !p.row_blocks ? (B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32) : 0;
+    MTV_CUDA_CHECK(launch_dependent(D == 128 ? kv_read_paged_kernel<128> : kv_read_paged_kernel<64>,
+                                    dim3(p.row_blocks + report, (unsigned)((n_layers + per - 1) / per)), PAGED_THREADS, 0, (cudaStream_t)stream, p));
     return MTV_OK;
 }

@@ -7,7 +7,7 @@
 
 namespace {
 
-enum { BF16 = 0, I32 = 1, I64 = 2, F32 = 3, ANY = 4, TYPES = 7, OPTIONAL = 16, STRIDED = 32, LIKE_PREVIOUS = 64 };
+enum { BF16 = 0, I32 = 1, I64 = 2, F32 = 3, ANY = 4, FP8 = 5, TYPES = 7, OPTIONAL = 16, STRIDED = 32, LIKE_PREVIOUS = 64 };
 
 bool is_kind(c10::ScalarType t, long kind) {
     using S = c10::ScalarType;
@@ -16,6 +16,7 @@ bool is_kind(c10::ScalarType t, long kind) {
     case I32: return t == S::Int || t == S::UInt32;
     case I64: return t == S::Long || t == S::UInt64;
     case F32: return t == S::Float;
+    case FP8: return t == S::Float8_e4m3fn;
     default: return true;
     }
 }
