@@ -2,23 +2,22 @@
 // and the workspace are those of the bf16 cache (attention_paged.cu, paged_attn.cuh); here stands what the codes change.
 //   s_ij = (scale k_scale) <q_i, K8_j>,  out_i = v_scale sum_j softmax(s_i)_j V8_j
 //
-// Every code is a number of fp16, so the products are fp16 x fp16 -> fp32 on the tensor cores, without a loss in K and V, and the scales are left to the
-// softmax' factor and to the end.  Nothing else than codes is read from memory; they become fp16 tiles in shared memory, one conversion instruction for
-// two codes.  (The tensor cores' own 8-bit products would want the queries and the weights in 8 bits, or as two terms of 8 bits at twice
-// the products, which is the time of one in fp16: the conversion costs warps that have nothing else to do.)
-//   q   bf16 has a wider range than fp16: a row is multiplied by the power of two that brings its largest value to [256, 512), and its factor of
-//       the scores divided by it.  8 bits of a bf16 then fit whatever is above 2^-25 of the largest.
+// K needs no conversion: its codes are operands of the 8-bit products.  Queries are brought to 8 bits in two terms, q = q1 + q2, both e4m3, which
+// holds the 8 bits of a bf16 exactly: a row is multiplied by the power of two that brings its largest value to [128, 256), q1 is that rounded to a code
+// and q2 what is left; values below 2^-9 of the row's largest are held to 2^-17 of it.  Two products of 8 bits take the time of one of 16.
+// Weights would want two terms too, at every key tile, on the warps that have the least time; so V is converted instead, to fp16 tiles
+// (every code is a number of fp16), by warps of their own, and the second product is fp16 x fp16.
 //   P   weights are fp16, 2^SHIFT at the reference (the maximum of a piece's first tile) and below 2^16: they lose bits below 2^(-14 - SHIFT) of the
 //       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.
-//
+// K in fp16 as well took 88 us of a long context's call where this takes
+// 
 // One persistent CTA per SM, two row tiles in flight, each with its scores, weights and accumulator in tensor memory and eight softmax warps:
-//   warps 0-7 / 8-15  softmax of row tile 0 / 1; in front of a piece they turn its queries into fp16
-//   warps 16-19       codes -> fp16 tiles (128 keys, 128-byte swizzle); rows behind the last key become zeros (their weight is 0, but 0 * NaN is not),
-//                     NaN codes of the tree's V rows too (they are given to the rows that see them at the end)
+//   warps 0-7 / 8-15  softmax of row tile 0 / 1; in front of a piece they split its queries
+//   warps 16-19       V's codes -> fp16 tiles (128 keys, 128-byte swizzle); rows behind the last key become zeros (their weight is 0, but 0 * NaN is
+//                     not), NaN codes of the tree's rows too (they are given to the rows that see them at the end)
 //   warps 20, 21      issue the products of row tile 0 / 1
 //   warp 22           derives the pieces, requests Q and the codes (a box per page)
-// Codes and tiles have a ring each.  A CTA of pairs shares K and V between its row tiles and is bound by the softmax and the products: four tiles,
-// two stages of codes (D = 128); one of single row tiles is bound by its bytes: three tiles, four stages of codes.
+// K's codes, V's and V's tiles have a ring each.
 // The softmax warpgroups have 96 registers, the others 48 (768 threads of 80 at the launch).
 #include <limits.h>
 
@@ -36,32 +35,32 @@ constexpr float P8_LIMIT = 15.99f;        // weights stay below 2^16, which fp16
 
 template <int D> struct P8Smem {
     static constexpr int HALVES = D / 64;
-    static constexpr uint32_t HALF = 128 * 128;          // 128 rows of 64 columns, 128-byte swizzle
+    static constexpr uint32_t HALF = 128 * 128;          // 128 rows of 128 bytes (64 columns of 2, or 128 of 1), 128-byte swizzle
     static constexpr uint32_t TILE = HALVES * HALF, CODES = 128 * D;
-    // stages with one list of key tiles (pairs) and with two (single row tiles)
-    __host__ __device__ static constexpr int tiles(int lists) { return (lists == 1 ? 4 : 3) * (3 - HALVES); }
-    __host__ __device__ static constexpr int codes(int lists) { return lists == 1 ? (D == 128 ? 2 : 8) : (D == 128 ? 4 : 12); }
-    static constexpr int MAX_TILES = tiles(1), MAX_CODES = codes(2);
-    static constexpr uint32_t RING = tiles(1) * TILE + codes(1) * CODES;
-    static_assert(RING == tiles(2) * TILE + codes(2) * CODES, "one region for either");
-    static constexpr uint32_t OFF_RING = 2 * TILE, OFF_BAR = OFF_RING + RING, TOTAL = 1024 + OFF_BAR + 1280;
+    static constexpr int K_STAGES = D == 128 ? 3 : 8, V_STAGES = K_STAGES, TILES = D == 128 ? 2 : 4;
+    static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + K_STAGES * CODES, OFF_TILES = OFF_V + V_STAGES * CODES, OFF_BAR = OFF_TILES + TILES * TILE,
+                              TOTAL = 1024 + OFF_BAR + 1280;
     static_assert(TOTAL <= 227 * 1024, "shared memory budget");
-    static constexpr uint32_t IDESC = (1u << 4) | (128u >> 4) << 24;                             // fp16 x fp16 -> fp32, M = 128
+    static constexpr uint32_t IDESC = (1u << 4) | (128u >> 4) << 24;                             // e4m3 x e4m3 or fp16 x fp16 -> fp32, M = 128
     static constexpr uint32_t IDESC_QK = IDESC | (128u >> 3) << 17;                               // N = 128 keys
     static constexpr uint32_t IDESC_PV = IDESC | (uint32_t)(D >> 3) << 17 | 1u << 16;             // N = D columns, B (= V) N-major
+    // K's codes: rows of D bytes in groups of 8, swizzled over as many bytes
+    static constexpr uint32_t K_DESC_HI = D == 128 ? ptx::DESC_HI : (512u >> 4) | 1u << 14 | 4u << 29;
+    static constexpr uint32_t Q2 = D == 128 ? HALF : 64;                                          // the second terms, from the first
 };
 
 enum {
-    P8_CFULL = 0, P8_CFREE = 12, P8_FULL = 24, P8_FREE = 32, P8_QFULL = 40, P8_QREADY = 42, P8_QFREE = 44, P8_SREADY = 46, P8_PREADY = 48, P8_ODONE = 50,
-    P8_FINAL = 52,
+    P8_KFULL = 0, P8_KFREE = 8, P8_VFULL = 16, P8_VFREE = 24, P8_FULL = 32, P8_FREE = 36, P8_QFULL = 40, P8_QREADY = 42, P8_QFREE = 44, P8_SREADY = 46,
+    P8_PREADY = 48, P8_ODONE = 50, P8_FINAL = 52,
     P8_PIECE = 53,                         // [3 queues][PA_QUEUE]: pairs; single tiles of either half of the CTA
     P8_TAKEN = P8_PIECE + 3 * PA_QUEUE,
     P8_TURN = P8_TAKEN + 3 * PA_QUEUE,     // [2] an issuing warp's turn at the tensor core
-    P8_COUNT = P8_TURN + 2
+    P8_ROLE = P8_TURN + 2,                 // whether the CTA has pairs is known
+    P8_COUNT = P8_ROLE + 1
 };
-constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 40 + 15) / 16 * 16;
+constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 + 15) / 16 * 16;
 static_assert(P8_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1280, "barrier region");
-static_assert(P8Smem<64>::MAX_TILES <= 8 && P8Smem<64>::MAX_CODES <= 12 && P8Smem<128>::MAX_TILES <= 8 && P8Smem<128>::MAX_CODES <= 12, "barriers of the rings");
+static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
 constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
 
@@ -72,17 +71,22 @@ struct P8Rows {
     int L;              // keys in front of the tree; more than there can be where it is not the piece's (the prefix)
 };
 
+// ... and the one that loads: this lane's entry of the page table for the tile.
+struct P8Load : PaPiece { int id; };
+
 struct P8Params {
     PaParams a;                            // (its k and v are not used)
     const uint8_t *k, *v;
     const float *k_scale, *v_scale;        // [Hkv]
 };
 
-// The power of two that brings a row of bf16 queries whose largest absolute value has these bits (as fp32) to [256, 512), and its reciprocal.
-__device__ __forceinline__ float2 row_factor(uint32_t largest) {
+// The power of two that brings a row of bf16 queries whose largest absolute value has these bits (as fp32) to [2^TO, 2^(TO + 1)), and its reciprocal; a row
+// that is not finite becomes NaN.
+template <int TO> __device__ __forceinline__ float2 row_factor(uint32_t largest) {
     const int e = (int)(largest >> 23);
-    if (largest == 0u || e == 255) return make_float2(1.f, 1.f);
-    const int k = min(135 - e, 126);
+    if (e == 255) return make_float2(__int_as_float(0x7fffffff), 1.f);
+    if (largest == 0u) return make_float2(1.f, 1.f);
+    const int k = min(127 + TO - e, 126);
     return make_float2(__int_as_float((127 + k) << 23), __int_as_float((127 - k) << 23));
 }
 __device__ __forceinline__ uint32_t larger_bits(uint32_t m, uint32_t pair) { return max(m, max(pair << 16, pair & 0xffff0000u)); }
@@ -91,7 +95,122 @@ __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor) {
     return pack2_f16(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
 }
 
+// The run of one worker of a CTA (which = 0: of pairs; 1, 2: of single row tiles) and the item it begins in.  One warp; length, prefix: of the phase's line.
+// (The same as begin_walks, one at a time: the kernel is as large as an SM's instruction cache can bear.)
+__device__ __forceinline__ void begin_walk(const PaParams &p, PaWalk &w, int which, int cta, int n_cta, int n_pairs, int length, int prefix, int lane) {
+    const int single = which > 0, ends = ITEM_COST(single), cost = item_cost(key_tiles(p.shared), ends);
+    const int workers = single ? 2 * (n_cta - n_pairs) : n_pairs;
+    w.worker = which == 0 ? cta : which == 1 ? cta - n_pairs : cta + n_cta - 2 * n_pairs;
+    w.ends = ends;
+    // none shorter than a key tile, so that no worker in the middle of an item is left without a tile
+    const int run = max((length + workers - 1) / workers, TILE_COST);
+    w.x0 = (int)min((int64_t)length, (int64_t)run * w.worker);
+    w.x1 = (int)min((int64_t)length, (int64_t)w.x0 + run);
+    w.b = -1;
+    w.idx = 0;
+    w.S = w.x0 == w.x1 ? w.x1 : 0;
+    if (w.x0 >= w.x1) return;
+    if (w.x0 < prefix) {
+        w.idx = w.x0 / cost;
+        w.S = w.idx * cost;
+    } else {
+        const int y = w.x0 - prefix, items = p.phase[single].seq_items;
+        int before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const int b = b0 + lane, own = b < p.B ? item_cost(seq_tiles(p, p.seq_lens[b]), ends) * items : 0;
+            int c = own;
+#pragma unroll 1
+            for (int o = 1; o < 32; o *= 2) {
+                const int x = __shfl_up_sync(0xffffffffu, c, o);
+                if (lane >= o) c += x;
+            }
+            const uint32_t behind = __ballot_sync(0xffffffffu, before + c > y);
+            if (behind) {
+                const int at = __ffs((int)behind) - 1, all = __shfl_sync(0xffffffffu, own, at), first = before + __shfl_sync(0xffffffffu, c, at) - all;
+                const int each = all / items;
+                w.b = b0 + at;
+                w.idx = (y - first) / each;
+                w.S = prefix + first + w.idx * each;
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, c, 31);
+        }
+    }
+    w.load(p);
+}
+
+// All key tiles of a CTA's one or two lists of pieces in the order of for_rounds, the lists taking turns.  P: what a warp wants of a piece.  next(list,
+// piece) -> whether there is one; f(list, piece and tile of V or none, piece and tile of K or none) -> whether to go on; ahead(piece, tile): its next tile.
+template <typename P, typename N, typename F, typename A>
+__device__ __forceinline__ bool in_turns(int lists, N &&next, F &&f, A &&ahead) {
+    struct List {
+        P cur, old;
+        int t, old_t;
+        bool live, pend, over;
+    } x, y;
+    x.live = x.pend = x.over = y.live = y.pend = false;
+    y.over = lists < 2;
+    int l = 0;
+#pragma unroll 1
+    while (!x.over || x.pend || !y.over || y.pend) {
+        if (!x.over && !x.live) {
+            x.live = next(l, x.cur);
+            x.over = !x.live;
+            x.t = x.cur.t0;
+        }
+        if (x.live || x.pend) {
+            if (!f(l, x.pend, x.old, x.old_t, x.live, x.cur, x.t)) return false;
+            x.pend = x.live;
+            if (x.live) {
+                x.old = x.cur;
+                x.old_t = x.t;
+                x.live = ++x.t < x.cur.t1;
+                if (x.live) ahead(x.cur, x.t);
+            }
+        }
+        if (lists == 2) {
+            const List z = x;
+            x = y;
+            y = z;
+            l ^= 1;
+        }
+    }
+    return true;
+}
+
+// ptx::mbar_wait in a few instructions (a 32-bit clock, asked between polls, each of which blocks for far less than it takes to wrap).
+__device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity) {
+    static_assert(ptx::WAIT_CYCLE_LIMIT < 1ll << 31, "half a turn of the clock");
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        ".reg .u32 t, u;\n"
+        "mov.u32 t, %%clock;\n"
+        "AGAIN:\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "@p bra DONE;\n"
+        "mov.u32 u, %%clock;\n"
+        "sub.u32 u, u, t;\n"
+        "setp.lt.u32 q, u, %3;\n"
+        "@q bra AGAIN;\n"
+        "DONE:\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok) : "r"(bar), "r"(parity), "n"((uint32_t)ptx::WAIT_CYCLE_LIMIT) : "memory");
+    return ok != 0;
+}
+
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P8_REGS_FEWER)); }
+
+// Four values times the factor, as codes of their first terms and of their second.
+__device__ __forceinline__ void to_terms(uint32_t pair0, uint32_t pair1, float factor, uint32_t &first, uint32_t &second) {
+    const float x[4] = {__uint_as_float(pair0 << 16) * factor, __uint_as_float(pair0 & 0xffff0000u) * factor,
+                        __uint_as_float(pair1 << 16) * factor, __uint_as_float(pair1 & 0xffff0000u) * factor};
+    first = e4m3x2(x[0], x[1]) | e4m3x2(x[2], x[3]) << 16;
+    const float2 a = f16x2_values(f16x2_lo(first)), b = f16x2_values(f16x2_hi(first));
+    second = e4m3x2(x[0] - a.x, x[1] - a.y) | e4m3x2(x[2] - b.x, x[3] - b.y) << 16;
+}
 
 // ---------------------------------------------------------------------------------------- pieces
 template <int D>
@@ -111,17 +230,20 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + SM::OFF_BAR + P8_OFF_MISC);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 4);
     volatile int *bad = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 8);   // [2][4]: 1 + the last piece with NaN in V
+    volatile int *role = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 40);
     int4 *queue = reinterpret_cast<int4 *>(gbase + SM::OFF_BAR + P8_OFF_QUEUE);                    // [3][PA_QUEUE] pieces
 
     if (warp == P8_TMA_WARP && lane == 0) {
         ptx::prefetch_tensormap(&q_map);
         ptx::prefetch_tensormap(&k_map);
         ptx::prefetch_tensormap(&v_map);
-        for (int s = 0; s < SM::MAX_CODES; ++s) {
-            ptx::mbar_init(bar(P8_CFULL + s), 1);
-            ptx::mbar_init(bar(P8_CFREE + s), P8_CONV_WARPS);
+        for (int s = 0; s < SM::K_STAGES; ++s) {
+            ptx::mbar_init(bar(P8_KFULL + s), 1);
+            ptx::mbar_init(bar(P8_KFREE + s), 2);
+            ptx::mbar_init(bar(P8_VFULL + s), 1);
+            ptx::mbar_init(bar(P8_VFREE + s), P8_CONV_WARPS);
         }
-        for (int s = 0; s < SM::MAX_TILES; ++s) {
+        for (int s = 0; s < SM::TILES; ++s) {
             ptx::mbar_init(bar(P8_FULL + s), P8_CONV_WARPS);
             ptx::mbar_init(bar(P8_FREE + s), 2);
         }
@@ -135,6 +257,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             ptx::mbar_init(bar(P8_TURN + s), 1);
         }
         ptx::mbar_init(bar(P8_FINAL), 2);
+        ptx::mbar_init(bar(P8_ROLE), 1);
         for (int q = 0; q < 3; ++q)
             for (int i = 0; i < PA_QUEUE; ++i) {
                 ptx::mbar_init(bar(P8_PIECE + q * PA_QUEUE + i), 1);
@@ -154,17 +277,17 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     previous_done();
     const int n_cta = gridDim.x, cta = blockIdx.x;
     const uint32_t tmem = *tmem_slot;
-    auto give_up = [&]() {
-        *abort_flag = 1;
-        atomicExch(p.dev_error, MTV_ERR_TIMEOUT);
-    };
     // a whole warp waits; the same answer for all lanes
     auto wait = [&](int b, uint32_t parity) {
-        const bool ok = ptx::mbar_wait(bar(b), parity);
-        if (__all_sync(0xffffffffu, ok)) return true;
-        if (lane == 0) give_up();
+        if (__all_sync(0xffffffffu, short_wait(bar(b), parity))) return true;
+        if (lane == 0) {
+            *abort_flag = 1;
+            atomicExch(p.dev_error, MTV_ERR_TIMEOUT);
+        }
         return false;
     };
+    // whether the CTA has pairs of row tiles, or single ones
+    auto is_pairs = [&]() { return wait(P8_ROLE, 0) && *role; };
     // the n-th piece of a queue; none (or nothing to be had): false
     auto take = [&](int q, int n, PaPiece &s) {
         const int at = q * PA_QUEUE + n % PA_QUEUE;
@@ -181,13 +304,41 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (warp == P8_TMA_WARP) {
         fewer_registers();
         // ------------------------------------------------------------ pieces; Q and the codes of K and V
-        PaWalk w[3];
-        begin_walks(p, w, cta, n_cta, lane, P8_COST_PAIRS, P8_COST_SINGLE);
+        int tiles = 0, seqs = 0;             // key tiles of an item of every sequence that is not left out, and their number
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const int t = b0 + lane < p.B ? seq_tiles(p, p.seq_lens[b0 + lane]) : 0;
+            tiles += t;
+            seqs += t > 0;
+        }
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
+        seqs = __reduce_add_sync(0xffffffffu, seqs);
+        int prefix[2], length[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            prefix[f] = item_cost(key_tiles(p.shared), ITEM_COST(f)) * p.phase[f].prefix_items;
+            length[f] = prefix[f] + (tiles * TILE_COST + seqs * ITEM_COST(f)) * p.phase[f].seq_items;
+        }
+        // the first CTAs take the pairs, the others the single row tiles
+        int n_pairs = n_cta;
+        if (length[1]) {
+            const float a = (float)length[0] * P8_COST_PAIRS, b = (float)length[1] * P8_COST_SINGLE;
+            n_pairs = length[0] ? max(1, min(n_cta - 1, __float2int_rn(n_cta * (a / (a + b))))) : 0;
+        }
+        const bool pairs = cta < n_pairs;
+        if (lane == 0) {
+            *role = pairs;
+            ptx::mbar_arrive(bar(P8_ROLE));
+        }
+        __syncwarp();
+        PaWalk walk[2];
+#pragma unroll 1
+        for (int k = 0; k < (pairs ? 1 : 2); ++k)
+            begin_walk(p, walk[k], pairs ? 0 : 1 + k, cta, n_cta, n_pairs, pairs ? length[0] : length[1], pairs ? prefix[0] : prefix[1], lane);
         // One piece more for a queue, or its end: a piece without tiles.  (There is room, or will be without this warp's doing: the queries
         // of a piece are only requested when the scores of the one before are complete, so this warp is never three pieces ahead.)
         auto hand_out = [&](int q, int n, PaPiece &s) {
             const int at = q * PA_QUEUE + n % PA_QUEUE;
-            const bool any = w[q].next(p, p.phase[q > 0], s);
+            const bool any = walk[q == 2].next(p, p.phase[q > 0], s);
             if (!any) s = PaPiece{};
             if (n >= PA_QUEUE && !wait(P8_TAKEN + at, (n / PA_QUEUE - 1) & 1)) { s.t0 = s.t1 = 0; return false; }
             if (lane == 0) {
@@ -198,7 +349,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             __syncwarp();
             return any;
         };
-        int n_q[2] = {0, 0};
+        int n_q0 = 0, n_q1 = 0;
         const int boxes = PA_KEYS / p.page_rows;
         const uint32_t q_bytes = (uint32_t)(p.npc * p.G) * 128u * SM::HALVES;
         // This lane's entry of the table for a key tile, requested here and looked at where the tile is: nothing waits for it meanwhile.
@@ -214,58 +365,56 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         auto row_in_page = [&](const PaPiece &s, int t) {
             return (t * PA_KEYS + lane * p.page_rows + (s.b < 0 ? 0 : p.shared)) & ((1 << p.pages.page_shift) - 1);
         };
-        // (a CTA has pieces of one phase alone, so both begin at the rings' first stages)
-        auto phase = [&](auto lists) {
-            constexpr int NL = decltype(lists)::value, STAGES = SM::codes(NL);
-            constexpr uint32_t OFF_CODES = SM::OFF_RING + SM::tiles(NL) * SM::TILE;
+        struct Ring {
             int entry = 0, stage = 0, turns = 0;
-            auto load = [&](const CUtensorMap *map, int id, int row, int g) {
-                if (entry >= STAGES && !wait(P8_CFREE + stage, (turns - 1) & 1)) return false;
-                if (lane == 0) ptx::mbar_arrive_expect_tx(bar(P8_CFULL + stage), SM::CODES);
-                __syncwarp();
-                if (lane < boxes)
-                    ptx::tma_load_4d(sbase + OFF_CODES + stage * SM::CODES + lane * p.page_rows * D, map, bar(P8_CFULL + stage), 0, row, g,
-                                     id >= 0 && id < p.pages.n_pages ? id : p.pages.n_pages);
-                ++entry;
-                if (++stage == STAGES) { stage = 0; ++turns; }
-                return true;
-            };
-            int v_id[NL] = {}, k_id[NL] = {}, n[NL] = {};
-            auto next = [&](int l, PaPiece &s) {
-                if (!hand_out(NL == 1 ? 0 : 1 + l, n[l]++, s)) return false;
-                k_id[l] = find(s, s.t0);
-                return true;
-            };
-            const bool ok = for_rounds<NL>(next, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
-                if (v && !load(&v_map, v_id[l], row_in_page(vs, vt), vs.g)) return false;
-                if (!k) return true;
-                if (!load(&k_map, k_id[l], row_in_page(ks, kt), ks.g)) return false;
-                v_id[l] = k_id[l];
-                if (kt + 1 < ks.t1) k_id[l] = find(ks, kt + 1);
-                if (kt == ks.t0)
-                    for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) {
-                        if (n_q[s] && !wait(P8_QFREE + s, (n_q[s] - 1) & 1)) return false;
-                        ++n_q[s];
-                        if (lane == 0) {
-                            ptx::mbar_arrive_expect_tx(bar(P8_QFULL + s), q_bytes);
-                            for (int h = 0; h < SM::HALVES; ++h)
-                                ptx::tma_load_4d(sbase + s * SM::TILE + h * SM::HALF, &q_map, bar(P8_QFULL + s), h * 64, ks.g * p.G,
-                                                 max(ks.b, 0) * p.T + (ks.tile0 + (NL == 1 ? s : 0)) * p.npc, 0);
-                        }
-                        __syncwarp();
-                    }
-                return true;
-            });
-            if (ok && !*abort_flag) return true;
-            // copies in flight get a bounded chance to land before the CTA can exit
-            for (int e = max(0, entry - STAGES); e < entry; ++e) ptx::mbar_wait(bar(P8_CFULL + e % STAGES), (e / STAGES) & 1);
-            for (int s = 0; s < 2; ++s)
-                if (n_q[s]) ptx::mbar_wait(bar(P8_QFULL + s), (n_q[s] - 1) & 1);
-            return false;
+        } rk, rv;
+        auto load = [&](Ring &r, const CUtensorMap *map, uint32_t off, int full, int free, int id, int row, int g) {
+            if (r.turns && !wait(free + r.stage, (r.turns - 1) & 1)) return false;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full + r.stage), SM::CODES);
+            __syncwarp();
+            if (lane < boxes)
+                ptx::tma_load_4d(sbase + off + r.stage * SM::CODES + lane * p.page_rows * D, map, bar(full + r.stage), 0, row, g,
+                                 id >= 0 && id < p.pages.n_pages ? id : p.pages.n_pages);
+            ++r.entry;
+            if (++r.stage == SM::K_STAGES) { r.stage = 0; ++r.turns; }
+            return true;
         };
-        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+        int n0 = 0, n1 = 0;
+        const int lists = pairs ? 1 : 2;
+        const bool ok = in_turns<P8Load>(lists, [&](int l, P8Load &s) {
+            int &n = l ? n1 : n0;
+            if (!hand_out(pairs ? 0 : 1 + l, n++, s)) return false;
+            s.id = find(s, s.t0);
+            return true;
+        }, [&](int l, bool v, const P8Load &vs, int vt, bool k, const P8Load &ks, int kt) {
+            if (v && !load(rv, &v_map, SM::OFF_V, P8_VFULL, P8_VFREE, vs.id, row_in_page(vs, vt), vs.g)) return false;
+            if (!k) return true;
+            if (!load(rk, &k_map, SM::OFF_K, P8_KFULL, P8_KFREE, ks.id, row_in_page(ks, kt), ks.g)) return false;
+            if (kt == ks.t0)
+#pragma unroll 1
+                for (int s = l; s < (pairs ? 2 : l + 1); ++s) {
+                    int &n = s ? n_q1 : n_q0;
+                    if (n && !wait(P8_QFREE + s, (n - 1) & 1)) return false;
+                    ++n;
+                    if (lane == 0) {
+                        ptx::mbar_arrive_expect_tx(bar(P8_QFULL + s), q_bytes);
+                        for (int h = 0; h < SM::HALVES; ++h)
+                            ptx::tma_load_4d(sbase + s * SM::TILE + h * SM::HALF, &q_map, bar(P8_QFULL + s), h * 64, ks.g * p.G,
+                                             max(ks.b, 0) * p.T + (ks.tile0 + (pairs ? s : 0)) * p.npc, 0);
+                    }
+                    __syncwarp();
+                }
+            return true;
+        }, [&](P8Load &s, int t) { s.id = find(s, t); });
+        if (!ok || *abort_flag) {
+            // copies in flight get a bounded chance to land before the CTA can exit
+            for (int e = max(0, rk.entry - SM::K_STAGES); e < rk.entry; ++e) ptx::mbar_wait(bar(P8_KFULL + e % SM::K_STAGES), (e / SM::K_STAGES) & 1);
+            for (int e = max(0, rv.entry - SM::V_STAGES); e < rv.entry; ++e) ptx::mbar_wait(bar(P8_VFULL + e % SM::V_STAGES), (e / SM::V_STAGES) & 1);
+            if (n_q0) ptx::mbar_wait(bar(P8_QFULL), (n_q0 - 1) & 1);
+            if (n_q1) ptx::mbar_wait(bar(P8_QFULL + 1), (n_q1 - 1) & 1);
+        }
     } else if (warp >= P8_CONV_WARP && warp < P8_CONV_WARP + P8_CONV_WARPS) {
-        // ------------------------------------------------------------ codes -> fp16
+        // ------------------------------------------------------------ V's codes -> fp16
         fewer_registers();
         const int tid = (warp - P8_CONV_WARP) * 32 + lane;
         constexpr int PER_ROW = D / 16;                        // 16 codes at a time
@@ -277,35 +426,39 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         static_assert(ROWS % 8 == 0, "the swizzle of a thread's chunks is the same");
         const uint32_t to_a = half * SM::HALF + row0 * 128 + ((first_c ^ (row0 & 7)) << 4), to_b = half * SM::HALF + row0 * 128 + ((first_c ^ 1 ^ (row0 & 7)) << 4);
         const bool swapped = first_c & 1;
-        int n_piece[2] = {0, 0};
-        auto phase = [&](auto lists) {
-            constexpr int NL = decltype(lists)::value, STAGES = SM::tiles(NL), CODES = SM::codes(NL);
-            const unsigned char *codes = gbase + SM::OFF_RING + STAGES * SM::TILE + tid * 16;
-            unsigned char *tiles = gbase + SM::OFF_RING;
-            int n[NL] = {}, stage = 0, turns = 0, from = 0, from_turns = 0;
-            // first, end: rows whose NaN codes become 0, and behind which all do; the whole tile as it is: end = 128, first = 128.
-            auto convert = [&](int first, int end, bool *odd) {
-                if (!wait(P8_CFULL + from, from_turns & 1)) return false;
+        const unsigned char *codes = gbase + SM::OFF_V + tid * 16;
+        unsigned char *tiles = gbase + SM::OFF_TILES;
+        int n0 = 0, n1 = 0, n_piece0 = 0, n_piece1 = 0, stage = 0, turns = 0, from = 0, from_turns = 0;
+        const bool pairs = is_pairs();
+        in_turns<P8Rows>(pairs ? 1 : 2, [&](int l, P8Rows &s) {
+                PaPiece pc;
+                int &n = l ? n1 : n0;
+                const bool any = take(pairs ? 0 : 1 + l, n++, pc);
+                s = {pc.t0, pc.t1, pc.b < 0 ? INT_MAX : pc.L};
+                return any;
+            }, [&](int l, bool v, const P8Rows &vs, int vt, bool, const P8Rows &, int) {
+                if (!v) return true;
+                if (!wait(P8_VFULL + from, from_turns & 1)) return false;
                 if (turns && !wait(P8_FREE + stage, (turns - 1) & 1)) return false;
                 const uint4 *src = reinterpret_cast<const uint4 *>(codes + from * SM::CODES);
                 unsigned char *dst = tiles + stage * SM::TILE;
-#pragma unroll
+                // rows of the tree are looked through, those behind them become zeros
+                const bool last = (vt + 1) * PA_KEYS > vs.L;
+                bool odd = false;
+#pragma unroll 1
                 for (int i0 = 0; i0 < TIMES; i0 += 4) {
                     uint4 u[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) u[i] = src[(i0 + i) * (P8_CONV_WARPS * 32)];
-                    if (first < 128 || end < 128) {
+                    if (last) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int row = row0 + (i0 + i) * ROWS;
-                            if (row >= end) {
-                                u[i] = make_uint4(0u, 0u, 0u, 0u);
-                            } else if (row >= first) {
-                                const uint32_t nx = nan_codes(u[i].x), ny = nan_codes(u[i].y), nz = nan_codes(u[i].z), nw = nan_codes(u[i].w);
-                                if (nx | ny | nz | nw) {
-                                    u[i] = make_uint4(without(u[i].x, nx), without(u[i].y, ny), without(u[i].z, nz), without(u[i].w, nw));
-                                    *odd = true;
-                                }
+                            const int a = vt * PA_KEYS + row0 + (i0 + i) * ROWS - vs.L;        // the row's node
+                            const uint32_t nans = nan_codes(u[i].x) | nan_codes(u[i].y) | nan_codes(u[i].z) | nan_codes(u[i].w);
+                            if (a >= p.T) u[i] = make_uint4(0u, 0u, 0u, 0u);
+                            else if (a >= 0 && nans) {
+                                u[i] = make_uint4(without_nans(u[i].x), without_nans(u[i].y), without_nans(u[i].z), without_nans(u[i].w));
+                                odd = true;
                             }
                         }
                     }
@@ -317,93 +470,76 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         *reinterpret_cast<uint4 *>(dst + to_b + (i0 + i) * ROWS * 128) = swapped ? lo : hi;
                     }
                 }
-                return true;
-            };
-            auto pass = [&]() {
+                if (last && __any_sync(0xffffffffu, odd) && lane == 0) {
+                    if (pairs || l == 0) bad[n_piece0 & 3] = n_piece0 + 1;
+                    if (pairs || l == 1) bad[4 + (n_piece1 & 3)] = n_piece1 + 1;
+                }
                 ptx::fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) {
                     ptx::mbar_arrive(bar(P8_FULL + stage));
-                    ptx::mbar_arrive(bar(P8_CFREE + from));
+                    ptx::mbar_arrive(bar(P8_VFREE + from));
                 }
                 __syncwarp();
-                if (++stage == STAGES) { stage = 0; ++turns; }
-                if (++from == CODES) { from = 0; ++from_turns; }
-            };
-            return for_rounds<NL, P8Rows>([&](int l, P8Rows &s) {
-                PaPiece pc;
-                const bool any = take(NL == 1 ? 0 : 1 + l, n[l]++, pc);
-                s = {pc.t0, pc.t1, pc.b < 0 ? INT_MAX : pc.L};
-                return any;
-            }, [&](int l, bool v, const P8Rows &vs, int vt, bool k, const P8Rows &ks, int kt) {
-                if (v) {
-                    bool odd = false;
-                    const bool last = (vt + 1) * PA_KEYS > vs.L;
-                    if (!convert(last ? max(0, vs.L - vt * PA_KEYS) : 128, last ? min(vs.L + p.T - vt * PA_KEYS, PA_KEYS) : 128, &odd)) return false;
-                    if (last && __any_sync(0xffffffffu, odd) && lane == 0)
-                        for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) bad[s * 4 + (n_piece[s] & 3)] = n_piece[s] + 1;
-                    pass();
-                    if (vt == vs.t1 - 1)
-                        for (int s = l; s < (NL == 1 ? 2 : l + 1); ++s) ++n_piece[s];
-                }
-                if (k) {
-                    if (!convert(128, 128, nullptr)) return false;
-                    pass();
+                if (++stage == SM::TILES) { stage = 0; ++turns; }
+                if (++from == SM::V_STAGES) { from = 0; ++from_turns; }
+                if (vt == vs.t1 - 1) {
+                    n_piece0 += pairs || l == 0;
+                    n_piece1 += pairs || l == 1;
                 }
                 return true;
-            });
-        };
-        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+            }, [](P8Rows &, int) {});
     } else if (warp == P8_MMA_WARP || warp == P8_MMA_WARP + 1) {
         // ------------------------------------------------------------ products of row tile s
         fewer_registers();
         const int s = warp - P8_MMA_WARP;
         const bool leader = ptx::elect_one();
-        const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_RING, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_RING, SM::HALF);
+        const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_K, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_TILES, SM::HALF);
         const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * D;
         int n_p = 0, n_q = 0, n_turn = 0;
-        auto phase = [&](auto lists) {
-            constexpr int NL = decltype(lists)::value, STAGES = SM::tiles(NL);
-            int n[NL] = {}, entry = 0;
-            return for_rounds<NL, P8Tiles>([&](int l, P8Tiles &x) {
+        int v_stage = 0, v_turns = 0, k_stage = 0, k_turns = 0;
+        int n0 = 0, n1 = 0;
+        const bool pairs = is_pairs();
+        in_turns<P8Tiles>(pairs ? 1 : 2, [&](int l, P8Tiles &x) {
                 PaPiece pc;
-                const bool any = take(NL == 1 ? 0 : 1 + l, n[l]++, pc);
+                int &n = l ? n1 : n0;
+                const bool any = take(pairs ? 0 : 1 + l, n++, pc);
                 x = {pc.t0, pc.t1};
                 return any;
             }, [&](int l, bool v, const P8Tiles &vs, int vt, bool k, const P8Tiles &ks, int kt) {
-                const int ve = entry, ke = entry + (v ? 1 : 0);
-                entry = ke + (k ? 1 : 0);
-                const int v_stage = ve % STAGES, k_stage = ke % STAGES;
-                if (NL == 2 && l != s) {
-                    // the other tile's: waited for and handed back all the same, so that this warp is never a turn of the ring ahead or
+                const int v_at = v_stage, k_at = k_stage, v_parity = v_turns & 1, k_parity = k_turns & 1;
+                if (v && ++v_stage == SM::TILES) { v_stage = 0; ++v_turns; }
+                if (k && ++k_stage == SM::K_STAGES) { k_stage = 0; ++k_turns; }
+                if (!pairs && l != s) {
+                    // the other tile's: waited for and handed back all the same, so that this warp is never a turn of a ring ahead or
                     // late (a parity wait cannot tell a phase from the one two before or behind)
-                    auto pass = [&](int e, int stage) {
-                        if (!wait(P8_FULL + stage, (e / STAGES) & 1)) return false;
-                        if (lane == 0) ptx::mbar_arrive(bar(P8_FREE + stage));
+                    auto pass = [&](int full, int free, int parity) {
+                        if (!wait(full, parity)) return false;
+                        if (lane == 0) ptx::mbar_arrive(bar(free));
                         __syncwarp();
                         return true;
                     };
-                    return (!v || pass(ve, v_stage)) && (!k || pass(ke, k_stage));
+                    return (!v || pass(P8_FULL + v_at, P8_FREE + v_at, v_parity)) && (!k || pass(P8_KFULL + k_at, P8_KFREE + k_at, k_parity));
                 }
-                auto k_there = [&]() { return wait(P8_FULL + k_stage, (ke / STAGES) & 1) && (kt != ks.t0 || wait(P8_QREADY + s, n_q++ & 1)); };
+                auto k_there = [&]() { return wait(P8_KFULL + k_at, k_parity) && (kt != ks.t0 || wait(P8_QREADY + s, n_q++ & 1)); };
                 // Pairs take turns: the products of a row tile go to the tensor core in one run.  Mixed with the other tile's, both tiles' scores
                 // would come when all are done, both softmaxes would then run at once, and the tensor core wait for both.
                 auto begin_run = [&]() {
-                    if (NL == 2) return true;
+                    if (!pairs) return true;
                     const int turn = n_turn++;
                     return s == 0 && turn == 0 ? true : wait(P8_TURN + s, (turn + s - 1) & 1);
                 };
                 auto end_run = [&]() {
-                    if (NL == 1 && lane == 0) ptx::mbar_arrive(bar(P8_TURN + (s ^ 1)));
+                    if (pairs && lane == 0) ptx::mbar_arrive(bar(P8_TURN + (s ^ 1)));
                     __syncwarp();
                 };
                 // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be)
                 const bool ahead = v && k && kt != ks.t0;
                 if (ahead && !k_there()) return false;
                 if (v) {
-                    if (!wait(P8_FULL + v_stage, (ve / STAGES) & 1) || !wait(P8_PREADY + s, n_p++ & 1) || !begin_run()) return false;
+                    if (!wait(P8_FULL + v_at, v_parity) || !wait(P8_PREADY + s, n_p++ & 1) || !begin_run()) return false;
                     ptx::tc_fence_after();
-                    const uint32_t dv = dv0 + (uint32_t)v_stage * (SM::TILE >> 4);
+                    const uint32_t dv = dv0 + (uint32_t)v_at * (SM::TILE >> 4);
 #pragma unroll
                     for (int kk = 0; kk < PA_KEYS / 16; ++kk)
                         ptx::mma_ts_elect(t_o, t_s + kk / 4 * 64 + kk % 4 * 8, dv + kk * 128, ptx::DESC_HI, SM::IDESC_PV, vt > vs.t0 || kk > 0, leader);
@@ -415,22 +551,20 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         if (!k_there() || !begin_run()) return false;
                         ptx::tc_fence_after();
                     }
-                    const uint32_t dk = dk0 + (uint32_t)k_stage * (SM::TILE >> 4);
+                    const uint32_t dk = dk0 + (uint32_t)k_at * (SM::CODES >> 4);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint32_t o = ((kk / 4) * SM::HALF + (kk % 4) * 32) >> 4;
-                        ptx::mma_ss_elect(t_s, dq + o, dk + o, ptx::DESC_HI, SM::IDESC_QK, kk > 0, leader);
-                    }
+                    for (int term = 0; term < 2; ++term)
+#pragma unroll
+                        for (int kk = 0; kk < D / 32; ++kk)
+                            ptx::mma_ss_f8_elect(t_s, dq + (term * SM::Q2 + kk * 32) / 16, ptx::DESC_HI, dk + kk * 2, SM::K_DESC_HI, SM::IDESC_QK, term + kk > 0, leader);
                     ptx::tc_commit_elect(bar(P8_SREADY + s), leader);
                     if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(P8_QFREE + s), leader);
                     end_run();
                 }
-                if (v) ptx::tc_commit_elect(bar(P8_FREE + v_stage), leader);
-                if (k) ptx::tc_commit_elect(bar(P8_FREE + k_stage), leader);
+                if (v) ptx::tc_commit_elect(bar(P8_FREE + v_at), leader);
+                if (k) ptx::tc_commit_elect(bar(P8_KFREE + k_at), leader);
                 return true;
-            });
-        };
-        phase(std::integral_constant<int, 1>()) && phase(std::integral_constant<int, 2>());
+            }, [](P8Tiles &, int) {});
         // what was issued is complete, and has signalled, before the CTA can exit
         ptx::tc_commit_elect(bar(P8_FINAL), leader);
         ptx::mbar_wait(bar(P8_FINAL), 0);
@@ -456,35 +590,44 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         };
         int n_s = 0, n_piece = 0;
         bool ok = true;
-        for (int f = 0; f < 2 && ok; ++f) {
+        {
+            const int f = is_pairs() ? 0 : 1;
             const PaPhase &ph = p.phase[f];
             PaPiece pc;
+#pragma unroll 1
             for (int n = 0; ok && take(f ? 1 + s : 0, n, pc); ++n) {
                 const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
                 const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
                 const bool some = __any_sync(0xffffffffu, mine);
-                // ---- the queries: each thread of a row takes half of its columns
+                // ---- the queries in two terms: each thread of a row takes half of its columns (both have read them when their maxima are exchanged)
+                const float ks = __ldg(pp.k_scale + pc.g);
                 if (!wait(P8_QFULL + s, n_piece & 1)) { ok = false; break; }
                 float sc;
                 {
                     constexpr int CHUNKS = D / 16;
-                    unsigned char *q = gbase + s * SM::TILE + (D == 128 ? hf * SM::HALF : 0) + row * 128;
-                    const int c0 = D == 128 ? 0 : hf * CHUNKS;
+                    unsigned char *q = gbase + s * SM::TILE + row * 128;
+                    uint4 u[CHUNKS];
                     uint32_t most = 0u;
-#pragma unroll 4
-                    for (int c = 0; c < CHUNKS; ++c) {
-                        const uint4 u = *reinterpret_cast<const uint4 *>(q + (((c0 + c) ^ (row & 7)) << 4));
-                        most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u.x)), abs2_bf16(u.y)), abs2_bf16(u.z)), abs2_bf16(u.w));
-                    }
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+                        u[c] = *reinterpret_cast<const uint4 *>(q + (D == 128 ? hf * SM::HALF : 0) + ((((D == 128 ? 0 : hf * CHUNKS) + c) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+                        most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u[c].x)), abs2_bf16(u[c].y)), abs2_bf16(u[c].z)), abs2_bf16(u[c].w));
                     most = max(most, __float_as_uint(exchange(X_COL, __uint_as_float(most))));
-                    const float2 factor = row_factor(most);
-#pragma unroll 4
-                    for (int c = 0; c < CHUNKS; ++c) {
-                        uint4 *at = reinterpret_cast<uint4 *>(q + (((c0 + c) ^ (row & 7)) << 4));
-                        const uint4 u = *at;
-                        *at = make_uint4(to_f16(u.x, factor.x), to_f16(u.y, factor.x), to_f16(u.z, factor.x), to_f16(u.w, factor.x));
+                    const float2 factor = row_factor<7>(most);
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; c += 2) {
+                        uint4 a, b;
+                        to_terms(u[c].x, u[c].y, factor.x, a.x, b.x);
+                        to_terms(u[c].z, u[c].w, factor.x, a.y, b.y);
+                        to_terms(u[c + 1].x, u[c + 1].y, factor.x, a.z, b.z);
+                        to_terms(u[c + 1].z, u[c + 1].w, factor.x, a.w, b.w);
+                        const int at = hf * (D / 32) + c / 2, at2 = D == 128 ? at : at + 4;      // 16 columns
+                        *reinterpret_cast<uint4 *>(q + ((at ^ (row & 7)) << 4)) = a;
+                        *reinterpret_cast<uint4 *>(q + (D == 128 ? SM::HALF : 0) + ((at2 ^ (row & 7)) << 4)) = b;
                     }
-                    sc = p.scale_log2 * __ldg(pp.k_scale + pc.g) * factor.y;
+                    sc = p.scale_log2 * ks * factor.y;
                     ptx::tc_fence_before();
                     ptx::fence_proxy_async();
                     __syncwarp();
@@ -496,6 +639,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if (mine && pc.b >= 0) anc = reinterpret_cast<const uint4 *>(p.anc)[node];
                 auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w == 0 ? anc.x : w == 1 ? anc.y : w == 2 ? anc.z : w == 3 ? anc.w : 0u; };
                 float m_used = -INFINITY, l = 0.f;
+#pragma unroll 1
                 for (int t = pc.t0; t < pc.t1; ++t) {
                     if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
                     ptx::tc_fence_after();
@@ -770,7 +914,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
             }
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            const float2 factor = row_factor(most);
+            const float2 factor = row_factor<8>(most);
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -851,8 +995,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
                         for (int e = 0; e < JW; ++e) {
-                            const uint32_t nans = nan_codes(vx[kk][k][e]);
-                            if (nans) { vx[kk][k][e] = without(vx[kk][k][e], nans); odd = true; }
+                            if (nan_codes(vx[kk][k][e])) { vx[kk][k][e] = without_nans(vx[kk][k][e]); odd = true; }
                         }
                 odd = __any_sync(0xffffffffu, odd);
             }
@@ -990,7 +1133,7 @@ extern "C" int tree_verify_attention_paged_fp8(const mtv_tree_t *tree, int B, in
         const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)pool->page_size, (cuuint64_t)Hkv, (cuuint64_t)pool->n_pages};
         const cuuint64_t str[3] = {(cuuint64_t)pool->stride_t, (cuuint64_t)pool->stride_h, (cuuint64_t)pool->stride_page};
         const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)p.page_rows, 1, 1};
-        if (!encode_map_bytes(&k_map, k_pool, 4, dims, str, box) || !encode_map_bytes(&v_map, v_pool, 4, dims, str, box)) return MTV_ERR_CUDA;
+        if (!encode_map_bytes(&k_map, k_pool, 4, dims, str, box, D) || !encode_map_bytes(&v_map, v_pool, 4, dims, str, box, 0)) return MTV_ERR_CUDA;
     }
     return D == 128 ? launch_paged8<128>(q_map, k_map, v_map, pp, (cudaStream_t)stream) : launch_paged8<64>(q_map, k_map, v_map, pp, (cudaStream_t)stream);
 }

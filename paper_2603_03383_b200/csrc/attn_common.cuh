@@ -54,7 +54,8 @@ bool tensor_map_bf16(CUtensorMap *map, const void *base, int rank, const cuuint6
                      const cuuint32_t *box);
 // The same, encoded anew.
 bool encode_map_bf16(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes, const cuuint32_t *box);
-// Over bytes, whose box lands row after row, without a swizzle.
-bool encode_map_bytes(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes, const cuuint32_t *box);
+// Over bytes, whose box lands row after row; swizzle: over 128 or 64 bytes, the box's innermost extent, or 0.
+bool encode_map_bytes(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes, const cuuint32_t *box,
+                      int swizzle);
 
 }  // namespace mtv

@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
 // The top bit of every byte of the result: the code there is NaN.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // Codes that are NaN become 0.
-__device__ __forceinline__ uint32_t without(uint32_t codes, uint32_t nans) { return codes & ~((nans >> 7) * 0xffu); }
+__device__ __forceinline__ uint32_t without_nans(uint32_t codes) { return codes & ~((nan_codes(codes) >> 7) * 0xffu); }
 __device__ __forceinline__ float2 f16x2_values(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
 
 }  // namespace mtv

@@ -5,6 +5,7 @@
 // can be read back as bf16.
 #include "fp8.cuh"
 #include "paged_common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace mtv {
 
@@ -354,12 +355,13 @@ struct ReadParams {
 };
 
 // Bound by memory: a byte read and two written per value.  A block takes READ_ROWS rows of some layers, finds their pages once, and its threads move
-// 8 codes at a time, READ_DEEP requested together; the blocks behind the rows' own report one sequence per warp.
-constexpr int READ_ROWS = 16, READ_DEEP = 8;
-template <int D>
+// 16 codes at a time, READ_DEEP requested together; the blocks behind the rows' own report one sequence per warp.
+// WIDE: the outputs begin at multiples of 32 bytes.
+constexpr int READ_ROWS = 16, READ_DEEP = 4;
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(PAGED_THREADS)
 kv_read_paged_kernel(const ReadParams p) {
-    constexpr int PER_HEAD = D / 8;
+    constexpr int PER_HEAD = D / 16;
     __shared__ int64_t src_of[READ_ROWS];      // of the row inside a pool; -1: the row is left alone
     const int tid = threadIdx.x;
     let_next_start();
@@ -385,37 +387,43 @@ kv_read_paged_kernel(const ReadParams p) {
         src_of[tid] = src;
     }
     __syncthreads();
-    const int l0 = (int)blockIdx.y * p.layers_per_block, layers = min(p.n_layers - l0, p.layers_per_block);
-    const int per_row = p.Hkv * PER_HEAD, per_layer = 2 * READ_ROWS * per_row;
-    for (int l = l0; l < l0 + layers; ++l) {
-        const uint8_t *const pool[2] = {p.k_pools[l], p.v_pools[l]};
-        for (int e0 = tid; e0 < per_layer; e0 += READ_DEEP * PAGED_THREADS) {
-            uint2 x[READ_DEEP];
-            float scale[READ_DEEP];
-            __nv_bfloat16 *dst[READ_DEEP];
+    // Chunks of a row, rows of a pool, K and V, layers, one behind the other: (row, in_row) of a thread's next chunk, the row counted over pools and layers.
+    const int l0 = (int)blockIdx.y * p.layers_per_block, end = min(p.n_layers - l0, p.layers_per_block) * 2 * READ_ROWS;
+    const int per_row = p.Hkv * PER_HEAD, step_rows = PAGED_THREADS / per_row, step_chunks = PAGED_THREADS - step_rows * per_row;
+    int row = tid / per_row, in_row = tid - row * per_row;
+    while (row < end) {
+        uint4 x[READ_DEEP];
+        float scale[READ_DEEP];
+        __nv_bfloat16 *dst[READ_DEEP];
 #pragma unroll
-            for (int k = 0; k < READ_DEEP; ++k) {
-                const int e = e0 + k * PAGED_THREADS;
-                const int v = e >= per_layer / 2, in_pool = v ? e - per_layer / 2 : e, j = in_pool / per_row, in_row = in_pool - j * per_row;
-                const int g = in_row / PER_HEAD, c = in_row % PER_HEAD * 8;
-                dst[k] = nullptr;
-                if (e >= per_layer || src_of[j] < 0) continue;
-                x[k] = __ldg(reinterpret_cast<const uint2 *>((v ? pool[1] : pool[0]) + src_of[j] + g * p.pages.stride_h + c));
+        for (int k = 0; k < READ_DEEP; ++k) {
+            const int l = l0 + row / (2 * READ_ROWS), v = row / READ_ROWS & 1, j = row % READ_ROWS, g = in_row / PER_HEAD, c = in_row % PER_HEAD * 16;
+            dst[k] = nullptr;
+            if (row < end && src_of[j] >= 0) {
+                x[k] = __ldg(reinterpret_cast<const uint4 *>((v ? p.v_pools : p.k_pools)[l] + src_of[j] + g * p.pages.stride_h + c));
                 scale[k] = (v ? p.v_scale : p.k_scale)[l * p.Hkv + g];
                 dst[k] = (v ? p.v_out : p.k_out) + (((size_t)l * p.n_rows + r0 + j) * p.Hkv + g) * D + c;
             }
+            row += step_rows;
+            in_row += step_chunks;
+            if (in_row >= per_row) { in_row -= per_row; ++row; }
+        }
 #pragma unroll
-            for (int k = 0; k < READ_DEEP; ++k) {
-                if (!dst[k]) continue;
-                uint32_t w[4];
+        for (int k = 0; k < READ_DEEP; ++k) {
+            if (!dst[k]) continue;
+            const uint32_t codes[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+            uint32_t w[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t codes = i < 2 ? x[k].x : x[k].y;
-                    const float2 f = f16x2_values(i % 2 ? f16x2_hi(codes) : f16x2_lo(codes));
-                    const __nv_bfloat162 o = __floats2bfloat162_rn(f.x * scale[k], f.y * scale[k]);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&o);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float2 f = f16x2_values(i % 2 ? f16x2_hi(codes[i / 2]) : f16x2_lo(codes[i / 2]));
+                const __nv_bfloat162 o = __floats2bfloat162_rn(f.x * scale[k], f.y * scale[k]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&o);
+            }
+            if constexpr (WIDE) {
+                ptx::st_global_32(dst[k], w);
+            } else {
                 *reinterpret_cast<uint4 *>(dst[k]) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(dst[k] + 8) = make_uint4(w[4], w[5], w[6], w[7]);
             }
         }
     }
@@ -568,7 +576,9 @@ extern "C" int kv_read_paged_fp8(int B, int n_rows, int Hkv, int D, int n_layers
     per = per < 1 ? 1 : per > n_layers ? n_layers : per;
     p.layers_per_block = (int)per;
     const int report = status || !p.row_blocks ? (B + PAGED_THREADS / 32 - 1) / (PAGED_THREADS / 32) : 0;
-    MTV_CUDA_CHECK(launch_dependent(D == 128 ? kv_read_paged_kernel<128> : kv_read_paged_kernel<64>,
-                                    dim3(p.row_blocks + report, (unsigned)((n_layers + per - 1) / per)), PAGED_THREADS, 0, (cudaStream_t)stream, p));
+    const bool wide = (((uintptr_t)k_out_layers | (uintptr_t)v_out_layers) & 31) == 0;
+    auto kernel = D == 128 ? (wide ? kv_read_paged_kernel<128, true> : kv_read_paged_kernel<128, false>)
+                           : (wide ? kv_read_paged_kernel<64, true> : kv_read_paged_kernel<64, false>);
+    MTV_CUDA_CHECK(launch_dependent(kernel, dim3(p.row_blocks + report, (unsigned)((n_layers + per - 1) / per)), PAGED_THREADS, 0, (cudaStream_t)stream, p));
     return MTV_OK;
 }

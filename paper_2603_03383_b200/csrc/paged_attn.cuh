@@ -172,10 +172,9 @@ __device__ __forceinline__ void begin_walks(const PaParams &p, PaWalk (&w)[3], i
 
 // All of a phase's key tiles in the order in which the ring holds them: a round takes, list after list, V of the tile before and K of the
 // tile after.  next(list, piece) -> whether there is one; f(list, piece and tile of V or none, piece and tile of K or none) -> whether to go on.
-// P: what a warp wants of a piece, t0 and t1 at least.
-template <int NL, typename P = PaPiece, typename N, typename F>
+template <int NL, typename N, typename F>
 __device__ __forceinline__ bool for_rounds(N &&next, F &&f) {
-    P cur[NL], old[NL];
+    PaPiece cur[NL], old[NL];
     int t[NL], old_t[NL];
     bool live[NL], pend[NL];
 #pragma unroll

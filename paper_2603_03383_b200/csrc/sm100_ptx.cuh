@@ -172,6 +172,21 @@ __device__ __forceinline__ void mma_ss_elect(uint32_t d_tmem, uint32_t a_lo, uin
         "}\n"
         ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"((uint32_t)accumulate), "r"((uint32_t)leader) : "memory");
 }
+// 8-bit inputs (32 of the contraction at a time); the operands' swizzles may differ.
+__device__ __forceinline__ void mma_ss_f8_elect(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                bool accumulate, bool leader) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        ".reg .b64 a, b;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "setp.ne.b32 q, %7, 0;\n"
+        "mov.b64 a, {%1, %2};\n"
+        "mov.b64 b, {%3, %4};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n"
+        "}\n"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"((uint32_t)accumulate), "r"((uint32_t)leader) : "memory");
+}
 // The same over a CTA pair, and its commit to the barriers at the same offset in the CTAs of `mask`.
 __device__ __forceinline__ void mma_pair_ss_elect(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc,
                                                   bool accumulate, bool leader) {
