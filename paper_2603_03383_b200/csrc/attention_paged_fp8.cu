@@ -28,18 +28,15 @@ namespace mtv {
 
 constexpr int P8_THREADS = 768;
 constexpr int P8_CONV_WARP = 16, P8_CONV_WARPS = 4, P8_MMA_WARP = 20, P8_TMA_WARP = 22;
-constexpr int P8_REGS_FEWER = 48, P8_REGS_MORE = 96;
-static_assert(4 * P8_REGS_MORE + 2 * P8_REGS_FEWER <= 6 * 80, "registers of the warpgroups against those of the launch");
-constexpr float P8_SHIFT = 8.f;
-constexpr float P8_LIMIT = 15.99f;        // weights stay below 2^16, which fp16 ends at
+constexpr float P8_SHIFT = 8.f, P8_LIMIT = 15.99f;     // weights stay below 2^16, which fp16 ends at
 
 template <int D> struct P8Smem {
     static constexpr int HALVES = D / 64;
     static constexpr uint32_t HALF = 128 * 128;          // 128 rows of 128 bytes (64 columns of 2, or 128 of 1), 128-byte swizzle
     static constexpr uint32_t TILE = HALVES * HALF, CODES = 128 * D;
     static constexpr int K_STAGES = D == 128 ? 3 : 8, V_STAGES = K_STAGES, TILES = D == 128 ? 2 : 4;
-    static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + K_STAGES * CODES, OFF_TILES = OFF_V + V_STAGES * CODES, OFF_BAR = OFF_TILES + TILES * TILE,
-                              TOTAL = 1024 + OFF_BAR + 1280;
+    static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + K_STAGES * CODES, OFF_TILES = OFF_V + V_STAGES * CODES, OFF_ROWS = OFF_TILES + TILES * TILE,
+                              OFF_BAR = OFF_ROWS + 2048, TOTAL = OFF_BAR + 960;
     static_assert(TOTAL <= 227 * 1024, "shared memory budget");
     static constexpr uint32_t IDESC = (1u << 4) | (128u >> 4) << 24;                             // e4m3 x e4m3 or fp16 x fp16 -> fp32, M = 128
     static constexpr uint32_t IDESC_QK = IDESC | (128u >> 3) << 17;                               // N = 128 keys
@@ -52,14 +49,14 @@ template <int D> struct P8Smem {
 enum {
     P8_KFULL = 0, P8_KFREE = 8, P8_VFULL = 16, P8_VFREE = 24, P8_FULL = 32, P8_FREE = 36, P8_QFULL = 40, P8_QREADY = 42, P8_QFREE = 44, P8_SREADY = 46,
     P8_PREADY = 48, P8_ODONE = 50, P8_FINAL = 52,
-    P8_PIECE = 53,                         // [3 queues][PA_QUEUE]: pairs; single tiles of either half of the CTA
-    P8_TAKEN = P8_PIECE + 3 * PA_QUEUE,
-    P8_TURN = P8_TAKEN + 3 * PA_QUEUE,     // [2] an issuing warp's turn at the tensor core
+    P8_PIECE = 53,                         // [2 queues][PA_QUEUE]: pairs, or single tiles of one half of the CTA; those of the other half
+    P8_TAKEN = P8_PIECE + 2 * PA_QUEUE,
+    P8_TURN = P8_TAKEN + 2 * PA_QUEUE,     // [2] an issuing warp's turn at the tensor core
     P8_ROLE = P8_TURN + 2,                 // whether the CTA has pairs is known
     P8_COUNT = P8_ROLE + 1
 };
 constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 + 15) / 16 * 16;
-static_assert(P8_OFF_QUEUE + 3 * PA_QUEUE * 32 <= 1280, "barrier region");
+static_assert(P8_OFF_QUEUE + 2 * PA_QUEUE * 32 <= 960, "barrier region");
 static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
 constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
@@ -201,8 +198,6 @@ __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P8_REGS_FEWER)); }
-
 // Four values times the factor, as codes of their first terms and of their second.
 __device__ __forceinline__ void to_terms(uint32_t pair0, uint32_t pair1, float factor, uint32_t &first, uint32_t &second) {
     const float x[4] = {__uint_as_float(pair0 << 16) * factor, __uint_as_float(pair0 & 0xffff0000u) * factor,
@@ -218,20 +213,24 @@ __global__ void __launch_bounds__(P8_THREADS, 1)
 paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    const __grid_constant__ P8Params pp) {
     using SM = P8Smem<D>;
-    constexpr int X_COL = 40;              // of a half's tensor-memory columns, behind P: what the threads of a row exchange
     const PaParams &p = pp.a;
-    extern __shared__ unsigned char smem_raw[];
+    extern __shared__ __align__(1024) unsigned char gbase[];
     let_next_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u, sbase = raw + pad;
-    unsigned char *gbase = smem_raw + pad;
+    const uint32_t sbase = ptx::smem_u32(gbase);
+    if (sbase & 1023u) {                   // (the swizzles count on it)
+        previous_done();
+        if (threadIdx.x == 0) atomicExch(p.dev_error, MTV_ERR_TIMEOUT);
+        return;
+    }
+    float *of_rows = reinterpret_cast<float *>(gbase + SM::OFF_ROWS);                              // [2][2][128]: what the two threads of a row exchange
     const uint32_t bars = sbase + SM::OFF_BAR;
     auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + SM::OFF_BAR + P8_OFF_MISC);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 4);
     volatile int *bad = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 8);   // [2][4]: 1 + the last piece with NaN in V
     volatile int *role = reinterpret_cast<volatile int *>(gbase + SM::OFF_BAR + P8_OFF_MISC + 40);
-    int4 *queue = reinterpret_cast<int4 *>(gbase + SM::OFF_BAR + P8_OFF_QUEUE);                    // [3][PA_QUEUE] pieces
+    int4 *queue = reinterpret_cast<int4 *>(gbase + SM::OFF_BAR + P8_OFF_QUEUE);                    // [2][PA_QUEUE] pieces
 
     if (warp == P8_TMA_WARP && lane == 0) {
         ptx::prefetch_tensormap(&q_map);
@@ -258,10 +257,10 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
         ptx::mbar_init(bar(P8_FINAL), 2);
         ptx::mbar_init(bar(P8_ROLE), 1);
-        for (int q = 0; q < 3; ++q)
+        for (int q = 0; q < 2; ++q)
             for (int i = 0; i < PA_QUEUE; ++i) {
                 ptx::mbar_init(bar(P8_PIECE + q * PA_QUEUE + i), 1);
-                ptx::mbar_init(bar(P8_TAKEN + q * PA_QUEUE + i), 2 + P8_CONV_WARPS + (q ? 8 : 16));
+                ptx::mbar_init(bar(P8_TAKEN + q * PA_QUEUE + i), 2 + P8_CONV_WARPS + 8);
             }
         ptx::fence_mbar_init();
         *abort_flag = 0;
@@ -289,20 +288,30 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     // whether the CTA has pairs of row tiles, or single ones
     auto is_pairs = [&]() { return wait(P8_ROLE, 0) && *role; };
     // the n-th piece of a queue; none (or nothing to be had): false
-    auto take = [&](int q, int n, PaPiece &s) {
+    auto piece_at = [&](int q, int n) {
         const int at = q * PA_QUEUE + n % PA_QUEUE;
-        if (__any_sync(0xffffffffu, *abort_flag) || !wait(P8_PIECE + at, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
         const int4 a = queue[at * 2], c = queue[at * 2 + 1];
+        PaPiece s;
         s.b = a.x; s.g = a.y; s.tile0 = a.z; s.t0 = a.w; s.t1 = c.x; s.L = c.y; s.slot = c.z; s.whole = c.w;
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(P8_TAKEN + at));
-        __syncwarp();
+        return s;
+    };
+    auto look = [&](int q, int n, PaPiece &s) {
+        if (__any_sync(0xffffffffu, *abort_flag) || !wait(P8_PIECE + q * PA_QUEUE + n % PA_QUEUE, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
+        s = piece_at(q, n);
         return s.t1 > 0;
     };
+    auto taken = [&](int q, int n) {       // its place may be given to another
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(P8_TAKEN + q * PA_QUEUE + n % PA_QUEUE));
+        __syncwarp();
+    };
+    auto take = [&](int q, int n, PaPiece &s) {
+        const bool any = look(q, n, s);
+        taken(q, n);
+        return any;
+    };
 
-    // (in the branches themselves: where they met again the compiler would count on the smaller number)
     if (warp == P8_TMA_WARP) {
-        fewer_registers();
         // ------------------------------------------------------------ pieces; Q and the codes of K and V
         int tiles = 0, seqs = 0;             // key tiles of an item of every sequence that is not left out, and their number
         for (int b0 = 0; b0 < p.B; b0 += 32) {
@@ -338,7 +347,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         // of a piece are only requested when the scores of the one before are complete, so this warp is never three pieces ahead.)
         auto hand_out = [&](int q, int n, PaPiece &s) {
             const int at = q * PA_QUEUE + n % PA_QUEUE;
-            const bool any = walk[q == 2].next(p, p.phase[q > 0], s);
+            const bool any = walk[q].next(p, p.phase[pairs ? 0 : 1], s);
             if (!any) s = PaPiece{};
             if (n >= PA_QUEUE && !wait(P8_TAKEN + at, (n / PA_QUEUE - 1) & 1)) { s.t0 = s.t1 = 0; return false; }
             if (lane == 0) {
@@ -383,7 +392,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const int lists = pairs ? 1 : 2;
         const bool ok = in_turns<P8Load>(lists, [&](int l, P8Load &s) {
             int &n = l ? n1 : n0;
-            if (!hand_out(pairs ? 0 : 1 + l, n++, s)) return false;
+            if (!hand_out(l, n++, s)) return false;
             s.id = find(s, s.t0);
             return true;
         }, [&](int l, bool v, const P8Load &vs, int vt, bool k, const P8Load &ks, int kt) {
@@ -415,7 +424,6 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
     } else if (warp >= P8_CONV_WARP && warp < P8_CONV_WARP + P8_CONV_WARPS) {
         // ------------------------------------------------------------ V's codes -> fp16
-        fewer_registers();
         const int tid = (warp - P8_CONV_WARP) * 32 + lane;
         constexpr int PER_ROW = D / 16;                        // 16 codes at a time
         constexpr int TIMES = 128 * PER_ROW / (P8_CONV_WARPS * 32);
@@ -433,7 +441,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         in_turns<P8Rows>(pairs ? 1 : 2, [&](int l, P8Rows &s) {
                 PaPiece pc;
                 int &n = l ? n1 : n0;
-                const bool any = take(pairs ? 0 : 1 + l, n++, pc);
+                const bool any = take(l, n++, pc);
                 s = {pc.t0, pc.t1, pc.b < 0 ? INT_MAX : pc.L};
                 return any;
             }, [&](int l, bool v, const P8Rows &vs, int vt, bool, const P8Rows &, int) {
@@ -491,7 +499,6 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }, [](P8Rows &, int) {});
     } else if (warp == P8_MMA_WARP || warp == P8_MMA_WARP + 1) {
         // ------------------------------------------------------------ products of row tile s
-        fewer_registers();
         const int s = warp - P8_MMA_WARP;
         const bool leader = ptx::elect_one();
         const uint32_t dq = ptx::desc_lo(sbase + s * SM::TILE, 16), dk0 = ptx::desc_lo(sbase + SM::OFF_K, 16), dv0 = ptx::desc_lo(sbase + SM::OFF_TILES, SM::HALF);
@@ -503,7 +510,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         in_turns<P8Tiles>(pairs ? 1 : 2, [&](int l, P8Tiles &x) {
                 PaPiece pc;
                 int &n = l ? n1 : n0;
-                const bool any = take(pairs ? 0 : 1 + l, n++, pc);
+                const bool any = take(l, n++, pc);
                 x = {pc.t0, pc.t1};
                 return any;
             }, [&](int l, bool v, const P8Tiles &vs, int vt, bool k, const P8Tiles &ks, int kt) {
@@ -570,172 +577,80 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         ptx::mbar_wait(bar(P8_FINAL), 0);
     } else if (warp < P8_CONV_WARP) {
         // ------------------------------------------------------------ softmax: thread (row, hf) of row tile s: columns [64 hf, 64 hf + 64)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P8_REGS_MORE));
         const int s = warp >> 3, hf = (warp >> 2) & 1, qd = warp & 3, row = qd * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
         const uint32_t t_s = lane_base + s * 128 + hf * 64;      // this half's scores, and P over them
-        const uint32_t t_x = lane_base + s * 128 + (hf ^ 1) * 64;
         const uint32_t t_o = lane_base + 256 + s * D + hf * (D / 2);
         const int pair_bar = 2 + s * 4 + qd;
         const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
-        const bool in_tile = node_in_tile < p.npc;
-        // what the other half of the row has: both put theirs where nothing is any more
-        auto exchange = [&](int col, float v) {
-            tmem_put(t_s + col, v);
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
-            ptx::tc_fence_after();
-            return tmem_get(t_x + col);
+        const bool pairs = is_pairs();
+        const PaPhase &ph = p.phase[pairs ? 0 : 1];
+        const int q = pairs ? 0 : s;
+        // what the other thread of the row has (two barriers: what was exchanged before has been read)
+        auto pair_sync = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory"); };
+        auto exchange = [&](float v) {
+            pair_sync();
+            of_rows[(s * 2 + hf) * 128 + row] = v;
+            pair_sync();
+            return of_rows[(s * 2 + (hf ^ 1)) * 128 + row];
         };
-        int n_s = 0, n_piece = 0;
-        bool ok = true;
-        {
-            const int f = is_pairs() ? 0 : 1;
-            const PaPhase &ph = p.phase[f];
+        auto node_of = [&](const PaPiece &pc) { return (pc.tile0 + (pairs ? s : 0)) * p.npc + node_in_tile; };
+        // (what is needed of a piece at its start and end alone stays in the queue until then)
+        int n_s = 0;                       // key tiles so far
+        float m = 0.f, l = 0.f;
+        bool mine = false;
+        int node = -1;                     // the row's, if it sees some of the tree's rows; -1: none, or no row
+        bool ok = true, more = true;
+#pragma unroll 1
+        for (int n = 0; ok && more; ++n) {
             PaPiece pc;
-#pragma unroll 1
-            for (int n = 0; ok && take(f ? 1 + s : 0, n, pc); ++n) {
-                const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
-                const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
-                const bool some = __any_sync(0xffffffffu, mine);
-                // ---- the queries in two terms: each thread of a row takes half of its columns (both have read them when their maxima are exchanged)
+            more = look(q, n, pc);
+            float sc = 0.f;
+            if (more) {
+                // ---- the piece's queries in two terms: each thread of a row takes half of its columns (both have read them when their maxima are exchanged).
+                // Their first product then runs beside the end of the piece before.
                 const float ks = __ldg(pp.k_scale + pc.g);
-                if (!wait(P8_QFULL + s, n_piece & 1)) { ok = false; break; }
-                float sc;
-                {
-                    constexpr int CHUNKS = D / 16;
-                    unsigned char *q = gbase + s * SM::TILE + row * 128;
-                    uint4 u[CHUNKS];
-                    uint32_t most = 0u;
+                if (!wait(P8_QFULL + s, n & 1)) { ok = false; break; }
+                constexpr int CHUNKS = D / 16;
+                unsigned char *at = gbase + s * SM::TILE + row * 128;
+                auto chunk = [&](int c) { return (c ^ (row & 7)) << 4; };
+                uint4 u[CHUNKS];
+                uint32_t most = 0u;
 #pragma unroll
-                    for (int c = 0; c < CHUNKS; ++c)
-                        u[c] = *reinterpret_cast<const uint4 *>(q + (D == 128 ? hf * SM::HALF : 0) + ((((D == 128 ? 0 : hf * CHUNKS) + c) ^ (row & 7)) << 4));
+                for (int c = 0; c < CHUNKS; ++c) u[c] = *reinterpret_cast<const uint4 *>(at + (D == 128 ? hf * SM::HALF : 0) + chunk(D == 128 ? c : hf * CHUNKS + c));
 #pragma unroll
-                    for (int c = 0; c < CHUNKS; ++c)
-                        most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u[c].x)), abs2_bf16(u[c].y)), abs2_bf16(u[c].z)), abs2_bf16(u[c].w));
-                    most = max(most, __float_as_uint(exchange(X_COL, __uint_as_float(most))));
-                    const float2 factor = row_factor<7>(most);
+                for (int c = 0; c < CHUNKS; ++c)
+                    most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u[c].x)), abs2_bf16(u[c].y)), abs2_bf16(u[c].z)), abs2_bf16(u[c].w));
+                most = max(most, __float_as_uint(exchange(__uint_as_float(most))));
+                const float2 factor = row_factor<7>(most);
 #pragma unroll
-                    for (int c = 0; c < CHUNKS; c += 2) {
-                        uint4 a, b;
-                        to_terms(u[c].x, u[c].y, factor.x, a.x, b.x);
-                        to_terms(u[c].z, u[c].w, factor.x, a.y, b.y);
-                        to_terms(u[c + 1].x, u[c + 1].y, factor.x, a.z, b.z);
-                        to_terms(u[c + 1].z, u[c + 1].w, factor.x, a.w, b.w);
-                        const int at = hf * (D / 32) + c / 2, at2 = D == 128 ? at : at + 4;      // 16 columns
-                        *reinterpret_cast<uint4 *>(q + ((at ^ (row & 7)) << 4)) = a;
-                        *reinterpret_cast<uint4 *>(q + (D == 128 ? SM::HALF : 0) + ((at2 ^ (row & 7)) << 4)) = b;
-                    }
-                    sc = p.scale_log2 * ks * factor.y;
-                    ptx::tc_fence_before();
-                    ptx::fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(bar(P8_QREADY + s));
+                for (int c = 0; c < CHUNKS; c += 2) {
+                    uint4 a, b;
+                    to_terms(u[c].x, u[c].y, factor.x, a.x, b.x);
+                    to_terms(u[c].z, u[c].w, factor.x, a.y, b.y);
+                    to_terms(u[c + 1].x, u[c + 1].y, factor.x, a.z, b.z);
+                    to_terms(u[c + 1].z, u[c + 1].w, factor.x, a.w, b.w);
+                    const int to = (hf * CHUNKS + c) / 2;                      // 16 columns
+                    *reinterpret_cast<uint4 *>(at + chunk(to)) = a;
+                    *reinterpret_cast<uint4 *>(at + (D == 128 ? SM::HALF : 0) + chunk(D == 128 ? to : to + 4)) = b;
                 }
-                const float2 sc2 = make_float2(sc, sc);
-                // visibility of the tree rows as 32-bit words; the rows in front of them are visible to every node, those behind to none
-                uint4 anc = make_uint4(0u, 0u, 0u, 0u);
-                if (mine && pc.b >= 0) anc = reinterpret_cast<const uint4 *>(p.anc)[node];
-                auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w == 0 ? anc.x : w == 1 ? anc.y : w == 2 ? anc.z : w == 3 ? anc.w : 0u; };
-                float m_used = -INFINITY, l = 0.f;
-#pragma unroll 1
-                for (int t = pc.t0; t < pc.t1; ++t) {
-                    if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
-                    ptx::tc_fence_after();
-                    if (some) {
-                        uint32_t pk[32];                         // fp16 pairs
-                        float2 la, lb;
-                        bool move = t == pc.t0;
-                        for (;;) {
-                            uint32_t sr[64];
-                            ptx::tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-                            ptx::tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-                            ptx::tmem_ld_wait_for(*reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-                            if ((t + 1) * PA_KEYS > pc.L) {
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const int a0 = t * PA_KEYS + hf * 64 + h * 32 - pc.L;      // tree row of the first column
-                                    const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
-#pragma unroll
-                                    for (int e = 0; e < 32; ++e)
-                                        if (!((vis >> e) & 1u)) sr[h * 32 + e] = 0xff800000u;   // -inf
-                                }
-                            }
-                            if (move) {
-                                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                                for (int e = 0; e < 64; e += 8)
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) mx[k] = max3_nan(mx[k], __uint_as_float(sr[e + 2 * k]), __uint_as_float(sr[e + 2 * k + 1]));
-                                float mxs = max_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3]) * sc;
-                                mxs = max_nan(mxs, exchange(X_COL, mxs));
-                                if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
-                                const float m_new = mxs <= m_used ? m_used : mxs;            // (a NaN is taken over)
-                                const bool need = m_new != m_used && m_used != -INFINITY && mine;
-                                if (__any_sync(0xffffffffu, need)) {
-                                    const float alpha = need ? ex2(m_used - m_new) : 1.f;
-#pragma unroll 1
-                                    for (int h = 0; h < D / 32; ++h) {
-                                        uint32_t o[16];
-                                        ptx::tmem_ld16(t_o + h * 16, o);
-                                        ptx::tmem_ld_wait_for16(o);
-#pragma unroll
-                                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                                        ptx::tmem_st16(t_o + h * 16, o);
-                                    }
-                                    l *= alpha;
-                                }
-                                m_used = m_new;
-                            }
-                            const float m_eff = m_used == -INFINITY ? 0.f : m_used;
-                            const float2 nm2 = make_float2(P8_SHIFT - m_eff, P8_SHIFT - m_eff);
-                            la = lb = make_float2(0.f, 0.f);
-                            float px = -INFINITY;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                const uint32_t *x = sr + 2 * e;
-                                const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm2);
-                                const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm2);
-                                float2 p01, p23;
-                                if (e % 8 == 6) {   // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
-                                    px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
-                                    p01 = exp2_poly2(x01);
-                                    p23 = exp2_poly2(x23);
-                                } else {
-                                    p01 = make_float2(ex2(x01.x), ex2(x01.y));
-                                    p23 = make_float2(ex2(x23.x), ex2(x23.y));
-                                }
-                                la = __fadd2_rn(la, p01);
-                                lb = __fadd2_rn(lb, p23);
-                                pk[e] = pack2_f16(p01.x, p01.y);
-                                pk[e + 1] = pack2_f16(p23.x, p23.y);
-                            }
-                            if (move) break;
-                            // a sum that is too large, infinite or NaN (a weight then may be beyond fp16), and a row that has met no visible key yet
-                            const bool ask = !(max_nan(max_nan(la.x, la.y), max_nan(lb.x, lb.y)) < 65504.f) || !(px <= P8_LIMIT) || m_used == -INFINITY;
-                            if (!any_of_rows(pair_bar, mine && ask)) break;
-                            move = true;
-                        }
-                        l += (la.x + la.y) + (lb.x + lb.y);
-                        ptx::tmem_st32(t_s, pk);
-                        if (t == pc.t1 - 1) l += exchange(X_COL + 1, l);      // the row's sum; S is another tile's behind this one's P
-                        ptx::tmem_st_wait();
-                    }
-                    ptx::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(bar(P8_PREADY + s));
-                }
-                if (!ok || !wait(P8_ODONE + s, n_piece & 1)) { ok = false; break; }
+                sc = p.scale_log2 * ks * factor.y;
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(P8_QREADY + s));
+            }
+            if (n) {
+                // ---- the piece before
+                if (!wait(P8_ODONE + s, (n - 1) & 1)) { ok = false; break; }
                 ptx::tc_fence_after();
-                if (some) {
-                    const bool odd = bad[s * 4 + (n_piece & 3)] == n_piece + 1;
-                    const bool direct = p.shared == 0 && pc.whole;
-                    const float vs = __ldg(pp.v_scale + pc.g), factor = direct ? vs / l : vs;
-                    const int slot_row = f ? row : s * 128 + row;
-                    float *o_out = ph.o + ((size_t)pc.slot * ph.rows * (D / 8) + (size_t)(hf * (D / 16)) * ph.rows + slot_row) * 8;
-                    __nv_bfloat16 *out = p.out + (((size_t)max(pc.b, 0) * p.T + node) * p.Hq + pc.g * p.G + head) * D + hf * (D / 2);
+                const PaPiece old = piece_at(q, n - 1);
+                if (__any_sync(0xffffffffu, mine)) {
+                    const bool odd = bad[s * 4 + ((n - 1) & 3)] == n;
+                    const bool direct = p.shared == 0 && old.whole;
+                    const float vs = __ldg(pp.v_scale + old.g), factor = direct ? vs / l : vs;
+                    const int slot_row = pairs ? s * 128 + row : row;
+                    float *o_out = ph.o + ((size_t)old.slot * ph.rows * (D / 8) + (size_t)(hf * (D / 16)) * ph.rows + slot_row) * 8;
+                    __nv_bfloat16 *out = p.out + (((size_t)max(old.b, 0) * p.T + node_of(old)) * p.Hq + old.g * p.G + head) * D + hf * (D / 2);
 #pragma unroll 1
                     for (int h = 0; h < D / 32; ++h) {
                         uint32_t o[16];
@@ -746,11 +661,12 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
                         if (odd) {
                             // V codes that the tensor core did not see: NaN with any weight is NaN
-                            for (int a = max(0, pc.t0 * PA_KEYS - pc.L); a < p.T && pc.L + a < pc.t1 * PA_KEYS; ++a) {
-                                if (!(anc_word(a >> 5) >> (a & 31) & 1)) continue;
-                                const int64_t at = p.pages.row(pc.b, p.shared + pc.L + a);
+#pragma unroll 1
+                            for (int a = max(0, old.t0 * PA_KEYS - old.L); a < p.T && old.L + a < old.t1 * PA_KEYS; ++a) {
+                                if (node < 0 || !(p.anc[node * 2 + (a >> 6)] >> (a & 63) & 1)) continue;
+                                const int64_t at = p.pages.row(old.b, p.shared + old.L + a);
                                 if (at < 0) continue;
-                                const uint8_t *v = pp.v + at + pc.g * p.pages.stride_h + hf * (D / 2) + h * 16;
+                                const uint8_t *v = pp.v + at + old.g * p.pages.stride_h + hf * (D / 2) + h * 16;
 #pragma unroll
                                 for (int e = 0; e < 16; ++e)
                                     if ((v[e] & 0x7fu) == 0x7fu) o[e] = 0x7fffffffu;
@@ -767,13 +683,129 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             ptx::st_global_32(o_out + (size_t)(2 * h + 1) * ph.rows * 8, *reinterpret_cast<const uint32_t(*)[8]>(&o[8]));
                         }
                     }
-                    if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(l == 0.f ? -INFINITY : m_used - P8_SHIFT, l);   // (what weighs 1)
+                    if (mine && !direct && hf == 0)                // (what weighs 1)
+                        ph.ml[(size_t)old.slot * ph.rows + slot_row] = make_float2(l == 0.f ? -INFINITY : m - P8_SHIFT, l);
                 }
-                ++n_piece;
+                if (!pairs || s) taken(q, n - 1);                  // (in a pair the second row tile's warps: its place is not used again before the next but two's scores, both tiles')
+            }
+            if (!more) break;
+            mine = node_in_tile < p.npc && node_of(pc) < (pc.b < 0 ? p.B * p.T : p.T);
+            node = mine && pc.b >= 0 ? node_of(pc) : -1;
+            m = -INFINITY;
+            l = 0.f;
+            const bool some = __any_sync(0xffffffffu, mine);
+            const float2 sc2 = make_float2(sc, sc);
+#pragma unroll 1
+            for (int t = pc.t0; t < pc.t1; ++t) {
+                if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
+                ptx::tc_fence_after();
+                if (some) {
+                    uint32_t pk[32];                               // fp16 pairs
+                    if ((t + 1) * PA_KEYS > pc.L) {
+                        // Hidden scores become -inf where they are.  Visibility of the tree's rows as 32-bit words; the rows in front of them are visible to every
+                        // node, those behind to none.
+                        auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w < 4 && node >= 0 ? reinterpret_cast<const uint32_t *>(p.anc)[node * 4 + w] : 0u; };
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const int a0 = t * PA_KEYS + hf * 64 + c * 16 - pc.L;      // tree row of the first column
+                            const uint32_t vis = __funnelshift_r(anc_word(a0 >> 5), anc_word((a0 >> 5) + 1), a0 & 31);
+                            uint32_t x[16];
+                            ptx::tmem_ld16(t_s + c * 16, x);
+                            ptx::tmem_ld_wait_for16(x);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (!((vis >> e) & 1u)) x[e] = 0xff800000u;
+                            ptx::tmem_st16(t_s + c * 16, x);
+                        }
+                        ptx::tmem_st_wait();
+                    }
+                    bool move = __any_sync(0xffffffffu, mine && m == -INFINITY);      // (the piece's first tile, or no key was visible so far)
+                    float sum;
+                    for (;;) {
+                        if (move) {
+                            float mxs = -INFINITY;
+#pragma unroll 1
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t x[16];
+                                ptx::tmem_ld16(t_s + c * 16, x);
+                                ptx::tmem_ld_wait_for16(x);
+#pragma unroll
+                                for (int e = 0; e < 16; e += 2) mxs = max3_nan(mxs, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                            }
+                            mxs *= sc;
+                            mxs = max_nan(mxs, exchange(mxs));
+                            if (mxs == INFINITY) mxs = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+                            const float m_new = mxs <= m ? m : mxs;                      // (a NaN is taken over)
+                            const bool need = m_new != m && m != -INFINITY && mine;
+                            if (__any_sync(0xffffffffu, need)) {
+                                const float alpha = need ? ex2(m - m_new) : 1.f;
+#pragma unroll 1
+                                for (int h = 0; h < D / 32; ++h) {
+                                    uint32_t o[16];
+                                    ptx::tmem_ld16(t_o + h * 16, o);
+                                    ptx::tmem_ld_wait_for16(o);
+#pragma unroll
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                                    ptx::tmem_st16(t_o + h * 16, o);
+                                }
+                                l *= alpha;
+                            }
+                            m = m_new;
+                        }
+                        const float shift = m == -INFINITY ? P8_SHIFT : P8_SHIFT - m;
+                        const float2 nm2 = make_float2(shift, shift);
+                        float2 la = make_float2(0.f, 0.f), lb = la;
+                        float px = -INFINITY;
+                        // sixteen columns at a time, the next ones on their way meanwhile
+                        auto weights = [&](int c, uint32_t (&x)[16]) {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float2 x01 = __ffma2_rn(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), sc2, nm2);
+                                const float2 x23 = __ffma2_rn(make_float2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), sc2, nm2);
+                                float2 p01, p23;
+                                if (e == 12) {      // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
+                                    px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
+                                    p01 = exp2_poly2(x01);
+                                    p23 = exp2_poly2(x23);
+                                } else {
+                                    p01 = make_float2(ex2(x01.x), ex2(x01.y));
+                                    p23 = make_float2(ex2(x23.x), ex2(x23.y));
+                                }
+                                la = __fadd2_rn(la, p01);
+                                lb = __fadd2_rn(lb, p23);
+                                pk[c * 8 + e / 2] = pack2_f16(p01.x, p01.y);
+                                pk[c * 8 + e / 2 + 1] = pack2_f16(p23.x, p23.y);
+                            }
+                        };
+                        uint32_t a[16], b[16];
+                        ptx::tmem_ld16(t_s, a);
+                        ptx::tmem_ld_wait_for16(a);
+                        ptx::tmem_ld16(t_s + 16, b);
+                        weights(0, a);
+                        ptx::tmem_ld_wait_for16(b);
+                        ptx::tmem_ld16(t_s + 32, a);
+                        weights(1, b);
+                        ptx::tmem_ld_wait_for16(a);
+                        ptx::tmem_ld16(t_s + 48, b);
+                        weights(2, a);
+                        ptx::tmem_ld_wait_for16(b);
+                        weights(3, b);
+                        sum = (la.x + la.y) + (lb.x + lb.y);
+                        if (move) break;
+                        // a sum that is too large, infinite or NaN: a weight then may be beyond fp16
+                        if (!any_of_rows(pair_bar, mine && (!(sum < 65504.f) || !(px <= P8_LIMIT)))) break;
+                        move = true;
+                    }
+                    l += sum;
+                    ptx::tmem_st32(t_s, pk);
+                    if (t == pc.t1 - 1) l += exchange(l);          // the row's sum
+                    ptx::tmem_st_wait();
+                }
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(P8_PREADY + s));
             }
         }
-    } else {
-        fewer_registers();                // (all warps of a warpgroup)
     }
     // ---- nobody leaves while the tensor core may still work for the CTA
     __syncwarp();
