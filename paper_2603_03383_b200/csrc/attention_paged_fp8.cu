@@ -817,34 +817,71 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 
 // ---------------------------------------------------------------------------------------- thin items
 // At most 16 query rows against a KV head's keys (plain decoding; the smallest trees): nothing but the bytes counts.  As for the bf16 cache, warps of
-// their own with mma.sync, K and V straight from global memory into registers.  A contraction's order is free as long as both operands have it, and so is
-// the order of O's columns: 16 bytes of a K row are four products' B operands of a thread, converted as they stand; 16 bytes of V rows (8 at D = 64) are
-// its column in 16 products (8), two keys' codes side by side by a byte permutation in front of the conversion.
-// A CTA of four warps walks a run of the line of all thin items, 32 keys to a warp at a time; K of the next keys is requested when the scores are taken,
-// V of them when the products with V are, so that each is on its way during the other's work.  At a piece's end the warps join in shared memory.
-constexpr int T8_WARPS = 4, T8_KEYS = 32, T8_STEP = T8_WARPS * T8_KEYS;
-constexpr int T8_ENDS = 2;                 // what an item's start and end take, in steps of 128 keys
+// their own with mma.sync, but with the operands the other way round: S^T = K Q^T and O^T = V^T P^T.  Keys and columns of V then fill the products' 16
+// rows, and up to 8 query rows their 8 columns (up to 16 take two products, NR = 2), where query rows as the 16 left three quarters of the products and of O's
+// registers to nothing for groups of four.
+// A contraction's order is free as long as both operands have it, and so is the order of O's columns: 16 bytes of two K rows are four products' A operands of
+// a thread, converted as they stand; 16 bytes of four V rows (8 at D = 64) are two columns in each of 8 products (4), two keys' codes side by side by a byte
+// permutation in front of the conversion.  P^T is P transposed, 8 x 8 at a time, by movmatrix.
+// A CTA walks a run of the line of all thin items, KEYS keys to a warp at a time.  Asynchronous copies bring them to the warp's own part of shared memory,
+// STAGES - 1 blocks ahead: no warp waits for another, and no register holds what is on its way.  At a piece's end the warps join.
+// An instruction of copies covers whole rows: where it took half a row of each of 8 keys (as the operands have them), the other half crossed from L2 with it, twice
+// in all.
 constexpr float T8_SHIFT = 7.f, T8_SLACK = 8.f;   // weights are 2^SHIFT at the reference, which may be SLACK too small: below 2^16
 
-__device__ __forceinline__ void mma16816_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+// NR: products of 8 query rows.
+template <int D, int NR> struct T8 {
+    static constexpr int WARPS = NR == 1 ? 8 : 4, KEYS = NR == 1 ? 16 : 32, STAGES = 3;
+    static constexpr int STEP = WARPS * KEYS;
+    static constexpr int ENDS = 2;                 // what an item's start and end take, in steps
+    static constexpr uint32_t K_BYTES = KEYS * D, STAGE = 2 * K_BYTES, RING = WARPS * STAGES * STAGE;     // a warp's stages side by side
+    static constexpr uint32_t JOIN = WARPS * 8 * NR * (D + 4) * 4;
+    static constexpr uint32_t TOTAL = RING > JOIN ? RING : JOIN;                                          // (the warps join where the ring was)
+    static_assert(2 * (TOTAL + 2048 + 1024) <= 227 * 1024, "two CTAs on an SM");
+};
+
+__device__ __forceinline__ void mma16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+// 16 bytes from global to shared memory, or zeros
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool is) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(is ? 16 : 0) : "memory");
+}
+// Where 16-byte chunk c of a row lies in it, so that the eight lanes that read two neighbouring rows of K, or four rows of V of one parity, together meet
+// different banks.
+template <int D> __device__ __forceinline__ int chunk_at(int row, int c) {
+    return D == 128 ? c ^ (row >> 1 & 3) << 1 ^ (row & 1) << 2 : c ^ (row >> 1 & 3);
 }
 
-template <int D>
-__global__ void __launch_bounds__(T8_WARPS * 32, 2)
+template <int D, int NR>
+__global__ void __launch_bounds__(T8<D, NR>::WARPS * 32, 2)
 paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
-    using Line = ThinLine<T8_STEP, T8_ENDS>;
+    using SM = T8<D, NR>;
+    using Line = ThinLine<SM::STEP, SM::ENDS>;
+    constexpr int WARPS = SM::WARPS, STAGES = SM::STAGES;
     constexpr int C = D / 64;              // 64-column parts of a row: 16 bytes of each are a thread's
-    constexpr int J = D / 8, JW = J / 4;   // products of 8 columns of O; words of a V row that are a thread's
+    constexpr int J = D / 8, JW = J / 4;   // columns of V that are a thread's, and their words
+    constexpr int MT = SM::KEYS / 16;      // products of 16 keys
     const PaParams &p = pp.a;
-    __shared__ float o_x[T8_WARPS][TH_ROWS][D + 4];
-    __shared__ float2 ml_x[T8_WARPS][TH_ROWS];
+    extern __shared__ __align__(16) unsigned char ring[];
+    float (*o_x)[8 * NR][D + 4] = reinterpret_cast<float (*)[8 * NR][D + 4]>(ring);      // [WARPS]
+    __shared__ float2 ml_x[WARPS][8 * NR];
     __shared__ int start[5];               // x0, x1, S, b, idx
     let_next_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r0 = lane / 4, quad = lane % 4;
     const PaPhase &ph = p.phase[2];
     const int worker = blockIdx.x, workers = gridDim.x;
+    // this warp's stages: rows of K, then of V
+    const unsigned char *mine = ring + warp * STAGES * SM::STAGE;
+    const uint32_t mine_at = ptx::smem_u32(mine);
+    constexpr int PER_ROW = D / 16, ROWS = 32 / PER_ROW;         // lanes of a row, rows of an instruction of copies
+    const int my_row = lane / PER_ROW, my_chunk = lane % PER_ROW;
     previous_done();
     if (warp == 0) Line::begin(p, worker, workers, lane, start);
     __syncthreads();
@@ -854,13 +891,14 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
     auto load_item = [&]() {
         if (b < 0) {
             L = p.shared;
-            cost = Line::steps(p.shared) + T8_ENDS;
+            cost = Line::steps(p.shared) + SM::ENDS;
         } else {
             cost = Line::cost_of(p, b);
             L = p.seq_lens[b] - p.shared;
         }
     };
     if (x0 < x1) load_item();
+#pragma unroll 1
     while (S < x1) {
         if (idx >= (b < 0 ? ph.prefix_items : ph.seq_items) || cost == 0) {
             if (++b >= p.B) break;
@@ -868,8 +906,8 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
             load_item();
             continue;
         }
-        const int steps = cost - T8_ENDS;
-        const int t0 = max(0, min(x0 - S - T8_ENDS, steps)), t1 = max(0, min(x1 - S - T8_ENDS, steps));
+        const int steps = cost - SM::ENDS;
+        const int t0 = max(0, min(x0 - S - SM::ENDS, steps)), t1 = max(0, min(x1 - S - SM::ENDS, steps));
         S += cost;
         const int g = idx++;
         if (t0 >= t1) continue;
@@ -880,58 +918,46 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
             if (t0 == 0) ph.span[item].x = worker;
             if (t1 == steps) ph.span[item].y = worker;
         }
-        // ---- this warp's blocks of 32 keys: key (t * T8_WARPS + warp) * 32, in two halves that may lie on two pages
+        // ---- this warp's blocks of keys, sixteen by sixteen: they may lie on two pages
         const int32_t *table = p.pages.table + (int64_t)max(b, 0) * p.pages.max_pages;
-        auto key_of = [&](int t, int half) { return (t * T8_WARPS + warp) * T8_KEYS + half * 16; };
-        auto page_of = [&](int t, int half) { return t < t1 && key_of(t, half) < n_keys ? table[(key_of(t, half) + key0) >> p.pages.page_shift] : -1; };
-        auto row_at = [&](int t, int half, int id) {     // byte offset of the half's first row; < 0: there is none
+        auto key_of = [&](int t, int mt) { return (t * WARPS + warp) * SM::KEYS + mt * 16; };
+        auto page_of = [&](int t, int mt) { return t < t1 && key_of(t, mt) < n_keys ? table[(key_of(t, mt) + key0) >> p.pages.page_shift] : -1; };
+        auto row_at = [&](int t, int mt, int id) {       // byte offset of the first row; < 0: there is none
             return id < 0 || id >= p.pages.n_pages ? -1ll
-                   : (long long)id * p.pages.stride_page + (long long)((key_of(t, half) + key0) & ((1 << p.pages.page_shift) - 1)) * p.pages.stride_t +
+                   : (long long)id * p.pages.stride_page + (long long)((key_of(t, mt) + key0) & ((1 << p.pages.page_shift) - 1)) * p.pages.stride_t +
                          g * p.pages.stride_h;
         };
-        uint4 kx[4][C];                    // keys r0 + 8 h of the block
-        uint32_t vx[2][4][JW];             // of half kk: keys 2 quad, 2 quad + 1 and the same + 8; columns r0 * J + [0, J)
-        auto load_k = [&](const long long (&at)[2]) {
+        // The blocks up to the one STAGES - 1 ahead are requested; the pages of the one behind them are looked up.
+        int id_next[MT];
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+        for (int mt = 0; mt < MT; ++mt) id_next[mt] = page_of(t0, mt);
+        auto request = [&](int t) {
+            const uint32_t to = mine_at + (uint32_t)((t - t0) % STAGES) * SM::STAGE;
 #pragma unroll
-                for (int c = 0; c < C; ++c)
-                    kx[h][c] = at[h / 2] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(pp.k + at[h / 2] + (r0 + 8 * (h % 2)) * p.pages.stride_t + c * 64 + quad * 16))
-                                              : make_uint4(0u, 0u, 0u, 0u);
-        };
-        auto load_v = [&](const long long (&at)[2], int t) {
+            for (int mt = 0; mt < MT; ++mt) {
+                const long long at = row_at(t, mt, id_next[mt]);
+                id_next[mt] = page_of(t + 1, mt);
+                if (t >= t1) continue;
+                const long long from = (at >= 0 ? at : 0) + my_row * p.pages.stride_t + my_chunk * 16;
+                const int left = at >= 0 ? n_keys - key_of(t, mt) - my_row : 0;      // rows behind the last key may hold anything
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int key = 2 * quad + (k & 1) + 8 * (k >> 1);
-                    const uint8_t *src = pp.v + at[kk] + key * p.pages.stride_t + r0 * J;
-                    const bool is = at[kk] >= 0 && key_of(t, kk) + key < n_keys;     // rows behind the last key may hold anything
-                    if constexpr (JW == 4) {
-                        const uint4 u = is ? __ldg(reinterpret_cast<const uint4 *>(src)) : make_uint4(0u, 0u, 0u, 0u);
-                        vx[kk][k][0] = u.x; vx[kk][k][1] = u.y; vx[kk][k][2] = u.z; vx[kk][k][3] = u.w;
-                    } else {
-                        const uint2 u = is ? __ldg(reinterpret_cast<const uint2 *>(src)) : make_uint2(0u, 0u);
-                        vx[kk][k][0] = u.x; vx[kk][k][1] = u.y;
-                    }
+                for (int i = 0; i < 16; i += ROWS) {
+                    const uint32_t to_row = to + (mt * 16 + i + my_row) * D + chunk_at<D>(i + my_row, my_chunk) * 16;
+                    copy_async(to_row, pp.k + from + i * p.pages.stride_t, i < left);
+                    copy_async(to_row + SM::K_BYTES, pp.v + from + i * p.pages.stride_t, i < left);
                 }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        int id_next[2];
-        long long at[2];
+#pragma unroll 1
+        for (int t = t0; t < t0 + STAGES - 1; ++t) request(t);       // (the barrier at a piece's end is between these and the last reads)
+        // ---- the query rows as B operands: product (c, i) has columns c * 64 + quad * 16 + 4 i + [0, 2) and [2, 4) of row r0 + 8 nr
+        uint32_t qb[NR][C][4][2];
+        uint32_t see[NR][2];               // tree rows that are visible to rows 8 nr + 2 quad and the next (at most 16 nodes)
+        float sc[NR][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            at[h] = row_at(t0, h, page_of(t0, h));
-            id_next[h] = page_of(t0 + 1, h);
-        }
-        load_k(at);
-        load_v(at, t0);
-        // ---- the query rows as A operands: product (c, i) has columns c * 64 + quad * 16 + 4 i + [0, 2) and [2, 4) of rows r0 and r0 + 8
-        uint32_t qa[C][4][4];
-        uint32_t see[2];                   // tree rows that are visible to rows r0 and r0 + 8 (at most 16 nodes)
-        float sc[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = r0 + 8 * h, n = r / p.G;
+        for (int nr = 0; nr < NR; ++nr) {
+            const int r = r0 + 8 * nr, n = r / p.G;
             const bool is = r < rows;
             const __nv_bfloat16 *src = p.q + (((size_t)(own ? b * p.T : 0) + n) * p.Hq + g * p.G + (r - n * p.G)) * D + quad * 16;
             uint32_t most = 0u;
@@ -939,10 +965,10 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
             for (int c = 0; c < C; ++c) {
                 const uint4 u = is ? *reinterpret_cast<const uint4 *>(src + c * 64) : make_uint4(0u, 0u, 0u, 0u);
                 const uint4 v = is ? *reinterpret_cast<const uint4 *>(src + c * 64 + 8) : make_uint4(0u, 0u, 0u, 0u);
-                qa[c][0][h] = u.x; qa[c][0][h + 2] = u.y; qa[c][1][h] = u.z; qa[c][1][h + 2] = u.w;
-                qa[c][2][h] = v.x; qa[c][2][h + 2] = v.y; qa[c][3][h] = v.z; qa[c][3][h + 2] = v.w;
+                qb[nr][c][0][0] = u.x; qb[nr][c][0][1] = u.y; qb[nr][c][1][0] = u.z; qb[nr][c][1][1] = u.w;
+                qb[nr][c][2][0] = v.x; qb[nr][c][2][1] = v.y; qb[nr][c][3][0] = v.z; qb[nr][c][3][1] = v.w;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) most = larger_bits(larger_bits(most, abs2_bf16(qa[c][i][h])), abs2_bf16(qa[c][i][h + 2]));
+                for (int i = 0; i < 4; ++i) most = larger_bits(larger_bits(most, abs2_bf16(qb[nr][c][i][0])), abs2_bf16(qb[nr][c][i][1]));
             }
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
@@ -951,138 +977,186 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    qa[c][i][h] = to_f16(qa[c][i][h], factor.x);
-                    qa[c][i][h + 2] = to_f16(qa[c][i][h + 2], factor.x);
+                    qb[nr][c][i][0] = to_f16(qb[nr][c][i][0], factor.x);
+                    qb[nr][c][i][1] = to_f16(qb[nr][c][i][1], factor.x);
                 }
-            sc[h] = p.scale_log2 * __ldg(pp.k_scale + g) * factor.y;
-            see[h] = is && own ? (uint32_t)p.anc[n * 2] : 0u;
+            const float of_row = p.scale_log2 * __ldg(pp.k_scale + g) * factor.y;
+            const uint32_t seen = is && own ? (uint32_t)p.anc[n * 2] : 0u;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sc[nr][e] = __shfl_sync(0xffffffffu, of_row, (2 * quad + e) * 4);
+                see[nr][e] = __shfl_sync(0xffffffffu, seen, (2 * quad + e) * 4);
+            }
         }
-        float o[J][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float o[NR][D / 16][4] = {}, m[NR][2], l[NR][2];
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+            m[nr][0] = m[nr][1] = -INFINITY;
+            l[nr][0] = l[nr][1] = 0.f;
+        }
+#pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const int first = key_of(t, 0);
             if (first >= n_keys) break;    // (the item's last step: no keys for this warp)
-            // ---- scores of keys 8 h + [0, 8): c0, c1 row r0, c2, c3 row r0 + 8, keys 8 h + 2 quad and 8 h + 2 quad + 1
-            float x[4][4] = {};
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            __syncwarp();                  // all lanes' copies of this block are there, and all are done with the block before
+            request(t + STAGES - 1);
+            const unsigned char *block = mine + (uint32_t)((t - t0) % STAGES) * SM::STAGE;
+            // ---- scores: x[mt][nr]: key mt * 16 + r0 (+ 8: elements 2 and 3), rows 8 nr + 2 quad and the next
+            float x[MT][NR][4] = {};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const uint32_t w[4] = {kx[h][c].x, kx[h][c].y, kx[h][c].z, kx[h][c].w};
+                for (int c = 0; c < C; ++c) {
+                    const unsigned char *src = block + (mt * 16 + r0) * D + chunk_at<D>(r0, c * 4 + quad) * 16;      // (of row r0 + 8 too)
+                    const uint4 k0 = *reinterpret_cast<const uint4 *>(src), k8 = *reinterpret_cast<const uint4 *>(src + 8 * D);
+                    const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w8[4] = {k8.x, k8.y, k8.z, k8.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mma16816_f16(x[h], qa[c][i], f16x2_lo(w[i]), f16x2_hi(w[i]));
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr)
+                            mma16816_f16(x[mt][nr], f16x2_lo(w0[i]), f16x2_lo(w8[i]), f16x2_hi(w0[i]), f16x2_hi(w8[i]), qb[nr][c][i][0], qb[nr][c][i][1]);
                 }
-            const long long at_now[2] = {at[0], at[1]};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                at[h] = row_at(t + 1, h, id_next[h]);
-                id_next[h] = page_of(t + 2, h);
-            }
-            if (t + 1 < t1) load_k(at);
-            const bool edge = first + T8_KEYS > L;
+            const bool edge = first + SM::KEYS > L;
             if (edge) {
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int a = first + 8 * h + 2 * quad + (e & 1) - L;
-                        if (a >= 0 && (!own || a >= p.T || !(see[e >> 1] >> a & 1u))) x[h][e] = -INFINITY;
+                        const int a = first + mt * 16 + r0 + 8 * (e >> 1) - L;
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr)
+                            if (a >= 0 && (!own || a >= p.T || !(see[nr][e & 1] >> a & 1u))) x[mt][nr][e] = -INFINITY;
                     }
             }
-            float mx[2];
+            // the reference moves where a score of the row is too far above it, and where there is none yet
+            bool ask = false;
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                mx[r] = max_nan(max3_nan(x[0][2 * r], x[0][2 * r + 1], x[1][2 * r]), max3_nan(x[1][2 * r + 1], x[2][2 * r], x[2][2 * r + 1]));
-                mx[r] = max3_nan(mx[r], x[3][2 * r], x[3][2 * r + 1]);
-                mx[r] = max_nan(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
-                mx[r] = max_nan(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2)) * sc[r];
-                if (mx[r] == INFINITY) mx[r] = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
-            }
-            if (__any_sync(0xffffffffu, !(mx[0] <= m[0] + T8_SLACK) || !(mx[1] <= m[1] + T8_SLACK))) {
+            for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float m_new = mx[r] <= m[r] ? m[r] : mx[r];
-                    const float w = m[r] == -INFINITY ? 0.f : ex2(m[r] - m_new);
-                    m[r] = m_new;
-                    l[r] *= w;
+                for (int e = 0; e < 2; ++e) {
+                    float mx = max_nan(x[0][nr][e], x[0][nr][e + 2]);
 #pragma unroll
-                    for (int j = 0; j < J; ++j) { o[j][2 * r] *= w; o[j][2 * r + 1] *= w; }
+                    for (int mt = 1; mt < MT; ++mt) mx = max3_nan(mx, x[mt][nr][e], x[mt][nr][e + 2]);
+                    ask = ask || !(mx * sc[nr][e] <= m[nr][e] + T8_SLACK);
                 }
+            if (__any_sync(0xffffffffu, ask)) {
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = max_nan(x[0][nr][e], x[0][nr][e + 2]);
+#pragma unroll
+                        for (int mt = 1; mt < MT; ++mt) mx = max3_nan(mx, x[mt][nr][e], x[mt][nr][e + 2]);
+#pragma unroll
+                        for (int k = 4; k < 32; k *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+                        mx *= sc[nr][e];
+                        if (mx == INFINITY) mx = __int_as_float(0x7fffffff);     // inf - inf: the row is NaN, as from the formula
+                        const float m_new = mx <= m[nr][e] ? m[nr][e] : mx;
+                        const float w = m[nr][e] == -INFINITY ? 0.f : ex2(m[nr][e] - m_new);
+                        m[nr][e] = m_new;
+                        l[nr][e] *= w;
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) { o[nr][j][e] *= w; o[nr][j][e + 2] *= w; }
+                    }
             }
-            const float me[2] = {m[0] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[0], m[1] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[1]};
-            uint32_t pa[2][4];
+            uint32_t pb[MT][NR][2];        // P^T: keys mt * 16 + 2 quad and the next (+ 8: [1]), row 8 nr + r0
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+            for (int nr = 0; nr < NR; ++nr) {
+                const float me[2] = {m[nr][0] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[nr][0], m[nr][1] == -INFINITY ? T8_SHIFT : T8_SHIFT - m[nr][1]};
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float w0 = ex2(fmaf(x[h][2 * r], sc[r], me[r])), w1 = ex2(fmaf(x[h][2 * r + 1], sc[r], me[r]));
-                    l[r] += w0 + w1;
-                    pa[h / 2][h % 2 * 2 + r] = pack2_f16(w0, w1);
-                }
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float w0 = ex2(fmaf(x[mt][nr][2 * h], sc[nr][0], me[0])), w1 = ex2(fmaf(x[mt][nr][2 * h + 1], sc[nr][1], me[1]));
+                        l[nr][0] += w0;
+                        l[nr][1] += w1;
+                        pb[mt][nr][h] = transposed(pack2_f16(w0, w1));
+                    }
+            }
             bool odd = false;
-            if (edge && own) {
-                // NaN codes of the tree's rows are left out here and given below to the rows that see them
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
+            for (int mt = 0; mt < MT; ++mt) {
+                uint32_t vx[4][JW];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int key = 2 * quad + (k & 1) + 8 * (k >> 1);
+                    const unsigned char *src = block + SM::K_BYTES + (mt * 16 + key) * D + chunk_at<D>(key, r0 * J / 16) * 16 + r0 * J % 16;
+                    if constexpr (JW == 4) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(src);
+                        vx[k][0] = u.x; vx[k][1] = u.y; vx[k][2] = u.z; vx[k][3] = u.w;
+                    } else {
+                        const uint2 u = *reinterpret_cast<const uint2 *>(src);
+                        vx[k][0] = u.x; vx[k][1] = u.y;
+                    }
+                }
+                if (edge && own) {
+                    // NaN codes of the tree's rows are left out here and given below to the rows that see them
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int e = 0; e < JW; ++e) {
-                            if (nan_codes(vx[kk][k][e])) { vx[kk][k][e] = without_nans(vx[kk][k][e]); odd = true; }
-                        }
-                odd = __any_sync(0xffffffffu, odd);
-            }
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
+                        for (int e = 0; e < JW; ++e)
+                            if (nan_codes(vx[k][e])) { vx[k][e] = without_nans(vx[k][e]); odd = true; }
+                }
 #pragma unroll
                 for (int w = 0; w < JW; ++w) {
                     // keys 2 quad and 2 quad + 1 side by side, columns 4 w + [0, 2) and [2, 4); the same of the keys 8 behind
-                    const uint32_t a = __byte_perm(vx[kk][0][w], vx[kk][1][w], 0x5140), a2 = __byte_perm(vx[kk][0][w], vx[kk][1][w], 0x7362);
-                    const uint32_t c = __byte_perm(vx[kk][2][w], vx[kk][3][w], 0x5140), c2 = __byte_perm(vx[kk][2][w], vx[kk][3][w], 0x7362);
-                    mma16816_f16(o[4 * w], pa[kk], f16x2_lo(a), f16x2_lo(c));
-                    mma16816_f16(o[4 * w + 1], pa[kk], f16x2_hi(a), f16x2_hi(c));
-                    mma16816_f16(o[4 * w + 2], pa[kk], f16x2_lo(a2), f16x2_lo(c2));
-                    mma16816_f16(o[4 * w + 3], pa[kk], f16x2_hi(a2), f16x2_hi(c2));
+                    const uint32_t a = __byte_perm(vx[0][w], vx[1][w], 0x5140), a2 = __byte_perm(vx[0][w], vx[1][w], 0x7362);
+                    const uint32_t c = __byte_perm(vx[2][w], vx[3][w], 0x5140), c2 = __byte_perm(vx[2][w], vx[3][w], 0x7362);
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) {
+                        mma16816_f16(o[nr][2 * w], f16x2_lo(a), f16x2_hi(a), f16x2_lo(c), f16x2_hi(c), pb[mt][nr][0], pb[mt][nr][1]);
+                        mma16816_f16(o[nr][2 * w + 1], f16x2_lo(a2), f16x2_hi(a2), f16x2_lo(c2), f16x2_hi(c2), pb[mt][nr][0], pb[mt][nr][1]);
+                    }
                 }
-            if (t + 1 < t1) load_v(at, t + 1);
-            if (odd)
-                for (int k = 0; k < T8_KEYS; ++k) {
+            }
+            if (edge && own && __any_sync(0xffffffffu, odd))
+#pragma unroll 1
+                for (int k = 0; k < SM::KEYS; ++k) {
                     const int a = first + k - L;
                     if (a >= p.T) break;
-                    if (at_now[k / 16] < 0) continue;
+                    const long long at = row_at(t, k / 16, page_of(t, k / 16));
+                    if (at < 0) continue;
 #pragma unroll
-                    for (int j = 0; j < J; ++j)
+                    for (int j = 0; j < D / 16; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const uint8_t y = pp.v[at_now[k / 16] + k % 16 * p.pages.stride_t + (2 * quad + (e & 1)) * J + j];
+                            const uint8_t y = pp.v[at + k % 16 * p.pages.stride_t + r0 * J + 2 * j + (e >> 1)];
                             // (the shared keys and those in front of the tree are seen by all)
-                            if ((y & 0x7fu) == 0x7fu && (a < 0 || (see[e >> 1] >> a & 1u))) o[j][e] = __int_as_float(0x7fffffff);
+#pragma unroll
+                            for (int nr = 0; nr < NR; ++nr)
+                                if ((y & 0x7fu) == 0x7fu && (a < 0 || (see[nr][e & 1] >> a & 1u))) o[nr][j][e] = __int_as_float(0x7fffffff);
                         }
                 }
         }
-        // ---- the four warps' shares of a row are joined: O[row][column (2 quad + (e & 1)) * J + j]
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();                   // the ring is the joining's now
+        // ---- the warps' shares of a row are joined: o[nr][j][e] is row 8 nr + 2 quad + (e & 1), column r0 * J + 2 j + (e >> 1)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            if (quad == 0) ml_x[warp][r0 + 8 * h] = make_float2(m[h], l[h]);
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                o_x[warp][r0 + 8 * h][2 * quad * J + j] = o[j][2 * h];
-                o_x[warp][r0 + 8 * h][(2 * quad + 1) * J + j] = o[j][2 * h + 1];
+            for (int e = 0; e < 2; ++e) {
+                const int row = 8 * nr + 2 * quad + e;
+                float sum = l[nr][e];
+#pragma unroll
+                for (int k = 4; k < 32; k *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                if (r0 == 0) ml_x[warp][row] = make_float2(m[nr][e], sum);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) *reinterpret_cast<float2 *>(&o_x[warp][row][r0 * J + 2 * j]) = make_float2(o[nr][j][e], o[nr][j][e + 2]);
             }
-        }
         __syncthreads();
         const bool direct = p.shared == 0 && t1 - t0 == steps;      // the item's only piece
         const size_t slot = (size_t)item + worker;
         const float vs = __ldg(pp.v_scale + g);
-        for (int e = threadIdx.x; e < rows * (D / 8); e += T8_WARPS * 32) {
+#pragma unroll 1
+        for (int e = threadIdx.x; e < rows * (D / 8); e += WARPS * 32) {
             const int row = e % rows, chunk = e / rows;
             float mm = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < T8_WARPS; ++w) mm = max_nan(mm, ml_x[w][row].x);
+            for (int w = 0; w < WARPS; ++w) mm = max_nan(mm, ml_x[w][row].x);
             float acc[8] = {}, ll = 0.f;
 #pragma unroll
-            for (int w = 0; w < T8_WARPS; ++w) {
+            for (int w = 0; w < WARPS; ++w) {
                 const float2 ml = ml_x[w][row];
                 const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
                 ll = fmaf(f, ml.y, ll);
@@ -1104,7 +1178,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                 if (chunk == 0) ph.ml[slot * TH_ROWS + row] = make_float2(ll == 0.f ? -INFINITY : mm - T8_SHIFT, ll);
             }
         }
-        __syncthreads();                   // before the next piece's shares
+        __syncthreads();                   // before the next piece's codes
     }
 }
 
@@ -1115,12 +1189,19 @@ static int launch_paged8(const CUtensorMap &q, const CUtensorMap &k, const CUten
     bool *done = once.flag();
     if (!done || !*done) {
         MTV_CUDA_CHECK(cudaFuncSetAttribute(paged_attn8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, P8Smem<D>::TOTAL));
+        MTV_CUDA_CHECK(cudaFuncSetAttribute(paged_attn8_thin_kernel<D, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, T8<D, 1>::TOTAL));
+        MTV_CUDA_CHECK(cudaFuncSetAttribute(paged_attn8_thin_kernel<D, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, T8<D, 2>::TOTAL));
         if (done) *done = true;
     }
     const PaPhase (&ph)[3] = p.a.phase;
     if (ph[0].prefix_items + ph[0].seq_items + ph[1].prefix_items + ph[1].seq_items)
         MTV_CUDA_CHECK(launch_dependent(paged_attn8_kernel<D>, dim3(sm_count()), P8_THREADS, P8Smem<D>::TOTAL, stream, q, k, v, p));
-    if (ph[2].prefix_items + ph[2].seq_items) MTV_CUDA_CHECK(launch_dependent(paged_attn8_thin_kernel<D>, dim3(2 * sm_count()), T8_WARPS * 32, 0, stream, p));
+    if (ph[2].prefix_items + ph[2].seq_items) {
+        // at most 8 rows in every item: products of 8
+        const int rows = (ph[2].prefix_items ? p.a.B : 1) * p.a.T * p.a.G;
+        if (rows <= 8) MTV_CUDA_CHECK(launch_dependent(paged_attn8_thin_kernel<D, 1>, dim3(2 * sm_count()), T8<D, 1>::WARPS * 32, T8<D, 1>::TOTAL, stream, p));
+        else MTV_CUDA_CHECK(launch_dependent(paged_attn8_thin_kernel<D, 2>, dim3(2 * sm_count()), T8<D, 2>::WARPS * 32, T8<D, 2>::TOTAL, stream, p));
+    }
     return pa_combine(p.a, D, stream);
 }
 
