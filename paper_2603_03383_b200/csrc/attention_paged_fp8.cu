@@ -198,6 +198,18 @@ __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
+// exp2_poly2 for weights that are rounded to fp16: what it gives at its lower end, 2^-126, is 0 there, so that nothing need be taken off.
+__device__ __forceinline__ float2 exp2_poly2_f16(float2 x) {
+    const float2 magic = make_float2(12582912.f, 12582912.f);
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float2 t = __fadd2_rn(x, magic), jf = __fadd2_rn(t, make_float2(-magic.x, -magic.y)), f = __fadd2_rn(x, make_float2(-jf.x, -jf.y));
+    float2 q = __ffma2_rn(make_float2(0.055171650f, 0.055171650f), f, make_float2(0.24261113f, 0.24261113f));
+    q = __ffma2_rn(q, f, make_float2(0.69326097f, 0.69326097f));
+    q = __ffma2_rn(q, f, make_float2(0.99992806f, 0.99992806f));
+    return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23)));
+}
+
 // Four values times the factor, as codes of their first terms and of their second.
 __device__ __forceinline__ void to_terms(uint32_t pair0, uint32_t pair1, float factor, uint32_t &first, uint32_t &second) {
     const float x[4] = {__uint_as_float(pair0 << 16) * factor, __uint_as_float(pair0 & 0xffff0000u) * factor,
@@ -765,8 +777,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                 float2 p01, p23;
                                 if (e == 12) {      // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
                                     px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
-                                    p01 = exp2_poly2(x01);
-                                    p23 = exp2_poly2(x23);
+                                    p01 = exp2_poly2_f16(x01);
+                                    p23 = exp2_poly2_f16(x23);
                                 } else {
                                     p01 = make_float2(ex2(x01.x), ex2(x01.y));
                                     p23 = make_float2(ex2(x23.x), ex2(x23.y));
@@ -1235,18 +1247,17 @@ extern "C" int tree_verify_attention_paged_fp8(const mtv_tree_t *tree, int B, in
     p.status = status; p.dev_error = tree->d_error;
     p.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
     pp.k = k_pool; pp.v = v_pool; pp.k_scale = k_scale; pp.v_scale = v_scale;
-    CUtensorMap q_map, k_map, v_map;
-    {
+    CUtensorMap q_map = {}, k_map = {}, v_map = {};
+    const PaPhase (&ph)[3] = p.phase;
+    if (ph[0].prefix_items + ph[0].seq_items + ph[1].prefix_items + ph[1].seq_items) {      // (thin items need no maps)
         const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)B * p.T, 1};
         const cuuint64_t str[3] = {(cuuint64_t)D * 2, (cuuint64_t)Hq * D * 2, (cuuint64_t)B * p.T * Hq * D * 2};
         const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)p.npc, 1};
         if (!encode_map_bf16(&q_map, q, 4, dims, str, box)) return MTV_ERR_CUDA;
-    }
-    {
-        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)pool->page_size, (cuuint64_t)Hkv, (cuuint64_t)pool->n_pages};
-        const cuuint64_t str[3] = {(cuuint64_t)pool->stride_t, (cuuint64_t)pool->stride_h, (cuuint64_t)pool->stride_page};
-        const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)p.page_rows, 1, 1};
-        if (!encode_map_bytes(&k_map, k_pool, 4, dims, str, box, D) || !encode_map_bytes(&v_map, v_pool, 4, dims, str, box, 0)) return MTV_ERR_CUDA;
+        const cuuint64_t dims8[4] = {(cuuint64_t)D, (cuuint64_t)pool->page_size, (cuuint64_t)Hkv, (cuuint64_t)pool->n_pages};
+        const cuuint64_t str8[3] = {(cuuint64_t)pool->stride_t, (cuuint64_t)pool->stride_h, (cuuint64_t)pool->stride_page};
+        const cuuint32_t box8[4] = {(cuuint32_t)D, (cuuint32_t)p.page_rows, 1, 1};
+        if (!encode_map_bytes(&k_map, k_pool, 4, dims8, str8, box8, D) || !encode_map_bytes(&v_map, v_pool, 4, dims8, str8, box8, 0)) return MTV_ERR_CUDA;
     }
     return D == 128 ? launch_paged8<128>(q_map, k_map, v_map, pp, (cudaStream_t)stream) : launch_paged8<64>(q_map, k_map, v_map, pp, (cudaStream_t)stream);
 }
