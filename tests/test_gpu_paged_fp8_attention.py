@@ -3,6 +3,8 @@
 Element by element, with A = sum of the weights times |v| (the formula on |v|): the output's rounding to bf16 is at most 2^-8 of the result, a
 weight's rounding to fp16 at most 2^-11 of it (the weights that lose more are below 2^-22 of the largest, and vanish in the rest), an exponential off by at
 most 7.5e-5, in the weights and in their sum.  Scores are fp32 sums of exact products: 1e-4 of A covers them at the scores of these inputs (below 2^6)."""
+import random
+
 import pytest
 import torch
 
@@ -91,6 +93,19 @@ def check(tree, tb, Hq, Hkv, D, page, shared, lens, seed=1, tokens_outside=False
 def test_against_the_formula(K, T, Hq, Hkv, D, page, shared, lens):
     tb, tree = tree_of(K, T)
     check(tree, tb, Hq, Hkv, D, page, shared, lens)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_sizes_at_random(seed):
+    """Trees, groups, batches, prefixes and lengths as they come, short ones more often than long ones."""
+    r = random.Random(seed)
+    K, T = r.choice([2, 3, 4, 5]), 1 if seed % 4 == 0 else int(2 ** r.uniform(1, 7))
+    D, page, Hkv, G = r.choice([64, 128]), r.choice([16, 32, 64, 128, 256]), r.choice([1, 2, 3]), r.randint(1, 8)
+    B = int(2 ** r.uniform(0, 5))
+    shared = r.choice([0, 0, int(2 ** r.uniform(4, 11))]) // page * page
+    lens = [shared + int(2 ** r.uniform(0, 11)) - 1 for _ in range(B)]
+    tb, tree = tree_of(K, T)
+    check(tree, tb, Hkv * G, Hkv, D, page, shared, lens, seed=seed, tokens_outside=bool(seed & 1))
 
 
 @pytest.mark.parametrize("T,Hq,Hkv,D,page,shared,lens", [
