@@ -8,6 +8,7 @@ is missing, loading fails with an error.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -446,6 +447,7 @@ def _layout_of(pool, dtype, where):
 
 _APPEND = ("q_layers", "q_out_layers", "k_new_layers", "v_new_layers", "k_ptrs", "v_ptrs", "page_table", "seq_lens", "status")
 _SCALES = ("k_scale", "v_scale")
+_APPEND_FP8, _APPEND_ROWS, _APPEND_ROWS_FP8 = _APPEND + _SCALES, _APPEND + ("row_starts",), _APPEND + _SCALES + ("row_starts",)
 
 
 def _scales(scales, n):
@@ -467,7 +469,7 @@ def _append_tree(where, call, dtype, scales, tree, q_layers, q_out_layers, k_new
     _layout_of(pool, dtype, where)
     rows = n_layers * B * T * D
     _, q, q_out, k, v, kp, vp, table, lens, st, *sc = _look(
-        where, _APPEND + _SCALES, q_layers, _BF16, rows * Hq, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
+        where, _APPEND_FP8, q_layers, _BF16, rows * Hq, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
         v_new_layers, _BF16 | _LIKE_PREVIOUS, -1, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, B * max_pages, seq_lens, _I32, B,
         status, _MAYBE_I32, B, *_scales(scales, n_layers * Hkv))
     _check(call(tree.handle, B, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, *sc, rope_theta, st, _stream(stream)), where)
@@ -483,7 +485,7 @@ def _append_rows(where, call, dtype, scales, q_layers, q_out_layers, k_new_layer
         _refuse(where, "k_new_layers")
     _layout_of(pool, dtype, where)
     _, q, q_out, k, v, kp, vp, table, lens, st, *sc, starts = _look(
-        where, _APPEND + (_SCALES if scales else ()) + ("row_starts",), q_layers, _BF16, -1, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
+        where, _APPEND_ROWS_FP8 if scales else _APPEND_ROWS, q_layers, _BF16, -1, q_out_layers, _BF16 | _LIKE_PREVIOUS, -1, k_new_layers, _BF16, -1,
         v_new_layers, _BF16 | _LIKE_PREVIOUS, -1, k_ptrs, _I64, n_layers, v_ptrs, _I64, n_layers, page_table, _I32, -1, seq_lens, _I32, B,
         status, _MAYBE_I32, B, *_scales(scales, n_layers * Hkv), row_starts, _I32, B + 1)
     _check(call(B, n_rows, Hq, Hkv, D, n_layers, q, q_out, k, v, kp, vp, pool, table, max_pages, lens, starts, *sc, rope_theta, st, _stream(stream)), where)
@@ -571,7 +573,8 @@ def paged_workspace_bytes(tree, B, Hq, Hkv, D, shared_len=0) -> int:
     return lib().tree_attention_paged_workspace_bytes(tree.handle, B, Hq, Hkv, D, shared_len)
 
 
-_ATTENTION = ("q", "out", "k_pool", "v_pool", "page_table", "seq_lens", "status", "ws")
+_ATTENTION = ("q", "out", "k_pool", "v_pool", "page_table", "seq_lens", "status", "ws") + _SCALES
+_layout_of_sizes = functools.lru_cache(maxsize=256)(PoolLayout)      # (numbers alone; making one costs as much as looking at three tensors)
 
 
 def _attention(where, call, kind, scales, tree, q, k_pool, v_pool, page_table, seq_lens, out, ws, shared_len, scale, status, stream):
@@ -587,10 +590,10 @@ def _attention(where, call, kind, scales, tree, q, k_pool, v_pool, page_table, s
         _refuse(where, "page_table")
     max_pages = page_table.shape[1]
     _, q_at, out_at, k, v, table, lens, st, ws_at, *sc = _look(
-        where, _ATTENTION + _SCALES, q, _BF16, -1, out, _BF16 | _LIKE_PREVIOUS, -1, k_pool, kind | _STRIDED, -1,
+        where, _ATTENTION, q, _BF16, -1, out, _BF16 | _LIKE_PREVIOUS, -1, k_pool, kind | _STRIDED, -1,
         v_pool, kind | _STRIDED | _LIKE_PREVIOUS, -1, page_table, _I32, B * max_pages, seq_lens, _I32, B, status, _MAYBE_I32, B, ws, _ANY, -1,
         *_scales(scales, pools[1]))
-    _check(call(tree.handle, B, Hq, pools[1], D, q_at, k, v, PoolLayout(strides[0], strides[1], strides[2], pools[2], pools[0]), table, max_pages,
+    _check(call(tree.handle, B, Hq, pools[1], D, q_at, k, v, _layout_of_sizes(strides[0], strides[1], strides[2], pools[2], pools[0]), table, max_pages,
                 shared_len, lens, *sc, scale, out_at, st, ws_at, ws.nbytes, _stream(stream)), where)
 
 

@@ -43,7 +43,6 @@ template <int D> struct P8Smem {
     static constexpr uint32_t IDESC_PV = IDESC | (uint32_t)(D >> 3) << 17 | 1u << 16;             // N = D columns, B (= V) N-major
     // K's codes: rows of D bytes in groups of 8, swizzled over as many bytes
     static constexpr uint32_t K_DESC_HI = D == 128 ? ptx::DESC_HI : (512u >> 4) | 1u << 14 | 4u << 29;
-    static constexpr uint32_t Q2 = D == 128 ? HALF : 64;                                          // the second terms, from the first
 };
 
 enum {
@@ -575,7 +574,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     for (int term = 0; term < 2; ++term)
 #pragma unroll
                         for (int kk = 0; kk < D / 32; ++kk)
-                            ptx::mma_ss_f8_elect(t_s, dq + (term * SM::Q2 + kk * 32) / 16, ptx::DESC_HI, dk + kk * 2, SM::K_DESC_HI, SM::IDESC_QK, term + kk > 0, leader);
+                            ptx::mma_ss_f8_elect(t_s, dq + (kk / 2 * SM::HALF + kk % 2 * 64 + term * 32) / 16, ptx::DESC_HI, dk + kk * 2, SM::K_DESC_HI, SM::IDESC_QK, term + kk > 0, leader);
                     ptx::tc_commit_elect(bar(P8_SREADY + s), leader);
                     if (kt == ks.t1 - 1) ptx::tc_commit_elect(bar(P8_QFREE + s), leader);
                     end_run();
@@ -609,7 +608,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         auto node_of = [&](const PaPiece &pc) { return (pc.tile0 + (pairs ? s : 0)) * p.npc + node_in_tile; };
         // (what is needed of a piece at its start and end alone stays in the queue until then)
         int n_s = 0;                       // key tiles so far
-        float m = 0.f, l = 0.f;
+        float m = 0.f, l = 0.f, vs = 0.f;  // the piece's: reference, sum, scale of V
         bool mine = false;
         int node = -1;                     // the row's, if it sees some of the tree's rows; -1: none, or no row
         bool ok = true, more = true;
@@ -617,34 +616,38 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         for (int n = 0; ok && more; ++n) {
             PaPiece pc;
             more = look(q, n, pc);
-            float sc = 0.f;
+            float sc = 0.f, vs_next = 0.f;
             if (more) {
-                // ---- the piece's queries in two terms: each thread of a row takes half of its columns (both have read them when their maxima are exchanged).
-                // Their first product then runs beside the end of the piece before.
+                // ---- the piece's queries in two terms, where they are: each thread of a row takes half of its columns.  Their first product then runs beside
+                // the end of the piece before.
                 const float ks = __ldg(pp.k_scale + pc.g);
+                vs_next = __ldg(pp.v_scale + pc.g);
                 if (!wait(P8_QFULL + s, n & 1)) { ok = false; break; }
                 constexpr int CHUNKS = D / 16;
-                unsigned char *at = gbase + s * SM::TILE + row * 128;
-                auto chunk = [&](int c) { return (c ^ (row & 7)) << 4; };
-                uint4 u[CHUNKS];
+                unsigned char *at = gbase + s * SM::TILE + (D == 128 ? hf * SM::HALF : 0) + row * 128;
+                auto chunk = [&](int c) { return reinterpret_cast<uint4 *>(at + (((D == 128 ? 0 : hf * CHUNKS) + c ^ (row & 7)) << 4)); };
                 uint32_t most = 0u;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) u[c] = *reinterpret_cast<const uint4 *>(at + (D == 128 ? hf * SM::HALF : 0) + chunk(D == 128 ? c : hf * CHUNKS + c));
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-                    most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u[c].x)), abs2_bf16(u[c].y)), abs2_bf16(u[c].z)), abs2_bf16(u[c].w));
+#pragma unroll 4
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const uint4 u = *chunk(c);
+                    most = larger_bits(larger_bits(larger_bits(larger_bits(most, abs2_bf16(u.x)), abs2_bf16(u.y)), abs2_bf16(u.z)), abs2_bf16(u.w));
+                }
                 most = max(most, __float_as_uint(exchange(__uint_as_float(most))));
                 const float2 factor = row_factor<7>(most);
+                // 32 columns at a time, where they are: the first terms' 32 bytes, then the second terms'
+#pragma unroll 1
+                for (int c = 0; c < CHUNKS; c += 4) {
+                    uint32_t first[8], second[8];
 #pragma unroll
-                for (int c = 0; c < CHUNKS; c += 2) {
-                    uint4 a, b;
-                    to_terms(u[c].x, u[c].y, factor.x, a.x, b.x);
-                    to_terms(u[c].z, u[c].w, factor.x, a.y, b.y);
-                    to_terms(u[c + 1].x, u[c + 1].y, factor.x, a.z, b.z);
-                    to_terms(u[c + 1].z, u[c + 1].w, factor.x, a.w, b.w);
-                    const int to = (hf * CHUNKS + c) / 2;                      // 16 columns
-                    *reinterpret_cast<uint4 *>(at + chunk(to)) = a;
-                    *reinterpret_cast<uint4 *>(at + (D == 128 ? SM::HALF : 0) + chunk(D == 128 ? to : to + 4)) = b;
+                    for (int e = 0; e < 4; ++e) {
+                        const uint4 u = *chunk(c + e);
+                        to_terms(u.x, u.y, factor.x, first[2 * e], second[2 * e]);
+                        to_terms(u.z, u.w, factor.x, first[2 * e + 1], second[2 * e + 1]);
+                    }
+                    *chunk(c) = make_uint4(first[0], first[1], first[2], first[3]);
+                    *chunk(c + 1) = make_uint4(first[4], first[5], first[6], first[7]);
+                    *chunk(c + 2) = make_uint4(second[0], second[1], second[2], second[3]);
+                    *chunk(c + 3) = make_uint4(second[4], second[5], second[6], second[7]);
                 }
                 sc = p.scale_log2 * ks * factor.y;
                 ptx::fence_proxy_async();
@@ -659,7 +662,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if (__any_sync(0xffffffffu, mine)) {
                     const bool odd = bad[s * 4 + ((n - 1) & 3)] == n;
                     const bool direct = p.shared == 0 && old.whole;
-                    const float vs = __ldg(pp.v_scale + old.g), factor = direct ? vs / l : vs;
+                    const float factor = direct ? vs / l : vs;
                     const int slot_row = pairs ? s * 128 + row : row;
                     float *o_out = ph.o + ((size_t)old.slot * ph.rows * (D / 8) + (size_t)(hf * (D / 16)) * ph.rows + slot_row) * 8;
                     __nv_bfloat16 *out = p.out + (((size_t)max(old.b, 0) * p.T + node_of(old)) * p.Hq + old.g * p.G + head) * D + hf * (D / 2);
@@ -705,6 +708,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             node = mine && pc.b >= 0 ? node_of(pc) : -1;
             m = -INFINITY;
             l = 0.f;
+            vs = vs_next;
             const bool some = __any_sync(0xffffffffu, mine);
             const float2 sc2 = make_float2(sc, sc);
 #pragma unroll 1
