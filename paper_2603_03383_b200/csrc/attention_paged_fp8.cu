@@ -58,6 +58,7 @@ constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 
 static_assert(P8_OFF_QUEUE + 2 * PA_QUEUE * 32 <= 960, "barrier region");
 static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
+__host__ __device__ constexpr int P8_ITEM_COST(int single) { return single ? 8 : 12; }   // what the start and end of an item take, in quarters of a key tile
 constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
 
 // What the issuing warps and the converting ones want of a piece (their registers are few).
@@ -94,7 +95,7 @@ __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor) {
 // The run of one worker of a CTA (which = 0: of pairs; 1, 2: of single row tiles) and the item it begins in.  One warp; length, prefix: of the phase's line.
 // (The same as begin_walks, one at a time: the kernel is as large as an SM's instruction cache can bear.)
 __device__ __forceinline__ void begin_walk(const PaParams &p, PaWalk &w, int which, int cta, int n_cta, int n_pairs, int length, int prefix, int lane) {
-    const int single = which > 0, ends = ITEM_COST(single), cost = item_cost(key_tiles(p.shared), ends);
+    const int single = which > 0, ends = P8_ITEM_COST(single), cost = item_cost(key_tiles(p.shared), ends);
     const int workers = single ? 2 * (n_cta - n_pairs) : n_pairs;
     w.worker = which == 0 ? cta : which == 1 ? cta - n_pairs : cta + n_cta - 2 * n_pairs;
     w.ends = ends;
@@ -195,18 +196,6 @@ __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity) {
         "}\n"
         : "=r"(ok) : "r"(bar), "r"(parity), "n"((uint32_t)ptx::WAIT_CYCLE_LIMIT) : "memory");
     return ok != 0;
-}
-
-// exp2_poly2 for weights that are rounded to fp16: what it gives at its lower end, 2^-126, is 0 there, so that nothing need be taken off.
-__device__ __forceinline__ float2 exp2_poly2_f16(float2 x) {
-    const float2 magic = make_float2(12582912.f, 12582912.f);
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 t = __fadd2_rn(x, magic), jf = __fadd2_rn(t, make_float2(-magic.x, -magic.y)), f = __fadd2_rn(x, make_float2(-jf.x, -jf.y));
-    float2 q = __ffma2_rn(make_float2(0.055171650f, 0.055171650f), f, make_float2(0.24261113f, 0.24261113f));
-    q = __ffma2_rn(q, f, make_float2(0.69326097f, 0.69326097f));
-    q = __ffma2_rn(q, f, make_float2(0.99992806f, 0.99992806f));
-    return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23)));
 }
 
 // Four values times the factor, as codes of their first terms and of their second.
@@ -335,8 +324,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         int prefix[2], length[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-            prefix[f] = item_cost(key_tiles(p.shared), ITEM_COST(f)) * p.phase[f].prefix_items;
-            length[f] = prefix[f] + (tiles * TILE_COST + seqs * ITEM_COST(f)) * p.phase[f].seq_items;
+            prefix[f] = item_cost(key_tiles(p.shared), P8_ITEM_COST(f)) * p.phase[f].prefix_items;
+            length[f] = prefix[f] + (tiles * TILE_COST + seqs * P8_ITEM_COST(f)) * p.phase[f].seq_items;
         }
         // the first CTAs take the pairs, the others the single row tiles
         int n_pairs = n_cta;
@@ -781,8 +770,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                 float2 p01, p23;
                                 if (e == 12) {      // every fourth quadruple on the FMA pipes: the special-function unit takes as long as the products
                                     px = max3_nan(max3_nan(px, x01.x, x01.y), x23.x, x23.y);   // (neither NaN nor what is above 127 survives there)
-                                    p01 = exp2_poly2_f16(x01);
-                                    p23 = exp2_poly2_f16(x23);
+                                    p01 = exp2_poly2(x01);
+                                    p23 = exp2_poly2(x23);
                                 } else {
                                     p01 = make_float2(ex2(x01.x), ex2(x01.y));
                                     p23 = make_float2(ex2(x23.x), ex2(x23.y));

@@ -100,7 +100,7 @@ template <bool VEC> __device__ __forceinline__ void store8(__nv_bfloat16 *p, con
 // take 34.9 and 15.4, one 36.5 and 17.4; two pairs in flight per thread 34.8 and 14.9, as fewer blocks fit.
 // VEC: the rows begin at multiples of 16 bytes.  FP8: the pools hold codes.
 template <int D, bool VEC, bool FP8>
-__global__ void __launch_bounds__(PAGED_THREADS)
+__global__ void __launch_bounds__(PAGED_THREADS, 6)
 kv_append_rope_paged_kernel(const AppendParams p) {
     constexpr int HALF = D / 2, PER_HEAD = D / 16, SLOTS = PAGED_THREADS / PER_HEAD;    // threads of a head; heads at a time
     __shared__ __align__(16) float cs[APPEND_ROWS][HALF], sn[APPEND_ROWS][HALF];
