@@ -511,9 +511,10 @@ int kv_compact_accepted_paged_fp8(const mtv_tree_t *tree, int B, int Hkv, int D,
                                   int32_t *status, void *stream);
 
 /* tree_verify_attention_paged over such a cache: the scores are scale * k_scale[g] * <q, codes of k>, the result v_scale[g] times the weighted sum of V's
- * codes.  fp16 products (codes are numbers of fp16; a query row is multiplied by the power of two that brings its largest value to [256, 512), in
- * which values below 2^-25 of it lose bits), fp32 sums and softmax, weights rounded to fp16 (2^-11 of a weight, and 2^-33 of the
- * row's largest at least).  NaN in q, or in a K or V row that a node sees, makes its output NaN; so does an infinity in q.
+ * codes.  Products of codes are exact; fp32 sums and softmax.  A query row is multiplied by the power of two that brings its largest value into e4m3's or
+ * fp16's range: where a KV head has at most 16 query rows, values below 2^-25 of the row's largest lose bits; else rows are two e4m3 terms, and
+ * values below 2^-9 of the largest are held to 2^-17 of it.  Weights are rounded to fp16: 2^-11 of a weight, 2^-33 of the row's largest at least.
+ * A NaN or an infinity in a query row makes the row's output NaN, as does a NaN in a K row that it sees; a NaN in a V row that it sees, that column.
  * Workspace: tree_attention_paged_workspace_bytes. */
 int tree_verify_attention_paged_fp8(const mtv_tree_t *tree, int B, int Hq, int Hkv, int D, const mtv_bf16 *q, const uint8_t *k_pool,
                                     const uint8_t *v_pool, const mtv_pool_layout *pool, const int32_t *page_table, int max_pages,

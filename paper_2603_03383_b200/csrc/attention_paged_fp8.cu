@@ -6,19 +6,27 @@
 // holds the 8 bits of a bf16 exactly: a row is multiplied by the power of two that brings its largest value to [128, 256), q1 is that rounded to a code
 // and q2 what is left; values below 2^-9 of the row's largest are held to 2^-17 of it.  Two products of 8 bits take the time of one of 16.
 // Weights would want two terms too, at every key tile, on the warps that have the least time; so V is converted instead, to fp16 tiles
-// (every code is a number of fp16), by warps of their own, and the second product is fp16 x fp16.
+// (every code is a number of fp16), by warps of their own, and the second product is fp16 x fp16.  (With K converted as well, those warps were what single
+// row tiles waited for: 16 trees of 29 nodes and up to 4000 keys took 106 us, now 60.)
 //   P   weights are fp16, 2^SHIFT at the reference (the maximum of a piece's first tile) and below 2^16: they lose bits below 2^(-14 - SHIFT) of the
-//       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.
-// K in fp16 as well took 88 us of a long context's call where this takes
-// 
+//       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.  The reference moves where a
+//       later tile's weights do not fit, as for the bf16 cache.
+//
 // One persistent CTA per SM, two row tiles in flight, each with its scores, weights and accumulator in tensor memory and eight softmax warps:
 //   warps 0-7 / 8-15  softmax of row tile 0 / 1; in front of a piece they split its queries
 //   warps 16-19       V's codes -> fp16 tiles (128 keys, 128-byte swizzle); rows behind the last key become zeros (their weight is 0, but 0 * NaN is
 //                     not), NaN codes of the tree's rows too (they are given to the rows that see them at the end)
 //   warps 20, 21      issue the products of row tile 0 / 1
 //   warp 22           derives the pieces, requests Q and the codes (a box per page)
-// K's codes, V's and V's tiles have a ring each.
-// The softmax warpgroups have 96 registers, the others 48 (768 threads of 80 at the launch).
+// K's codes, V's and V's tiles have a ring each.  A CTA works on pairs of row tiles or on single ones, never on both, and every warp's loop stands once for
+// either (in_turns): the kernel would else be 193 KB of code, of which an SM's instruction cache holds a part (now 81 KB; the same 16 trees of 29: 93 -> 73 us).
+// Sixteen scores of a row are in registers at a time, the next on their way: with all 64 the 80 registers of 768 threads spill (long context 97 -> 85 us).
+//
+// Measured, whole calls: one tree of 64 nodes, 32 / 8 heads of 128, 60001 keys (63 GFLOP): 81 us; 8 sequences of 64 nodes, 16384 shared keys and up to 2048 of
+// their own (147 GFLOP): 168 us, the tensor pipe at 49 % beside the joining.  A pair of key tiles takes 3.8 k cycles of the 2.06 k that its products need: the
+// chain scores -> weights (2.0 k) -> product of a row tile is hidden by the other row tile's alone.  Looked at and left: the warps of both row tiles on each in
+// turn (32 columns a thread: 299 us), halves of key tiles in turn (64 keys a product of scores, 189 us: the queries are read twice as often from shared memory,
+// which is what bounds those products), no turns between the issuing warps (192), more and fewer polynomials (178, 166 against 154 in one comparison).
 #include <limits.h>
 
 #include "fp8.cuh"
@@ -831,7 +839,9 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // A CTA walks a run of the line of all thin items, KEYS keys to a warp at a time.  Asynchronous copies bring them to the warp's own part of shared memory,
 // STAGES - 1 blocks ahead: no warp waits for another, and no register holds what is on its way.  At a piece's end the warps join.
 // An instruction of copies covers whole rows: where it took half a row of each of 8 keys (as the operands have them), the other half crossed from L2 with it, twice
-// in all.
+// in all (64 single tokens: 88 us so, 71 now).
+// Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 53.6 us = 5.2 TB/s, 79 % of the copy rate (61 us with the joining); one token
+// of 60001 keys 31 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces' starts and ends.
 constexpr float T8_SHIFT = 7.f, T8_SLACK = 8.f;   // weights are 2^SHIFT at the reference, which may be SLACK too small: below 2^16
 
 // NR: products of 8 query rows.
