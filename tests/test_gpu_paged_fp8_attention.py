@@ -158,6 +158,60 @@ def test_queries_of_any_size(D, T, G, power):
     assert ((out.double() - want).abs() / (bound(want, absolute) + 2 * 130 * 2.0 ** -24 * 128 * absolute)).max().item() <= 1.0
 
 
+@pytest.mark.parametrize("T,G", [(1, 4), (20, 3), (64, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_that_are_all_zero(D, T, G):
+    """Queries and a scale so small that their factor is none of fp32's: every visible key weighs the same."""
+    tb, tree = tree_of(4, T)
+    shared, lens, page, Hkv = 64, [64, 200, 517], 16, 2
+    t, _, kp, vp, ks, vs, q = inputs(T, Hkv * G, Hkv, D, page, shared, lens, seed=9)
+    out = run(tree, (q.float() * 2.0 ** -120).to(torch.bfloat16), kp, vp, ks, vs, t, lens, shared, scale=1e-20)
+    want, absolute = want_of(torch.zeros_like(q), kp, vp, ks, vs, t, lens, tb["mask"])
+    assert ((out.double() - want).abs() / bound(want, absolute)).max().item() <= 1.0
+
+
+@pytest.mark.parametrize("K,T,Hq,Hkv,D,page,shared,lens", [
+    (3, 20, 32, 8, 64, 16, 0, [(37 * i) % 400 for i in range(300)]),       # single row tiles, eight items a worker
+    (3, 20, 32, 8, 128, 16, 32, [32 + (91 * i) % 300 for i in range(150)]),
+    (4, 64, 32, 8, 128, 32, 0, [(53 * i) % 500 for i in range(100)]),      # pairs, five a worker, ten
+    (4, 64, 16, 4, 64, 16, 64, [64 + (29 * i) % 200 for i in range(400)]),
+    (5, 100, 24, 8, 128, 16, 0, [(17 * i) % 300 for i in range(60)]),      # three row tiles: pairs and single ones
+])
+def test_many_short_pieces(K, T, Hq, Hkv, D, page, shared, lens):
+    """More pieces a worker than are handed out at a time."""
+    tb, tree = tree_of(K, T)
+    check(tree, tb, Hq, Hkv, D, page, shared, lens)
+
+
+@pytest.mark.parametrize("T", [20, 64])
+@pytest.mark.parametrize("D", [64, 128])
+def test_row_tiles_beyond_32_bits(D, T):
+    """Pages whose offsets pass 2^32 bytes, with a NaN in a V row that some nodes see."""
+    tb, tree = tree_of(4, T)
+    Hq, Hkv, page, n_pages, stride = 8, 2, 64, 4, (1 << 30) + (1 << 29) + 48
+    g = torch.Generator().manual_seed(3)
+    small = _fp8.pools(g, 2, n_pages, Hkv, page, D)
+    t, lens = torch.tensor([[3, 1, 2]], dtype=torch.int32), [70]
+    mask = torch.tensor(tb["mask"], dtype=torch.bool)
+    ks, vs = _fp8.scales(g, Hkv), _fp8.scales(g, Hkv)
+    q = torch.randn(1, T, Hq, D, generator=g).to(torch.bfloat16)
+    want, absolute = want_of(q, *small, ks, vs, t, lens, tb["mask"])
+    node = T - 1
+    pg, r = int(t[0, (lens[0] + node) // page]), (lens[0] + node) % page
+    _fp8.put(small[1], (pg, 0, r, 5), NAN)
+    want[0][mask[:, node], :Hq // Hkv, 5] = NAN
+    big = []
+    for x in small:
+        buf = torch.empty((n_pages - 1) * stride + Hkv * page * D, dtype=torch.uint8, device=DEV)
+        y = buf.as_strided((n_pages, Hkv, page, D), (stride, page * D, D, 1))
+        y.copy_(x.view(torch.uint8))
+        big.append(y.view(_fp8.FP8))
+    out = run(tree, q, *big, ks, vs, t, lens, 0).double()
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    fine = ~torch.isnan(want)
+    assert ((out - want).abs() / bound(want, absolute))[fine].max().item() <= 1.0
+
+
 @pytest.mark.parametrize("T", [1, 4, 29, 64])
 @pytest.mark.parametrize("D", [64, 128])
 def test_nan_rows_reach_those_who_see_them(D, T):
