@@ -550,11 +550,12 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (pairs && lane == 0) ptx::mbar_arrive(bar(P8_TURN + (s ^ 1)));
                     __syncwarp();
                 };
-                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be)
+                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be), the turn too: a wait in
+                // vain costs this warp 400 cycles among the others' (16k document 150 -> 143 us, long context 73.2 -> 69.4 with the turn waited for in front)
                 const bool ahead = v && k && kt != ks.t0;
                 if (ahead && !k_there()) return false;
                 if (v) {
-                    if (!wait(P8_FULL + v_at, v_parity) || !wait(P8_PREADY + s, n_p++ & 1) || !begin_run()) return false;
+                    if (!wait(P8_FULL + v_at, v_parity) || !begin_run() || !wait(P8_PREADY + s, n_p++ & 1)) return false;
                     ptx::tc_fence_after();
                     const uint32_t dv = dv0 + (uint32_t)v_at * (SM::TILE >> 4);
 #pragma unroll
@@ -715,7 +716,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
                 ptx::tc_fence_after();
                 if (some) {
-                    uint32_t pk[32];                               // fp16 pairs
+                    uint32_t a[16], b[16], pk[32];                 // (pk: fp16 pairs)
+                    ptx::tmem_ld16(t_s, a);                        // on their way meanwhile
                     if ((t + 1) * PA_KEYS > pc.L) {
                         // Hidden scores become -inf where they are.  Visibility of the tree's rows as 32-bit words; the rows in front of them are visible to every
                         // node, those behind to none.
@@ -733,6 +735,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             ptx::tmem_st16(t_s + c * 16, x);
                         }
                         ptx::tmem_st_wait();
+                        ptx::tmem_ld16(t_s, a);
                     }
                     bool move = __any_sync(0xffffffffu, mine && m == -INFINITY);      // (the piece's first tile, or no key was visible so far)
                     float sum;
@@ -792,8 +795,6 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                 pk[c * 8 + e / 2 + 1] = pack2_f16(p23.x, p23.y);
                             }
                         };
-                        uint32_t a[16], b[16];
-                        ptx::tmem_ld16(t_s, a);
                         ptx::tmem_ld_wait_for16(a);
                         ptx::tmem_ld16(t_s + 16, b);
                         weights(0, a);
@@ -810,6 +811,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         // a sum that is too large, infinite or NaN: a weight then may be beyond fp16
                         if (!any_of_rows(pair_bar, mine && (!(sum < 65504.f) || !(px <= P8_LIMIT)))) break;
                         move = true;
+                        ptx::tmem_ld16(t_s, a);
                     }
                     l += sum;
                     ptx::tmem_st32(t_s, pk);
