@@ -42,7 +42,7 @@ template <int D> struct P8Smem {
     static constexpr int HALVES = D / 64;
     static constexpr uint32_t HALF = 128 * 128;          // 128 rows of 128 bytes (64 columns of 2, or 128 of 1), 128-byte swizzle
     static constexpr uint32_t TILE = HALVES * HALF, CODES = 128 * D;
-    static constexpr int K_STAGES = D == 128 ? 3 : 8, V_STAGES = K_STAGES, TILES = D == 128 ? 2 : 4;
+    static constexpr int K_STAGES = D == 128 ? 4 : 8, V_STAGES = D == 128 ? 2 : 8, TILES = D == 128 ? 2 : 4;
     static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + K_STAGES * CODES, OFF_TILES = OFF_V + V_STAGES * CODES, OFF_ROWS = OFF_TILES + TILES * TILE,
                               OFF_BAR = OFF_ROWS + 2048, TOTAL = OFF_BAR + 960;
     static_assert(TOTAL <= 227 * 1024, "shared memory budget");
@@ -64,7 +64,7 @@ enum {
 };
 constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 + 15) / 16 * 16;
 static_assert(P8_OFF_QUEUE + 2 * PA_QUEUE * 32 <= 960, "barrier region");
-static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
+static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::V_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
 __host__ __device__ constexpr int P8_ITEM_COST(int single) { return single ? 8 : 12; }   // what the start and end of an item take, in quarters of a key tile
 constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
@@ -226,7 +226,9 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const PaParams &p = pp.a;
     extern __shared__ __align__(1024) unsigned char gbase[];
     let_next_start();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    // (the shuffle tells the compiler that a warp's number is the same for its lanes: what follows from it needs no divergent branches, and operands of the products
+    // no way through vector registers; 16k document 143 -> 135 us, long context 69.1 -> 66.9, single row tiles 52.0 -> 47.7)
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t sbase = ptx::smem_u32(gbase);
     if (sbase & 1023u) {                   // (the swizzles count on it)
         previous_done();
@@ -387,7 +389,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         struct Ring {
             int entry = 0, stage = 0, turns = 0;
         } rk, rv;
-        auto load = [&](Ring &r, const CUtensorMap *map, uint32_t off, int full, int free, int id, int row, int g) {
+        auto load = [&](Ring &r, int stages, const CUtensorMap *map, uint32_t off, int full, int free, int id, int row, int g) {
             if (r.turns && !wait(free + r.stage, (r.turns - 1) & 1)) return false;
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full + r.stage), SM::CODES);
             __syncwarp();
@@ -395,7 +397,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 ptx::tma_load_4d(sbase + off + r.stage * SM::CODES + lane * p.page_rows * D, map, bar(full + r.stage), 0, row, g,
                                  id >= 0 && id < p.pages.n_pages ? id : p.pages.n_pages);
             ++r.entry;
-            if (++r.stage == SM::K_STAGES) { r.stage = 0; ++r.turns; }
+            if (++r.stage == stages) { r.stage = 0; ++r.turns; }
             return true;
         };
         int n0 = 0, n1 = 0;
@@ -406,9 +408,9 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             s.id = find(s, s.t0);
             return true;
         }, [&](int l, bool v, const P8Load &vs, int vt, bool k, const P8Load &ks, int kt) {
-            if (v && !load(rv, &v_map, SM::OFF_V, P8_VFULL, P8_VFREE, vs.id, row_in_page(vs, vt), vs.g)) return false;
+            if (v && !load(rv, SM::V_STAGES, &v_map, SM::OFF_V, P8_VFULL, P8_VFREE, vs.id, row_in_page(vs, vt), vs.g)) return false;
             if (!k) return true;
-            if (!load(rk, &k_map, SM::OFF_K, P8_KFULL, P8_KFREE, ks.id, row_in_page(ks, kt), ks.g)) return false;
+            if (!load(rk, SM::K_STAGES, &k_map, SM::OFF_K, P8_KFULL, P8_KFREE, ks.id, row_in_page(ks, kt), ks.g)) return false;
             if (kt == ks.t0)
 #pragma unroll 1
                 for (int s = l; s < (pairs ? 2 : l + 1); ++s) {
