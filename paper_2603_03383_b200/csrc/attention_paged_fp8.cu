@@ -66,7 +66,6 @@ constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 
 static_assert(P8_OFF_QUEUE + 2 * PA_QUEUE * 32 <= 960, "barrier region");
 static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::V_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
-__host__ __device__ constexpr int P8_ITEM_COST(int single) { return single ? 8 : 12; }   // what the start and end of an item take, in quarters of a key tile
 constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
 
 // What the issuing warps and the converting ones want of a piece (their registers are few).
@@ -105,7 +104,7 @@ __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor) {
 // The run of one worker of a CTA (which = 0: of pairs; 1, 2: of single row tiles) and the item it begins in.  One warp; length, prefix: of the phase's line.
 // (The same as begin_walks, one at a time: the kernel is as large as an SM's instruction cache can bear.)
 __device__ __forceinline__ void begin_walk(const PaParams &p, PaWalk &w, int which, int cta, int n_cta, int n_pairs, int length, int prefix, int lane) {
-    const int single = which > 0, ends = P8_ITEM_COST(single), cost = item_cost(key_tiles(p.shared), ends);
+    const int single = which > 0, ends = ITEM_COST(single), cost = item_cost(key_tiles(p.shared), ends);
     const int workers = single ? 2 * (n_cta - n_pairs) : n_pairs;
     w.worker = which == 0 ? cta : which == 1 ? cta - n_pairs : cta + n_cta - 2 * n_pairs;
     w.ends = ends;
@@ -336,8 +335,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         int prefix[2], length[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-            prefix[f] = item_cost(key_tiles(p.shared), P8_ITEM_COST(f)) * p.phase[f].prefix_items;
-            length[f] = prefix[f] + (tiles * TILE_COST + seqs * P8_ITEM_COST(f)) * p.phase[f].seq_items;
+            prefix[f] = item_cost(key_tiles(p.shared), ITEM_COST(f)) * p.phase[f].prefix_items;
+            length[f] = prefix[f] + (tiles * TILE_COST + seqs * ITEM_COST(f)) * p.phase[f].seq_items;
         }
         // the first CTAs take the pairs, the others the single row tiles
         int n_pairs = n_cta;
@@ -549,8 +548,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     return s == 0 && turn == 0 ? true : wait(P8_TURN + s, (turn + s - 1) & 1);
                 };
                 auto end_run = [&]() {
-                    if (pairs && lane == 0) ptx::mbar_arrive(bar(P8_TURN + (s ^ 1)));
-                    __syncwarp();
+                    if (pairs) ptx::tc_commit_elect(bar(P8_TURN + (s ^ 1)), leader);
                 };
                 // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be), the turn too: a wait in
                 // vain costs this warp 400 cycles among the others' (16k document 150 -> 143 us, long context 73.2 -> 69.4 with the turn waited for in front)
