@@ -842,7 +842,7 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
 // (max, sum) and their columns requested together: the kernel is a chain of loads from L2.  SPLIT > 1: that many threads share a row's columns,
 // each every SPLIT-th group of four pieces of an item, and meet in shared memory; the order of the additions depends on the pieces alone.  One thread (SPLIT = 1)
 // takes the pieces of both items as one list, so that an item of one or two does not take a trip to L2 of its own, and four blocks share an SM: 8 sequences of 64
-// nodes behind 16384 keys take 149 us in all (152 with a list an item and three blocks), 16 trees of 64 nodes 65 (68), the results the same.
+// nodes behind 16384 bf16 keys take 149 us in all (152 with a list an item and three blocks), 16 trees of 64 nodes 68 (71), the results the same.
 struct PaSource {
     const float *o;       // slot of the first piece, at the row
     const float2 *ml;

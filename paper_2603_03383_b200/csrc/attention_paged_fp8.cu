@@ -7,7 +7,7 @@
 // and q2 what is left; values below 2^-9 of the row's largest are held to 2^-17 of it.  Two products of 8 bits take the time of one of 16.
 // Weights would want two terms too, at every key tile, on the warps that have the least time; so V is converted instead, to fp16 tiles
 // (every code is a number of fp16), by warps of their own, and the second product is fp16 x fp16.  (With K converted as well, those warps were what single
-// row tiles waited for: 16 trees of 29 nodes and up to 4000 keys took 106 us, now 60.)
+// row tiles waited for: 16 trees of 29 nodes and up to 4000 keys took 106 us so and 60 without.)
 //   P   weights are fp16, 2^SHIFT at the reference (the maximum of a piece's first tile) and below 2^16: they lose bits below 2^(-14 - SHIFT) of the
 //       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.  The reference moves where a
 //       later tile's weights do not fit, as for the bf16 cache.
@@ -22,11 +22,15 @@
 // either (in_turns): the kernel would else be 193 KB of code, of which an SM's instruction cache holds a part (now 81 KB; the same 16 trees of 29: 93 -> 73 us).
 // Sixteen scores of a row are in registers at a time, the next on their way: with all 64 the 80 registers of 768 threads spill (long context 97 -> 85 us).
 //
-// Measured, whole calls: one tree of 64 nodes, 32 / 8 heads of 128, 60001 keys (63 GFLOP): 81 us; 8 sequences of 64 nodes, 16384 shared keys and up to 2048 of
-// their own (147 GFLOP): 168 us, the tensor pipe at 49 % beside the joining.  A pair of key tiles takes 3.8 k cycles of the 2.06 k that its products need: the
-// chain scores -> weights (2.0 k) -> product of a row tile is hidden by the other row tile's alone.  Looked at and left: the warps of both row tiles on each in
-// turn (32 columns a thread: 299 us), halves of key tiles in turn (64 keys a product of scores, 189 us: the queries are read twice as often from shared memory,
-// which is what bounds those products), no turns between the issuing warps (192), more and fewer polynomials (178, 166 against 154 in one comparison).
+// Measured, whole calls: one tree of 64 nodes, 32 / 8 heads of 128, 60001 keys (63 GFLOP): 78 us; 8 sequences of 64 nodes, 16384 shared keys and up to 2048 of
+// their own (147 GFLOP): 153 us, the tensor pipe at 57 % beside the joining.  A pair of key tiles takes 3.2 k cycles of the 2.06 k that its products need: the
+// chain scores -> weights (1.9 k) -> product (1.3 k from the last weight to the next scores) of a row tile is hidden by the other row tile's alone.
+// Looked at and left (us, or the kernel's cycles, of the latter case): the warps of both row tiles on each in turn (32 columns a thread: 299 us where 64 took
+// 171); halves of key tiles in turn (64 keys a product of scores, 189 us: the queries are read twice as often from shared memory, which is what bounds those
+// products); no turns between the issuing warps (192 us); turns passed in the middle of the other tile's softmax (cycles + 15 %); fewer polynomials (+ 4 %),
+// more (+ 9 %), other places for them (+ 4 %); waits that poll without suspending (+ 5 %: the issue slots they take are the softmax's); products in loops
+// (159 us for 143); weights stored as they come, and the scores computed once more where a weight does not fit, in place of the vote (+ 7 %: the issuing warps
+// have more to look at between the weights and the products).
 #include <limits.h>
 
 #include "fp8.cuh"
@@ -541,7 +545,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
                 auto k_there = [&]() { return wait(P8_KFULL + k_at, k_parity) && (kt != ks.t0 || wait(P8_QREADY + s, n_q++ & 1)); };
                 // Pairs take turns: the products of a row tile go to the tensor core in one run.  Mixed with the other tile's, both tiles' scores
-                // would come when all are done, both softmaxes would then run at once, and the tensor core wait for both.
+                // would come when all are done, both softmaxes would then run at once, and the tensor core wait for both.  (Passed on when the run's products are
+                // complete: 1 % fewer cycles than when they are issued.)
                 auto begin_run = [&]() {
                     if (!pairs) return true;
                     const int turn = n_turn++;
@@ -550,8 +555,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 auto end_run = [&]() {
                     if (pairs) ptx::tc_commit_elect(bar(P8_TURN + (s ^ 1)), leader);
                 };
-                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be), the turn too: a wait in
-                // vain costs this warp 400 cycles among the others' (16k document 150 -> 143 us, long context 73.2 -> 69.4 with the turn waited for in front)
+                // the weights are waited for last: what else there is to wait for is there by then (a new piece's queries may not be), the turn too: a wait
+                // for what is there took this warp 400 cycles among the others (16k document 150 us with the turn waited for last, 143 so; long context 73.2, 69.4)
                 const bool ahead = v && k && kt != ks.t0;
                 if (ahead && !k_there()) return false;
                 if (v) {
@@ -844,8 +849,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // STAGES - 1 blocks ahead: no warp waits for another, and no register holds what is on its way.  At a piece's end the warps join.
 // An instruction of copies covers whole rows: where it took half a row of each of 8 keys (as the operands have them), the other half crossed from L2 with it, twice
 // in all (64 single tokens: 88 us so, 71 now).
-// Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 53.6 us = 5.2 TB/s, 79 % of the copy rate (61 us with the joining); one token
-// of 60001 keys 31 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces' starts and ends.
+// Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 53 us = 5.2 TB/s, 79 % of the copy rate (60 us with the joining); one token
+// of 60001 keys 30 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces' starts and ends.
 constexpr float T8_SHIFT = 7.f, T8_SLACK = 8.f;   // weights are 2^SHIFT at the reference, which may be SLACK too small: below 2^16
 
 // NR: products of 8 query rows.
@@ -893,7 +898,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
     __shared__ float2 ml_x[WARPS][8 * NR];
     __shared__ int start[5];               // x0, x1, S, b, idx
     let_next_start();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r0 = lane / 4, quad = lane % 4;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, r0 = lane / 4, quad = lane % 4;
     const PaPhase &ph = p.phase[2];
     const int worker = blockIdx.x, workers = gridDim.x;
     // this warp's stages: rows of K, then of V
