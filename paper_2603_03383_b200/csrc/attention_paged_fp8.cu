@@ -34,6 +34,7 @@
 #include <limits.h>
 
 #include "fp8.cuh"
+#include "in_step.cuh"
 #include "paged_attn.cuh"
 
 namespace mtv {
@@ -302,7 +303,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     };
     // whether the CTA has pairs of row tiles, or single ones
     auto is_pairs = [&]() { return wait(P8_ROLE, 0) && *role; };
-    // the n-th piece of a queue; none (or nothing to be had): false
+    // the n-th piece of a queue (without tiles: there are no more); nothing to be had: false
     auto piece_at = [&](int q, int n) {
         const int at = q * PA_QUEUE + n % PA_QUEUE;
         const int4 a = queue[at * 2], c = queue[at * 2 + 1];
@@ -313,7 +314,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     auto look = [&](int q, int n, PaPiece &s) {
         if (__any_sync(0xffffffffu, *abort_flag) || !wait(P8_PIECE + q * PA_QUEUE + n % PA_QUEUE, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
         s = piece_at(q, n);
-        return s.t1 > 0;
+        return true;
     };
     auto taken = [&](int q, int n) {       // its place may be given to another
         __syncwarp();
@@ -321,7 +322,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         __syncwarp();
     };
     auto take = [&](int q, int n, PaPiece &s) {
-        const bool any = look(q, n, s);
+        const bool any = look(q, n, s) && s.t1 > 0;
         taken(q, n);
         return any;
     };
@@ -599,7 +600,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const uint32_t t_o = lane_base + 256 + s * D + hf * (D / 2);
         const int pair_bar = 2 + s * 4 + qd;
         const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
-        const bool pairs = is_pairs();
+        const bool there = wait(P8_ROLE, 0), pairs = there && *role;
         const PaPhase &ph = p.phase[pairs ? 0 : 1];
         const int q = pairs ? 0 : s;
         // what the other thread of the row has (two barriers: what was exchanged before has been read)
@@ -616,18 +617,19 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         float m = 0.f, l = 0.f, vs = 0.f;  // the piece's: reference, sum, scale of V
         bool mine = false;
         int node = -1;                     // the row's, if it sees some of the tree's rows; -1: none, or no row
-        bool ok = true, more = true;
-#pragma unroll 1
-        for (int n = 0; ok && more; ++n) {
-            PaPiece pc;
-            more = look(q, n, pc);
+        PaPiece pc = {};
+        int left_at = 0;                   // the key tile in which a wait ran out; -1: in front of the exchange of the queries' maxima
+        auto is_mine = [&]() { return node_in_tile < p.npc && node_of(pc) < (pc.b < 0 ? p.B * p.T : p.T); };
+        if (!there) all_of_rows(pair_bar, false);
+        else pieces_in_step([&](int n) { return look(q, n, pc); }, [&](bool x) { return all_of_rows(pair_bar, x); }, [&](int n) {
+            const bool more = pc.t1 > 0;
             float sc = 0.f, vs_next = 0.f;
             if (more) {
                 // ---- the piece's queries in two terms, where they are: each thread of a row takes half of its columns.  Their first product then runs beside
                 // the end of the piece before.
                 const float ks = __ldg(pp.k_scale + pc.g);
                 vs_next = __ldg(pp.v_scale + pc.g);
-                if (!wait(P8_QFULL + s, n & 1)) { ok = false; break; }
+                if (!wait(P8_QFULL + s, n & 1)) { left_at = -1; return Way::LEFT; }
                 constexpr int CHUNKS = D / 16;
                 unsigned char *at = gbase + s * SM::TILE + (D == 128 ? hf * SM::HALF : 0) + row * 128;
                 auto chunk = [&](int c) { return reinterpret_cast<uint4 *>(at + (((D == 128 ? 0 : hf * CHUNKS) + c ^ (row & 7)) << 4)); };
@@ -661,7 +663,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }
             if (n) {
                 // ---- the piece before
-                if (!wait(P8_ODONE + s, (n - 1) & 1)) { ok = false; break; }
+                if (!wait(P8_ODONE + s, (n - 1) & 1)) { left_at = pc.t0; return more ? Way::LEFT : Way::END; }
                 ptx::tc_fence_after();
                 const PaPiece old = piece_at(q, n - 1);
                 if (__any_sync(0xffffffffu, mine)) {
@@ -708,8 +710,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
                 if (!pairs || s) taken(q, n - 1);                  // (in a pair the second row tile's warps: its place is not used again before the next but two's scores, both tiles')
             }
-            if (!more) break;
-            mine = node_in_tile < p.npc && node_of(pc) < (pc.b < 0 ? p.B * p.T : p.T);
+            if (!more) return Way::END;
+            mine = is_mine();
             node = mine && pc.b >= 0 ? node_of(pc) : -1;
             m = -INFINITY;
             l = 0.f;
@@ -718,7 +720,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const float2 sc2 = make_float2(sc, sc);
 #pragma unroll 1
             for (int t = pc.t0; t < pc.t1; ++t) {
-                if (!wait(P8_SREADY + s, n_s++ & 1)) { ok = false; break; }
+                if (!wait(P8_SREADY + s, n_s++ & 1)) { left_at = t; return Way::LEFT; }
                 ptx::tc_fence_after();
                 if (some) {
                     uint32_t a[16], b[16], pk[32];                 // (pk: fp16 pairs)
@@ -742,7 +744,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         ptx::tmem_st_wait();
                         ptx::tmem_ld16(t_s, a);
                     }
-                    bool move = __any_sync(0xffffffffu, mine && m == -INFINITY);      // (the piece's first tile, or no key was visible so far)
+                    bool move = t == pc.t0;
                     float sum;
                     for (;;) {
                         if (move) {
@@ -813,8 +815,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         weights(3, b);
                         sum = (la.x + la.y) + (lb.x + lb.y);
                         if (move) break;
-                        // a sum that is too large, infinite or NaN: a weight then may be beyond fp16
-                        if (!any_of_rows(pair_bar, mine && (!(sum < 65504.f) || !(px <= P8_LIMIT)))) break;
+                        // a sum that is too large, infinite or NaN: a weight then may be beyond fp16; and a row that has met no visible key so far
+                        if (!any_of_rows(pair_bar, mine && (!(sum < 65504.f) || !(px <= P8_LIMIT) || m == -INFINITY))) break;
                         move = true;
                         ptx::tmem_ld16(t_s, a);
                     }
@@ -827,7 +829,15 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar(P8_PREADY + s));
             }
-        }
+            return Way::ON;
+        }, [&]() {
+            if (left_at < 0) {
+                exchange(0.f);
+                left_at = pc.t0;
+            }
+            if (__any_sync(0xffffffffu, is_mine()))
+                follow_tiles(left_at, pc.t0, pc.t1, [&]() { return any_of_rows(pair_bar, false); }, [&]() { exchange(0.f); }, [&]() { exchange(0.f); });
+        });
     }
     // ---- nobody leaves while the tensor core may still work for the CTA
     __syncwarp();

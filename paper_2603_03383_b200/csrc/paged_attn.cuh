@@ -230,6 +230,19 @@ __device__ __forceinline__ bool any_of_rows(int barrier, bool mine) {
         : "=r"(r) : "r"((uint32_t)mine), "r"(barrier) : "memory");
     return r != 0;
 }
+// ... whether all of them do.
+__device__ __forceinline__ bool all_of_rows(int barrier, bool mine) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "barrier.cta.red.and.pred q, %2, 64, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r) : "r"((uint32_t)mine), "r"(barrier) : "memory");
+    return r != 0;
+}
 __device__ __forceinline__ void tmem_put(uint32_t taddr, float v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
 }
