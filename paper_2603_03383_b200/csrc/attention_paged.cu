@@ -35,6 +35,7 @@
 // products need; the rest is the chain scores -> exponentials -> weights -> product of each row tile, which its one other row tile does not hide.
 // 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 33 to 37 us for 6.4 us of bytes; start, first tile and joining are two thirds of it.
 // All 20 warps have 96 registers; the softmax warps spill (160 bytes stored, 204 loaded a thread at D = 128, 144 and 244 at D = 64).
+#include "in_step.cuh"
 #include "paged_attn.cuh"
 
 namespace mtv {
@@ -94,7 +95,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     constexpr int X_COL = TWO ? 16 : 40;
     extern __shared__ unsigned char smem_raw[];
     let_next_start();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    // (the shuffle tells the compiler that a warp's number is the same for its lanes)
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u, sbase = raw + pad;
     unsigned char *gbase = smem_raw + pad;
     const uint32_t bars = sbase + SM::OFF_BAR;
@@ -152,7 +154,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         if (lane == 0) give_up();
         return false;
     };
-    // the n-th piece of a queue; none (or nothing to be had): false
+    // the n-th piece of a queue (without tiles: there are no more); nothing to be had: false
     auto take = [&](int q, int n, PaPiece &s) {
         const int at = q * PA_QUEUE + n % PA_QUEUE;
         if (__any_sync(0xffffffffu, *abort_flag) || !wait(PB_PIECE + at, (n / PA_QUEUE) & 1)) { s.t0 = s.t1 = 0; return false; }
@@ -161,7 +163,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(PB_TAKEN + at));
         __syncwarp();
-        return s.t1 > 0;
+        return true;
     };
 
     if (warp == PA_TMA_WARP) {
@@ -257,7 +259,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
             int n[NL] = {};
-            return for_rounds<NL>([&](int l, PaPiece &x) { return take(NL == 1 ? 0 : 1 + l, n[l]++, x); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            return for_rounds<NL>([&](int l, PaPiece &x) { return take(NL == 1 ? 0 : 1 + l, n[l]++, x) && x.t1 > 0; }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 const int ve = entry, ke = entry + (v ? 1 : 0);
                 entry = ke + (k ? 1 : 0);
                 const int v_stage = ve % SM::STAGES, k_stage = ke % SM::STAGES;
@@ -338,7 +340,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         auto phase = [&](auto lists) {
             constexpr int NL = decltype(lists)::value;
             int n[NL] = {};
-            return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s); }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
+            return for_rounds<NL>([&](int l, PaPiece &s) { return take(NL == 1 ? 0 : 1 + l, n[l]++, s) && s.t1 > 0; }, [&](int l, bool v, const PaPiece &vs, int vt, bool k, const PaPiece &ks, int kt) {
                 // Every entry is waited for, and handed back by this warp too (as above).
                 auto landed = [&]() { return wait(PB_FULL + stage, turns & 1); };
                 auto pass = [&]() {
@@ -402,21 +404,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         const int node_in_tile = row / p.G, head = row - node_in_tile * p.G;
         const bool in_tile = node_in_tile < p.npc;
         const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
+        auto pair_sync = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory"); };
         // what the other half of the row has: both put theirs where nothing is any more
         auto exchange = [&](int col, float v) {
             tmem_put(t_s + col, v);
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
-            asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            pair_sync();
             ptx::tc_fence_after();
             return tmem_get(t_x + col);
         };
-        int n_s = 0, n_piece = 0;
-        bool ok = true;
-        for (int f = 0; f < 2 && ok; ++f) {
+        int n_s = 0, n_piece = 0, left_at = 0;       // left_at: the key tile in which a wait ran out
+        bool more = true;
+        for (int f = 0; f < 2 && more; ++f) {
             const PaPhase &ph = p.phase[f];
-            PaPiece pc;
-            for (int n = 0; ok && take(f ? 1 + s : 0, n, pc); ++n) {
+            PaPiece pc = {};
+            more = pieces_in_step([&](int n) { return take(f ? 1 + s : 0, n, pc); }, [&](bool x) { return all_of_rows(pair_bar, x); }, [&](int) {
+                if (pc.t1 == 0) return Way::END;
                 const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
                 const bool mine = in_tile && node < (pc.b < 0 ? p.B * p.T : p.T);
                 const bool some = __any_sync(0xffffffffu, mine);
@@ -426,7 +430,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                 auto anc_word = [&](int w) -> uint32_t { return w < 0 ? 0xffffffffu : w == 0 ? anc.x : w == 1 ? anc.y : w == 2 ? anc.z : w == 3 ? anc.w : 0u; };
                 float m_used = -INFINITY, l = 0.f;
                 for (int t = pc.t0; t < pc.t1; ++t) {
-                    if (!wait(PB_SREADY + s, n_s++ & 1)) { ok = false; break; }
+                    if (!wait(PB_SREADY + s, n_s++ & 1)) { left_at = t; return Way::LEFT; }
                     ptx::tc_fence_after();
                     if (some) {
                         uint32_t pk[32], rest[TWO ? 32 : 1];     // bf16 pairs; what their rounding left
@@ -513,7 +517,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                         if constexpr (TWO) {
                             if (last) l += exchange(X_COL + 1, l);      // the row's sum
                             // (second terms go over what was exchanged when the other half has read it)
-                            if (move || last) asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory");
+                            if (move || last) pair_sync();
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 ptx::tmem_st16(t_s + h * 32, *reinterpret_cast<uint32_t(*)[16]>(&pk[h * 16]));
@@ -529,7 +533,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(bar(PB_PREADY + s));
                 }
-                if (!ok || !wait(PB_ODONE + s, n_piece & 1)) { ok = false; break; }
+                if (!wait(PB_ODONE + s, n_piece & 1)) { left_at = pc.t1; return Way::LEFT; }
                 ptx::tc_fence_after();
                 if (some) {
                     const bool odd = bad[s * 4 + (n_piece & 3)] == n_piece + 1;
@@ -570,7 +574,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
                     if (mine && !direct && hf == 0) ph.ml[(size_t)pc.slot * ph.rows + slot_row] = make_float2(l == 0.f ? -INFINITY : m_used, l);
                 }
                 ++n_piece;
-            }
+                return Way::ON;
+            }, [&]() {
+                const int node = (pc.tile0 + (f ? 0 : s)) * p.npc + node_in_tile;
+                if (__any_sync(0xffffffffu, in_tile && node < (pc.b < 0 ? p.B * p.T : p.T)))
+                    follow_tiles(left_at, pc.t0, pc.t1, [&]() { return any_of_rows(pair_bar, false); }, [&](bool last) {
+                        pair_sync();
+                        if (TWO && !last) pair_sync();
+                    }, [&]() {
+                        pair_sync();
+                        if (TWO) pair_sync();
+                    });
+            });
         }
     }
     // ---- nobody leaves while the tensor core may still work for the CTA

@@ -836,7 +836,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 left_at = pc.t0;
             }
             if (__any_sync(0xffffffffu, is_mine()))
-                follow_tiles(left_at, pc.t0, pc.t1, [&]() { return any_of_rows(pair_bar, false); }, [&]() { exchange(0.f); }, [&]() { exchange(0.f); });
+                follow_tiles(left_at, pc.t0, pc.t1, [&]() { return any_of_rows(pair_bar, false); }, [&](bool) { exchange(0.f); }, [&]() { exchange(0.f); });
         });
     }
     // ---- nobody leaves while the tensor core may still work for the CTA

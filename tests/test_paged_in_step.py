@@ -61,8 +61,9 @@ struct Warp {
 
 static float shared_value[2];
 
-// Pieces of `tiles` tiles each, as the softmax warps of the attention over pages go through them.  carried: the end of a piece behind the next one's queries.
-static void walk(Warp &w, int n_pieces, int tiles, bool carried, bool sees_flag) {
+// Pieces of `tiles` tiles each, as the softmax warps of the attention over pages go through them.  Of codes (carried): the end of a piece is behind the next one's
+// queries, and an exchange meets twice.  Of bf16: it meets once, and once more in front of a tile's second terms, where there are such.
+static void walk(Warp &w, int n_pieces, int tiles, bool carried, bool two, bool sees_flag) {
     using namespace mtv;
     const float none = -1e30f;
     float m = none;
@@ -71,11 +72,12 @@ static void walk(Warp &w, int n_pieces, int tiles, bool carried, bool sees_flag)
         shared_value[w.id] = x;
         w.m->meet(true);
         const float other = shared_value[w.id ^ 1];
-        w.m->meet(true);
+        if (carried) w.m->meet(true);
         return other;
     };
     // what the two halves of a row have in a tile: nothing in some, more and more in others
     auto own = [&](int n, int t) { return (n + t + w.id) % 3 == 0 ? none : (float)(t * (n % 2 ? 5 : 1) + w.id); };
+    auto other_half = [&](int n, int t) { return (n + t + (w.id ^ 1)) % 3 == 0 ? none : (float)(t * (n % 2 ? 5 : 1) + (w.id ^ 1)); };
     auto asked = [&](bool ask) { return !w.m->meet(!ask); };
     pieces_in_step([&](int) { return !(sees_flag && *w.flag) && w.wait(); }, [&](bool x) { return w.m->meet(x); }, [&](int n) {
         const bool more = n < n_pieces;
@@ -91,16 +93,19 @@ static void walk(Warp &w, int n_pieces, int tiles, bool carried, bool sees_flag)
         m = none;
         for (int t = 0; t < tiles; ++t) {
             if (!w.wait()) { left_at = t; return Way::LEFT; }
-            for (bool move = t == 0;;) {
+            bool move = t == 0;
+            for (;;) {
                 if (move) {
                     const float x = own(n, t);
-                    m = std::max(m, std::max(x, exchange(x)));
+                    exchange(x);
+                    m = std::max(m, std::max(own(n, t), other_half(n, t)));
                     break;
                 }
                 if (!asked(m == none || own(n, t) > m + 3.f)) break;
                 move = true;
             }
             if (t == tiles - 1) exchange(1.f);
+            if (two && (move || t == tiles - 1)) w.m->meet(true);
         }
         if (!carried && !w.wait()) { left_at = tiles; return Way::LEFT; }
         return Way::ON;
@@ -109,7 +114,13 @@ static void walk(Warp &w, int n_pieces, int tiles, bool carried, bool sees_flag)
             exchange(0.f);
             left_at = 0;
         }
-        follow_tiles(left_at, 0, tiles, [&] { return asked(false); }, [&] { exchange(none); }, [&] { exchange(1.f); });
+        follow_tiles(left_at, 0, tiles, [&] { return asked(false); }, [&](bool last) {
+            exchange(none);
+            if (two && !last) w.m->meet(true);
+        }, [&] {
+            exchange(1.f);
+            if (two) w.m->meet(true);
+        });
     });
 }
 
@@ -122,15 +133,15 @@ static void walk_alone(Warp &w, int n_pieces, int tiles) {
         }
 }
 
-extern "C" int run(int fails0, int fails1, int sees, int n_pieces, int tiles, int carried, int alone, int limit_ms, int *out) {
+extern "C" int run(int fails0, int fails1, int sees, int n_pieces, int tiles, int kind, int alone, int limit_ms, int *out) {
     Meeting m;
     std::atomic<bool> flag(false);
     m.limit_ms = limit_ms;
     // (one flag of both, or each sees its own alone: a flag may be set behind the other's look)
     std::atomic<bool> flags[2] = {{false}, {false}};
     Warp w[2] = {{&m, fails0, 0, sees >> 2 ? &flag : &flags[0]}, {&m, fails1, 1, sees >> 2 ? &flag : &flags[1]}};
-    std::thread t0([&] { alone ? walk_alone(w[0], n_pieces, tiles) : walk(w[0], n_pieces, tiles, carried, sees & 1); });
-    std::thread t1([&] { alone ? walk_alone(w[1], n_pieces, tiles) : walk(w[1], n_pieces, tiles, carried, sees >> 1 & 1); });
+    std::thread t0([&] { alone ? walk_alone(w[0], n_pieces, tiles) : walk(w[0], n_pieces, tiles, kind == 1, kind == 2, sees & 1); });
+    std::thread t1([&] { alone ? walk_alone(w[1], n_pieces, tiles) : walk(w[1], n_pieces, tiles, kind == 1, kind == 2, sees >> 1 & 1); });
     t0.join();
     t1.join();
     for (int i = 0; i < 2; ++i) {
@@ -150,21 +161,21 @@ def run(tmp_path_factory):
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-fPIC", "-shared", "-pthread", "-I", CSRC, "-o", str(lib), str(src)])
     L = C.CDLL(str(lib))
 
-    def call(fails0, fails1, sees=3, pieces=3, tiles=3, carried=1, alone=0, limit_ms=20000):
+    def call(fails0, fails1, sees=3, pieces=3, tiles=3, kind=1, alone=0, limit_ms=20000):
         out = (C.c_int * 4)()
-        return L.run(fails0, fails1, sees, pieces, tiles, carried, alone, limit_ms, out), list(out)
+        return L.run(fails0, fails1, sees, pieces, tiles, kind, alone, limit_ms, out), list(out)
     return call
 
 
-@pytest.mark.parametrize("carried", [0, 1])
+@pytest.mark.parametrize("kind", [0, 1, 2])
 @pytest.mark.parametrize("sees", [0, 3, 5, 7])
 @pytest.mark.parametrize("tiles", [1, 4])
-def test_waits_that_run_out(run, tiles, sees, carried):
-    met, (pieces, waits, *other) = run(-1, -1, sees, tiles=tiles, carried=carried)
+def test_waits_that_run_out(run, tiles, sees, kind):
+    met, (pieces, waits, *other) = run(-1, -1, sees, tiles=tiles, kind=kind)
     assert met > 0 and pieces == 3 and other == [pieces, waits]
     for fails0 in range(-1, waits):
         for fails1 in range(-1, waits):
-            met, (pieces0, waits0, pieces1, waits1) = run(fails0, fails1, sees, tiles=tiles, carried=carried)
+            met, (pieces0, waits0, pieces1, waits1) = run(fails0, fails1, sees, tiles=tiles, kind=kind)
             assert met >= 1, (fails0, fails1)                              # (-1: one stands at a barrier; -2: one stood there at the end)
             assert abs(pieces0 - pieces1) <= 1 and waits0 <= waits and waits1 <= waits
             assert fails0 < 0 or waits0 <= fails0 + 1, (fails0, fails1)    # nothing is waited for behind a wait that ran out
@@ -175,7 +186,7 @@ def test_a_warp_that_leaves_alone_is_noticed(run):
     assert run(4, -1, alone=1, limit_ms=200)[0] == -1
 
 
-@pytest.mark.parametrize("name", ["attention_paged_fp8.cu"])
+@pytest.mark.parametrize("name", ["attention_paged.cu", "attention_paged_fp8.cu"])
 def test_the_kernels_go_this_way(name):
     """No way out of the softmax warps' part but the common one, in front of which they meet."""
     text = open(os.path.join(CSRC, name)).read()
