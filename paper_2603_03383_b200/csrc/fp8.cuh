@@ -11,9 +11,6 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint2 e4m3x8(const float (&x)[8]) {
-    return make_uint2(e4m3x2(x[0], x[1]) | e4m3x2(x[2], x[3]) << 16, e4m3x2(x[4], x[5]) | e4m3x2(x[6], x[7]) << 16);
-}
 // Every code is a number of fp16.  Codes in the lower or upper half of a word.
 __device__ __forceinline__ uint32_t f16x2_lo(uint32_t codes) {
     uint32_t r;

@@ -14,15 +14,6 @@ constexpr int APPEND_DEEP = 1;       // pairs of 16-byte chunks that a thread as
 constexpr int PAGED_MAX_HEADS = 4096;
 constexpr int APPEND_ROWS = 2;       // rows of a block
 
-__device__ __forceinline__ void unpack8(const uint4 &u, float (&x)[8]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        x[2 * k] = __uint_as_float(w[k] << 16);
-        x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-    }
-}
-
 // (x[d], x[d + D/2]) -> (x[d] cos - x[d + D/2] sin, x[d + D/2] cos + x[d] sin) for 8 columns, in fp32, rounded once to bf16
 __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float *cs, const float *sn) {
     uint32_t *wa = reinterpret_cast<uint32_t *>(&a), *wb = reinterpret_cast<uint32_t *>(&b);
@@ -38,19 +29,31 @@ __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float *cs, con
     }
 }
 
-// The same times `factor`, rounded once to codes; cs null: nothing is rotated.
-__device__ __forceinline__ void quantise8(const uint4 &a, const uint4 &b, const float *cs, const float *sn, float factor, uint2 &ca, uint2 &cb) {
-    float x[8], y[8];
-    unpack8(a, x);
-    unpack8(b, y);
+// The same over `scale`, rounded once to codes; cs null: nothing is rotated.
+__device__ __forceinline__ void quantise8(const uint4 &a, const uint4 &b, const float *cs, const float *sn, float scale, uint2 &ca, uint2 &cb) {
+    // (1 / scale is infinite in fp32 up to 2^-128, and 0 times it would be NaN: with a subnormal scale both are taken 2^64 larger)
+    const bool tiny = scale < 0x1p-126f;
+    const float factor = __frcp_rn(tiny ? scale * 0x1p64f : scale);
+    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+    uint32_t pa[4], pb[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float c = cs ? cs[k] : 1.f, s = cs ? sn[k] : 0.f, x0 = x[k], y0 = y[k];
-        x[k] = (cs ? x0 * c - y0 * s : x0) * factor;
-        y[k] = (cs ? y0 * c + x0 * s : y0) * factor;
+    for (int k = 0; k < 4; ++k) {
+        float x0 = __uint_as_float(wa[k] << 16), x1 = __uint_as_float(wa[k] & 0xffff0000u);
+        float y0 = __uint_as_float(wb[k] << 16), y1 = __uint_as_float(wb[k] & 0xffff0000u);
+        if (cs) {
+            const float2 c = *reinterpret_cast<const float2 *>(cs + 2 * k), s = *reinterpret_cast<const float2 *>(sn + 2 * k);
+            const float u0 = fmaf(x0, c.x, -__fmul_rn(y0, s.x)), u1 = fmaf(x1, c.y, -__fmul_rn(y1, s.y));
+            y0 = fmaf(x0, s.x, __fmul_rn(y0, c.x));
+            y1 = fmaf(x1, s.y, __fmul_rn(y1, c.y));
+            x0 = u0;
+            x1 = u1;
+        }
+        if (tiny) { x0 *= 0x1p64f; x1 *= 0x1p64f; y0 *= 0x1p64f; y1 *= 0x1p64f; }
+        pa[k] = e4m3x2(x0 * factor, x1 * factor);
+        pb[k] = e4m3x2(y0 * factor, y1 * factor);
     }
-    ca = e4m3x8(x);
-    cb = e4m3x8(y);
+    ca = make_uint2(pa[0] | pa[1] << 16, pa[2] | pa[3] << 16);
+    cb = make_uint2(pb[0] | pb[1] << 16, pb[2] | pb[3] << 16);
 }
 
 struct AppendParams {
@@ -198,9 +201,8 @@ kv_append_rope_paged_kernel(const AppendParams p) {
                 void *pool = (is_v ? p.v_pools : p.k_pools)[layer];
                 if constexpr (FP8) {
                     uint2 a, b;
-                    const float factor = __frcp_rn(scale[k]);
-                    if (is_v) quantise8(x[k][0], x[k][1], nullptr, nullptr, factor, a, b);
-                    else quantise8(x[k][0], x[k][1], &cs[j][c], &sn[j][c], factor, a, b);
+                    if (is_v) quantise8(x[k][0], x[k][1], nullptr, nullptr, scale[k], a, b);
+                    else quantise8(x[k][0], x[k][1], &cs[j][c], &sn[j][c], scale[k], a, b);
                     *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + at + c) = a;
                     *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + at + HALF + c) = b;
                     continue;
