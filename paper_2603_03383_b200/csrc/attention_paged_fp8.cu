@@ -31,6 +31,7 @@
 // more (+ 9 %), other places for them (+ 4 %); waits that poll without suspending (+ 5 %: the issue slots they take are the softmax's); products in loops
 // (159 us for 143); weights stored as they come, and the scores computed once more where a weight does not fit, in place of the vote (+ 7 %: the issuing warps
 // have more to look at between the weights and the products).
+#include <float.h>
 #include <limits.h>
 
 #include "fp8.cuh"
@@ -98,8 +99,12 @@ template <int TO> __device__ __forceinline__ float2 row_factor(uint32_t largest)
     const int k = min(127 + TO - e, 126);
     return make_float2(__int_as_float((127 + k) << 23), __int_as_float((127 - k) << 23));
 }
-// (A factor that is too small for fp32 is not 0: a hidden score times it is to stay -inf.)
-__device__ __forceinline__ float scores_factor(float f) { return f == 0.f ? __int_as_float(1) : f; }
+// The factor of a row's scores.  The product of the two scales alone may be beyond fp32 on either side (back, the reciprocal of the row's, spans 2^246); a factor that
+// is too small for fp32 is not 0, as a hidden score times it is to stay -inf, nor is one that is too large infinite, as 0 times it is to stay 0.
+__device__ __forceinline__ float scores_factor(float scale, float k_scale, float back) {
+    const float f = (float)((double)scale * k_scale * back);
+    return fminf(fmaxf(f, __int_as_float(1)), FLT_MAX);
+}
 __device__ __forceinline__ uint32_t larger_bits(uint32_t m, uint32_t pair) { return max(m, max(pair << 16, pair & 0xffff0000u)); }
 __device__ __forceinline__ uint32_t abs2_bf16(uint32_t pair) { return pair & 0x7fff7fffu; }
 __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor) {
@@ -656,7 +661,7 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     *chunk(c + 2) = make_uint4(second[0], second[1], second[2], second[3]);
                     *chunk(c + 3) = make_uint4(second[4], second[5], second[6], second[7]);
                 }
-                sc = scores_factor(p.scale_log2 * ks * factor.y);
+                sc = scores_factor(p.scale_log2, ks, factor.y);
                 ptx::fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar(P8_QREADY + s));
@@ -1014,7 +1019,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                     qb[nr][c][i][0] = to_f16(qb[nr][c][i][0], factor.x);
                     qb[nr][c][i][1] = to_f16(qb[nr][c][i][1], factor.x);
                 }
-            const float of_row = scores_factor(p.scale_log2 * __ldg(pp.k_scale + g) * factor.y);
+            const float of_row = scores_factor(p.scale_log2, __ldg(pp.k_scale + g), factor.y);
             const uint32_t seen = is && own ? (uint32_t)p.anc[n * 2] : 0u;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {

@@ -7,6 +7,8 @@ import torch
 
 from paper_2603_03383_b200 import binding
 from tests import _fp8
+from tests._cases import make_tree
+from tests._paged import table
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -66,3 +68,48 @@ def test_codes(scale, D, whole_tree):
         ok = (c - y).abs() <= step / 2 + 2.0 ** -20 * y.abs()
         assert (ok | torch.isnan(y)).all(), (x[:first][~ok & ~torch.isnan(y)][:4], c[~ok & ~torch.isnan(y)][:4])
     assert not torch.isnan(kc).any()
+
+
+def attend(tree, q, kp, vp, ks, vs, t, lens, scale):
+    B, T, Hq, D = q.shape
+    ws = torch.full((binding.paged_workspace_bytes(tree, B, Hq, kp.shape[1], D),), 0xff, dtype=U8, device=DEV)
+    out = torch.full(q.shape, 7.0, dtype=BF16, device=DEV)
+    move = lambda p: p.view(U8).to(DEV).view(_fp8.FP8)  # noqa: E731
+    binding.tree_verify_attention_paged_fp8(tree, q.to(DEV), move(kp), move(vp), t.to(DEV), i32(lens), out, ws, ks.to(DEV), vs.to(DEV), scale=scale)
+    torch.cuda.synchronize()
+    assert binding.mtv_device_error(tree) == 0
+    return out.cpu().double()
+
+
+def bound(want, absolute):
+    """As for other scales: the output's rounding, weights in fp16 and their exponentials (in the weights and in their sum), fp32 sums."""
+    return 2.0 ** -8 * want.abs() + (1 + 2.0 ** -8) * (2.0 ** -11 + 2 * 7.5e-5 + 1e-4) * absolute
+
+
+@pytest.mark.parametrize("T,G", [(1, 4), (4, 4), (20, 3), (64, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("large", [False, True])
+def test_scores_whose_scales_have_no_product(D, T, G, large):
+    """scale * k_scale is below fp32's normal numbers, or beyond its largest; with the queries, which make up for it, the scores are ordinary."""
+    g = torch.Generator().manual_seed(6)
+    Hkv, page, lens = 2, 16, [300, 77]
+    tb, tree = (dict(mask=[[1]]), binding.tree_build_static(1, [])) if T == 1 else make_tree("rank_prior", 4, (), T)
+    t, n_pages = table(g, len(lens), max(lens) + T, page)
+    kp, vp = _fp8.pools(g, 2, n_pages, Hkv, page, D)
+    vs = torch.tensor([0.01, 0.02])
+    if large:
+        q = (torch.randn(2, T, Hkv * G, D, generator=g) * 2.0 ** -66).mul(2.0 ** -64).to(BF16)       # a few steps of the smallest bf16
+        kp = (kp.float() / 1600).to(_fp8.FP8)
+        ks, scale = torch.tensor([2.0 ** 110, 1.5 * 2.0 ** 110]), 2.0 ** 20
+    else:
+        # keys of +-448 along or against the queries; V has the sign of a key's score, so that a factor that is off shows at first order
+        sign = torch.where(torch.rand(n_pages, Hkv, page, 1, generator=g) < 0.5, -1.0, 1.0)
+        kp = (448.0 * sign).expand(n_pages, Hkv, page, D).contiguous().to(_fp8.FP8)
+        vp = (100.0 * sign).expand(n_pages, Hkv, page, D).contiguous().to(_fp8.FP8)
+        q = torch.full((2, T, Hkv * G, D), 1.9921875 * 2.0 ** 127).to(BF16)
+        ks, scale = torch.tensor([2.0 ** -100, 1.25 * 2.0 ** -100]), 1.0625 / 1.4426950408889634 * 2.0 ** -46
+    out = attend(tree, q, kp, vp, ks, vs, t, lens, scale)
+    want, absolute = _fp8.attention(q, kp, vp, ks, vs, t, lens, tb["mask"], scale)
+    assert want.isfinite().all()
+    worst = ((out - want).abs() / bound(want, absolute)).max().item()
+    assert worst <= 1.0, worst
