@@ -866,7 +866,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // in all (64 single tokens: 88 us so, 71 now).
 // Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 53 us = 5.2 TB/s, 79 % of the copy rate (60 us with the joining); one token
 // of 60001 keys 30 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces' starts and ends.
-constexpr float T8_SHIFT = 7.f, T8_SLACK = 8.f;   // weights are 2^SHIFT at the reference, which may be SLACK too small: below 2^16
+// Weights are 2^SHIFT at the reference, as in row tiles (so that as small ones count); it may be SLACK too small: they stay below 2^16, which fp16 ends at.
+constexpr float T8_SHIFT = 8.f, T8_SLACK = 7.9f;
 
 // NR: products of 8 query rows.
 template <int D, int NR> struct T8 {
