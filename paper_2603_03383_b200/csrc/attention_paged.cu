@@ -614,6 +614,14 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// 16 bytes of K or V.  Not by __ldg, which wants data that nobody writes as long as the kernel lives: this one starts beside the end of the one that appends.  (As a plain
+// load under a condition it is not requested ahead: 64 single tokens 124 us, 102 so.)
+__device__ __forceinline__ uint4 load_16(const void *p) {
+    uint4 u;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
+}
+
 template <int D>
 __global__ void __launch_bounds__(TH_WARPS * 32, 2)
 paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
@@ -694,7 +702,7 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int c = 0; c < C; ++c)
-                    kx[h][c] = at >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p.k + at + (r0 + 8 * h) * p.pages.stride_t + c * 32 + quad * 8)) : make_uint4(0u, 0u, 0u, 0u);
+                    kx[h][c] = at >= 0 ? load_16(p.k + at + (r0 + 8 * h) * p.pages.stride_t + c * 32 + quad * 8) : make_uint4(0u, 0u, 0u, 0u);
         };
         int id = page_of(t0), id_next = page_of(t0 + 1);
         long long at = row_at(t0, id);
@@ -711,7 +719,7 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
                 const bool is = at >= 0 && first + key < n_keys;     // rows behind the last key may hold anything
 #pragma unroll
                 for (int c = 0; c < J / 8; ++c) {
-                    const uint4 u = is ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 u = is ? load_16(src + c) : make_uint4(0u, 0u, 0u, 0u);
                     vx[k][c * 4] = u.x; vx[k][c * 4 + 1] = u.y; vx[k][c * 4 + 2] = u.z; vx[k][c * 4 + 3] = u.w;
                 }
             }

@@ -632,8 +632,8 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (more) {
                 // ---- the piece's queries in two terms, where they are: each thread of a row takes half of its columns.  Their first product then runs beside
                 // the end of the piece before.
-                const float ks = __ldg(pp.k_scale + pc.g);
-                vs_next = __ldg(pp.v_scale + pc.g);
+                const float ks = pp.k_scale[pc.g];
+                vs_next = pp.v_scale[pc.g];
                 if (!wait(P8_QFULL + s, n & 1)) { left_at = -1; return Way::LEFT; }
                 constexpr int CHUNKS = D / 16;
                 unsigned char *at = gbase + s * SM::TILE + (D == 128 ? hf * SM::HALF : 0) + row * 128;
@@ -1020,7 +1020,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                     qb[nr][c][i][0] = to_f16(qb[nr][c][i][0], factor.x);
                     qb[nr][c][i][1] = to_f16(qb[nr][c][i][1], factor.x);
                 }
-            const float of_row = scores_factor(p.scale_log2, __ldg(pp.k_scale + g), factor.y);
+            const float of_row = scores_factor(p.scale_log2, pp.k_scale[g], factor.y);
             const uint32_t seen = is && own ? (uint32_t)p.anc[n * 2] : 0u;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -1187,7 +1187,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
         __syncthreads();
         const bool direct = p.shared == 0 && t1 - t0 == steps;      // the item's only piece
         const size_t slot = (size_t)item + worker;
-        const float vs = __ldg(pp.v_scale + g);
+        const float vs = pp.v_scale[g];
 #pragma unroll 1
         for (int e = threadIdx.x; e < rows * (D / 8); e += WARPS * 32) {
             const int row = e % rows, chunk = e / rows;

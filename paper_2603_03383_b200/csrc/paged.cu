@@ -406,7 +406,7 @@ kv_read_paged_kernel(const ReadParams p) {
             const int l = l0 + row / (2 * READ_ROWS), v = row / READ_ROWS & 1, j = row % READ_ROWS, g = in_row / PER_HEAD, c = in_row % PER_HEAD * 16;
             dst[k] = nullptr;
             if (row < end && src_of[j] >= 0) {
-                x[k] = __ldg(reinterpret_cast<const uint4 *>((v ? p.v_pools : p.k_pools)[l] + src_of[j] + g * p.pages.stride_h + c));
+                x[k] = *reinterpret_cast<const uint4 *>((v ? p.v_pools : p.k_pools)[l] + src_of[j] + g * p.pages.stride_h + c);
                 scale[k] = (v ? p.v_scale : p.k_scale)[l * p.Hkv + g];
                 dst[k] = (v ? p.v_out : p.k_out) + (((size_t)l * p.n_rows + r0 + j) * p.Hkv + g) * D + c;
             }
