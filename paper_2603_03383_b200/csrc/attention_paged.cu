@@ -884,7 +884,7 @@ struct PaSum {
 };
 
 template <int D, int SPLIT>
-__global__ void __launch_bounds__(256, SPLIT == 1 ? 4 : 1)
+__global__ void __launch_bounds__(256, 4)
 paged_attn_combine_kernel(const __grid_constant__ PaParams p) {
     constexpr int CHUNKS = D / 8, ROWS = 256 / (CHUNKS * SPLIT);
     __shared__ PaSource src[2][ROWS];
