@@ -478,6 +478,7 @@ int tree_verify_attention_paged(const mtv_tree_t *tree, int B, int Hq, int Hkv, 
  *                  counted in elements, which are bytes here: multiples of 16 and at least D
  *   k_scale, v_scale   device fp32 [n_layers][Hkv] (the attention takes one layer's [Hkv]), positive and finite: a code c of head g stands for
  *                  c * scale[g].  Scales of a head that differ from call to call give rows that stand for other values: keep them with the cache.
+ *                  The attention holds v_scale times sums of weights and codes in fp32: v_scale from 2^-64 to 2^64 there.
  *   a value x is stored as the code nearest to x * (1 / scale) (in fp32; ties to the even code; for a scale below 2^-126, whose reciprocal fp32 does not
  *                  reach, from 2^64 x and 2^64 scale); beyond 448, infinities too, as +-448; NaN as NaN
  * Everything else — page tables, lengths, limits, errors and status — is as in the calls without the suffix.

@@ -31,10 +31,11 @@
 // the scores again, exchange their maxima (through tensor memory) and rescale O.
 //
 // Measured, whole calls: trees of 64 nodes of 8 sequences, 32 / 8 heads of 128, 16384 shared keys and up to 2048 of their own (147 GFLOP):
-// 178 us (one card of several took 153), the tensor pipe at 50 %: a pair of key tiles takes some 3.9 k cycles of the 2.05 k that its
+// 165 us (139 over the same inputs again and again), the tensor pipe at 55 %: a pair of key tiles takes some 3.4 k cycles of the 2.05 k that its
 // products need; the rest is the chain scores -> exponentials -> weights -> product of each row tile, which its one other row tile does not hide.
-// 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 33 to 37 us for 6.4 us of bytes; start, first tile and joining are two thirds of it.
-// All 20 warps have 96 registers; the softmax warps spill (160 bytes stored, 204 loaded a thread at D = 128, 144 and 244 at D = 64).
+// 7 sequences of up to 5001 keys, 29 nodes, 28 / 4 heads: 36 us for 6.4 us of bytes; start, first tile and joining are two thirds of it.
+// All 20 warps have 96 registers; the softmax warps spill (56 bytes stored, 128 loaded a thread at D = 128, 76 and 116 at D = 64).
+// The two warps that share a row's threads (columns) meet at named barriers, which have no limit: a wait of one of them that runs out is followed as in_step.cuh says.
 #include "in_step.cuh"
 #include "paged_attn.cuh"
 
@@ -46,11 +47,11 @@ constexpr float PA_LIMIT = 64.f;          // weights stay below 2^64
 // P goes to the second product as bf16, whose rounding is the largest error beside the output's own (relative 2-norm against 64 bits, N(0, 1) inputs:
 // .0023 with it, .00166 without).  As in tree_verify_attention, head size 64 has a second bf16 term, what the rounding of the first left, in every tile
 // (three trees of 128 nodes, 16 / 2 heads of 64, 4096 shared keys: 31.2 us without, 35.3 with), and so have thin items, whose products cost nothing beside
-// their bytes.  At head size 128 a row tile has one term (its products are a third of the time there: 16384 shared keys 179 us, 238 with two in every tile,
+// their bytes.  At head size 128 a row tile has one term (its products are a third of the time there: 16384 shared keys took 179 us, 238 with two in every tile,
 // 192 in four of a piece; one-layer calls of tree_verify_attention are at .0027, short ones at .0017).
 template <int D> constexpr bool TWO_TERMS = D == 64;
 __host__ __device__ constexpr int PHASE_COST(int single) { return single ? 4 : 7; }   // and what a quarter of a key tile takes a CTA, one against the other: pairs are bound by the tensor core and
-                                          // its waits (3.9 k cycles a key tile at D = 128), single row tiles by their K and V (2.2 k, two at a time); measured at D = 128, taken at D = 64 too
+                                          // its waits (3.9 k cycles a key tile at D = 128 when this was measured, 3.4 k now), single row tiles by their K and V (2.2 k, two at a time); measured at D = 128, taken at D = 64 too
 
 template <int D> struct PaSmem {
     static constexpr int HALVES = D / 64;
@@ -95,7 +96,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     constexpr int X_COL = TWO ? 16 : 40;
     extern __shared__ unsigned char smem_raw[];
     let_next_start();
-    // (the shuffle tells the compiler that a warp's number is the same for its lanes)
+    // (the shuffle tells the compiler that a warp's number is the same for its lanes: 16k document 155 us -> 139, long context 76.5 -> 71.2, three trees of 128 nodes at
+    // D = 64 37.5 -> 35, replayed graphs)
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u, sbase = raw + pad;
     unsigned char *gbase = smem_raw + pad;
@@ -865,7 +867,8 @@ paged_attn_thin_kernel(const __grid_constant__ PaParams p) {
 // (max, sum) and their columns requested together: the kernel is a chain of loads from L2.  SPLIT > 1: that many threads share a row's columns,
 // each every SPLIT-th group of four pieces of an item, and meet in shared memory; the order of the additions depends on the pieces alone.  One thread (SPLIT = 1)
 // takes the pieces of both items as one list, so that an item of one or two does not take a trip to L2 of its own, and four blocks share an SM: 8 sequences of 64
-// nodes behind 16384 bf16 keys take 149 us in all (152 with a list an item and three blocks), 16 trees of 64 nodes 68 (71), the results the same.
+// nodes behind 16384 bf16 keys took 149 us in all (152 with a list an item and three blocks), 16 trees of 64 nodes 68 (71), the results the same.  Four blocks of the kernel with
+// four threads a row too: 64 single tokens behind 8192 shared bf16 keys take 74 us, 79 with the 80 registers that it has without that bound.
 struct PaSource {
     const float *o;       // slot of the first piece, at the row
     const float2 *ml;

@@ -7,7 +7,7 @@
 // and q2 what is left; values below 2^-9 of the row's largest are held to 2^-17 of it.  Two products of 8 bits take the time of one of 16.
 // Weights would want two terms too, at every key tile, on the warps that have the least time; so V is converted instead, to fp16 tiles
 // (every code is a number of fp16), by warps of their own, and the second product is fp16 x fp16.  (With K converted as well, those warps were what single
-// row tiles waited for: 16 trees of 29 nodes and up to 4000 keys took 106 us so and 60 without.)
+// row tiles waited for: 16 trees of 29 nodes and up to 4000 keys took 106 us so and 60 without, in the form of the kernel that this was measured in; 46 now.)
 //   P   weights are fp16, 2^SHIFT at the reference (the maximum of a piece's first tile) and below 2^16: they lose bits below 2^(-14 - SHIFT) of the
 //       reference and vanish below 2^(-25 - SHIFT).  11 bits, where bf16 has 8: no second term is needed at any head size.  The reference moves where a
 //       later tile's weights do not fit, as for the bf16 cache.
@@ -16,16 +16,21 @@
 //   warps 0-7 / 8-15  softmax of row tile 0 / 1; in front of a piece they split its queries
 //   warps 16-19       V's codes -> fp16 tiles (128 keys, 128-byte swizzle); rows behind the last key become zeros (their weight is 0, but 0 * NaN is
 //                     not), NaN codes of the tree's rows too (they are given to the rows that see them at the end)
-//   warps 20, 21      issue the products of row tile 0 / 1
+//   warps 20, 21      issue the products of row tile 0 / 1.  As for the bf16 cache, a key tile's scores go over the weights of the tile before, which the product
+//                     issued in front of them reads, with no wait between: products that one thread issues are carried out in the order in which it issues
+//                     them.  Here the two differ in kind (fp16 in front of 8 bits) and in their accumulators; the order is counted on all the same.
 //   warp 22           derives the pieces, requests Q and the codes (a box per page)
 // K's codes, V's and V's tiles have a ring each.  A CTA works on pairs of row tiles or on single ones, never on both, and every warp's loop stands once for
-// either (in_turns): the kernel would else be 193 KB of code, of which an SM's instruction cache holds a part (now 81 KB; the same 16 trees of 29: 93 -> 73 us).
-// Sixteen scores of a row are in registers at a time, the next on their way: with all 64 the 80 registers of 768 threads spill (long context 97 -> 85 us).
+// either (in_turns): the kernel would else be 193 KB of code, of which an SM's instruction cache holds a part (71 KB; that step took the same 16 trees of 29 from
+// 93 to 73 us).  Sixteen scores of a row are in registers at a time, the next on their way: with all 64 the 80 registers of 768 threads spill (that step took the
+// long context from 97 to 85 us; 12 bytes stored and 8 loaded a thread are left at D = 128, 20 and 40 at D = 64).
+// The two warps that share a row's threads (columns) meet at named barriers, which have no limit: a wait of one of them that runs out is followed as in_step.cuh says.
 //
-// Measured, whole calls: one tree of 64 nodes, 32 / 8 heads of 128, 60001 keys (63 GFLOP): 78 us; 8 sequences of 64 nodes, 16384 shared keys and up to 2048 of
-// their own (147 GFLOP): 153 us, the tensor pipe at 57 % beside the joining.  A pair of key tiles takes 3.2 k cycles of the 2.06 k that its products need: the
+// Measured, whole calls: one tree of 64 nodes, 32 / 8 heads of 128, 60001 keys (63 GFLOP): 77 us; 8 sequences of 64 nodes, 16384 shared keys and up to 2048 of
+// their own (147 GFLOP): 153 us, the tensor pipe at 58 % beside the joining (replayed graphs over the same inputs: 64 and 131).  A pair of key tiles takes some
+// 3.1 k cycles of the 2.06 k that its products need: the
 // chain scores -> weights (1.9 k) -> product (1.3 k from the last weight to the next scores) of a row tile is hidden by the other row tile's alone.
-// Looked at and left (us, or the kernel's cycles, of the latter case): the warps of both row tiles on each in turn (32 columns a thread: 299 us where 64 took
+// Looked at and left (us, or the kernel's cycles, of the latter case, each beside the form of the kernel that it was tried in): the warps of both row tiles on each in turn (32 columns a thread: 299 us where 64 took
 // 171); halves of key tiles in turn (64 keys a product of scores, 189 us: the queries are read twice as often from shared memory, which is what bounds those
 // products); no turns between the issuing warps (192 us); turns passed in the middle of the other tile's softmax (cycles + 15 %); fewer polynomials (+ 4 %),
 // more (+ 9 %), other places for them (+ 4 %); waits that poll without suspending (+ 5 %: the issue slots they take are the softmax's); products in loops
@@ -72,7 +77,10 @@ constexpr uint32_t P8_OFF_MISC = P8_COUNT * 8, P8_OFF_QUEUE = (P8_OFF_MISC + 44 
 static_assert(P8_OFF_QUEUE + 2 * PA_QUEUE * 32 <= 960, "barrier region");
 static_assert(P8Smem<64>::K_STAGES <= 8 && P8Smem<64>::V_STAGES <= 8 && P8Smem<64>::TILES <= 4, "barriers of the rings");
 
-constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;      // what a quarter of a key tile takes a CTA, pairs against single row tiles
+// What a quarter of a key tile takes a CTA, pairs against single row tiles: the bf16 kernel's numbers.  Pairs gain less from the codes than this says: with 3 : 2 in
+// place of 7 : 4 three row tiles over 30001 keys take 65.6 us for 69.0, 12 such trees of up to 3000 keys 55.6 for 59.4, 8 behind 4096 shared keys 85.4 for 91.4 (D = 64:
+// 53.6 for 57.3, 44.8 for 48.4), with 1 : 1 69.1, 56.1, 76.2 (53.4, 44.4), with 2 : 1 72.7, 61.9, 98.7 (61.7, 50.5); five row tiles of four trees 38.3 whatever it is.
+constexpr int P8_COST_PAIRS = 7, P8_COST_SINGLE = 4;
 
 // What the issuing warps and the converting ones want of a piece (their registers are few).
 struct P8Tiles { int t0, t1; };
@@ -863,9 +871,12 @@ paged_attn8_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // A CTA walks a run of the line of all thin items, KEYS keys to a warp at a time.  Asynchronous copies bring them to the warp's own part of shared memory,
 // STAGES - 1 blocks ahead: no warp waits for another, and no register holds what is on its way.  At a piece's end the warps join.
 // An instruction of copies covers whole rows: where it took half a row of each of 8 keys (as the operands have them), the other half crossed from L2 with it, twice
-// in all (64 single tokens: 88 us so, 71 now).
-// Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 53 us = 5.2 TB/s, 79 % of the copy rate (60 us with the joining); one token
-// of 60001 keys 30 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces' starts and ends.
+// in all (that step took 64 single tokens from 88 us to 71).
+// Measured: 64 single tokens, 8 KV heads of 128, 500 to 4000 keys each: 277 MB in 52 us = 5.3 TB/s, 81 % of the copy rate (58 us with the joining, 53 in replayed
+// graphs); one token of 60001 keys 30 us (18.8 at the memory's rate).  8 warps and 16 keys, 6 and 32, 4 and 32 are within a percent: what is left is the pieces'
+// starts and ends.
+// Two products for up to 8 rows too (NR = 2 for all): 32 sequences, 8 rows a KV head 36 us for 33.5 (D = 64: 28.9 for 21.4), 64 of 4 or of 1 row 56.5 for 53.  9 and 16 rows, which
+// need them, 37.5 and 36.7 (floor 22.8; D = 64, 16 rows: 29.8, floor 11.4).
 // Weights are 2^SHIFT at the reference, as in row tiles (so that as small ones count); it may be SLACK too small: they stay below 2^16, which fp16 ends at.
 constexpr float T8_SHIFT = 8.f, T8_SLACK = 7.9f;
 

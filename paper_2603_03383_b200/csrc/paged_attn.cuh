@@ -10,7 +10,10 @@ constexpr int PA_QUEUE = 4;               // pieces that are handed out and may 
 constexpr int PA_KEYS = 128;              // keys of a tile
 constexpr int PA_MAX_B = 1024;
 constexpr int TILE_COST = 4;              // a key tile on a line
-__host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }   // what the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles
+// What the start and end of an item take, in the same quarters of a key tile, for pairs and for single row tiles.  With codes, replayed graphs: 8 for pairs takes a 16k document of 8
+// trees from 131 to 147 us and 16 trees of 64 nodes from 59 to 62, 24 these from 59 to 62.6; at D = 64 the latter 47.3 with 16, 47.9 with 8, 49.7 with 24.  Single row tiles
+// (16 trees of 29 nodes) take 46 us with 4, 8, 12 or 16, at D = 64 38.
+__host__ __device__ constexpr int ITEM_COST(int single) { return single ? 8 : 16; }
 
 struct PaParams {
     PagedRef pages;
