@@ -1080,7 +1080,8 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                             if (a >= 0 && (!own || a >= p.T || !(see[nr][e & 1] >> a & 1u))) x[mt][nr][e] = -INFINITY;
                     }
             }
-            // the reference moves where a score of the row is too far above it, and where there is none yet
+            // The reference moves where a score of the row is too far above it, and where there is none yet.  (Asked of the exponent that the weight is taken of: far from
+            // zero, m + SLACK would be rounded up to a step of fp32, and a weight beyond fp16 could pass.)
             bool ask = false;
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr)
@@ -1089,7 +1090,7 @@ paged_attn8_thin_kernel(const __grid_constant__ P8Params pp) {
                     float mx = max_nan(x[0][nr][e], x[0][nr][e + 2]);
 #pragma unroll
                     for (int mt = 1; mt < MT; ++mt) mx = max3_nan(mx, x[mt][nr][e], x[mt][nr][e + 2]);
-                    ask = ask || !(mx * sc[nr][e] <= m[nr][e] + T8_SLACK);
+                    ask = ask || !(fmaf(mx, sc[nr][e], T8_SHIFT - m[nr][e]) <= T8_SHIFT + T8_SLACK);
                 }
             if (__any_sync(0xffffffffu, ask)) {
 #pragma unroll
