@@ -111,7 +111,7 @@ template <int TO> __device__ __forceinline__ float2 row_factor(uint32_t largest)
 // is too small for fp32 is not 0, as a hidden score times it is to stay -inf, nor is one that is too large infinite, as 0 times it is to stay 0.
 __device__ __forceinline__ float scores_factor(float scale, float k_scale, float back) {
     const float f = (float)((double)scale * k_scale * back);
-    return fminf(fmaxf(f, __int_as_float(1)), FLT_MAX);
+    return f == 0.f ? __int_as_float(1) : f == INFINITY && k_scale != INFINITY ? FLT_MAX : f;      // (a k_scale that is not finite shows)
 }
 __device__ __forceinline__ uint32_t larger_bits(uint32_t m, uint32_t pair) { return max(m, max(pair << 16, pair & 0xffff0000u)); }
 __device__ __forceinline__ uint32_t abs2_bf16(uint32_t pair) { return pair & 0x7fff7fffu; }

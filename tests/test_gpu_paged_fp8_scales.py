@@ -113,3 +113,22 @@ def test_scores_whose_scales_have_no_product(D, T, G, large):
     assert want.isfinite().all()
     worst = ((out - want).abs() / bound(want, absolute)).max().item()
     assert worst <= 1.0, worst
+
+
+@pytest.mark.parametrize("T,G", [(1, 4), (4, 4), (20, 3), (64, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("of_v", [False, True])
+def test_a_scale_that_is_no_number_shows(D, T, G, of_v):
+    """NaN as a head's scale: that head's rows are NaN, the other's as ever."""
+    g = torch.Generator().manual_seed(6)
+    Hkv, page, lens = 2, 16, [300, 77]
+    tb, tree = (dict(mask=[[1]]), binding.tree_build_static(1, [])) if T == 1 else make_tree("rank_prior", 4, (), T)
+    t, n_pages = table(g, len(lens), max(lens) + T, page)
+    kp, vp = _fp8.pools(g, 2, n_pages, Hkv, page, D)
+    q = torch.randn(2, T, Hkv * G, D, generator=g).to(BF16)
+    ks, vs = torch.tensor([0.01, 0.012]), torch.tensor([0.01, 0.012])
+    want, absolute = _fp8.attention(q, kp, vp, ks, vs, t, lens, tb["mask"])
+    (vs if of_v else ks)[0] = float("nan")
+    out = attend(tree, q, kp, vp, ks, vs, t, lens, 0.0)
+    assert torch.isnan(out[:, :, :G]).all()
+    assert ((out - want).abs() / bound(want, absolute))[:, :, G:].max().item() <= 1.0
